@@ -260,7 +260,9 @@ int treekv_wavelet_components(const float* a, const void* V, int dtype, int head
  *   positions [U][c] int32   stream positions of the kept tokens, ascending; -1 past n
  *   slots     [U][c] int32   the cache row each token sits in (0 .. c); -1 past n.  Restoring rows to the same
  *                            slots makes the steps after an import repeat bit for bit what followed the export.
- *                            A snapshot built by hand may set slots[u][0] = -1: token i then takes row i.
+ *                            A snapshot built by hand may set slots[u][0] = -1: token i then takes row i.  It does so
+ *                            too where one of the first n_sink tokens is not in the row of its position, as the
+ *                            library keeps them.
  *   S         [U][c] float32 accumulated attention weight of each kept token (Algorithm 1's S); 0 past n
  *   K, V      [U][c][d]      storage dtype; the kept tokens' rows, zero past n
  */

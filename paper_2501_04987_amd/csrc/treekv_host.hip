@@ -213,6 +213,7 @@ __global__ __launch_bounds__(256) void import_state_kernel(Params p, const int* 
   const bool full = n == c;
   if (!bad && !full && (t != n || j != 0)) bad = 1;                  // nothing has been evicted while the cache fills
   const bool own_slots = !bad && full && sl[0] >= 0;                 // else: token i goes to slot i
+  int moved = 0;                                                     // a sink that is not in its slot
   if (!bad) {
     for (int i = tid; i < n; i += 256) {
       const int x = po[i];
@@ -222,9 +223,11 @@ __global__ __launch_bounds__(256) void import_state_kernel(Params p, const int* 
       if (k < 0 && x != i) bad = 1;                                  // the sinks are the first tokens
       if (k >= m && x != t - r + (k - m)) bad = 1;                   // the recent window is the last r tokens
       if (own_slots && (sl[i] < 0 || sl[i] >= cap)) bad = 1;
+      if (own_slots && k < 0 && sl[i] != i) moved = 1;
     }
   }
   bad = __syncthreads_or(bad);
+  moved = __syncthreads_or(moved);
   if (!bad && own_slots) {                                           // every slot claimed once
     for (int s = tid; s < cap; s += 256) mark[s] = -1;
     __syncthreads();
@@ -236,13 +239,13 @@ __global__ __launch_bounds__(256) void import_state_kernel(Params p, const int* 
   if (status && tid == 0) status[unit] = bad ? TREEKV_EINVAL : TREEKV_OK;
   const int n_eff = bad ? 0 : n;
 
+  const bool use_slots = own_slots && !bad && !moved, use_pos = full && !bad;
   int free_slot = n_eff;                                             // filling, or token i in slot i: the next slot
-  if (!bad && own_slots) {
+  if (use_slots) {
     for (int s = tid; s < cap; s += 256) if (mark[s] < 0) sm_free = s;   // cap = n + 1 slots: exactly one is unclaimed
     __syncthreads();
     free_slot = sm_free;
   }
-  const bool use_slots = own_slots && !bad, use_pos = full && !bad;
   auto slot_of = [&](int i) { return use_slots ? sl[i] : i; };
   auto pos_of = [&](int i) { return use_pos ? po[i] : i; };
   const int jd = bad ? 0 : j;
