@@ -291,6 +291,100 @@ int treekv_export_state(treekv_ctx* ctx, void* dst, size_t bytes, void* stream);
  */
 int treekv_import_state(treekv_ctx* ctx, const void* src, size_t bytes, int32_t* status, void* stream);
 
+/*
+ * Speculative decoding.  A drafter proposes a tree of tokens behind each sequence; treekv_tree_attend verifies all of
+ * them in one pass over the cache and changes nothing, and treekv_tree_commit takes the accepted path into the cache.
+ * For every sequence the two together give what treekv_prefill_chunk gives for the path's tokens (another kernel adds
+ * the same numbers in another order: the last bits may differ), and, with a path of one token, treekv_decode_step.
+ * Sequences accept different numbers of tokens: after a commit each goes on from its own position.
+ *
+ * The tree of a sequence has n tokens (nodes), every one after its parent: parents[b][i] is a node before i, or -1 for a
+ * child of the last cached token.  A node attends the cached tokens, its ancestors and itself.  A node whose chain of
+ * parents does not end in -1 is absent (trees of unequal sizes are padded with any other negative number): its out is 0,
+ * its lse minus infinity, and nobody attends it.  What a node does not attend (absent or on another branch) has no part
+ * in its results, whatever it holds, infinities and NaNs too.
+ * With TREEKV_POSITION_RERANK cached token i is at position i and a node with d ancestors at n_retained + d.
+ */
+enum { TREEKV_TREE_MAX_NODES = 256 };
+
+/* Device memory treekv_tree_attend needs beside the workspace for trees of n nodes; 0 if it needs none (or n is not
+ * accepted).  It holds nothing between calls: one piece serves every context whose calls do not overlap. */
+size_t treekv_tree_scratch_bytes(const treekv_ctx* ctx, int n);
+
+/*
+ * treekv_tree_attend - o = SoftMax(q K^T * scale) V of every node.
+ *   q [B, n, H, d], k [B, n, Hkv, d], v [B, n, Hkv, d]   storage dtype, read only
+ *   parents [B, n] int32 (device)
+ *   out     [B, n, H, d] float32
+ *   lse     [B, n, H] float32 (may be NULL): log of the sum of exp(q k * scale) over what the node attends;
+ *           treekv_tree_commit takes it
+ *   scratch 16-byte aligned, at least treekv_tree_scratch_bytes(ctx, n) (NULL if that is 0)
+ * Errors: TREEKV_EINVAL unless 1 <= n <= min(TREEKV_TREE_MAX_NODES, max_chunk), for null or misaligned pointers and for
+ * scratch that is too small.
+ */
+int treekv_tree_attend(treekv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* parents, int n,
+                       float* out, float* lse, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * treekv_tree_commit - the tokens path[b][0 .. path_len[b]) of sequence b's tree (the first a child of the last cached
+ * token, each of the others a child of the one before) become its next tokens: their probabilities are added to the scores
+ * and counts, then, with the averaged scores frozen, Algorithm 1's append / compare / evict / advance runs for
+ * them in order.
+ *   q, k, v, parents, n as given to treekv_tree_attend, lse as it wrote it, the context unchanged since
+ *   path     [B, max_len] int32 (device), 1 <= max_len <= n;  path_len [B] int32 (device), 0 .. max_len
+ *   retained [B, Hkv, c] int32, n_retained [B, Hkv] (may be NULL): as treekv_decode_step
+ *   evicted  [B, Hkv, max_len] int32 (may be NULL): position evicted when the path's i-th token was appended, or -1
+ *   status   [B] int32 (may be NULL): TREEKV_OK, or TREEKV_EINVAL where path and path_len describe no such path of
+ *            the tree.  Such a sequence is left as it was, as one with path_len 0 is; the others are committed.
+ * Errors: as treekv_tree_attend, and TREEKV_EINVAL for a max_len out of range.
+ */
+int treekv_tree_commit(treekv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* parents,
+                       const float* lse, int n, const int32_t* path, const int32_t* path_len, int max_len,
+                       int32_t* retained, int32_t* n_retained, int32_t* evicted, int32_t* status, void* stream);
+
+/*
+ * treekv_fork - sequence dst[i] of ctx becomes a copy of sequence src[i] of `from` (which may be ctx), i < count: samples
+ * and beams that share a prefix, a prompt compressed in a context of its own that joins a batch.  src[i] = -1 empties
+ * dst[i], as treekv_reset does for all sequences.  The sequences of ctx that dst does not name stay as they are.
+ * The copies go on exactly as their source would.  src and dst are HOST arrays and are read before the call returns.
+ * Both contexts must have been reset once since their workspaces were bound.
+ * Errors: TREEKV_EINVAL for an index out of range, a dst that appears twice or, inside one context, is also the src of
+ * another pair (a pair of the same sequence changes nothing and is no such dst), and unless the two contexts' configurations agree in all but batch, max_chunk, kv_splits and max_prompt.
+ */
+int treekv_fork(treekv_ctx* ctx, const treekv_ctx* from, const int32_t* src, const int32_t* dst, int count, void* stream);
+
+/*
+ * treekv_qkv_prepare - from a projection's rows to the operands of the calls above, stateless: each head of q and k
+ * normalised (x / sqrt(mean(x^2) + eps) * weight) and turned by the rotary encoding of the token's position, v (and what
+ * is neither normalised nor turned) copied as it is.  Worked out in fp32 (angles in double) and rounded once.
+ *   q [tokens, q_heads, d], k, v [tokens, kv_heads, d]: the heads of a token are contiguous, tokens are *_stride elements
+ *              apart, so that all three can lie in one packed row; q_out, k_out, v_out contiguous.  A pair of input and
+ *              output may be left out (both NULL).  q_out may be q itself where q is contiguous, likewise k and v; other
+ *              overlaps of an output are refused.
+ *   weights    [d] storage dtype, or NULL: no norm
+ *   positions  [tokens] int32 and inv_freq [rotary_dim / 2] float64 (both device), or both NULL: no rotation (what a
+ *              context with TREEKV_POSITION_RERANK takes).  Plane i is turned by position * inv_freq[i].
+ *   rotary_dim leading dimensions of a head that are turned (a multiple of 16, at most d; 0: none); the others pass.
+ * Planes are dimensions (2i, 2i+1), the library's convention, or with TREEKV_ROPE_HALVES (i, i + rotary_dim/2).
+ * TREEKV_ROPE_TO_PLANES (with TREEKV_ROPE_HALVES) writes that pair to dimensions (2i, 2i+1): the permutation
+ * TREEKV_POSITION_RERANK asks of models that pair halves.
+ * Errors: TREEKV_EINVAL; TREEKV_EUNSUPPORTED for d other than 64 or 128 or a rotary_dim that is not a multiple of 16.
+ */
+enum { TREEKV_ROPE_HALVES = 1, TREEKV_ROPE_TO_PLANES = 2 };
+typedef struct treekv_qkv_args {
+  const void *q, *k, *v;                    /* 16-byte aligned */
+  void *q_out, *k_out, *v_out;
+  const void *q_weight, *k_weight;
+  const int32_t* positions;
+  const double* inv_freq;
+  int64_t q_stride, k_stride, v_stride;     /* elements from one token to the next; rows stay 16-byte aligned */
+  int32_t tokens, q_heads, kv_heads, head_dim;
+  int32_t dtype;                            /* TREEKV_BF16 or TREEKV_F32: inputs, weights and outputs */
+  int32_t rotary_dim, flags;
+  float eps;
+} treekv_qkv_args;
+int treekv_qkv_prepare(const treekv_qkv_args* args, void* stream);
+
 /* Static description of a status code. */
 const char* treekv_strerror(int status);
 

@@ -6,6 +6,7 @@ built, `load()` raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -24,12 +25,16 @@ TREEKV_KEEP_LEFT = 1
 TREEKV_SCORE_ACCUMULATED = 4
 TREEKV_POSITION_RERANK = 8
 TREEKV_DEFAULT_LAYOUT = -1
+TREEKV_TREE_MAX_NODES = 256
+TREEKV_ROPE_HALVES = 1
+TREEKV_ROPE_TO_PLANES = 2
 
 EXPORTS = [
     "treekv_init", "treekv_init_ex", "treekv_destroy", "treekv_get_config", "treekv_workspace_bytes",
     "treekv_bind_workspace", "treekv_reset", "treekv_decode_step", "treekv_decode_step_static", "treekv_prefill_chunk", "treekv_prefill_prompt",
     "treekv_scores", "treekv_state_bytes", "treekv_get_state_layout", "treekv_export_state", "treekv_import_state",
     "treekv_gather_kv", "treekv_wavelet_components", "treekv_strerror", "treekv_last_hip_error",
+    "treekv_tree_scratch_bytes", "treekv_tree_attend", "treekv_tree_commit", "treekv_fork", "treekv_qkv_prepare",
 ]
 PROBE_EXPORTS = ["treekv_probe_read", "treekv_probe_copy", "treekv_probe_mfma"]       # include/treekv_probe.h
 
@@ -45,6 +50,13 @@ class treekv_config(C.Structure):
 
 class treekv_state_layout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("header", "positions", "slots", "S", "K", "V", "bytes")]
+
+
+class treekv_qkv_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "k_out", "v_out", "q_weight", "k_weight", "positions", "inv_freq")]
+    _fields_ += [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
+    _fields_ += [(n, C.c_int32) for n in ("tokens", "q_heads", "kv_heads", "head_dim", "dtype", "rotary_dim", "flags")]
+    _fields_ += [("eps", C.c_float)]
 
 
 _lib = None
@@ -83,6 +95,12 @@ def load() -> C.CDLL:
     lib.treekv_export_state.argtypes = [vp, vp, C.c_size_t, vp]
     lib.treekv_import_state.argtypes = [vp, vp, C.c_size_t, i32p, vp]
     lib.treekv_wavelet_components.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp]
+    lib.treekv_tree_scratch_bytes.argtypes = [vp, C.c_int]
+    lib.treekv_tree_scratch_bytes.restype = C.c_size_t
+    lib.treekv_tree_attend.argtypes = [vp, vp, vp, vp, i32p, C.c_int, vp, vp, vp, C.c_size_t, vp]
+    lib.treekv_tree_commit.argtypes = [vp, vp, vp, vp, i32p, vp, C.c_int, i32p, i32p, C.c_int, i32p, i32p, i32p, i32p, vp]
+    lib.treekv_fork.argtypes = [vp, vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int, vp]
+    lib.treekv_qkv_prepare.argtypes = [C.POINTER(treekv_qkv_args), vp]
     lib.treekv_probe_read.argtypes = [vp, C.c_size_t, C.c_int, C.c_int, vp, vp]
     lib.treekv_probe_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.treekv_probe_mfma.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), vp]
@@ -135,6 +153,85 @@ def wavelet_components(a, V, levels: int, per_head=None, mean=None):
     if rc != TREEKV_OK:
         raise TreeKVError(rc, "treekv_wavelet_components")
     return per_head, mean
+
+
+def _want(t, what: str, dtype, shape, device):
+    """`t` is what a kernel will take it for: contiguous, of this type and shape, on this device."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what}: {dtype} {tuple(shape)}, contiguous, on {device} is wanted, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _on(device):
+    """A context in which `device` is the current one: kernels are launched there, and the null stream is its."""
+    import torch
+
+    if device.type != "cuda" or device.index is None or torch.cuda.current_device() == device.index:
+        return _NOTHING
+    return torch.cuda.device(device)
+
+
+_NOTHING = contextlib.nullcontext()
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, device="cuda"):
+    """base^(-2i / rotary_dim) for i < rotary_dim / 2, float64: the angle per position of each plane (`inv_freq`)."""
+    import torch
+
+    i = torch.arange(rotary_dim // 2, dtype=torch.float64)
+    return torch.pow(torch.tensor(float(base), dtype=torch.float64), -2.0 * i / rotary_dim).to(device)
+
+
+def qkv_prepare(q, k=None, v=None, *, q_weight=None, k_weight=None, eps: float = 1e-6, positions=None, inv_freq=None,
+                halves: bool = False, to_planes: bool = False, out=None):
+    """treekv_qkv_prepare on torch tensors: q [tokens, q_heads, d], k and v [tokens, kv_heads, d] (any may be None), bf16 or
+    float32; the heads of a token are contiguous, tokens any distance apart, so slices of a packed projection go in as they
+    are.  `inv_freq` [rotary_dim / 2] float64 (rope_frequencies) and `positions` [tokens] int32 turn the heads.  `out`: the
+    three contiguous results, allocated if None.  Returns them."""
+    import torch
+
+    lib = load()
+    given = [x for x in (q, k, v) if x is not None]
+    if not given:
+        raise ValueError("one of q, k and v at least")
+    tokens, _, d = given[0].shape
+    device, dtype = given[0].device, given[0].dtype
+    a = treekv_qkv_args(tokens=tokens, head_dim=d, flags=(TREEKV_ROPE_HALVES if halves else 0) | (TREEKV_ROPE_TO_PLANES if to_planes else 0),
+                        eps=eps, dtype={torch.bfloat16: TREEKV_BF16, torch.float32: TREEKV_F32}[dtype])
+    out = list(out) if out is not None else [None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v)]
+    for name, x, y in zip("qkv", (q, k, v), out):
+        if x is None:
+            continue
+        if x.dtype != dtype or x.device != device or x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != d:
+            raise ValueError(f"{name}: {dtype} [{tokens}, heads, {d}] on {device} is wanted, not {x.dtype} {tuple(x.shape)} on {x.device}")
+        if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
+            raise ValueError(f"{name}: the heads of a token must be contiguous, not strides {x.stride()}")
+        _want(y, f"out of {name}", dtype, x.shape, device)
+        setattr(a, name, x.data_ptr())
+        setattr(a, name + "_out", y.data_ptr())
+        setattr(a, name + "_stride", x.stride(0))
+    if k is not None and v is not None and k.shape != v.shape:
+        raise ValueError("k and v have the same heads")
+    a.q_heads = q.shape[1] if q is not None else 0
+    a.kv_heads = (k if k is not None else v).shape[1] if k is not None or v is not None else 0
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _want(w, name, dtype, (d,), device)
+            setattr(a, name, w.data_ptr())
+    if positions is not None or inv_freq is not None:
+        if positions is None or inv_freq is None:
+            raise ValueError("positions and inv_freq come together")
+        _want(positions, "positions", torch.int32, (tokens,), device)
+        _want(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),), device)
+        a.positions, a.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
+        a.rotary_dim = 2 * inv_freq.numel()
+    elif to_planes:
+        a.rotary_dim = d
+    with _on(device):
+        rc = lib.treekv_qkv_prepare(C.byref(a), _raw_stream(device))
+    if rc != TREEKV_OK:
+        raise TreeKVError(rc, "treekv_qkv_prepare")
+    return tuple(out)
 
 
 class TreeKV:
@@ -268,3 +365,71 @@ class TreeKV:
             V_out = self._torch.empty(shape, dtype=self.storage_dtype, device=self.device)
         self._check(self._lib.treekv_gather_kv(self._h, _ptr(K_out), _ptr(V_out), self._stream()), "treekv_gather_kv")
         return K_out, V_out
+
+    # -- speculative decoding ------------------------------------------------------------
+    def tree_scratch_bytes(self, nodes: int) -> int:
+        return self._lib.treekv_tree_scratch_bytes(self._h, int(nodes))
+
+    def new_tree_outputs(self, nodes: int):
+        """Allocate (out, lse, scratch) for trees of `nodes` tokens; scratch is None where none is needed."""
+        t, c = self._torch, self.cfg
+        out = t.empty(c.batch, nodes, c.q_heads, c.head_dim, dtype=t.float32, device=self.device)
+        lse = t.empty(c.batch, nodes, c.q_heads, dtype=t.float32, device=self.device)
+        need = self.tree_scratch_bytes(nodes)
+        return out, lse, t.empty(need, dtype=t.uint8, device=self.device) if need else None
+
+    def _want_tree(self, q, k, v, parents):
+        c, t, dev = self.cfg, self.storage_dtype, self.workspace.device
+        n = parents.shape[-1]
+        _want(parents, "parents", self._torch.int32, (c.batch, n), dev)
+        _want(q, "q", t, (c.batch, n, c.q_heads, c.head_dim), dev)
+        _want(k, "k", t, (c.batch, n, c.kv_heads, c.head_dim), dev)
+        _want(v, "v", t, (c.batch, n, c.kv_heads, c.head_dim), dev)
+        return n, dev
+
+    def tree_attend(self, q, k, v, parents, out, lse=None, scratch=None):
+        """Attention of drafted trees; `scratch` (uint8, tree_scratch_bytes) is allocated for the call if None."""
+        n, dev = self._want_tree(q, k, v, parents)
+        f32, c = self._torch.float32, self.cfg
+        _want(out, "out", f32, (c.batch, n, c.q_heads, c.head_dim), dev)
+        if lse is not None:
+            _want(lse, "lse", f32, (c.batch, n, c.q_heads), dev)
+        if scratch is None:
+            need = self.tree_scratch_bytes(n)
+            scratch = self._torch.empty(need, dtype=self._torch.uint8, device=dev) if need else None
+        elif scratch.device != dev or not scratch.is_contiguous():
+            raise ValueError(f"scratch: contiguous memory on {dev} is wanted")
+        with _on(dev):
+            self._check(self._lib.treekv_tree_attend(self._h, _ptr(q), _ptr(k), _ptr(v), _ptr(parents), n, _ptr(out), _ptr(lse),
+                                                     _ptr(scratch), 0 if scratch is None else scratch.nbytes, _raw_stream(dev)),
+                        "treekv_tree_attend")
+
+    def tree_commit(self, q, k, v, parents, lse, path, path_len, retained, n_retained=None, evicted=None, status=None):
+        """The accepted paths [batch, max_len] (path_len [batch] of them) of the attended trees enter the cache."""
+        n, dev = self._want_tree(q, k, v, parents)
+        c, i32 = self.cfg, self._torch.int32
+        longest = path.shape[-1]
+        _want(lse, "lse", self._torch.float32, (c.batch, n, c.q_heads), dev)
+        _want(path, "path", i32, (c.batch, longest), dev)
+        _want(path_len, "path_len", i32, (c.batch,), dev)
+        _want(retained, "retained", i32, (c.batch, c.kv_heads, c.budget), dev)
+        for t, what, shape in ((n_retained, "n_retained", (c.batch, c.kv_heads)),
+                               (evicted, "evicted", (c.batch, c.kv_heads, longest)), (status, "status", (c.batch,))):
+            if t is not None:
+                _want(t, what, i32, shape, dev)
+        with _on(dev):
+            self._check(self._lib.treekv_tree_commit(self._h, _ptr(q), _ptr(k), _ptr(v), _ptr(parents), _ptr(lse), n, _ptr(path),
+                                                     _ptr(path_len), longest, _ptr(retained), _ptr(n_retained), _ptr(evicted),
+                                                     _ptr(status), _raw_stream(dev)), "treekv_tree_commit")
+
+    def fork(self, source: "TreeKV", src, dst):
+        """Sequence dst[i] becomes a copy of `source`'s sequence src[i] (-1: is emptied); lists of host integers."""
+        src, dst = [int(x) for x in src], [int(x) for x in dst]
+        if len(src) != len(dst):
+            raise ValueError("src and dst have the same length")
+        if source.workspace.device != self.workspace.device:
+            raise ValueError("both contexts on one device")
+        ints = C.c_int32 * len(src)
+        with _on(self.workspace.device):
+            self._check(self._lib.treekv_fork(self._h, source._h, ints(*src), ints(*dst), len(src), _raw_stream(self.workspace.device)),
+                        "treekv_fork")

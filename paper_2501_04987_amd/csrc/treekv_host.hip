@@ -15,19 +15,8 @@
 // the process ends.  In host code this name is only a handle for hipGetSymbolAddress, never a device address.
 static __device__ __align__(256) unsigned char scratch[TREEKV_STATIC_SCRATCH_BYTES];
 
-struct treekv_ctx {
-  treekv_config cfg;
-  tkv::Params p;
-  size_t ws_bytes;
-  bool bound;
-  char hip_err[256];
-};
-
 namespace tkv {
 namespace {
-
-constexpr size_t ALIGN = 256;
-size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 
 size_t rope_rows(const Params& p) {
   const size_t chunk = (size_t)p.cap + p.max_chunk;
@@ -301,6 +290,15 @@ hipError_t take_hip_error() {
   tl_hip_error = hipSuccess;
   return e;
 }
+void fresh() {
+  (void)hipGetLastError();
+  (void)take_hip_error();
+}
+int record_hip(treekv_ctx* ctx, int rc) {
+  const hipError_t e = take_hip_error();
+  if (rc == TREEKV_EHIP) snprintf(ctx->hip_err, sizeof(ctx->hip_err), "%s", hipGetErrorString(e));
+  return rc;
+}
 
 int launch_export_state(const Params& p, char* dst, hipStream_t s) {
   const treekv_state_layout l = state_layout(p);
@@ -346,20 +344,9 @@ int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s) {
 // --------------------------------------------------------------------------------------
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Every entry point that launches calls fresh() first: an error an earlier, unrelated HIP call of this thread
-// left behind is dropped there, so it is not taken for a failure of this library's launches.
-void fresh() {
-  (void)hipGetLastError();
-  (void)tkv::take_hip_error();
-}
-
-int record_hip(treekv_ctx* ctx, int rc) {
-  const hipError_t e = tkv::take_hip_error();
-  if (rc == TREEKV_EHIP) snprintf(ctx->hip_err, sizeof(ctx->hip_err), "%s", hipGetErrorString(e));
-  return rc;
-}
+using tkv::aligned16;
+using tkv::fresh;
+using tkv::record_hip;
 
 // Device address of `scratch` on the current device, looked up once per device.
 constexpr int MAX_DEVICES = 64;

@@ -6,6 +6,8 @@
 
 #include "treekv.h"
 
+struct treekv_ctx;
+
 namespace tkv {
 
 // Per-unit bookkeeping words (unit = one (batch, KV head) stream).
@@ -16,6 +18,7 @@ enum MetaField : int {
   META_RHEAD = 3,  // oldest entry of the recent-window ring
   META_T = 4,      // tokens processed so far == position of the next token
   META_ARRIVED = 5,   // workgroups of the decode kernel in flight that are done with their slice (0 between kernels)
+  META_PATH = 6,      // tokens of the drafted path being committed (from the column sums to the replay of one call)
   META_STRIDE = 8
 };
 
@@ -76,6 +79,13 @@ constexpr int DECODE_MAX_SPLITS = 64;    // slices of a unit the decode step's m
 int finish_launch();
 bool hip_failed(hipError_t e);
 hipError_t take_hip_error();
+// Every entry point that launches calls fresh() first: an error an earlier, unrelated HIP call of this thread
+// left behind is dropped there, so it is not taken for a failure of this library's launches.
+void fresh();
+int record_hip(treekv_ctx* ctx, int rc);
+constexpr size_t ALIGN = 256;
+inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // true if the decode kernels of the current shape (p.nsplit, p.rows_per_split) fit in LDS
 bool decode_shape_fits(const Params& p);
@@ -93,6 +103,37 @@ int launch_scores(const Params& p, float* scores, hipStream_t s);
 int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s);
 int launch_export_state(const Params& p, char* dst, hipStream_t s);
 int launch_import_state(const Params& p, const char* src, int32_t* status, hipStream_t s);
+
+// A tree of n drafted tokens and, for a commit, the accepted path through it (device arrays).
+struct Tree {
+  const void *q, *k, *v;    // [B, n, H, d], [B, n, Hkv, d]
+  const int32_t* parents;   // [B, n]
+  int n;
+  const float* lse;         // [B, n, H]
+  const int32_t* path;      // [B, max_len] nodes
+  const int32_t* path_len;  // [B]
+  int max_len;
+};
+size_t tree_scratch_bytes(const Params& p, int n);
+int launch_tree_attend(const Params& p, const Tree& t, float* out, float* lse, void* scratch, hipStream_t s);
+// Scores of the path's tokens: their probabilities summed per column into pf_colacc, the path's length into META_PATH.
+int launch_tree_colsums(const Params& p, const Tree& t, int32_t* status, hipStream_t s);
+// What follows: the chunk path's replay, with each unit's own number of tokens.
+int launch_tree_replay(const Params& p, const Tree& t, int32_t* retained, int32_t* n_retained, int32_t* evicted, hipStream_t s);
+int launch_fork(const Params& to, const Params& from, const int32_t* src, const int32_t* dst, int count, hipStream_t s);
+int launch_qkv(const treekv_qkv_args& a, hipStream_t s);
+
+}  // namespace tkv
+
+struct treekv_ctx {
+  treekv_config cfg;
+  tkv::Params p;
+  size_t ws_bytes;
+  bool bound;
+  char hip_err[256];
+};
+
+namespace tkv {
 
 // ---- device helpers shared by the kernels ---------------------------------
 #if defined(__HIPCC__)

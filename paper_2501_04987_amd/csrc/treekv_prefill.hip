@@ -1488,12 +1488,21 @@ __host__ __device__ inline size_t replay_lds_words(int m, int cap, int r, int L)
 // HELD > 0: the kernel also copies the surviving rows into their slots.  A thread asks for HELD 16-byte pieces of the
 // chunk's K and of its V at the start, holds them while the evictions are worked out and stores those whose token lives:
 // the loads cost nothing beside the replay's own round trips, and the launch of the scatter kernel is saved.
-template <bool IN_LDS, int HELD>
-__global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, int L, const uint4* __restrict__ Kc,
+//
+// TREE: the tokens are the accepted path of a drafted tree.  Every unit has its own number of them, which the column sums'
+// kernel has left in META_PATH (none: nothing changes but `evicted`), at most L, and token i's rows are those of node path[i].
+struct NoPath {};
+struct DraftPath {
+  const int32_t* path;      // [B, L] nodes
+  int nodes;                // of a tree: Kc and Vc are [B, nodes, Hkv, D]
+};
+template <bool IN_LDS, int HELD, bool TREE = false>
+__global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, int L_max, const uint4* __restrict__ Kc,
                                                                     const uint4* __restrict__ Vc, int row_vec,
                                                                     int32_t* __restrict__ retained,
                                                                     int32_t* __restrict__ n_retained,
-                                                                    int32_t* __restrict__ evicted) {
+                                                                    int32_t* __restrict__ evicted,
+                                                                    std::conditional_t<TREE, DraftPath, NoPath> draft) {
   __shared__ int sm_wave[RP_WAVES];
   extern __shared__ __attribute__((aligned(16))) int rp_smem[];
   const int unit = blockIdx.x, tid = threadIdx.x;
@@ -1502,7 +1511,9 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
   int* Eg = p.E + (size_t)unit * 2 * p.m;
   int* PEg = p.PE + (size_t)unit * 2 * p.m;
   int* Rg = p.R + (size_t)unit * max(p.n_recent, 1);
-  int32_t* evu = evicted ? evicted + (size_t)unit * L : nullptr;
+  int32_t* evu = evicted ? evicted + (size_t)unit * L_max : nullptr;
+  int L = L_max;
+  if constexpr (TREE) L = meta[META_PATH];
   const int cap = p.cap, c = p.budget, m = p.m, r = p.n_recent;
 
   float* Su = Sg;
@@ -1510,16 +1521,16 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
   float* snew = p.pf_snew + (size_t)unit * p.max_chunk;                  // [L] the chunk tokens' scores
   int* dest = p.pf_flag + (size_t)unit * (cap + p.max_chunk) + cap;     // [L] 1: the token lost a scope; later: its slot or -1
   int* loser = p.pf_list + (size_t)unit * (cap + p.max_chunk);          // [L] slot freed at eviction step e, or -1
-  int* free_list = loser + L;                                           // [L + 1] freed slots in the order they are handed out
+  int* free_list = loser + L_max;                                       // [L + 1] freed slots in the order they are handed out
   if constexpr (IN_LDS) {
     int* w = rp_smem;
     Eu = w; w += 2 * m;
     PEu = w; w += 2 * m;
     Su = reinterpret_cast<float*>(w); w += cap;
-    snew = reinterpret_cast<float*>(w); w += L;
-    dest = w; w += L;
-    loser = w; w += L;
-    free_list = w; w += L + 1;
+    snew = reinterpret_cast<float*>(w); w += L_max;
+    dest = w; w += L_max;
+    loser = w; w += L_max;
+    free_list = w; w += L_max + 1;
     Ru = w;
   }
 
@@ -1559,8 +1570,10 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
     const int kvh = unit % p.Hkv, b = unit / p.Hkv;
 #pragma unroll
     for (int u = 0; u < HELD; ++u) {
-      const int x = min(u * RP_THREADS + tid, L * row_vec - 1), i = x / row_vec, e = x - i * row_vec;
-      const size_t src = (((size_t)b * L + i) * p.Hkv + kvh) * row_vec + e;
+      const int x = max(min(u * RP_THREADS + tid, L * row_vec - 1), 0), i = x / row_vec, e = x - i * row_vec;
+      size_t row = (size_t)b * L + i;
+      if constexpr (TREE) row = (size_t)b * draft.nodes + (L > 0 ? draft.path[(size_t)b * L_max + i] : 0);
+      const size_t src = (row * p.Hkv + kvh) * row_vec + e;
       k_held[u] = reinterpret_cast<const uint4v_t*>(Kc)[src];
       v_held[u] = reinterpret_cast<const uint4v_t*>(Vc)[src];
     }
@@ -1605,6 +1618,10 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
   const int t_end = t0 + L - 1;            // every count C is t_end - position + 1 once the chunk is in
   const int tev = t0 + F;                  // position of the first evicting token
   for (int i = tid; i < L; i += RP_THREADS) { dest[i] = 0; loser[i] = -1; }
+  if constexpr (TREE) {
+    if (evu)
+      for (int i = L + tid; i < L_max; i += RP_THREADS) evu[i] = -1;
+  }
   __syncthreads();
 
   // ---- tokens that got slots while filling ----
@@ -1616,6 +1633,9 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
   __syncthreads();
 
   int j_final = j0, rhead_final = rhead0, f_final = n0 + F, n_final = n0 + F;
+  if constexpr (TREE) {
+    if (L == 0) f_final = f0;
+  }
   if (Lev > 0) {
     n_final = c;
     const int fstart = F > 0 ? c : f0;     // the one free slot when the evictions start
@@ -1810,12 +1830,12 @@ int launch_replay(const Params& p, const void* K, const void* V, int L, int32_t*
         hip_failed(hipFuncSetAttribute((const void*)replay, hipFuncAttributeMaxDynamicSharedMemorySize, (int)rp_lds)))
       return TREEKV_EHIP;
     hipLaunchKernelGGL(replay, dim3(p.U), dim3(RP_THREADS), rp_lds, s, p, L, (const uint4*)K, (const uint4*)V, row_vec,
-                       retained, n_retained, evicted);
+                       retained, n_retained, evicted, NoPath());
     if (held <= HELD_MAX) return finish_launch();
   } else {
     if (2 * (size_t)L + 1 > (size_t)p.cap + p.max_chunk) return TREEKV_EUNSUPPORTED;   // its lists live in pf_list
     hipLaunchKernelGGL((prefill_replay_kernel<false, 0>), dim3(p.U), dim3(RP_THREADS), 0, s, p, L, (const uint4*)K,
-                       (const uint4*)V, row_vec, retained, n_retained, evicted);
+                       (const uint4*)V, row_vec, retained, n_retained, evicted, NoPath());
   }
   hipLaunchKernelGGL(prefill_scatter_kernel, dim3((L + 256 / row_vec - 1) / (256 / row_vec), p.U), dim3(256), 0, s, p, (const uint4*)K, (const uint4*)V, L, row_vec);
   return finish_launch();
@@ -1928,6 +1948,22 @@ int launch_prefill_f32(const Params& p, const void* Q, const void* K, const void
 }
 
 }  // namespace
+
+int launch_tree_replay(const Params& p, const Tree& t, int32_t* retained, int32_t* n_retained, int32_t* evicted, hipStream_t s) {
+  const int L = t.max_len, row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16;
+  const size_t rp_lds = replay_lds_words(p.m, p.cap, p.n_recent, L) * sizeof(int);
+  static_assert(TREEKV_TREE_MAX_NODES * 32 <= 8 * RP_THREADS, "the longest path's rows fit the pieces held");
+  const int held = (L * row_vec + RP_THREADS - 1) / RP_THREADS;
+  const bool in_lds = rp_lds <= 140 * 1024;        // else the lists live in pf_list: 2 L + 1 words of its cap + max_chunk
+  auto replay = !in_lds ? prefill_replay_kernel<false, 8, true> : held <= 1 ? prefill_replay_kernel<true, 1, true>
+                        : held <= 4 ? prefill_replay_kernel<true, 4, true> : prefill_replay_kernel<true, 8, true>;
+  if (in_lds && rp_lds > 48 * 1024 &&
+      hip_failed(hipFuncSetAttribute((const void*)replay, hipFuncAttributeMaxDynamicSharedMemorySize, (int)rp_lds)))
+    return TREEKV_EHIP;
+  hipLaunchKernelGGL(replay, dim3(p.U), dim3(RP_THREADS), in_lds ? rp_lds : 0, s, p, L, (const uint4*)t.k, (const uint4*)t.v,
+                     row_vec, retained, n_retained, evicted, DraftPath{t.path, t.n});
+  return finish_launch();
+}
 
 int launch_prefill(const Params& p, const void* Q, const void* K, const void* V, int len, float* out,
                    int32_t* retained, int32_t* n_retained, int32_t* evicted, hipStream_t s) {

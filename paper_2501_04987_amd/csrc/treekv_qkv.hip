@@ -1,0 +1,137 @@
+// treekv_qkv_prepare: the heads of q and k normalised and turned, v copied, out of the rows of a projection.
+//
+//   y = R(position) (x / sqrt(mean(x^2) + eps) * w),   R: plane i turned by position * inv_freq[i]
+//
+// A head is D elements in D / 8 (bf16) or D / 4 (fp32) lanes of 16 bytes; the mean of squares is one sum over those lanes,
+// the two dimensions of a plane lie in one lane (2i, 2i+1) or, for halves, rotary_dim / 2 dimensions apart in the same head:
+// one exchange of lanes, since rotary_dim is a multiple of 16.  A token's angles are formed once per workgroup, in double (a
+// position of a million times a frequency near 1 leaves 2^-33 of a turn), reduced to a turn and then to fp32.
+// Bound by memory: every head once in and once out.
+
+#include "treekv_internal.h"
+
+namespace tkv {
+
+namespace {
+
+constexpr int QKV_THREADS = 256;
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+
+__device__ inline uint4 narrow(const float (&y)[8], uint16_t) {
+  unsigned w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2_t v = {y[2 * i], y[2 * i + 1]};
+    w[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2_t));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ inline uint4 narrow(const float (&y)[4], float) {
+  return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int chunks) {
+  constexpr int EPL = Storage<T>::EPL, LPR = D / EPL, ROWS = QKV_THREADS / LPR;
+  __shared__ float2 cs[D / 2];
+  const int tid = threadIdx.x, part = tid % LPR, half = a.rotary_dim / 2;
+  const int nq = a.q ? a.q_heads : 0, nk = a.k ? a.kv_heads : 0, nv = a.v ? a.kv_heads : 0;
+  const long long items = (long long)a.tokens * chunks;
+  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int token = (int)(item / chunks), row = (int)(item % chunks) * ROWS + tid / LPR;
+    const bool live = row < nq + nk + nv;
+    // the row's source, destination and what happens to it
+    const int kind = row < nq ? 0 : row < nq + nk ? 1 : 2;
+    const int head = row - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk);
+    const T* src = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
+                   (long long)token * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) + (long long)head * D;
+    T* dst = (T*)(kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out) +
+             ((long long)token * (kind == 0 ? a.q_heads : a.kv_heads) + head) * D;
+    const T* weight = (const T*)(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
+    uint4 raw = make_uint4(0, 0, 0, 0), wraw = raw;
+    if (live) {
+      raw = reinterpret_cast<const uint4*>(src)[part];
+      if (weight) wraw = reinterpret_cast<const uint4*>(weight)[part];
+    }
+    if (a.positions && tid < half) {
+      // turns: the fraction is exact, whatever the number of whole ones
+      const double turns = (double)a.positions[token] * a.inv_freq[tid] * 0.15915494309189533577;
+      float s, c;
+      sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+      cs[tid] = make_float2(c, s);
+    }
+    __syncthreads();
+    float x[EPL];
+    Storage<T>::widen(raw, x);
+    if (weight) {
+      float sum = 0.f, w[EPL];
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], x[e], sum);
+      const float inv = rsqrtf(group_sum<LPR>(sum) * (1.0f / D) + a.eps);
+      Storage<T>::widen(wraw, w);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * w[e];
+    }
+    int to_part = part;                              // the 16-byte piece of the output this lane writes
+    if (kind < 2 && (a.flags & TREEKV_ROPE_HALVES) && half > 0) {
+      // lanes of the first half hold the first dimensions of planes part * EPL .., those of the second half the second ones
+      const int lanes = half / EPL;
+      const bool turned = part < 2 * lanes, second = part >= lanes;
+      const int other = turned ? (second ? -lanes : lanes) : 0, plane = (second ? part - lanes : part) * EPL;
+      float ya[EPL], yb[EPL];
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) {
+        const float o = __shfl(x[e], (tid & 63) + other, 64);
+        const float2 t = a.positions && turned ? cs[plane + e] : make_float2(1.f, 0.f);
+        const float p0 = second ? o : x[e], p1 = second ? x[e] : o;
+        ya[e] = p0 * t.x - p1 * t.y;
+        yb[e] = p0 * t.y + p1 * t.x;
+      }
+      if (turned) {
+        if (a.flags & TREEKV_ROPE_TO_PLANES) {
+          // planes plane .. plane + EPL - 1 are 2 EPL output dimensions; this lane writes the first or the second EPL of them
+          to_part = 2 * (plane / EPL) + (second ? 1 : 0);
+#pragma unroll
+          for (int e = 0; e < EPL / 2; ++e) {
+            x[2 * e] = second ? ya[EPL / 2 + e] : ya[e];
+            x[2 * e + 1] = second ? yb[EPL / 2 + e] : yb[e];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) x[e] = second ? yb[e] : ya[e];
+        }
+      }
+    } else if (kind < 2 && a.positions && part * EPL < a.rotary_dim) {
+#pragma unroll
+      for (int e = 0; e < EPL; e += 2) {
+        const float2 t = cs[(part * EPL + e) / 2];
+        const float p0 = x[e], p1 = x[e + 1];
+        x[e] = p0 * t.x - p1 * t.y;
+        x[e + 1] = p0 * t.y + p1 * t.x;
+      }
+    }
+    if (live) reinterpret_cast<uint4*>(dst)[to_part] = kind == 2 ? raw : narrow(x, T());
+    __syncthreads();                                 // the next item's angles
+  }
+}
+
+template <typename T, int D>
+int launch_qkv_d(const treekv_qkv_args& a, hipStream_t s) {
+  constexpr int ROWS = QKV_THREADS / (D / Storage<T>::EPL);
+  const int rows = (a.q ? a.q_heads : 0) + (a.k ? a.kv_heads : 0) + (a.v ? a.kv_heads : 0);
+  const int chunks = (rows + ROWS - 1) / ROWS;
+  const long long items = (long long)a.tokens * chunks, most = 1 << 20;
+  hipLaunchKernelGGL((qkv_kernel<T, D>), dim3((unsigned)(items < most ? items : most)), dim3(QKV_THREADS), 0, s, a, chunks);
+  return finish_launch();
+}
+
+}  // namespace
+
+int launch_qkv(const treekv_qkv_args& a, hipStream_t s) {
+  if (a.dtype == TREEKV_F32) return a.head_dim == 128 ? launch_qkv_d<float, 128>(a, s) : launch_qkv_d<float, 64>(a, s);
+  return a.head_dim == 128 ? launch_qkv_d<uint16_t, 128>(a, s) : launch_qkv_d<uint16_t, 64>(a, s);
+}
+
+}  // namespace tkv

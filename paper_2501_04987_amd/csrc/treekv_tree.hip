@@ -1,0 +1,898 @@
+// Drafted trees of TreeKV for gfx950: the attention of treekv_tree_attend and the column sums of treekv_tree_commit.
+//
+// attend   o = SoftMax(q K^T * scale) V for the n nodes of every sequence's tree, over the cached rows, the node's
+//          ancestors and the node.  The n * G query rows of a unit share its K and V, so they are the rows of one matrix
+//          product.  Logits and probabilities are held in fp32; P enters the second product whole: with bf16 storage it
+//          is cut into three bf16 parts (8 + 8 + 8 bits, exact), so nothing of it is rounded.
+// commit   the probabilities of the accepted nodes, p = exp(q K^T * scale - lse), summed down the rows into the column
+//          accumulators of the chunk path, whose replay then evicts.  K is read again (half the bytes of the attention);
+//          keeping the attention's probabilities instead would cost n * G floats a slot.
+//
+// A wave owns blocks of columns (32 cached rows with bf16 storage, 16 with fp32) and takes them from memory straight into
+// registers, in the layout the matrix instructions want: no LDS and no barrier in the loop.
+//   S^T = K Q^T      A operand: lane (r, g) holds 16 bytes of K row r: the row's pieces 4 s + g in step s
+//   O^T += V^T P^T   a lane's logits are columns 4 g + i (+ 16) of row r, which is the B operand as it lies.  The A
+//                    operand wants those columns of one dimension; the lane loads 16 bytes (8 at head_dim 64) of each of
+//                    those rows, that is, its columns of dimensions r * D/16 .. + D/16 - 1, and one byte permutation per
+//                    pair of columns makes the operand of each dimension.
+// Column order is free (attention does not depend on it): cached columns are slots in slot order without the free one, or,
+// with positions re-assigned, logical order, so that column j is at position j.  The tree's own columns follow in blocks of
+// their own, masked by the ancestors' bits.
+//
+// Positions re-assigned: keys are turned in the registers (angles from the context's table), the queries once per workgroup
+// in LDS; with bf16 storage both are cut into three bf16 parts, and a logit is the six products above 2^-24.
+
+#include "treekv_internal.h"
+
+namespace tkv {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+
+constexpr int TR_THREADS = 512, TR_WAVES = TR_THREADS / 64;
+constexpr int MAX_NODES = TREEKV_TREE_MAX_NODES, MAX_WORDS = MAX_NODES / 32;
+constexpr float REF_NONE = -1.0e30f;               // reference of a row that has seen nothing: finite, so that exp2(-inf - it) = 0
+constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
+constexpr float COLSUM_FIX = 1099511627776.0f;      // 2^40: column sums cross kernels as 64-bit fixed point
+constexpr int COLSUM_TILE = 128;                    // their two parts are rounded up to this
+
+__device__ inline f32x4_t mfma_bf16(const uint4& a, const uint4& b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// The high halves of two floats' bits, packed: bf16 by truncation, the first in the low half.
+__device__ inline unsigned high_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ inline float top8(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+// Two fp32 values as bf16 parts whose sum they are: 8 + 8 + 8 bits of the 24.
+__device__ inline void cut3(float a, float b, unsigned& h, unsigned& m, unsigned& l) {
+  const float a1 = a - top8(a), b1 = b - top8(b);
+  h = high_halves(a, b);
+  m = high_halves(a1, b1);
+  l = high_halves(a1 - top8(a1), b1 - top8(b1));
+}
+__device__ inline float row_max(float v) {          // over the four lanes, 16 apart, of a row
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ inline float row_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// The tree of one sequence, worked out by the whole workgroup: bit j of sm.anc[i] says that node i attends node j; `up` is
+// -1 for a node of the tree and -2 for an absent one.  Generations double from round to round.
+struct TreeBits {
+  unsigned anc[MAX_NODES][MAX_WORDS];
+  int up[MAX_NODES];
+};
+__device__ inline void build_tree(TreeBits& sm, const int32_t* parents, int n) {
+  const int i = threadIdx.x, words = (n + 31) / 32;
+  if (i < n) {
+    const int p = parents[i];
+    sm.up[i] = p >= -1 && p < i ? p : -2;
+#pragma unroll
+    for (int w = 0; w < MAX_WORDS; ++w)
+      if (w < words) sm.anc[i][w] = w == i / 32 ? 1u << (i & 31) : 0u;
+  }
+  for (;;) {
+    __syncthreads();
+    const int up = i < n ? sm.up[i] : -1;
+    unsigned bits[MAX_WORDS] = {};
+    int next = up;
+    if (up >= 0) {
+      next = sm.up[up];
+#pragma unroll
+      for (int w = 0; w < MAX_WORDS; ++w)
+        if (w < words) bits[w] = sm.anc[up][w];
+    }
+    if (!__syncthreads_or(up >= 0)) break;
+    if (up >= 0) {
+      sm.up[i] = next;
+#pragma unroll
+      for (int w = 0; w < MAX_WORDS; ++w)
+        if (w < words) sm.anc[i][w] |= bits[w];
+    }
+  }
+}
+__device__ inline int depth_of(const TreeBits& sm, int i, int n) {
+  int d = -1;
+  for (int w = 0; w < (n + 31) / 32; ++w) d += __popc(sm.anc[i][w]);
+  return d;
+}
+
+// What the kernels need to know of a unit.
+template <typename T, int D>
+struct Unit {
+  const T *K, *V;            // cached rows by slot
+  const T *Kn, *Vn;          // the tree's
+  size_t node_stride;        // elements from one node's row to the next
+  int n, fslot, nodes;       // cached tokens, the free slot, nodes
+  const int *E, *R;
+  int rhead, j;              // order arrays' state (logical order)
+};
+template <typename T, int D>
+__device__ inline Unit<T, D> load_unit(const Params& p, const Tree& t, int unit) {
+  const int* meta = p.meta + (size_t)unit * META_STRIDE;
+  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
+  Unit<T, D> u;
+  u.K = (const T*)p.K + (size_t)unit * p.cap * D;
+  u.V = (const T*)p.V + (size_t)unit * p.cap * D;
+  u.node_stride = (size_t)p.Hkv * D;
+  u.Kn = (const T*)t.k + ((size_t)b * t.n * p.Hkv + kvh) * D;
+  u.Vn = (const T*)t.v + ((size_t)b * t.n * p.Hkv + kvh) * D;
+  u.n = __builtin_amdgcn_readfirstlane(meta[META_N]);
+  u.fslot = __builtin_amdgcn_readfirstlane(meta[META_FREE]);
+  u.rhead = __builtin_amdgcn_readfirstlane(meta[META_RHEAD]);
+  u.j = __builtin_amdgcn_readfirstlane(meta[META_J]);
+  u.nodes = t.n;
+  u.E = p.E + (size_t)unit * 2 * p.m;
+  u.R = p.R + (size_t)unit * max(p.n_recent, 1);
+  return u;
+}
+// Slot of cached column c (clamped to the last one: what lies behind is masked).
+template <typename T, int D, bool ROPE>
+__device__ inline int slot_of(const Params& p, const Unit<T, D>& u, int c) {
+  c = min(c, u.n - 1);
+  if (ROPE) return u.n < p.budget ? c : logical_to_slot(p, u.E, u.R, u.rhead, u.j, c);
+  return c + (c >= u.fslot ? 1 : 0);
+}
+
+// Operands by storage type.  COLS: columns of a block.  Parts: bf16 parts of a turned value.
+template <typename T, int D> struct Ops;
+
+template <int D>
+struct Ops<uint16_t, D> {
+  static constexpr int COLS = 32, KS = D / 32, NCOL = 8, DPL = D / 16;     // NCOL: columns a lane holds; DPL: its dimensions
+  struct Keys { uint4 x[2][KS]; };
+  struct Values { uint4 x[8]; };                     // head_dim 64: the first half of each
+  __device__ static inline int col(int q4, int j) { return (j >> 2) * 16 + q4 * 4 + (j & 3); }
+  __device__ static inline void load_k(Keys& k, int bk, const uint16_t* row, int q4) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k.x[bk][s] = *reinterpret_cast<const uint4*>(row + s * 32 + q4 * 8);
+  }
+  __device__ static inline void load_v(Values& v, int j, const uint16_t* row, int lr) {
+    if constexpr (D == 128) v.x[j] = *reinterpret_cast<const uint4*>(row + lr * 8);
+    else {
+      const uint2 r = *reinterpret_cast<const uint2*>(row + lr * 4);
+      v.x[j] = make_uint4(r.x, r.y, 0, 0);
+    }
+  }
+  __device__ static inline void clear_v(Values& v, int j) { v.x[j] = make_uint4(0, 0, 0, 0); }
+  __device__ static inline unsigned word(const uint4& r, int w) { return w == 0 ? r.x : w == 1 ? r.y : w == 2 ? r.z : r.w; }
+  // the operand of dimension e: its NCOL columns
+  __device__ static inline uint4 dim(const Values& v, int e) {
+    const unsigned sel = (e & 1) ? 0x07060302u : 0x05040100u;
+    return make_uint4(__builtin_amdgcn_perm(word(v.x[1], e >> 1), word(v.x[0], e >> 1), sel),
+                      __builtin_amdgcn_perm(word(v.x[3], e >> 1), word(v.x[2], e >> 1), sel),
+                      __builtin_amdgcn_perm(word(v.x[5], e >> 1), word(v.x[4], e >> 1), sel),
+                      __builtin_amdgcn_perm(word(v.x[7], e >> 1), word(v.x[6], e >> 1), sel));
+  }
+  static constexpr int QPARTS = 3;                   // of a turned query
+  // queries of one block of 16 rows, from memory (ROPE: from LDS, three parts of `part` elements)
+  struct Query { uint4 x[KS]; };
+  __device__ static inline void load_q(Query& q, const uint16_t* row, int q4) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q.x[s] = *reinterpret_cast<const uint4*>(row + s * 32 + q4 * 8);
+  }
+  struct Logits { f32x4_t x[2]; };
+  __device__ static inline float& at(Logits& s, int j) { return reinterpret_cast<float*>(&s)[j]; }
+};
+
+template <int D>
+struct Ops<float, D> {
+  static constexpr int COLS = 16, KS = D / 16, NCOL = 4, DPL = D / 16;
+  struct Keys { float4 x[1][KS]; };
+  struct Values { float x[4][DPL]; };
+  __device__ static inline int col(int q4, int j) { return q4 * 4 + j; }
+  __device__ static inline void load_k(Keys& k, int, const float* row, int q4) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k.x[0][s] = *reinterpret_cast<const float4*>(row + s * 16 + q4 * 4);
+  }
+  __device__ static inline void load_v(Values& v, int j, const float* row, int lr) {
+#pragma unroll
+    for (int e = 0; e < DPL; e += 4) {
+      const float4 r = *reinterpret_cast<const float4*>(row + lr * DPL + e);
+      v.x[j][e] = r.x; v.x[j][e + 1] = r.y; v.x[j][e + 2] = r.z; v.x[j][e + 3] = r.w;
+    }
+  }
+  __device__ static inline void clear_v(Values& v, int j) {
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) v.x[j][e] = 0.f;
+  }
+  static constexpr int QPARTS = 1;
+  struct Query { float4 x[KS]; };
+  __device__ static inline void load_q(Query& q, const float* row, int q4) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q.x[s] = *reinterpret_cast<const float4*>(row + s * 16 + q4 * 4);
+  }
+  struct Logits { f32x4_t x[1]; };
+  __device__ static inline float& at(Logits& s, int j) { return reinterpret_cast<float*>(&s)[j]; }
+};
+
+// Turned queries in LDS: QPARTS images of `rows` rows of D elements, rows padded against bank conflicts.
+template <typename T, int D>
+constexpr int q_row_elems() { return D + 16 / (int)sizeof(T); }
+
+// S^T of one block of columns against one block of 16 rows.
+template <int D>
+__device__ inline void logits(typename Ops<uint16_t, D>::Logits& s, const typename Ops<uint16_t, D>::Keys& k,
+                              const typename Ops<uint16_t, D>::Query& q) {
+#pragma unroll
+  for (int bk = 0; bk < 2; ++bk) {
+    s.x[bk] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) s.x[bk] = mfma_bf16(k.x[bk][x], q.x[x], s.x[bk]);
+  }
+}
+template <int D>
+__device__ inline void logits(typename Ops<float, D>::Logits& s, const typename Ops<float, D>::Keys& k,
+                              const typename Ops<float, D>::Query& q) {
+  f32x4_t a = {0.f, 0.f, 0.f, 0.f}, c = a;
+#pragma unroll
+  for (int x = 0; x < D / 16; ++x) {
+    a = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[0][x].x, q.x[x].x, a, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[0][x].y, q.x[x].y, c, 0, 0, 0);
+    a = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[0][x].z, q.x[x].z, a, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[0][x].w, q.x[x].w, c, 0, 0, 0);
+  }
+  s.x[0] = a + c;
+}
+
+// One 16-byte piece turned: pairs (2i, 2i+1) by the angles at `cs` (the piece's planes, in order).
+__device__ inline void turn_piece(const uint4& raw, const float2* cs, float (&y)[8]) {
+  const float4 c01 = reinterpret_cast<const float4*>(cs)[0], c23 = reinterpret_cast<const float4*>(cs)[1];
+  const float co[4] = {c01.x, c01.z, c23.x, c23.z}, si[4] = {c01.y, c01.w, c23.y, c23.w};
+  float x[8];
+  Storage<uint16_t>::widen(raw, x);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    y[2 * e] = x[2 * e] * co[e] - x[2 * e + 1] * si[e];
+    y[2 * e + 1] = x[2 * e] * si[e] + x[2 * e + 1] * co[e];
+  }
+}
+__device__ inline float4 turn_piece(const float4& x, const float2* cs) {
+  const float4 c = *reinterpret_cast<const float4*>(cs);
+  return make_float4(x.x * c.x - x.y * c.y, x.x * c.y + x.y * c.x, x.z * c.z - x.w * c.w, x.z * c.w + x.w * c.z);
+}
+__device__ inline void cut_piece(const float (&y)[8], uint4& h, uint4& m, uint4& l) {
+  cut3(y[0], y[1], h.x, m.x, l.x);
+  cut3(y[2], y[3], h.y, m.y, l.y);
+  cut3(y[4], y[5], h.z, m.z, l.z);
+  cut3(y[6], y[7], h.w, m.w, l.w);
+}
+
+// The same with positions re-assigned, RB blocks of rows at once (turning the keys is the larger part): `pos[bk]` is the
+// position of this lane's key row, `qs` its query row of the first block in LDS (16 rows and QPARTS images further for the
+// others).
+template <int D, int RB>
+__device__ inline void turned_logits(typename Ops<uint16_t, D>::Logits (&s)[RB], const typename Ops<uint16_t, D>::Keys& k,
+                                     const float2* tab, const int (&pos)[2], const uint16_t* qs, int part, int q4) {
+  constexpr int QR = q_row_elems<uint16_t, D>();
+#pragma unroll
+  for (int bk = 0; bk < 2; ++bk) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) s[rb].x[bk] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const float2* cs = tab + (size_t)pos[bk] * (D / 2) + q4 * 4;
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+      float y[8];
+      uint4 kh, km, kl;
+      turn_piece(k.x[bk][x], cs + x * 16, y);
+      cut_piece(y, kh, km, kl);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const uint16_t* q = qs + rb * 16 * QR + x * 32 + q4 * 8;
+        const uint4 qh = *reinterpret_cast<const uint4*>(q), qm = *reinterpret_cast<const uint4*>(q + part),
+                    ql = *reinterpret_cast<const uint4*>(q + 2 * part);
+        f32x4_t a = s[rb].x[bk];
+        a = mfma_bf16(kl, qh, a);
+        a = mfma_bf16(kh, ql, a);
+        a = mfma_bf16(km, qm, a);
+        a = mfma_bf16(km, qh, a);
+        a = mfma_bf16(kh, qm, a);
+        s[rb].x[bk] = mfma_bf16(kh, qh, a);
+      }
+    }
+  }
+}
+template <int D, int RB>
+__device__ inline void turned_logits(typename Ops<float, D>::Logits (&s)[RB], const typename Ops<float, D>::Keys& k,
+                                     const float2* tab, const int (&pos)[1], const float* qs, int, int q4) {
+  constexpr int QR = q_row_elems<float, D>();
+  typename Ops<float, D>::Keys y;
+#pragma unroll
+  for (int x = 0; x < D / 16; ++x) y.x[0][x] = turn_piece(k.x[0][x], tab + (size_t)pos[0] * (D / 2) + x * 8 + q4 * 2);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    typename Ops<float, D>::Query q;
+    Ops<float, D>::load_q(q, qs + rb * 16 * QR, q4);
+    logits<D>(s[rb], y, q);
+  }
+}
+
+// Turned queries of the workgroup's rows into LDS; `row(r)` gives a row's source and position.
+template <typename T, int D, class RowFn>
+__device__ inline void stage_turned(T* sq, int rows, int part, const float2* tab, RowFn row) {
+  constexpr int EPL = Storage<T>::EPL, PIECES = D / EPL, QR = q_row_elems<T, D>();
+  for (int x = threadIdx.x; x < rows * PIECES; x += blockDim.x) {
+    const int r = x / PIECES, piece = x % PIECES;
+    const T* src;
+    int pos;
+    row(r, src, pos);
+    const float2* cs = tab + (size_t)pos * (D / 2) + piece * (EPL / 2);
+    T* dst = sq + r * QR + piece * EPL;
+    if constexpr (sizeof(T) == 2) {
+      float y[8];
+      uint4 h, m, l;
+      turn_piece(reinterpret_cast<const uint4*>(src)[piece], cs, y);
+      cut_piece(y, h, m, l);
+      *reinterpret_cast<uint4*>(dst) = h;
+      *reinterpret_cast<uint4*>(dst + part) = m;
+      *reinterpret_cast<uint4*>(dst + 2 * part) = l;
+    } else {
+      *reinterpret_cast<float4*>(dst) = turn_piece(reinterpret_cast<const float4*>(src)[piece], cs);
+    }
+  }
+}
+
+// O^T += V^T P^T for one block of rows; the probabilities are used up.
+template <int D>
+__device__ inline void add_values(f32x4_t (&o)[D / 16], const typename Ops<uint16_t, D>::Values& v,
+                                  const typename Ops<uint16_t, D>::Logits& p) {
+  uint4 h, m, l;
+  cut3(p.x[0][0], p.x[0][1], h.x, m.x, l.x);
+  cut3(p.x[0][2], p.x[0][3], h.y, m.y, l.y);
+  cut3(p.x[1][0], p.x[1][1], h.z, m.z, l.z);
+  cut3(p.x[1][2], p.x[1][3], h.w, m.w, l.w);
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) {
+    const uint4 a = Ops<uint16_t, D>::dim(v, e);
+    o[e] = mfma_bf16(a, l, o[e]);
+    o[e] = mfma_bf16(a, m, o[e]);
+    o[e] = mfma_bf16(a, h, o[e]);
+  }
+}
+template <int D>
+__device__ inline void add_values(f32x4_t (&o)[D / 16], const typename Ops<float, D>::Values& v,
+                                  const typename Ops<float, D>::Logits& p) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x[j][e], p.x[0][j], o[e], 0, 0, 0);
+}
+
+// Infinities and NaNs among a block's values.  A probability of zero times one of them is a NaN, so a node that a row does
+// not attend must not bring them in: they are taken out of V, and what the rows that do attend them get is added from
+// counts.  A count is the product of "attended" (1 or 0) and a code: 1 for +inf, 2^9 for -inf, 2^18 for NaN (sums over 32
+// columns stay exact).
+__device__ inline bool not_finite_bits(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u; }
+__device__ inline float code_of(unsigned bits) {     // of an fp32 pattern that is not finite
+  return (bits & 0x007fffffu) ? 262144.0f : (bits >> 31) ? 512.0f : 1.0f;
+}
+__device__ inline float decode_counts(float c) {     // what those counts add to a finite sum
+  if (c == 0.f) return 0.f;
+  if (c >= 262144.0f) return __builtin_nanf("");
+  const int k = (int)c;
+  const bool plus = (k & 511) != 0, minus = k >= 512;
+  return plus ? (minus ? __builtin_nanf("") : INFINITY) : -INFINITY;
+}
+template <int D>
+__device__ inline bool any_not_finite(const typename Ops<uint16_t, D>::Values& v) {
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int w = 0; w < (D == 128 ? 4 : 2); ++w) {
+      const unsigned x = Ops<uint16_t, D>::word(v.x[j], w);
+      bad |= not_finite_bits(x) || not_finite_bits(x << 16);
+    }
+  return __any(bad);
+}
+template <int D>
+__device__ inline bool any_not_finite(const typename Ops<float, D>::Values& v) {
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) bad |= not_finite_bits(__float_as_uint(v.x[j][e]));
+  return __any(bad);
+}
+// Takes them out of v and leaves their codes in c.
+template <int D>
+__device__ inline void part_not_finite(typename Ops<uint16_t, D>::Values& v, typename Ops<uint16_t, D>::Values& c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    unsigned w[4] = {v.x[j].x, v.x[j].y, v.x[j].z, v.x[j].w}, k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned lo = w[i] << 16, hi = w[i] & 0xffff0000u;
+      const bool bl = not_finite_bits(lo), bh = not_finite_bits(hi);
+      k[i] = (bl ? __float_as_uint(code_of(lo)) >> 16 : 0u) | (bh ? __float_as_uint(code_of(hi)) : 0u);
+      w[i] = (bl ? 0u : lo >> 16) | (bh ? 0u : hi);
+    }
+    v.x[j] = make_uint4(w[0], w[1], w[2], w[3]);
+    c.x[j] = make_uint4(k[0], k[1], k[2], k[3]);
+  }
+}
+template <int D>
+__device__ inline void part_not_finite(typename Ops<float, D>::Values& v, typename Ops<float, D>::Values& c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      const unsigned x = __float_as_uint(v.x[j][e]);
+      c.x[j][e] = not_finite_bits(x) ? code_of(x) : 0.f;
+      v.x[j][e] = not_finite_bits(x) ? 0.f : v.x[j][e];
+    }
+}
+
+// Scratch of a call: one partial result per (unit, row tile, slice): [rows][D] sums relative to the row's reference, then
+// [rows][2] reference and sum.
+struct Shape {
+  int rows_per_tile, row_tiles, slices;
+};
+
+// grid: row tiles x slices x units (remapped so that what reads the same rows shares an XCD's L2).  RB: blocks of 16 rows.
+template <typename T, int D, int RB, bool ROPE>
+__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tree t, int row_tiles, int slices,
+                                                                    float* __restrict__ out, float* __restrict__ lse,
+                                                                    float* __restrict__ scratch) {
+  using O = Ops<T, D>;
+  constexpr int ROWS = RB * 16, DPL = O::DPL, OR = D + 4;        // OR: floats of a row of sums in LDS
+  extern __shared__ __attribute__((aligned(16))) float tr_smem[];
+  __shared__ TreeBits tree;
+  const int items = row_tiles * slices * p.U, per_xcd = (items + 7) / 8;
+  const int item = ((int)blockIdx.x % 8) * per_xcd + (int)blockIdx.x / 8;
+  if (item >= items) return;
+  const int tile = item % row_tiles, slice = item / row_tiles % slices, unit = item / (row_tiles * slices);
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
+  const Unit<T, D> u = load_unit<T, D>(p, t, unit);
+  const int rows = t.n * p.G;
+  const int cache_blocks = (u.n + O::COLS - 1) / O::COLS, blocks = cache_blocks + (t.n + O::COLS - 1) / O::COLS;
+  const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
+
+  build_tree(tree, t.parents + (size_t)b * t.n, t.n);
+
+  // this lane's rows (clamped: rows behind the last repeat it and are not written)
+  int node[RB];
+  const T* q_row[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = min(tile * ROWS + rb * 16 + lr, rows - 1);
+    node[rb] = r / p.G;
+    q_row[rb] = (const T*)t.q + (((size_t)b * t.n + node[rb]) * p.H + kvh * p.G + r % p.G) * D;
+  }
+  constexpr int QR = q_row_elems<T, D>(), Q_PART = ROWS * QR;
+  typename O::Query q[RB];
+  T* sq = reinterpret_cast<T*>(tr_smem);
+  if constexpr (ROPE) {
+    stage_turned<T, D>(sq, ROWS, Q_PART, p.rope_tab, [&](int r, const T*& src, int& pos) {
+      r = min(tile * ROWS + r, rows - 1);
+      const int i = r / p.G;
+      src = (const T*)t.q + (((size_t)b * t.n + i) * p.H + kvh * p.G + r % p.G) * D;
+      pos = u.n + depth_of(tree, i, t.n);
+    });
+    __syncthreads();
+  } else {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) O::load_q(q[rb], q_row[rb], q4);
+  }
+
+  f32x4_t o[RB][DPL];
+  float ref[RB], sum[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    ref[rb] = REF_NONE;
+    sum[rb] = 0.f;
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) o[rb][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sc = p.scale_log2e;
+
+  constexpr int BK = O::COLS / 16;
+  typename O::Keys k;
+  typename O::Values v;
+  auto load_keys = [&](int blk) {
+#pragma unroll
+    for (int bk = 0; bk < BK; ++bk) {
+      const T* row;
+      if (blk < cache_blocks) row = u.K + (size_t)slot_of<T, D, ROPE>(p, u, blk * O::COLS + bk * 16 + lr) * D;
+      else row = u.Kn + (size_t)min((blk - cache_blocks) * O::COLS + bk * 16 + lr, t.n - 1) * u.node_stride;
+      O::load_k(k, bk, row, q4);
+    }
+  };
+  auto load_values = [&](int blk) {
+#pragma unroll
+    for (int j = 0; j < O::NCOL; ++j) {
+      const T* row;
+      if (blk < cache_blocks) row = u.V + (size_t)slot_of<T, D, ROPE>(p, u, blk * O::COLS + O::col(q4, j)) * D;
+      else row = u.Vn + (size_t)min((blk - cache_blocks) * O::COLS + O::col(q4, j), t.n - 1) * u.node_stride;
+      O::load_v(v, j, row, lr);
+    }
+  };
+
+  if (begin + wave < end) {
+    load_keys(begin + wave);
+    load_values(begin + wave);
+  }
+  for (int blk = begin + wave; blk < end; blk += TR_WAVES) {
+    const bool cached = blk < cache_blocks;
+    const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS;
+    typename O::Logits s[RB];
+    if constexpr (ROPE) {
+      int pos[BK];
+#pragma unroll
+      for (int bk = 0; bk < BK; ++bk) {
+        const int c = col0 + bk * 16 + lr;
+        pos[bk] = cached ? min(c, u.n - 1) : u.n + depth_of(tree, min(c, t.n - 1), t.n);
+      }
+      turned_logits<D, RB>(s, k, p.rope_tab, pos, sq + lr * QR, Q_PART, q4);
+    } else {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) logits<D>(s[rb], k, q[rb]);
+    }
+    const int next = blk + TR_WAVES;
+    if (next < end) load_keys(next);
+    // what a row does not attend
+    if (cached && col0 + O::COLS > u.n) {
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) {
+        const bool hidden = col0 + O::col(q4, j) >= u.n;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+          if (hidden) O::at(s[rb], j) = -INFINITY;
+        if (hidden) O::clear_v(v, j);
+      }
+    }
+    if (!cached) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (col0 & 31);
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j)
+          if (!(bits >> O::col(q4, j) & 1)) O::at(s[rb], j) = -INFINITY;
+      }
+    }
+    // The reference need not be the maximum: it is raised when a row's sum passes 2^16 (or overflows, as at first), so the
+    // common path has no maxima and no rescaling.
+    float fresh_sum[RB];
+    typename O::Logits e[RB];
+    float worst = 0.f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      fresh_sum[rb] = sum[rb];
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) {
+        O::at(e[rb], j) = fast_exp2(fmaf(O::at(s[rb], j), sc, -ref[rb]));
+        fresh_sum[rb] += O::at(e[rb], j);
+      }
+      worst = fmaxf(worst, fresh_sum[rb]);
+    }
+    if (__any(worst > 0x1p16f)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float top = O::at(s[rb], 0);
+#pragma unroll
+        for (int j = 1; j < O::NCOL; ++j) top = fmaxf(top, O::at(s[rb], j));
+        const float raised = row_max(fmaxf(ref[rb], top * sc)), by = fast_exp2(ref[rb] - raised);
+        fresh_sum[rb] = sum[rb] * by;
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) {
+          O::at(e[rb], j) = fast_exp2(fmaf(O::at(s[rb], j), sc, -raised));
+          fresh_sum[rb] += O::at(e[rb], j);
+        }
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) o[rb][d] *= by;
+        ref[rb] = raised;
+      }
+    }
+    if (!cached && any_not_finite<D>(v)) {              // (after the raise, which would make a NaN of an infinity)
+      typename O::Values codes;
+      part_not_finite<D>(v, codes);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (col0 & 31);
+        typename O::Logits attended;
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) O::at(attended, j) = (bits >> O::col(q4, j) & 1) ? 1.f : 0.f;
+        f32x4_t count[DPL];
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) count[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        add_values<D>(count, codes, attended);
+#pragma unroll
+        for (int e = 0; e < DPL; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[rb][e][i] += decode_counts(count[e][i]);
+      }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      sum[rb] = fresh_sum[rb];
+      add_values<D>(o[rb], v, e[rb]);
+    }
+    if (next < end) load_values(next);
+  }
+
+  // ---- the waves' sums added: [wave][row][D] and [wave][row] reference and sum ----
+  float* so = tr_smem;
+  float2* sm = reinterpret_cast<float2*>(tr_smem + TR_WAVES * ROWS * OR);
+  __syncthreads();                                   // the queries' LDS is free
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = rb * 16 + lr;
+    const float l = row_sum(sum[rb]);
+    if (q4 == 0) sm[wave * ROWS + r] = make_float2(ref[rb], l);
+    float* dst = so + ((size_t)wave * ROWS + r) * OR + q4 * 4 * DPL;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < DPL; e += 4)
+        *reinterpret_cast<float4*>(dst + i * DPL + e) = make_float4(o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]);
+  }
+  __syncthreads();
+  for (int x = tid; x < ROWS * (D / 4); x += TR_THREADS) {
+    const int r = x / (D / 4), c = x % (D / 4) * 4, row = tile * ROWS + r;
+    if (row >= rows) break;
+    float M = REF_NONE, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < TR_WAVES; ++w) M = fmaxf(M, sm[w * ROWS + r].x);
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < TR_WAVES; ++w) {
+      const float2 ml = sm[w * ROWS + r];
+      const float f = fast_exp2(ml.x - M);
+      const float4 y = *reinterpret_cast<const float4*>(so + ((size_t)w * ROWS + r) * OR + c);
+      L = fmaf(ml.y, f, L);
+      a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
+    }
+    const int i = row / p.G;
+    const bool present = tree.up[i] == -1;
+    if (slices > 1) {
+      float* part = scratch + (((size_t)unit * row_tiles + tile) * slices + slice) * ROWS * (D + 4) + (size_t)r * (D + 4);
+      *reinterpret_cast<float4*>(part + c) = a;
+      if (c == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, present ? L : -1.f);   // below 0: the row is absent
+    } else {
+      const size_t at = ((size_t)b * t.n + i) * p.H + kvh * p.G + row % p.G;
+      const float inv = 1.0f / L;
+      *reinterpret_cast<float4*>(out + at * D + c) =
+          present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c == 0 && lse) lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
+    }
+  }
+}
+
+// The slices' partial results of one query row, added: a row takes D / 4 lanes.
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(Params p, int n, int rows_per_tile, int row_tiles, int slices,
+                                                         const float* __restrict__ scratch, float* __restrict__ out,
+                                                         float* __restrict__ lse) {
+  const int rows = n * p.G, unit = blockIdx.y;
+  const int row = blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4), c = threadIdx.x % (D / 4) * 4;
+  if (row >= rows) return;
+  const int tile = row / rows_per_tile, r = row % rows_per_tile;
+  const float* part = scratch + ((size_t)unit * row_tiles + tile) * slices * rows_per_tile * (D + 4) + (size_t)r * (D + 4);
+  const size_t step = (size_t)rows_per_tile * (D + 4);
+  float M = REF_NONE, L = 0.f;
+  for (int s = 0; s < slices; ++s) M = fmaxf(M, part[s * step + D]);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  bool present = true;
+  for (int s = 0; s < slices; ++s) {
+    const float2 ml = *reinterpret_cast<const float2*>(part + s * step + D);
+    const float4 y = *reinterpret_cast<const float4*>(part + s * step + c);
+    const float f = fast_exp2(ml.x - M);
+    present = present && !(ml.y < 0.f);
+    L = fmaf(ml.y, f, L);
+    a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
+  }
+  const int b = unit / p.Hkv, kvh = unit % p.Hkv;
+  const size_t at = ((size_t)b * n + row / p.G) * p.H + kvh * p.G + row % p.G;
+  const float inv = 1.0f / L;
+  *reinterpret_cast<float4*>(out + at * D + c) =
+      present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c == 0 && lse) lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------
+// commit: column sums of the path's rows
+// ---------------------------------------------------------------------------------------------
+constexpr int CS_ROWS = 64;                          // query rows taken at a time
+
+// Tokens of sequence b's path, -1 if it is none; every thread gets the answer.
+__device__ inline int path_length(const Tree& t, int b) {
+  const int len = t.path_len[b];
+  bool ok = len >= 0 && len <= t.max_len;
+  const int i = threadIdx.x;
+  if (ok && i < len) {
+    const int node = t.path[(size_t)b * t.max_len + i], before = i > 0 ? t.path[(size_t)b * t.max_len + i - 1] : -1;
+    ok = node > before && node >= 0 && node < t.n;   // (a parent comes before its child)
+    if (ok) ok = t.parents[(size_t)b * t.n + node] == before;
+  }
+  return __syncthreads_and(ok) ? len : -1;
+}
+
+// grid (slices, U).  A column belongs to one lane group of one wave for the whole call, so its accumulator is added to
+// without atomics.
+template <typename T, int D, bool ROPE>
+__global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tree t, int slices, int32_t* __restrict__ status) {
+  using O = Ops<T, D>;
+  constexpr int QR = q_row_elems<T, D>(), Q_PART = CS_ROWS * QR, BK = O::COLS / 16;
+  static_assert(TR_THREADS >= MAX_NODES, "one thread per token of the path");
+  extern __shared__ __attribute__((aligned(16))) float tr_smem[];
+  __shared__ float row_lse[CS_ROWS];
+  const int slice = blockIdx.x, unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
+  const Unit<T, D> u = load_unit<T, D>(p, t, unit);
+  const int found = path_length(t, b), L = max(found, 0);
+  const int* path = t.path + (size_t)b * t.max_len;
+  if (slice == 0 && tid == 0) {
+    p.meta[(size_t)unit * META_STRIDE + META_PATH] = L;
+    if (status && kvh == 0) status[b] = found < 0 ? TREEKV_EINVAL : TREEKV_OK;
+  }
+  if (L == 0) return;
+  const int rows = L * p.G;
+  const int cache_blocks = (u.n + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
+  const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
+  const int cap_cols = (p.cap + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
+  const int cs_stride = cap_cols + (p.max_chunk + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
+  unsigned long long* acc = p.pf_colacc + (size_t)unit * cs_stride;
+  T* sq = reinterpret_cast<T*>(tr_smem);
+  for (int r0 = 0; r0 < rows; r0 += CS_ROWS) {
+    const int here = min(CS_ROWS, rows - r0), tiles = (here + 15) / 16;
+    __syncthreads();                                 // the rows before are done with
+    auto row_of = [&](int r, const T*& src, int& i) {
+      r = min(r0 + r, rows - 1);
+      i = r / p.G;
+      src = (const T*)t.q + (((size_t)b * t.n + path[i]) * p.H + kvh * p.G + r % p.G) * D;
+    };
+    if constexpr (ROPE) {
+      stage_turned<T, D>(sq, tiles * 16, Q_PART, p.rope_tab, [&](int r, const T*& src, int& pos) {
+        row_of(r, src, pos);
+        pos += u.n;
+      });
+    } else {
+      constexpr int PIECES = D / Storage<T>::EPL;
+      for (int x = tid; x < tiles * 16 * PIECES; x += TR_THREADS) {
+        const T* src;
+        int i;
+        row_of(x / PIECES, src, i);
+        *reinterpret_cast<uint4*>(sq + (x / PIECES) * QR + (x % PIECES) * Storage<T>::EPL) = reinterpret_cast<const uint4*>(src)[x % PIECES];
+      }
+    }
+    if (tid < CS_ROWS) {
+      const int r = min(r0 + tid, rows - 1), i = r / p.G;
+      row_lse[tid] = t.lse[((size_t)b * t.n + path[i]) * p.H + kvh * p.G + r % p.G] * LOG2E;
+    }
+    __syncthreads();
+    for (int blk = begin + wave; blk < end; blk += TR_WAVES) {
+      const bool cached = blk < cache_blocks;
+      const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS;
+      typename O::Keys k;
+      int pos[BK];
+#pragma unroll
+      for (int bk = 0; bk < BK; ++bk) {
+        const int c = col0 + bk * 16 + lr;
+        const T* row;
+        if (cached) row = u.K + (size_t)slot_of<T, D, ROPE>(p, u, c) * D;
+        else row = u.Kn + (size_t)path[min(c, L - 1)] * u.node_stride;
+        pos[bk] = cached ? min(c, u.n - 1) : u.n + min(c, L - 1);
+        O::load_k(k, bk, row, q4);
+      }
+      float col_sum[O::NCOL];
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) col_sum[j] = 0.f;
+      for (int tile = 0; tile < tiles; ++tile) {
+        typename O::Logits s[1];
+        if constexpr (ROPE) {
+          turned_logits<D, 1>(s, k, p.rope_tab, pos, sq + (tile * 16 + lr) * QR, Q_PART, q4);
+        } else {
+          typename O::Query q;
+          O::load_q(q, sq + (tile * 16 + lr) * QR, q4);
+          logits<D>(s[0], k, q);
+        }
+        const int r = r0 + tile * 16 + lr, i = r / p.G;
+        const float l2 = row_lse[tile * 16 + lr];
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) {
+          const int c = col0 + O::col(q4, j);
+          const bool seen = r < rows && (cached ? c < u.n : c <= i);
+          const float e = fast_exp2(fmaf(O::at(s[0], j), p.scale_log2e, -l2));
+          col_sum[j] += seen ? e : 0.f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) {
+        const float x = group_sum<16>(col_sum[j]);
+        const int c = col0 + O::col(q4, j);
+        if (lr == j && (cached ? c < u.n : c < L)) {
+          unsigned long long* a = acc + (cached ? slot_of<T, D, ROPE>(p, u, c) : cap_cols + c);
+          *a += (unsigned long long)(long long)(x * COLSUM_FIX + 0.5f);
+        }
+      }
+    }
+  }
+}
+
+// Slices of a unit's columns: as many workgroups as the chip has compute units, each wave with a block at least.
+int pick_slices(const Params& p, int units_times_tiles, int blocks) {
+  int s = 256 / units_times_tiles;
+  const int most = (blocks + TR_WAVES - 1) / TR_WAVES;
+  s = s > most ? most : s;
+  return s < 1 ? 1 : s;
+}
+int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
+
+Shape attend_shape(const Params& p, int n) {
+  Shape s;
+  const int rows = n * p.G, cols = block_cols(p);
+  s.rows_per_tile = rows <= 16 ? 16 : 32;
+  s.row_tiles = (rows + s.rows_per_tile - 1) / s.rows_per_tile;
+  s.slices = pick_slices(p, p.U * s.row_tiles, (p.budget + cols - 1) / cols + (n + cols - 1) / cols);
+  return s;
+}
+
+template <typename T, int D, int RB, bool ROPE>
+int launch_attend_rb(const Params& p, const Tree& t, const Shape& s, float* out, float* lse, float* scratch, hipStream_t st) {
+  const size_t sums = (size_t)TR_WAVES * RB * 16 * ((D + 4) * sizeof(float) + sizeof(float2));
+  const size_t queries = ROPE ? (size_t)Ops<T, D>::QPARTS * RB * 16 * q_row_elems<T, D>() * sizeof(T) : 0;
+  const size_t lds = sums > queries ? sums : queries;
+  auto kernel = tree_attend_kernel<T, D, RB, ROPE>;
+  if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
+  const int items = s.row_tiles * s.slices * p.U;
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, p, t, s.row_tiles, s.slices, out, lse, scratch);
+  if (s.slices > 1) {
+    constexpr int PER = 256 / (D / 4);
+    hipLaunchKernelGGL(tree_merge_kernel<D>, dim3((t.n * p.G + PER - 1) / PER, p.U), dim3(256), 0, st, p, t.n, s.rows_per_tile,
+                       s.row_tiles, s.slices, scratch, out, lse);
+  }
+  return finish_launch();
+}
+template <typename T, int D>
+int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, float* scratch, hipStream_t st) {
+  const Shape s = attend_shape(p, t.n);
+  const bool rope = (p.flags & TREEKV_POSITION_RERANK) != 0;
+  if (s.rows_per_tile == 16)
+    return rope ? launch_attend_rb<T, D, 1, true>(p, t, s, out, lse, scratch, st) : launch_attend_rb<T, D, 1, false>(p, t, s, out, lse, scratch, st);
+  return rope ? launch_attend_rb<T, D, 2, true>(p, t, s, out, lse, scratch, st) : launch_attend_rb<T, D, 2, false>(p, t, s, out, lse, scratch, st);
+}
+
+template <typename T, int D, bool ROPE>
+int launch_colsums_d(const Params& p, const Tree& t, int32_t* status, hipStream_t st) {
+  const size_t lds = (size_t)(ROPE ? Ops<T, D>::QPARTS : 1) * CS_ROWS * q_row_elems<T, D>() * sizeof(T);
+  const int cols = block_cols(p), slices = pick_slices(p, p.U, (p.budget + cols - 1) / cols + (t.max_len + cols - 1) / cols);
+  auto kernel = tree_colsum_kernel<T, D, ROPE>;
+  if (lds > 48 * 1024 &&
+      hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)))
+    return TREEKV_EHIP;
+  hipLaunchKernelGGL(kernel, dim3(slices, p.U), dim3(TR_THREADS), lds, st, p, t, slices, status);
+  return finish_launch();
+}
+template <typename T, int D>
+int launch_colsums_t(const Params& p, const Tree& t, int32_t* status, hipStream_t st) {
+  return (p.flags & TREEKV_POSITION_RERANK) ? launch_colsums_d<T, D, true>(p, t, status, st) : launch_colsums_d<T, D, false>(p, t, status, st);
+}
+
+}  // namespace
+
+size_t tree_scratch_bytes(const Params& p, int n) {
+  const Shape s = attend_shape(p, n);
+  return s.slices > 1 ? align_up((size_t)p.U * s.row_tiles * s.slices * s.rows_per_tile * (p.D + 4) * sizeof(float)) : 0;
+}
+
+int launch_tree_attend(const Params& p, const Tree& t, float* out, float* lse, void* scratch, hipStream_t s) {
+  float* sc = static_cast<float*>(scratch);
+  if (p.dtype == TREEKV_F32) return p.D == 128 ? launch_attend_d<float, 128>(p, t, out, lse, sc, s) : launch_attend_d<float, 64>(p, t, out, lse, sc, s);
+  return p.D == 128 ? launch_attend_d<uint16_t, 128>(p, t, out, lse, sc, s) : launch_attend_d<uint16_t, 64>(p, t, out, lse, sc, s);
+}
+
+int launch_tree_colsums(const Params& p, const Tree& t, int32_t* status, hipStream_t s) {
+  if (p.dtype == TREEKV_F32) return p.D == 128 ? launch_colsums_t<float, 128>(p, t, status, s) : launch_colsums_t<float, 64>(p, t, status, s);
+  return p.D == 128 ? launch_colsums_t<uint16_t, 128>(p, t, status, s) : launch_colsums_t<uint16_t, 64>(p, t, status, s);
+}
+
+}  // namespace tkv
