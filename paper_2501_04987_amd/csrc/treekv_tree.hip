@@ -15,7 +15,7 @@
 //                    operand wants those columns of one dimension; the lane loads 16 bytes (8 at head_dim 64) of each of
 //                    those rows, that is, its columns of dimensions r * D/16 .. + D/16 - 1, and one byte permutation per
 //                    pair of columns makes the operand of each dimension.
-// Column order is free (attention does not depend on it): cached columns are slots in slot order without the free one, or,
+// Column order is free (attention does not depend on it): cached columns are slots in slot order, the free one masked, or,
 // with positions re-assigned, logical order, so that column j is at position j.  The tree's own columns follow in blocks of
 // their own, masked by the ancestors' bits.
 //
@@ -103,41 +103,48 @@ __device__ inline int depth_of(const TreeBits& sm, int i, int n) {
   return d;
 }
 
-// What the kernels need to know of a unit.
-template <typename T, int D>
-struct Unit {
-  const T *K, *V;            // cached rows by slot
-  const T *Kn, *Vn;          // the tree's
-  size_t node_stride;        // elements from one node's row to the next
-  int n, fslot, nodes;       // cached tokens, the free slot, nodes
-  const int *E, *R;
-  int rhead, j;              // order arrays' state (logical order)
+// What the kernels are given: the parts of the context and the call that they read (the whole of both would not stay in
+// scalar registers).
+struct Args {
+  const void *K, *V;                 // [U][cap][D]
+  const int *meta, *E, *R;
+  const float2* tab;                 // angles of distances (positions re-assigned)
+  const void *q, *k, *v;
+  const int32_t* parents;
+  float *out, *lse, *scratch;
+  int budget, cap, n_sink, n_recent, m, U, H, Hkv, g_bits, n;      // 2^g_bits query heads a KV head; n nodes
+  int row_tiles, slices;
+  float scale_log2e;
 };
-template <typename T, int D>
-__device__ inline Unit<T, D> load_unit(const Params& p, const Tree& t, int unit) {
-  const int* meta = p.meta + (size_t)unit * META_STRIDE;
-  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
-  Unit<T, D> u;
-  u.K = (const T*)p.K + (size_t)unit * p.cap * D;
-  u.V = (const T*)p.V + (size_t)unit * p.cap * D;
-  u.node_stride = (size_t)p.Hkv * D;
-  u.Kn = (const T*)t.k + ((size_t)b * t.n * p.Hkv + kvh) * D;
-  u.Vn = (const T*)t.v + ((size_t)b * t.n * p.Hkv + kvh) * D;
-  u.n = __builtin_amdgcn_readfirstlane(meta[META_N]);
-  u.fslot = __builtin_amdgcn_readfirstlane(meta[META_FREE]);
-  u.rhead = __builtin_amdgcn_readfirstlane(meta[META_RHEAD]);
-  u.j = __builtin_amdgcn_readfirstlane(meta[META_J]);
-  u.nodes = t.n;
-  u.E = p.E + (size_t)unit * 2 * p.m;
-  u.R = p.R + (size_t)unit * max(p.n_recent, 1);
+
+// A unit's columns.  Without re-assigned positions cached column c is slot c, the free slot among them (`hole`, masked), so
+// that a block's rows are contiguous; with them, column c is the token at position c.
+struct Unit {
+  int n, columns, hole;              // cached tokens; cached columns; the free slot, or -1 where it lies behind the tokens
+  int rhead, j;                      // order arrays' state
+  const int *E, *R;
+};
+template <bool ROPE>
+__device__ inline Unit load_unit(const int* meta, const int* E, const int* R, int m, int n_recent, int unit) {
+  const int* w = meta + (size_t)unit * META_STRIDE;
+  Unit u;
+  u.n = __builtin_amdgcn_readfirstlane(w[META_N]);
+  const int free_slot = __builtin_amdgcn_readfirstlane(w[META_FREE]);
+  u.hole = !ROPE && free_slot < u.n ? free_slot : -1;
+  u.columns = u.hole >= 0 ? u.n + 1 : u.n;
+  u.rhead = __builtin_amdgcn_readfirstlane(w[META_RHEAD]);
+  u.j = __builtin_amdgcn_readfirstlane(w[META_J]);
+  u.E = E + (size_t)unit * 2 * m;
+  u.R = R + (size_t)unit * max(n_recent, 1);
   return u;
 }
-// Slot of cached column c (clamped to the last one: what lies behind is masked).
-template <typename T, int D, bool ROPE>
-__device__ inline int slot_of(const Params& p, const Unit<T, D>& u, int c) {
-  c = min(c, u.n - 1);
-  if (ROPE) return u.n < p.budget ? c : logical_to_slot(p, u.E, u.R, u.rhead, u.j, c);
-  return c + (c >= u.fslot ? 1 : 0);
+// Slot of the token at position c.
+__device__ inline int slot_at(const Unit& u, int budget, int n_sink, int m, int n_recent, int c) {
+  if (u.n < budget || c < n_sink) return c;
+  c -= n_sink;
+  if (c < m) return u.E[tree_index(c, u.j)];
+  c += u.rhead - m;
+  return u.R[c >= n_recent ? c - n_recent : c];
 }
 
 // Operands by storage type.  COLS: columns of a block.  Parts: bf16 parts of a turned value.
@@ -149,14 +156,14 @@ struct Ops<uint16_t, D> {
   struct Keys { uint4 x[2][KS]; };
   struct Values { uint4 x[8]; };                     // head_dim 64: the first half of each
   __device__ static inline int col(int q4, int j) { return (j >> 2) * 16 + q4 * 4 + (j & 3); }
-  __device__ static inline void load_k(Keys& k, int bk, const uint16_t* row, int q4) {
+  __device__ static inline void load_k(Keys& k, int bk, const char* base, unsigned row) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) k.x[bk][s] = *reinterpret_cast<const uint4*>(row + s * 32 + q4 * 8);
+    for (int s = 0; s < KS; ++s) k.x[bk][s] = *reinterpret_cast<const uint4*>(base + row + s * 64);
   }
-  __device__ static inline void load_v(Values& v, int j, const uint16_t* row, int lr) {
-    if constexpr (D == 128) v.x[j] = *reinterpret_cast<const uint4*>(row + lr * 8);
+  __device__ static inline void load_v(Values& v, int j, const char* base, unsigned row) {
+    if constexpr (D == 128) v.x[j] = *reinterpret_cast<const uint4*>(base + row);
     else {
-      const uint2 r = *reinterpret_cast<const uint2*>(row + lr * 4);
+      const uint2 r = *reinterpret_cast<const uint2*>(base + row);
       v.x[j] = make_uint4(r.x, r.y, 0, 0);
     }
   }
@@ -187,14 +194,14 @@ struct Ops<float, D> {
   struct Keys { float4 x[1][KS]; };
   struct Values { float x[4][DPL]; };
   __device__ static inline int col(int q4, int j) { return q4 * 4 + j; }
-  __device__ static inline void load_k(Keys& k, int, const float* row, int q4) {
+  __device__ static inline void load_k(Keys& k, int, const char* base, unsigned row) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) k.x[0][s] = *reinterpret_cast<const float4*>(row + s * 16 + q4 * 4);
+    for (int s = 0; s < KS; ++s) k.x[0][s] = *reinterpret_cast<const float4*>(base + row + s * 64);
   }
-  __device__ static inline void load_v(Values& v, int j, const float* row, int lr) {
+  __device__ static inline void load_v(Values& v, int j, const char* base, unsigned row) {
 #pragma unroll
     for (int e = 0; e < DPL; e += 4) {
-      const float4 r = *reinterpret_cast<const float4*>(row + lr * DPL + e);
+      const float4 r = *reinterpret_cast<const float4*>(base + row + e * 4);
       v.x[j][e] = r.x; v.x[j][e + 1] = r.y; v.x[j][e + 2] = r.z; v.x[j][e + 3] = r.w;
     }
   }
@@ -364,69 +371,66 @@ __device__ inline void add_values(f32x4_t (&o)[D / 16], const typename Ops<float
     for (int e = 0; e < D / 16; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x[j][e], p.x[0][j], o[e], 0, 0, 0);
 }
 
-// Infinities and NaNs among a block's values.  A probability of zero times one of them is a NaN, so a node that a row does
-// not attend must not bring them in: they are taken out of V, and what the rows that do attend them get is added from
-// counts.  A count is the product of "attended" (1 or 0) and a code: 1 for +inf, 2^9 for -inf, 2^18 for NaN (sums over 32
-// columns stay exact).
-__device__ inline bool not_finite_bits(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u; }
-__device__ inline float code_of(unsigned bits) {     // of an fp32 pattern that is not finite
-  return (bits & 0x007fffffu) ? 262144.0f : (bits >> 31) ? 512.0f : 1.0f;
-}
-__device__ inline float decode_counts(float c) {     // what those counts add to a finite sum
-  if (c == 0.f) return 0.f;
-  if (c >= 262144.0f) return __builtin_nanf("");
-  const int k = (int)c;
-  const bool plus = (k & 511) != 0, minus = k >= 512;
-  return plus ? (minus ? __builtin_nanf("") : INFINITY) : -INFINITY;
-}
+// Infinities and NaNs among the values of a block of nodes.  A probability of zero times one of them is a NaN, so a node that
+// a row does not attend must not bring them in: they are taken out of the operand, and a row that does attend the node gets
+// them added as they are, from memory (a cold path, short rather than fast).
+// Per 16-bit half (or word): the top bit set where the value is finite.
+__device__ inline unsigned finite_halves(unsigned w) { return ((w & 0x7f807f80u) ^ 0x7f807f80u) + 0x7fff7fffu; }
+__device__ inline unsigned finite_word(unsigned w) { return ((w & 0x7f800000u) ^ 0x7f800000u) + 0x7fffffffu; }
 template <int D>
-__device__ inline bool any_not_finite(const typename Ops<uint16_t, D>::Values& v) {
-  bool bad = false;
+__device__ inline bool all_finite(const typename Ops<uint16_t, D>::Values& v) {
+  unsigned f = 0x80008000u;
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
-    for (int w = 0; w < (D == 128 ? 4 : 2); ++w) {
-      const unsigned x = Ops<uint16_t, D>::word(v.x[j], w);
-      bad |= not_finite_bits(x) || not_finite_bits(x << 16);
-    }
-  return __any(bad);
+    for (int w = 0; w < 4; ++w) f &= finite_halves(Ops<uint16_t, D>::word(v.x[j], w));
+  return __all(f == 0x80008000u);
 }
 template <int D>
-__device__ inline bool any_not_finite(const typename Ops<float, D>::Values& v) {
-  bool bad = false;
+__device__ inline bool all_finite(const typename Ops<float, D>::Values& v) {
+  unsigned f = 0x80000000u;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) bad |= not_finite_bits(__float_as_uint(v.x[j][e]));
-  return __any(bad);
+    for (int e = 0; e < D / 16; ++e) f &= finite_word(__float_as_uint(v.x[j][e]));
+  return __all(f == 0x80000000u);
 }
-// Takes them out of v and leaves their codes in c.
+__device__ inline unsigned keep_finite(unsigned w) { return w & ((finite_halves(w) >> 15 & 0x00010001u) * 0xffffu); }
 template <int D>
-__device__ inline void part_not_finite(typename Ops<uint16_t, D>::Values& v, typename Ops<uint16_t, D>::Values& c) {
+__device__ inline void drop_not_finite(typename Ops<uint16_t, D>::Values& v) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    unsigned w[4] = {v.x[j].x, v.x[j].y, v.x[j].z, v.x[j].w}, k[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned lo = w[i] << 16, hi = w[i] & 0xffff0000u;
-      const bool bl = not_finite_bits(lo), bh = not_finite_bits(hi);
-      k[i] = (bl ? __float_as_uint(code_of(lo)) >> 16 : 0u) | (bh ? __float_as_uint(code_of(hi)) : 0u);
-      w[i] = (bl ? 0u : lo >> 16) | (bh ? 0u : hi);
-    }
-    v.x[j] = make_uint4(w[0], w[1], w[2], w[3]);
-    c.x[j] = make_uint4(k[0], k[1], k[2], k[3]);
-  }
+  for (int j = 0; j < 8; ++j)
+    v.x[j] = make_uint4(keep_finite(v.x[j].x), keep_finite(v.x[j].y), keep_finite(v.x[j].z), keep_finite(v.x[j].w));
 }
 template <int D>
-__device__ inline void part_not_finite(typename Ops<float, D>::Values& v, typename Ops<float, D>::Values& c) {
+__device__ inline void drop_not_finite(typename Ops<float, D>::Values& v) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) {
       const unsigned x = __float_as_uint(v.x[j][e]);
-      c.x[j][e] = not_finite_bits(x) ? code_of(x) : 0.f;
-      v.x[j][e] = not_finite_bits(x) ? 0.f : v.x[j][e];
+      v.x[j][e] = __uint_as_float(x & (unsigned)((int)finite_word(x) >> 31));
     }
+}
+// `row`: this lane's dimensions (DPL x 4 of them, from 4 * DPL * q4) of the block's first node; `bits`: what its rows attend.
+template <typename T, int D, int RB>
+__device__ inline void add_not_finite(f32x4_t (&o)[RB][D / 16], const char* row, size_t node_bytes, int nodes, const unsigned (&bits)[RB]) {
+  constexpr int EPL = Storage<T>::EPL, N = D / 4;
+#pragma unroll 1
+  for (int c = 0; c < nodes; ++c, row += node_bytes) {
+#pragma unroll
+    for (int x = 0; x < N; x += EPL) {
+      float y[EPL];
+      Storage<T>::widen(*reinterpret_cast<const uint4*>(row + x * sizeof(T)), y);
+#pragma unroll
+      for (int z = 0; z < EPL; ++z) {
+        const unsigned w = __float_as_uint(y[z]);
+        const float odd = __uint_as_float(w & ~(unsigned)((int)finite_word(w) >> 31));       // 0 if it is finite
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) o[rb][(x + z) % (D / 16)][(x + z) / (D / 16)] += (bits[rb] >> c & 1) ? odd : 0.f;
+      }
+    }
+  }
 }
 
 // Scratch of a call: one partial result per (unit, row tile, slice): [rows][D] sums relative to the row's reference, then
@@ -437,50 +441,105 @@ struct Shape {
 
 // grid: row tiles x slices x units (remapped so that what reads the same rows shares an XCD's L2).  RB: blocks of 16 rows.
 template <typename T, int D, int RB, bool ROPE>
-__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tree t, int row_tiles, int slices,
-                                                                    float* __restrict__ out, float* __restrict__ lse,
-                                                                    float* __restrict__ scratch) {
+__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
   using O = Ops<T, D>;
   constexpr int ROWS = RB * 16, DPL = O::DPL, OR = D + 4;        // OR: floats of a row of sums in LDS
+  constexpr int BK = O::COLS / 16, ROWB = D * (int)sizeof(T);
   extern __shared__ __attribute__((aligned(16))) float tr_smem[];
   __shared__ TreeBits tree;
-  const int items = row_tiles * slices * p.U, per_xcd = (items + 7) / 8;
+  const int items = p.row_tiles * p.slices * p.U, per_xcd = (items + 7) / 8;
   const int item = ((int)blockIdx.x % 8) * per_xcd + (int)blockIdx.x / 8;
   if (item >= items) return;
-  const int tile = item % row_tiles, slice = item / row_tiles % slices, unit = item / (row_tiles * slices);
+  const int tile = item % p.row_tiles, slice = item / p.row_tiles % p.slices, unit = item / (p.row_tiles * p.slices);
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = unit % p.Hkv, b = unit / p.Hkv;
-  const Unit<T, D> u = load_unit<T, D>(p, t, unit);
-  const int rows = t.n * p.G;
-  const int cache_blocks = (u.n + O::COLS - 1) / O::COLS, blocks = cache_blocks + (t.n + O::COLS - 1) / O::COLS;
-  const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
+  const Unit u = load_unit<ROPE>(p.meta, p.E, p.R, p.m, p.n_recent, unit);
+  const int rows = p.n << p.g_bits, g_mask = (1 << p.g_bits) - 1;
+  const int cache_blocks = (u.columns + O::COLS - 1) / O::COLS, blocks = cache_blocks + (p.n + O::COLS - 1) / O::COLS;
+  const int begin = (int)((long long)blocks * slice / p.slices), end = (int)((long long)blocks * (slice + 1) / p.slices);
 
-  build_tree(tree, t.parents + (size_t)b * t.n, t.n);
+  const char* Ku = (const char*)p.K + (size_t)unit * p.cap * ROWB;
+  const char* Vu = (const char*)p.V + (size_t)unit * p.cap * ROWB;
+  const size_t node_bytes = (size_t)p.Hkv * ROWB;
+  const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+  const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+  const unsigned k_lane = q4 * 16, v_lane = lr * (DPL * (int)sizeof(T));       // this lane's piece of a row
+
+  typename O::Keys k;
+  typename O::Values v;
+  int slot = 0;                                      // ROPE: of column `lane` (mod COLS) of the block to be loaded next
+  auto load_slots = [&](int blk) {
+    if constexpr (ROPE)
+      if (blk < cache_blocks)
+        slot = slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(blk * O::COLS + (lane & (O::COLS - 1)), u.n - 1));
+  };
+  auto load_keys = [&](int blk) {
+    if (blk < cache_blocks) {
+      if constexpr (ROPE) {
+#pragma unroll
+        for (int bk = 0; bk < BK; ++bk)
+          O::load_k(k, bk, Ku + (size_t)(unsigned)__shfl(slot, bk * 16 + lr, 64) * ROWB, k_lane);
+      } else {
+        const char* base = Ku + (size_t)blk * (O::COLS * ROWB);
+        const int last = p.cap - 1 - blk * O::COLS;
+#pragma unroll
+        for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, base, (unsigned)min(bk * 16 + lr, last) * ROWB + k_lane);
+      }
+    } else {
+      const int c0 = (blk - cache_blocks) * O::COLS;
+#pragma unroll
+      for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, Kn + min(c0 + bk * 16 + lr, p.n - 1) * node_bytes, k_lane);
+    }
+  };
+  auto load_values = [&](int blk) {
+    if (blk < cache_blocks) {
+      if constexpr (ROPE) {
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j)
+          O::load_v(v, j, Vu + (size_t)(unsigned)__shfl(slot, O::col(q4, j), 64) * ROWB, v_lane);
+      } else {
+        const char* base = Vu + (size_t)blk * (O::COLS * ROWB);
+        const int last = p.cap - 1 - blk * O::COLS;
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, base, (unsigned)min(O::col(q4, j), last) * ROWB + v_lane);
+      }
+    } else {
+      const int c0 = (blk - cache_blocks) * O::COLS;
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, Vn + min(c0 + O::col(q4, j), p.n - 1) * node_bytes, v_lane);
+    }
+  };
+  load_slots(begin + wave);
+  if (begin + wave < end) {
+    load_keys(begin + wave);
+    load_values(begin + wave);
+  }
+  load_slots(begin + wave + TR_WAVES);
+
+  build_tree(tree, p.parents + (size_t)b * p.n, p.n);
 
   // this lane's rows (clamped: rows behind the last repeat it and are not written)
   int node[RB];
-  const T* q_row[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = min(tile * ROWS + rb * 16 + lr, rows - 1);
-    node[rb] = r / p.G;
-    q_row[rb] = (const T*)t.q + (((size_t)b * t.n + node[rb]) * p.H + kvh * p.G + r % p.G) * D;
-  }
   constexpr int QR = q_row_elems<T, D>(), Q_PART = ROWS * QR;
   typename O::Query q[RB];
   T* sq = reinterpret_cast<T*>(tr_smem);
+  auto query_row = [&](int r) {
+    return (const T*)p.q + (((size_t)b * p.n + (r >> p.g_bits)) * p.H + (kvh << p.g_bits) + (r & g_mask)) * D;
+  };
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = min(tile * ROWS + rb * 16 + lr, rows - 1);
+    node[rb] = r >> p.g_bits;
+    if constexpr (!ROPE) O::load_q(q[rb], query_row(r), q4);
+  }
   if constexpr (ROPE) {
-    stage_turned<T, D>(sq, ROWS, Q_PART, p.rope_tab, [&](int r, const T*& src, int& pos) {
+    stage_turned<T, D>(sq, ROWS, Q_PART, p.tab, [&](int r, const T*& src, int& pos) {
       r = min(tile * ROWS + r, rows - 1);
-      const int i = r / p.G;
-      src = (const T*)t.q + (((size_t)b * t.n + i) * p.H + kvh * p.G + r % p.G) * D;
-      pos = u.n + depth_of(tree, i, t.n);
+      src = query_row(r);
+      pos = u.n + depth_of(tree, r >> p.g_bits, p.n);
     });
     __syncthreads();
-  } else {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) O::load_q(q[rb], q_row[rb], q4);
   }
 
   f32x4_t o[RB][DPL];
@@ -494,62 +553,37 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tr
   }
   const float sc = p.scale_log2e;
 
-  constexpr int BK = O::COLS / 16;
-  typename O::Keys k;
-  typename O::Values v;
-  auto load_keys = [&](int blk) {
-#pragma unroll
-    for (int bk = 0; bk < BK; ++bk) {
-      const T* row;
-      if (blk < cache_blocks) row = u.K + (size_t)slot_of<T, D, ROPE>(p, u, blk * O::COLS + bk * 16 + lr) * D;
-      else row = u.Kn + (size_t)min((blk - cache_blocks) * O::COLS + bk * 16 + lr, t.n - 1) * u.node_stride;
-      O::load_k(k, bk, row, q4);
-    }
-  };
-  auto load_values = [&](int blk) {
-#pragma unroll
-    for (int j = 0; j < O::NCOL; ++j) {
-      const T* row;
-      if (blk < cache_blocks) row = u.V + (size_t)slot_of<T, D, ROPE>(p, u, blk * O::COLS + O::col(q4, j)) * D;
-      else row = u.Vn + (size_t)min((blk - cache_blocks) * O::COLS + O::col(q4, j), t.n - 1) * u.node_stride;
-      O::load_v(v, j, row, lr);
-    }
-  };
-
-  if (begin + wave < end) {
-    load_keys(begin + wave);
-    load_values(begin + wave);
-  }
   for (int blk = begin + wave; blk < end; blk += TR_WAVES) {
     const bool cached = blk < cache_blocks;
-    const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS;
+    const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS, next = blk + TR_WAVES;
     typename O::Logits s[RB];
     if constexpr (ROPE) {
       int pos[BK];
 #pragma unroll
       for (int bk = 0; bk < BK; ++bk) {
         const int c = col0 + bk * 16 + lr;
-        pos[bk] = cached ? min(c, u.n - 1) : u.n + depth_of(tree, min(c, t.n - 1), t.n);
+        pos[bk] = cached ? min(c, u.n - 1) : u.n + depth_of(tree, min(c, p.n - 1), p.n);
       }
-      turned_logits<D, RB>(s, k, p.rope_tab, pos, sq + lr * QR, Q_PART, q4);
+      turned_logits<D, RB>(s, k, p.tab, pos, sq + lr * QR, Q_PART, q4);
     } else {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) logits<D>(s[rb], k, q[rb]);
     }
-    const int next = blk + TR_WAVES;
     if (next < end) load_keys(next);
     // what a row does not attend
-    if (cached && col0 + O::COLS > u.n) {
+    if (cached) {
+      if (col0 + O::COLS > u.columns || (u.hole >= col0 && u.hole < col0 + O::COLS)) {
 #pragma unroll
-      for (int j = 0; j < O::NCOL; ++j) {
-        const bool hidden = col0 + O::col(q4, j) >= u.n;
+        for (int j = 0; j < O::NCOL; ++j) {
+          const int c = col0 + O::col(q4, j);
+          if (c >= u.columns || c == u.hole) {
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-          if (hidden) O::at(s[rb], j) = -INFINITY;
-        if (hidden) O::clear_v(v, j);
+            for (int rb = 0; rb < RB; ++rb) O::at(s[rb], j) = -INFINITY;
+            O::clear_v(v, j);                        // whatever the row holds
+          }
+        }
       }
-    }
-    if (!cached) {
+    } else {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (col0 & 31);
@@ -591,24 +625,12 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tr
         ref[rb] = raised;
       }
     }
-    if (!cached && any_not_finite<D>(v)) {              // (after the raise, which would make a NaN of an infinity)
-      typename O::Values codes;
-      part_not_finite<D>(v, codes);
+    if (!cached && !all_finite<D>(v)) {              // (after the raise, which would make a NaN of an infinity)
+      unsigned bits[RB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (col0 & 31);
-        typename O::Logits attended;
-#pragma unroll
-        for (int j = 0; j < O::NCOL; ++j) O::at(attended, j) = (bits >> O::col(q4, j) & 1) ? 1.f : 0.f;
-        f32x4_t count[DPL];
-#pragma unroll
-        for (int e = 0; e < DPL; ++e) count[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        add_values<D>(count, codes, attended);
-#pragma unroll
-        for (int e = 0; e < DPL; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[rb][e][i] += decode_counts(count[e][i]);
-      }
+      for (int rb = 0; rb < RB; ++rb) bits[rb] = tree.anc[node[rb]][col0 >> 5] >> (col0 & 31);
+      add_not_finite<T, D, RB>(o, Vn + col0 * node_bytes + q4 * (ROWB / 4), node_bytes, min(O::COLS, p.n - col0), bits);
+      drop_not_finite<D>(v);
     }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -616,6 +638,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tr
       add_values<D>(o[rb], v, e[rb]);
     }
     if (next < end) load_values(next);
+    load_slots(next + TR_WAVES);
   }
 
   // ---- the waves' sums added: [wave][row][D] and [wave][row] reference and sum ----
@@ -650,18 +673,18 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Params p, Tr
       L = fmaf(ml.y, f, L);
       a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
     }
-    const int i = row / p.G;
+    const int i = row >> p.g_bits;
     const bool present = tree.up[i] == -1;
-    if (slices > 1) {
-      float* part = scratch + (((size_t)unit * row_tiles + tile) * slices + slice) * ROWS * (D + 4) + (size_t)r * (D + 4);
+    if (p.slices > 1) {
+      float* part = p.scratch + (((size_t)unit * p.row_tiles + tile) * p.slices + slice) * ROWS * (D + 4) + (size_t)r * (D + 4);
       *reinterpret_cast<float4*>(part + c) = a;
       if (c == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, present ? L : -1.f);   // below 0: the row is absent
     } else {
-      const size_t at = ((size_t)b * t.n + i) * p.H + kvh * p.G + row % p.G;
+      const size_t at = ((size_t)b * p.n + i) * p.H + (kvh << p.g_bits) + (row & g_mask);
       const float inv = 1.0f / L;
-      *reinterpret_cast<float4*>(out + at * D + c) =
+      *reinterpret_cast<float4*>(p.out + at * D + c) =
           present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c == 0 && lse) lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
+      if (c == 0 && p.lse) p.lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
     }
   }
 }
@@ -720,14 +743,17 @@ __device__ inline int path_length(const Tree& t, int b) {
 template <typename T, int D, bool ROPE>
 __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tree t, int slices, int32_t* __restrict__ status) {
   using O = Ops<T, D>;
-  constexpr int QR = q_row_elems<T, D>(), Q_PART = CS_ROWS * QR, BK = O::COLS / 16;
+  constexpr int QR = q_row_elems<T, D>(), Q_PART = CS_ROWS * QR, BK = O::COLS / 16, ROWB = D * (int)sizeof(T);
   static_assert(TR_THREADS >= MAX_NODES, "one thread per token of the path");
   extern __shared__ __attribute__((aligned(16))) float tr_smem[];
   __shared__ float row_lse[CS_ROWS];
   const int slice = blockIdx.x, unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = unit % p.Hkv, b = unit / p.Hkv;
-  const Unit<T, D> u = load_unit<T, D>(p, t, unit);
+  const Unit u = load_unit<ROPE>(p.meta, p.E, p.R, p.m, p.n_recent, unit);
+  const char* Ku = (const char*)p.K + (size_t)unit * p.cap * ROWB;
+  const char* Kn = (const char*)t.k + ((size_t)b * t.n * p.Hkv + kvh) * ROWB;
+  const size_t node_bytes = (size_t)p.Hkv * ROWB;
   const int found = path_length(t, b), L = max(found, 0);
   const int* path = t.path + (size_t)b * t.max_len;
   if (slice == 0 && tid == 0) {
@@ -736,7 +762,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
   }
   if (L == 0) return;
   const int rows = L * p.G;
-  const int cache_blocks = (u.n + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
+  const int cache_blocks = (u.columns + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
   const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
   const int cap_cols = (p.cap + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
   const int cs_stride = cap_cols + (p.max_chunk + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
@@ -777,11 +803,12 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
 #pragma unroll
       for (int bk = 0; bk < BK; ++bk) {
         const int c = col0 + bk * 16 + lr;
-        const T* row;
-        if (cached) row = u.K + (size_t)slot_of<T, D, ROPE>(p, u, c) * D;
-        else row = u.Kn + (size_t)path[min(c, L - 1)] * u.node_stride;
+        const char* row;
+        if (!cached) row = Kn + path[min(c, L - 1)] * node_bytes;
+        else if (ROPE) row = Ku + (size_t)slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(c, u.n - 1)) * ROWB;
+        else row = Ku + (size_t)min(c, p.cap - 1) * ROWB;
         pos[bk] = cached ? min(c, u.n - 1) : u.n + min(c, L - 1);
-        O::load_k(k, bk, row, q4);
+        O::load_k(k, bk, row, q4 * 16);
       }
       float col_sum[O::NCOL];
 #pragma unroll
@@ -800,7 +827,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
 #pragma unroll
         for (int j = 0; j < O::NCOL; ++j) {
           const int c = col0 + O::col(q4, j);
-          const bool seen = r < rows && (cached ? c < u.n : c <= i);
+          const bool seen = r < rows && (cached ? c < u.columns && c != u.hole : c <= i);
           const float e = fast_exp2(fmaf(O::at(s[0], j), p.scale_log2e, -l2));
           col_sum[j] += seen ? e : 0.f;
         }
@@ -809,8 +836,9 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
       for (int j = 0; j < O::NCOL; ++j) {
         const float x = group_sum<16>(col_sum[j]);
         const int c = col0 + O::col(q4, j);
-        if (lr == j && (cached ? c < u.n : c < L)) {
-          unsigned long long* a = acc + (cached ? slot_of<T, D, ROPE>(p, u, c) : cap_cols + c);
+        if (lr == j && (cached ? c < u.columns && c != u.hole : c < L)) {
+          const int slot = ROPE && cached ? slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, c) : c;
+          unsigned long long* a = acc + (cached ? slot : cap_cols + c);
           *a += (unsigned long long)(long long)(x * COLSUM_FIX + 0.5f);
         }
       }
@@ -837,18 +865,18 @@ Shape attend_shape(const Params& p, int n) {
 }
 
 template <typename T, int D, int RB, bool ROPE>
-int launch_attend_rb(const Params& p, const Tree& t, const Shape& s, float* out, float* lse, float* scratch, hipStream_t st) {
+int launch_attend_rb(const Params& p, const Tree& t, const Shape& s, const Args& a, hipStream_t st) {
   const size_t sums = (size_t)TR_WAVES * RB * 16 * ((D + 4) * sizeof(float) + sizeof(float2));
   const size_t queries = ROPE ? (size_t)Ops<T, D>::QPARTS * RB * 16 * q_row_elems<T, D>() * sizeof(T) : 0;
   const size_t lds = sums > queries ? sums : queries;
   auto kernel = tree_attend_kernel<T, D, RB, ROPE>;
   if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
   const int items = s.row_tiles * s.slices * p.U;
-  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, p, t, s.row_tiles, s.slices, out, lse, scratch);
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
   if (s.slices > 1) {
     constexpr int PER = 256 / (D / 4);
     hipLaunchKernelGGL(tree_merge_kernel<D>, dim3((t.n * p.G + PER - 1) / PER, p.U), dim3(256), 0, st, p, t.n, s.rows_per_tile,
-                       s.row_tiles, s.slices, scratch, out, lse);
+                       s.row_tiles, s.slices, a.scratch, a.out, a.lse);
   }
   return finish_launch();
 }
@@ -856,9 +884,10 @@ template <typename T, int D>
 int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, float* scratch, hipStream_t st) {
   const Shape s = attend_shape(p, t.n);
   const bool rope = (p.flags & TREEKV_POSITION_RERANK) != 0;
-  if (s.rows_per_tile == 16)
-    return rope ? launch_attend_rb<T, D, 1, true>(p, t, s, out, lse, scratch, st) : launch_attend_rb<T, D, 1, false>(p, t, s, out, lse, scratch, st);
-  return rope ? launch_attend_rb<T, D, 2, true>(p, t, s, out, lse, scratch, st) : launch_attend_rb<T, D, 2, false>(p, t, s, out, lse, scratch, st);
+  const Args a = {p.K, p.V, p.meta, p.E, p.R, p.rope_tab, t.q, t.k, t.v, t.parents, out, lse, scratch, p.budget, p.cap, p.n_sink,
+                  p.n_recent, p.m, p.U, p.H, p.Hkv, p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3, t.n, s.row_tiles, s.slices, p.scale_log2e};
+  if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(p, t, s, a, st) : launch_attend_rb<T, D, 1, false>(p, t, s, a, st);
+  return rope ? launch_attend_rb<T, D, 2, true>(p, t, s, a, st) : launch_attend_rb<T, D, 2, false>(p, t, s, a, st);
 }
 
 template <typename T, int D, bool ROPE>
