@@ -436,8 +436,45 @@ __device__ inline void add_not_finite(f32x4_t (&o)[RB][D / 16], const char* row,
 // Scratch of a call: one partial result per (unit, row tile, slice): [rows][D] sums relative to the row's reference, then
 // [rows][2] reference and sum.
 struct Shape {
+  bool tiled;
   int rows_per_tile, row_tiles, slices;
 };
+
+// The workgroup's rows from LDS to where they go: the PARTS sums of a row ([part][row][D], rows D + 4 apart) and their
+// references and sums ([part][row]) added, then the output or, with several slices, the slice's partial result.
+template <int D, int PARTS, int ROWS>
+__device__ inline void finish_rows(const Args& p, const TreeBits& tree, const float* so, const float2* sm, int unit, int tile, int slice) {
+  const int rows = p.n << p.g_bits, kvh = unit % p.Hkv, b = unit / p.Hkv;
+  for (int x = threadIdx.x; x < ROWS * (D / 4); x += TR_THREADS) {
+    const int r = x / (D / 4), c = x % (D / 4) * 4, row = tile * ROWS + r;
+    if (row >= rows) break;
+    float M = REF_NONE, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < PARTS; ++w) M = fmaxf(M, sm[w * ROWS + r].x);
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < PARTS; ++w) {
+      const float2 ml = sm[w * ROWS + r];
+      const float f = fast_exp2(ml.x - M);
+      const float4 y = *reinterpret_cast<const float4*>(so + ((size_t)w * ROWS + r) * (D + 4) + c);
+      L = fmaf(ml.y, f, L);
+      a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
+    }
+    const int i = row >> p.g_bits;
+    const bool present = tree.up[i] == -1;
+    if (p.slices > 1) {
+      float* part = p.scratch + (((size_t)unit * p.row_tiles + tile) * p.slices + slice) * ROWS * (D + 4) + (size_t)r * (D + 4);
+      *reinterpret_cast<float4*>(part + c) = a;
+      if (c == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, present ? L : -1.f);   // below 0: the row is absent
+    } else {
+      const size_t at = ((size_t)b * p.n + i) * p.H + (kvh << p.g_bits) + (row & ((1 << p.g_bits) - 1));
+      const float inv = 1.0f / L;
+      *reinterpret_cast<float4*>(p.out + at * D + c) =
+          present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c == 0 && p.lse) p.lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
+    }
+  }
+}
 
 // grid: row tiles x slices x units (remapped so that what reads the same rows shares an XCD's L2).  RB: blocks of 16 rows.
 template <typename T, int D, int RB, bool ROPE>
@@ -641,16 +678,16 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
     load_slots(next + TR_WAVES);
   }
 
-  // ---- the waves' sums added: [wave][row][D] and [wave][row] reference and sum ----
+  // ---- the waves' sums added ----
   float* so = tr_smem;
   float2* sm = reinterpret_cast<float2*>(tr_smem + TR_WAVES * ROWS * OR);
   __syncthreads();                                   // the queries' LDS is free
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int r = rb * 16 + lr;
+    const int r = wave * ROWS + rb * 16 + lr;
     const float l = row_sum(sum[rb]);
-    if (q4 == 0) sm[wave * ROWS + r] = make_float2(ref[rb], l);
-    float* dst = so + ((size_t)wave * ROWS + r) * OR + q4 * 4 * DPL;
+    if (q4 == 0) sm[r] = make_float2(ref[rb], l);
+    float* dst = so + (size_t)r * OR + q4 * 4 * DPL;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -658,47 +695,256 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
         *reinterpret_cast<float4*>(dst + i * DPL + e) = make_float4(o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]);
   }
   __syncthreads();
-  for (int x = tid; x < ROWS * (D / 4); x += TR_THREADS) {
-    const int r = x / (D / 4), c = x % (D / 4) * 4, row = tile * ROWS + r;
-    if (row >= rows) break;
-    float M = REF_NONE, L = 0.f;
+  finish_rows<D, TR_WAVES, ROWS>(p, tree, so, sm, unit, tile, slice);
+}
+
+// ---------------------------------------------------------------------------------------------
+// attend, many rows: bf16 storage, tiles of columns shared by the workgroup's waves
+// ---------------------------------------------------------------------------------------------
+// With more than 32 rows a unit the kernel above reads every row of K and V once per 32 of them.  Here a workgroup owns 64
+// or 128 rows: RG groups of 32 rows x 8 / RG waves that share a tile's columns.  Tiles of 128 columns come by asynchronous
+// copies into LDS (two stages of K and of V), row-major as they lie in memory with the 16-byte pieces of a row swizzled, so
+// that the operand reads (16 bytes of 16 rows for K, the transposing read for V) touch every bank once.
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4_t;
+constexpr int TILE_COLS = 128;
+
+template <int D, int RG>
+__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p) {
+  constexpr int RB = 2, ROWS = RG * 32, CG = TR_WAVES / RG, KS = D / 32, DB = D / 16, OR = D + 4, ROWB = D * 2;
+  constexpr int PARTS = D / 8, RPC = 64 / PARTS, CPW = 16 / RPC;   // 16-byte pieces and rows of a 1 KB copy; copies per wave and tile
+  constexpr int TILE = TILE_COLS * D;                              // elements of a staged tile
+  extern __shared__ __attribute__((aligned(1024))) float tr_smem[];
+  __shared__ TreeBits tree;
+  uint16_t* stages = reinterpret_cast<uint16_t*>(tr_smem);         // K 0, K 1, V 0, V 1
+  auto kswz = [](int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); };
+  auto vswz = [](int r) { return D == 128 ? ((r & 7) << 1) : (((r >> 1) & 3) << 1); };
+  const int items = p.row_tiles * p.slices * p.U, per_xcd = (items + 7) / 8;
+  const int item = ((int)blockIdx.x % 8) * per_xcd + (int)blockIdx.x / 8;
+  if (item >= items) return;
+  const int tile = item % p.row_tiles, slice = item / p.row_tiles % p.slices, unit = item / (p.row_tiles * p.slices);
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave / CG, cg = wave % CG;
+  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
+  const Unit u = load_unit<false>(p.meta, p.E, p.R, p.m, p.n_recent, unit);
+  const int rows = p.n << p.g_bits, g_mask = (1 << p.g_bits) - 1, row0 = tile * ROWS + rg * 32;
+  const int cache_tiles = (u.columns + TILE_COLS - 1) / TILE_COLS, tiles = cache_tiles + (p.n + TILE_COLS - 1) / TILE_COLS;
+  const int begin = (int)((long long)tiles * slice / p.slices), end = (int)((long long)tiles * (slice + 1) / p.slices);
+
+  const char* Ku = (const char*)p.K + (size_t)unit * p.cap * ROWB;
+  const char* Vu = (const char*)p.V + (size_t)unit * p.cap * ROWB;
+  const size_t node_bytes = (size_t)p.Hkv * ROWB;
+  const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+  const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+
+  // copy x of wave w fills tile rows w * 16 + x * RPC + lane / PARTS; a lane takes the piece whose place its own is
+  const int a_row = lane / PARTS, a_slot = lane % PARTS;
+  const unsigned lds_wave = __builtin_amdgcn_readfirstlane(lds_address(stages)) + wave * CPW * 1024;
+  auto request = [=](int t, int stage) {             // (by value: by reference the choices below become choices of addresses)
+    const bool cached = t < cache_tiles;
+    const int c0 = (cached ? t : t - cache_tiles) * TILE_COLS, last = cached ? p.cap - 1 : p.n - 1;
+    const size_t step = cached ? ROWB : node_bytes;
 #pragma unroll
-    for (int w = 0; w < TR_WAVES; ++w) M = fmaxf(M, sm[w * ROWS + r].x);
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x = 0; x < CPW; ++x) {
+      const int r = x * RPC + a_row;                               // (a wave's first row is a multiple of 16)
+      const size_t row = min(c0 + wave * 16 + r, last) * step;
+      async_copy16((cached ? Ku : Kn) + row + (a_slot ^ kswz(r)) * 16, lds_wave + stage * (TILE * 2) + x * 1024);
+      async_copy16((cached ? Vu : Vn) + row + (a_slot ^ vswz(r)) * 16, lds_wave + (2 + stage) * (TILE * 2) + x * 1024);
+    }
+  };
+  if (begin < end) request(begin, 0);
+
+  // this lane's rows (clamped: rows behind the last repeat it and are not written)
+  int node[RB];
+  uint4 q[RB][KS];
 #pragma unroll
-    for (int w = 0; w < TR_WAVES; ++w) {
-      const float2 ml = sm[w * ROWS + r];
-      const float f = fast_exp2(ml.x - M);
-      const float4 y = *reinterpret_cast<const float4*>(so + ((size_t)w * ROWS + r) * OR + c);
-      L = fmaf(ml.y, f, L);
-      a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
-    }
-    const int i = row >> p.g_bits;
-    const bool present = tree.up[i] == -1;
-    if (p.slices > 1) {
-      float* part = p.scratch + (((size_t)unit * p.row_tiles + tile) * p.slices + slice) * ROWS * (D + 4) + (size_t)r * (D + 4);
-      *reinterpret_cast<float4*>(part + c) = a;
-      if (c == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, present ? L : -1.f);   // below 0: the row is absent
-    } else {
-      const size_t at = ((size_t)b * p.n + i) * p.H + (kvh << p.g_bits) + (row & g_mask);
-      const float inv = 1.0f / L;
-      *reinterpret_cast<float4*>(p.out + at * D + c) =
-          present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c == 0 && p.lse) p.lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
-    }
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = min(row0 + rb * 16 + lr, rows - 1);
+    node[rb] = r >> p.g_bits;
+    const uint16_t* src = (const uint16_t*)p.q + (((size_t)b * p.n + node[rb]) * p.H + (kvh << p.g_bits) + (r & g_mask)) * D + q4 * 8;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) q[rb][x] = *reinterpret_cast<const uint4*>(src + x * 32);
   }
+  build_tree(tree, p.parents + (size_t)b * p.n, p.n);
+
+  f32x4_t o[RB][DB];
+  float ref[RB], sum[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    ref[rb] = REF_NONE;
+    sum[rb] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[rb][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sc = p.scale_log2e;
+  // where this lane reads a 32-column block's operands from
+  const int k_off = lr * D, v_row = q4 * 4 + (lr >> 2), v_off = v_row * D + (lr & 1) * 4;
+  const int k_swz = kswz(lr), v_swz = vswz(v_row) ^ ((lr >> 1) & 1);           // (blocks and halves start at multiples of 16 rows)
+
+  auto block = [&](int t, int sb) __attribute__((always_inline)) {
+    const bool cached = t < cache_tiles;
+    const int col0 = (cached ? t : t - cache_tiles) * TILE_COLS + sb * 32, stage = (t - begin) & 1;
+    if (col0 >= (cached ? u.columns : p.n)) return;
+    const uint16_t* kp = stages + stage * TILE + sb * 32 * D + k_off;
+    const uint16_t* vp = stages + (2 + stage) * TILE + sb * 32 * D + v_off;
+    f32x4_t s[RB][2];
+    uint4 k[2][KS];
+#pragma unroll
+    for (int bk = 0; bk < 2; ++bk)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) k[bk][x] = *reinterpret_cast<const uint4*>(kp + bk * 16 * D + ((x * 4 + q4) ^ k_swz) * 8);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int bk = 0; bk < 2; ++bk) {
+        s[rb][bk] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < KS; ++x) s[rb][bk] = mfma_bf16(k[bk][x], q[rb][x], s[rb][bk]);
+      }
+    uint4 v[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const short4_t t0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + ((d * 2) ^ v_swz) * 8));
+      const short4_t t1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + 16 * D + ((d * 2) ^ v_swz) * 8));
+      const uint2 a0 = __builtin_bit_cast(uint2, t0), a1 = __builtin_bit_cast(uint2, t1);
+      v[d] = make_uint4(a0.x, a0.y, a1.x, a1.y);
+    }
+    // what a row does not attend
+    if (cached) {
+      if (col0 + 32 > u.columns || (u.hole >= col0 && u.hole < col0 + 32)) {
+        unsigned keep[4];                            // of the pairs of columns this lane holds
+#pragma unroll
+        for (int x = 0; x < 4; ++x) keep[x] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = col0 + (j >> 2) * 16 + q4 * 4 + (j & 3);
+          const bool seen = c < u.columns && c != u.hole;
+          keep[j >> 1] |= seen ? 0xffffu << (16 * (j & 1)) : 0u;
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) s[rb][j >> 2][j & 3] = seen ? s[rb][j >> 2][j & 3] : -INFINITY;
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) v[d] = make_uint4(v[d].x & keep[0], v[d].y & keep[1], v[d].z & keep[2], v[d].w & keep[3]);
+      }
+    } else {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (q4 * 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          s[rb][j >> 2][j & 3] = (bits >> ((j >> 2) * 16 + (j & 3)) & 1) ? s[rb][j >> 2][j & 3] : -INFINITY;
+      }
+    }
+    // the reference as in the kernel above
+    f32x4_t e[RB][2];
+    float fresh_sum[RB], worst = 0.f;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float add = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        e[rb][j >> 2][j & 3] = fast_exp2(fmaf(s[rb][j >> 2][j & 3], sc, -ref[rb]));
+        add += e[rb][j >> 2][j & 3];
+      }
+      fresh_sum[rb] = sum[rb] + add;
+      worst = fmaxf(worst, fresh_sum[rb]);
+    }
+    if (__any(worst > 0x1p16f)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float top = s[rb][0][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, s[rb][j >> 2][j & 3]);
+        const float raised = row_max(fmaxf(ref[rb], top * sc)), by = fast_exp2(ref[rb] - raised);
+        float add = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          e[rb][j >> 2][j & 3] = fast_exp2(fmaf(s[rb][j >> 2][j & 3], sc, -raised));
+          add += e[rb][j >> 2][j & 3];
+        }
+        fresh_sum[rb] = fmaf(sum[rb], by, add);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[rb][d] *= by;
+        ref[rb] = raised;
+      }
+    }
+    if (!cached) {
+      unsigned f = 0x80008000u;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) f &= finite_halves(v[d].x) & finite_halves(v[d].y) & finite_halves(v[d].z) & finite_halves(v[d].w);
+      if (!__all(f == 0x80008000u)) {
+        unsigned bits[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) bits[rb] = tree.anc[node[rb]][col0 >> 5];
+        const char* row = Vn + col0 * node_bytes + q4 * 8;
+#pragma unroll 1
+        for (int c = 0; c < min(32, p.n - col0); ++c, row += node_bytes) {
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const uint2 w = *reinterpret_cast<const uint2*>(row + d * 32);
+            const unsigned x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float odd = __uint_as_float(x[i] & ~(unsigned)((int)finite_word(x[i]) >> 31));       // 0 if it is finite
+#pragma unroll
+              for (int rb = 0; rb < RB; ++rb) o[rb][d][i] += (bits[rb] >> c & 1) ? odd : 0.f;
+            }
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) v[d] = make_uint4(keep_finite(v[d].x), keep_finite(v[d].y), keep_finite(v[d].z), keep_finite(v[d].w));
+      }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      sum[rb] = fresh_sum[rb];
+      uint4 h, m, l;
+      cut3(e[rb][0][0], e[rb][0][1], h.x, m.x, l.x);
+      cut3(e[rb][0][2], e[rb][0][3], h.y, m.y, l.y);
+      cut3(e[rb][1][0], e[rb][1][1], h.z, m.z, l.z);
+      cut3(e[rb][1][2], e[rb][1][3], h.w, m.w, l.w);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], l, o[rb][d]);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], m, o[rb][d]);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], h, o[rb][d]);
+    }
+  };
+
+  wait_vmcnt<0>();
+  __syncthreads();
+  for (int t = begin; t < end; ++t) {
+    if (t + 1 < end) request(t + 1, (t + 1 - begin) & 1);
+    if (row0 < rows)
+      for (int sb = cg; sb < 4; sb += CG) block(t, sb);
+    wait_vmcnt<0>();
+    __syncthreads();
+  }
+
+  float* so = tr_smem;                               // [CG][ROWS][D + 4]
+  float2* sm = reinterpret_cast<float2*>(tr_smem + CG * ROWS * OR);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int r = cg * ROWS + rg * 32 + rb * 16 + lr;
+    const float l = row_sum(sum[rb]);
+    if (q4 == 0) sm[r] = make_float2(ref[rb], l);
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      *reinterpret_cast<float4*>(so + (size_t)r * OR + d * 16 + q4 * 4) = make_float4(o[rb][d][0], o[rb][d][1], o[rb][d][2], o[rb][d][3]);
+  }
+  __syncthreads();
+  finish_rows<D, CG, ROWS>(p, tree, so, sm, unit, tile, slice);
 }
 
 // The slices' partial results of one query row, added: a row takes D / 4 lanes.
 template <int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(Params p, int n, int rows_per_tile, int row_tiles, int slices,
-                                                         const float* __restrict__ scratch, float* __restrict__ out,
-                                                         float* __restrict__ lse) {
-  const int rows = n * p.G, unit = blockIdx.y;
+__global__ __launch_bounds__(256) void tree_merge_kernel(Args p, int rows_per_tile) {
+  const int rows = p.n << p.g_bits, unit = blockIdx.y, slices = p.slices;
   const int row = blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4), c = threadIdx.x % (D / 4) * 4;
   if (row >= rows) return;
   const int tile = row / rows_per_tile, r = row % rows_per_tile;
-  const float* part = scratch + ((size_t)unit * row_tiles + tile) * slices * rows_per_tile * (D + 4) + (size_t)r * (D + 4);
+  const float* part = p.scratch + ((size_t)unit * p.row_tiles + tile) * slices * rows_per_tile * (D + 4) + (size_t)r * (D + 4);
   const size_t step = (size_t)rows_per_tile * (D + 4);
   float M = REF_NONE, L = 0.f;
   for (int s = 0; s < slices; ++s) M = fmaxf(M, part[s * step + D]);
@@ -713,11 +959,11 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(Params p, int n, int ro
     a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
   }
   const int b = unit / p.Hkv, kvh = unit % p.Hkv;
-  const size_t at = ((size_t)b * n + row / p.G) * p.H + kvh * p.G + row % p.G;
+  const size_t at = ((size_t)b * p.n + (row >> p.g_bits)) * p.H + (kvh << p.g_bits) + (row & ((1 << p.g_bits) - 1));
   const float inv = 1.0f / L;
-  *reinterpret_cast<float4*>(out + at * D + c) =
+  *reinterpret_cast<float4*>(p.out + at * D + c) =
       present ? make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
-  if (c == 0 && lse) lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
+  if (c == 0 && p.lse) p.lse[at] = present ? (M + log2f(L)) * LN2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -858,27 +1104,47 @@ int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
 Shape attend_shape(const Params& p, int n) {
   Shape s;
   const int rows = n * p.G, cols = block_cols(p);
-  s.rows_per_tile = rows <= 16 ? 16 : 32;
+  s.tiled = rows > 32 && p.dtype == TREEKV_BF16 && !(p.flags & TREEKV_POSITION_RERANK);
+  s.rows_per_tile = rows <= 16 ? 16 : !s.tiled ? 32 : rows <= 64 ? 64 : 128;
   s.row_tiles = (rows + s.rows_per_tile - 1) / s.rows_per_tile;
-  s.slices = pick_slices(p, p.U * s.row_tiles, (p.budget + cols - 1) / cols + (n + cols - 1) / cols);
+  if (s.tiled) {
+    const int tiles = (p.cap + TILE_COLS - 1) / TILE_COLS + (n + TILE_COLS - 1) / TILE_COLS;
+    s.slices = 256 / (p.U * s.row_tiles);
+    s.slices = s.slices < 1 ? 1 : s.slices > tiles ? tiles : s.slices;
+  } else {
+    s.slices = pick_slices(p, p.U * s.row_tiles, (p.cap + cols - 1) / cols + (n + cols - 1) / cols);
+  }
   return s;
 }
 
+template <int D>
+int launch_merge(const Shape& s, const Args& a, hipStream_t st) {
+  if (s.slices > 1) {
+    constexpr int PER = 256 / (D / 4);
+    hipLaunchKernelGGL(tree_merge_kernel<D>, dim3(((a.n << a.g_bits) + PER - 1) / PER, a.U), dim3(256), 0, st, a, s.rows_per_tile);
+  }
+  return finish_launch();
+}
 template <typename T, int D, int RB, bool ROPE>
-int launch_attend_rb(const Params& p, const Tree& t, const Shape& s, const Args& a, hipStream_t st) {
+int launch_attend_rb(const Shape& s, const Args& a, hipStream_t st) {
   const size_t sums = (size_t)TR_WAVES * RB * 16 * ((D + 4) * sizeof(float) + sizeof(float2));
   const size_t queries = ROPE ? (size_t)Ops<T, D>::QPARTS * RB * 16 * q_row_elems<T, D>() * sizeof(T) : 0;
   const size_t lds = sums > queries ? sums : queries;
   auto kernel = tree_attend_kernel<T, D, RB, ROPE>;
   if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
-  const int items = s.row_tiles * s.slices * p.U;
+  const int items = s.row_tiles * s.slices * a.U;
   hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
-  if (s.slices > 1) {
-    constexpr int PER = 256 / (D / 4);
-    hipLaunchKernelGGL(tree_merge_kernel<D>, dim3((t.n * p.G + PER - 1) / PER, p.U), dim3(256), 0, st, p, t.n, s.rows_per_tile,
-                       s.row_tiles, s.slices, a.scratch, a.out, a.lse);
-  }
-  return finish_launch();
+  return launch_merge<D>(s, a, st);
+}
+template <int D, int RG>
+int launch_attend_tiled(const Shape& s, const Args& a, hipStream_t st) {
+  const size_t sums = (size_t)TR_WAVES * 32 * ((D + 4) * sizeof(float) + sizeof(float2)), stages = (size_t)4 * TILE_COLS * D * 2;
+  const size_t lds = sums > stages ? sums : stages;
+  auto kernel = tree_attend_tiled_kernel<D, RG>;
+  if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
+  const int items = s.row_tiles * s.slices * a.U;
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
+  return launch_merge<D>(s, a, st);
 }
 template <typename T, int D>
 int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, float* scratch, hipStream_t st) {
@@ -886,8 +1152,11 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
   const bool rope = (p.flags & TREEKV_POSITION_RERANK) != 0;
   const Args a = {p.K, p.V, p.meta, p.E, p.R, p.rope_tab, t.q, t.k, t.v, t.parents, out, lse, scratch, p.budget, p.cap, p.n_sink,
                   p.n_recent, p.m, p.U, p.H, p.Hkv, p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3, t.n, s.row_tiles, s.slices, p.scale_log2e};
-  if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(p, t, s, a, st) : launch_attend_rb<T, D, 1, false>(p, t, s, a, st);
-  return rope ? launch_attend_rb<T, D, 2, true>(p, t, s, a, st) : launch_attend_rb<T, D, 2, false>(p, t, s, a, st);
+  if constexpr (sizeof(T) == 2) {
+    if (s.tiled) return s.rows_per_tile == 64 ? launch_attend_tiled<D, 2>(s, a, st) : launch_attend_tiled<D, 4>(s, a, st);
+  }
+  if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(s, a, st) : launch_attend_rb<T, D, 1, false>(s, a, st);
+  return rope ? launch_attend_rb<T, D, 2, true>(s, a, st) : launch_attend_rb<T, D, 2, false>(s, a, st);
 }
 
 template <typename T, int D, bool ROPE>
