@@ -30,6 +30,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 constexpr int TR_THREADS = 512, TR_WAVES = TR_THREADS / 64;
 constexpr int MAX_NODES = TREEKV_TREE_MAX_NODES, MAX_WORDS = MAX_NODES / 32;
@@ -40,6 +41,9 @@ constexpr int COLSUM_TILE = 128;                    // their two parts are round
 
 __device__ inline f32x4_t mfma_bf16(const uint4& a, const uint4& b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+__device__ inline f32x16_t mfma_wide(const uint4& a, const uint4& b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 // The high halves of two floats' bits, packed: bf16 by truncation, the first in the low half.
 __device__ inline unsigned high_halves(float a, float b) {
@@ -445,7 +449,7 @@ struct Shape {
 template <int D, int PARTS, int ROWS>
 __device__ inline void finish_rows(const Args& p, const TreeBits& tree, const float* so, const float2* sm, int unit, int tile, int slice) {
   const int rows = p.n << p.g_bits, kvh = unit % p.Hkv, b = unit / p.Hkv;
-  for (int x = threadIdx.x; x < ROWS * (D / 4); x += TR_THREADS) {
+  for (int x = threadIdx.x; x < ROWS * (D / 4); x += blockDim.x) {
     const int r = x / (D / 4), c = x % (D / 4) * 4, row = tile * ROWS + r;
     if (row >= rows) break;
     float M = REF_NONE, L = 0.f;
@@ -702,32 +706,48 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
 // attend, many rows: bf16 storage, tiles of columns shared by the workgroup's waves
 // ---------------------------------------------------------------------------------------------
 // With more than 32 rows a unit the kernel above reads every row of K and V once per 32 of them.  Here a workgroup owns 64
-// or 128 rows: RG groups of 32 rows x 8 / RG waves that share a tile's columns.  Tiles of 128 columns come by asynchronous
-// copies into LDS (two stages of K and of V), row-major as they lie in memory with the 16-byte pieces of a row swizzled, so
-// that the operand reads (16 bytes of 16 rows for K, the transposing read for V) touch every bank once.
+// or 128 rows: RG groups of 32 rows x two waves that take one half of a tile's 64 columns each.  Tiles come by asynchronous
+// copies into LDS, row-major as they lie in memory with the 16-byte pieces of a row swizzled, so that the operand reads (16
+// bytes of a row for K, the transposing read for V) spread over the banks.  v_mfma_f32_32x32x16_bf16: a wave's vector
+// instructions issue beside it, while a 16x16x32 holds them up (256 rows into 4096 slots 149 us with those).  A lane then
+// holds 16 columns of one row.
+// Iteration t forms the logits of tile t + 1 (matrix unit) beside the probabilities of tile t (vector unit) and ends with tile
+// t's product with V.  Four stages: tile t + 1 has landed, t + 2 and t + 3 are on their way, and the stage that t + 3 goes to
+// was last read in iteration t - 1, before the barrier.
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t lds_short4_t;
-constexpr int TILE_COLS = 128;
+constexpr int TILE_COLS = 64, STAGES = 4;
+
+// async_copy16 with the source as a wave-uniform base and a lane's byte offset.
+__device__ inline void async_copy16_at(const char* uniform_base, unsigned lane_offset, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(lane_offset), "s"(uniform_base), "s"(lds_base) : "memory");
+}
 
 template <int D, int RG>
-__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p) {
-  constexpr int RB = 2, ROWS = RG * 32, CG = TR_WAVES / RG, KS = D / 32, DB = D / 16, OR = D + 4, ROWB = D * 2;
-  constexpr int PARTS = D / 8, RPC = 64 / PARTS, CPW = 16 / RPC;   // 16-byte pieces and rows of a 1 KB copy; copies per wave and tile
+__global__ __launch_bounds__(RG * 128, RG / 2) void tree_attend_tiled_kernel(Args p) {
+  constexpr int CG = 2, WAVES = RG * CG, THREADS = WAVES * 64;
+  constexpr int ROWS = RG * 32, KS = D / 16, DB = D / 32, OR = D + 4, ROWB = D * 2;
+  constexpr int PARTS = D / 8, RPC = 64 / PARTS;                   // 16-byte pieces of a row, rows of a 1 KB copy
+  constexpr int WROWS = TILE_COLS / WAVES, CPW = WROWS / RPC;   // tile rows a wave copies, its copies of K (and of V) a tile
   constexpr int TILE = TILE_COLS * D;                              // elements of a staged tile
+  static_assert(TILE_COLS == CG * 32, "a wave takes 32 columns of every tile");
+  static_assert(THREADS >= MAX_NODES, "one thread per node");
   extern __shared__ __attribute__((aligned(1024))) float tr_smem[];
   __shared__ TreeBits tree;
-  uint16_t* stages = reinterpret_cast<uint16_t*>(tr_smem);         // K 0, K 1, V 0, V 1
+  uint16_t* k_stages = reinterpret_cast<uint16_t*>(tr_smem);
+  uint16_t* v_stages = k_stages + STAGES * TILE;
   auto kswz = [](int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); };
   auto vswz = [](int r) { return D == 128 ? ((r & 7) << 1) : (((r >> 1) & 3) << 1); };
   const int items = p.row_tiles * p.slices * p.U, per_xcd = (items + 7) / 8;
   const int item = ((int)blockIdx.x % 8) * per_xcd + (int)blockIdx.x / 8;
   if (item >= items) return;
   const int tile = item % p.row_tiles, slice = item / p.row_tiles % p.slices, unit = item / (p.row_tiles * p.slices);
-  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, q4 = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave / CG, cg = wave % CG;
   const int kvh = unit % p.Hkv, b = unit / p.Hkv;
   const Unit u = load_unit<false>(p.meta, p.E, p.R, p.m, p.n_recent, unit);
-  const int rows = p.n << p.g_bits, g_mask = (1 << p.g_bits) - 1, row0 = tile * ROWS + rg * 32;
+  const int rows = p.n << p.g_bits, g_mask = (1 << p.g_bits) - 1, row = min(tile * ROWS + rg * 32 + lr, rows - 1);
   const int cache_tiles = (u.columns + TILE_COLS - 1) / TILE_COLS, tiles = cache_tiles + (p.n + TILE_COLS - 1) / TILE_COLS;
   const int begin = (int)((long long)tiles * slice / p.slices), end = (int)((long long)tiles * (slice + 1) / p.slices);
 
@@ -737,201 +757,210 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
   const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
   const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
 
-  // copy x of wave w fills tile rows w * 16 + x * RPC + lane / PARTS; a lane takes the piece whose place its own is
-  const int a_row = lane / PARTS, a_slot = lane % PARTS;
-  const unsigned lds_wave = __builtin_amdgcn_readfirstlane(lds_address(stages)) + wave * CPW * 1024;
-  auto request = [=](int t, int stage) {             // (by value: by reference the choices below become choices of addresses)
-    const bool cached = t < cache_tiles;
-    const int c0 = (cached ? t : t - cache_tiles) * TILE_COLS, last = cached ? p.cap - 1 : p.n - 1;
-    const size_t step = cached ? ROWB : node_bytes;
+  // copy x of wave w fills tile rows w * WROWS + x * RPC + lane / PARTS; a lane takes the piece whose place its own is
+  const unsigned lds_wave = __builtin_amdgcn_readfirstlane(lds_address(k_stages)) + wave * CPW * 1024;
+  const int a_row = wave * WROWS + lane / PARTS, a_slot = lane % PARTS;
+  auto request = [=](int t) {
+    const unsigned m0 = lds_wave + ((t - begin) & (STAGES - 1)) * (TILE * 2), vm0 = m0 + STAGES * (TILE * 2);
+    if (t < cache_tiles) {
+      const char* kb = Ku + (size_t)t * (TILE_COLS * ROWB);
+      const char* vb = Vu + (size_t)t * (TILE_COLS * ROWB);
+      const int last = p.cap - 1 - t * TILE_COLS;                  // rows behind the last slot repeat it
 #pragma unroll
-    for (int x = 0; x < CPW; ++x) {
-      const int r = x * RPC + a_row;                               // (a wave's first row is a multiple of 16)
-      const size_t row = min(c0 + wave * 16 + r, last) * step;
-      async_copy16((cached ? Ku : Kn) + row + (a_slot ^ kswz(r)) * 16, lds_wave + stage * (TILE * 2) + x * 1024);
-      async_copy16((cached ? Vu : Vn) + row + (a_slot ^ vswz(r)) * 16, lds_wave + (2 + stage) * (TILE * 2) + x * 1024);
+      for (int x = 0; x < CPW; ++x) {
+        const int r = a_row + x * RPC;
+        const unsigned row = (unsigned)min(r, last) * ROWB;
+        async_copy16_at(kb, row + (a_slot ^ kswz(r)) * 16, m0 + x * 1024);
+        async_copy16_at(vb, row + (a_slot ^ vswz(r)) * 16, vm0 + x * 1024);
+      }
+    } else {
+      const int c0 = (t - cache_tiles) * TILE_COLS;
+#pragma unroll
+      for (int x = 0; x < CPW; ++x) {
+        const int r = a_row + x * RPC;
+        const size_t row = min(c0 + r, p.n - 1) * node_bytes;
+        async_copy16(Kn + row + (a_slot ^ kswz(r)) * 16, m0 + x * 1024);
+        async_copy16(Vn + row + (a_slot ^ vswz(r)) * 16, vm0 + x * 1024);
+      }
     }
   };
-  if (begin < end) request(begin, 0);
+#pragma unroll
+  for (int x = 0; x < STAGES - 1; ++x)
+    if (begin + x < end) request(begin + x);
 
-  // this lane's rows (clamped: rows behind the last repeat it and are not written)
-  int node[RB];
-  uint4 q[RB][KS];
+  // this lane's row (clamped: rows behind the last repeat it and are not written)
+  const int node = row >> p.g_bits;
+  uint4 q[KS];
+  {
+    const uint16_t* src = (const uint16_t*)p.q + (((size_t)b * p.n + node) * p.H + (kvh << p.g_bits) + (row & g_mask)) * D + hi * 8;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = min(row0 + rb * 16 + lr, rows - 1);
-    node[rb] = r >> p.g_bits;
-    const uint16_t* src = (const uint16_t*)p.q + (((size_t)b * p.n + node[rb]) * p.H + (kvh << p.g_bits) + (r & g_mask)) * D + q4 * 8;
-#pragma unroll
-    for (int x = 0; x < KS; ++x) q[rb][x] = *reinterpret_cast<const uint4*>(src + x * 32);
+    for (int x = 0; x < KS; ++x) q[x] = *reinterpret_cast<const uint4*>(src + x * 16);
   }
   build_tree(tree, p.parents + (size_t)b * p.n, p.n);
 
-  f32x4_t o[RB][DB];
-  float ref[RB], sum[RB];
+  f32x16_t o[DB];
+  float ref = REF_NONE, sum = 0.f;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    ref[rb] = REF_NONE;
-    sum[rb] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[rb][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
   const float sc = p.scale_log2e;
-  // where this lane reads a 32-column block's operands from
-  const int k_off = lr * D, v_row = q4 * 4 + (lr >> 2), v_off = v_row * D + (lr & 1) * 4;
-  const int k_swz = kswz(lr), v_swz = vswz(v_row) ^ ((lr >> 1) & 1);           // (blocks and halves start at multiples of 16 rows)
+  // where this lane reads its wave's operands from, inside a stage: K row lr; for V, 16 lanes fetch 4 rows x 16 dimensions
+  // and each gets one dimension's column of them
+  const int l16 = lane & 15, v_row = hi * 4 + (l16 >> 2);
+  const int k_swz = kswz(lr), k_off = (cg * 32 + lr) * D, v_off = (cg * 32 + v_row) * D + (lane & 1) * 4;
+  const int v_piece = ((lane >> 4) & 1) * 2 + ((l16 >> 1) & 1);
 
-  auto block = [&](int t, int sb) __attribute__((always_inline)) {
-    const bool cached = t < cache_tiles;
-    const int col0 = (cached ? t : t - cache_tiles) * TILE_COLS + sb * 32, stage = (t - begin) & 1;
-    if (col0 >= (cached ? u.columns : p.n)) return;
-    const uint16_t* kp = stages + stage * TILE + sb * 32 * D + k_off;
-    const uint16_t* vp = stages + (2 + stage) * TILE + sb * 32 * D + v_off;
-    f32x4_t s[RB][2];
-    uint4 k[2][KS];
+  // S^T of this wave's columns of tile t
+  auto form_logits = [&](int t, f32x16_t& s) __attribute__((always_inline)) {
+    const uint16_t* kp = k_stages + ((t - begin) & (STAGES - 1)) * TILE + k_off;
+    s = f32x16_t{};
 #pragma unroll
-    for (int bk = 0; bk < 2; ++bk)
-#pragma unroll
-      for (int x = 0; x < KS; ++x) k[bk][x] = *reinterpret_cast<const uint4*>(kp + bk * 16 * D + ((x * 4 + q4) ^ k_swz) * 8);
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-      for (int bk = 0; bk < 2; ++bk) {
-        s[rb][bk] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < KS; ++x) s[rb][bk] = mfma_bf16(k[bk][x], q[rb][x], s[rb][bk]);
-      }
-    uint4 v[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const short4_t t0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + ((d * 2) ^ v_swz) * 8));
-      const short4_t t1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + 16 * D + ((d * 2) ^ v_swz) * 8));
-      const uint2 a0 = __builtin_bit_cast(uint2, t0), a1 = __builtin_bit_cast(uint2, t1);
-      v[d] = make_uint4(a0.x, a0.y, a1.x, a1.y);
-    }
-    // what a row does not attend
-    if (cached) {
-      if (col0 + 32 > u.columns || (u.hole >= col0 && u.hole < col0 + 32)) {
-        unsigned keep[4];                            // of the pairs of columns this lane holds
-#pragma unroll
-        for (int x = 0; x < 4; ++x) keep[x] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int c = col0 + (j >> 2) * 16 + q4 * 4 + (j & 3);
-          const bool seen = c < u.columns && c != u.hole;
-          keep[j >> 1] |= seen ? 0xffffu << (16 * (j & 1)) : 0u;
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) s[rb][j >> 2][j & 3] = seen ? s[rb][j >> 2][j & 3] : -INFINITY;
-        }
-#pragma unroll
-        for (int d = 0; d < DB; ++d) v[d] = make_uint4(v[d].x & keep[0], v[d].y & keep[1], v[d].z & keep[2], v[d].w & keep[3]);
-      }
-    } else {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const unsigned bits = tree.anc[node[rb]][col0 >> 5] >> (q4 * 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          s[rb][j >> 2][j & 3] = (bits >> ((j >> 2) * 16 + (j & 3)) & 1) ? s[rb][j >> 2][j & 3] : -INFINITY;
-      }
-    }
-    // the reference as in the kernel above
-    f32x4_t e[RB][2];
-    float fresh_sum[RB], worst = 0.f;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      float add = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        e[rb][j >> 2][j & 3] = fast_exp2(fmaf(s[rb][j >> 2][j & 3], sc, -ref[rb]));
-        add += e[rb][j >> 2][j & 3];
-      }
-      fresh_sum[rb] = sum[rb] + add;
-      worst = fmaxf(worst, fresh_sum[rb]);
-    }
-    if (__any(worst > 0x1p16f)) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float top = s[rb][0][0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, s[rb][j >> 2][j & 3]);
-        const float raised = row_max(fmaxf(ref[rb], top * sc)), by = fast_exp2(ref[rb] - raised);
-        float add = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          e[rb][j >> 2][j & 3] = fast_exp2(fmaf(s[rb][j >> 2][j & 3], sc, -raised));
-          add += e[rb][j >> 2][j & 3];
-        }
-        fresh_sum[rb] = fmaf(sum[rb], by, add);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[rb][d] *= by;
-        ref[rb] = raised;
-      }
-    }
-    if (!cached) {
-      unsigned f = 0x80008000u;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) f &= finite_halves(v[d].x) & finite_halves(v[d].y) & finite_halves(v[d].z) & finite_halves(v[d].w);
-      if (!__all(f == 0x80008000u)) {
-        unsigned bits[RB];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) bits[rb] = tree.anc[node[rb]][col0 >> 5];
-        const char* row = Vn + col0 * node_bytes + q4 * 8;
-#pragma unroll 1
-        for (int c = 0; c < min(32, p.n - col0); ++c, row += node_bytes) {
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const uint2 w = *reinterpret_cast<const uint2*>(row + d * 32);
-            const unsigned x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float odd = __uint_as_float(x[i] & ~(unsigned)((int)finite_word(x[i]) >> 31));       // 0 if it is finite
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb) o[rb][d][i] += (bits[rb] >> c & 1) ? odd : 0.f;
-            }
-          }
-        }
-#pragma unroll
-        for (int d = 0; d < DB; ++d) v[d] = make_uint4(keep_finite(v[d].x), keep_finite(v[d].y), keep_finite(v[d].z), keep_finite(v[d].w));
-      }
-    }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      sum[rb] = fresh_sum[rb];
-      uint4 h, m, l;
-      cut3(e[rb][0][0], e[rb][0][1], h.x, m.x, l.x);
-      cut3(e[rb][0][2], e[rb][0][3], h.y, m.y, l.y);
-      cut3(e[rb][1][0], e[rb][1][1], h.z, m.z, l.z);
-      cut3(e[rb][1][2], e[rb][1][3], h.w, m.w, l.w);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], l, o[rb][d]);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], m, o[rb][d]);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) o[rb][d] = mfma_bf16(v[d], h, o[rb][d]);
+    for (int x = 0; x < KS; ++x) {
+      const uint4 k = *reinterpret_cast<const uint4*>(kp + ((x * 2 + hi) ^ k_swz) * 8);
+      s = mfma_wide(k, q[x], s);
     }
   };
+  // column, inside the wave's 32, of element i
+  auto col_of = [&](int i) { return (i >> 2) * 8 + hi * 4 + (i & 3); };
+  // Rows of V that must not reach the product whatever they hold, cleared in a tile that has landed: the free slot's and those
+  // behind the last token, and the nodes' infinities and NaNs (true: there were some).
+  auto clear_rows = [&](int t) -> bool {
+    uint16_t* vp = v_stages + ((t - begin) & (STAGES - 1)) * TILE;
+    if (t < cache_tiles) {
+      const int c0 = t * TILE_COLS;
+      if (c0 + TILE_COLS > u.columns || (u.hole >= c0 && u.hole < c0 + TILE_COLS))
+        for (int x = tid; x < TILE_COLS * PARTS; x += THREADS) {
+          const int c = c0 + x / PARTS;
+          if (c >= u.columns || c == u.hole) reinterpret_cast<uint4*>(vp)[x] = make_uint4(0, 0, 0, 0);
+        }
+      return false;
+    }
+    bool odd = false;
+    for (int x = tid; x < TILE_COLS * PARTS; x += THREADS) {
+      uint4 w = reinterpret_cast<uint4*>(vp)[x];
+      const uint4 was = w;
+      w = make_uint4(keep_finite(w.x), keep_finite(w.y), keep_finite(w.z), keep_finite(w.w));
+      if (w.x != was.x || w.y != was.y || w.z != was.z || w.w != was.w) {
+        odd = true;
+        reinterpret_cast<uint4*>(vp)[x] = w;
+      }
+    }
+    return __syncthreads_or(odd);
+  };
 
-  wait_vmcnt<0>();
+  // The queries have arrived, in a form the compiler sees: it does not know of the copies above, and a wait of its own for
+  // them inside the loop would wait for the tiles on their way.
+  __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0)
+  __syncthreads();
+  bool odd = begin < end && clear_rows(begin);       // of tile t
+  f32x16_t s = {};
+  if (begin < end) form_logits(begin, s);
   __syncthreads();
   for (int t = begin; t < end; ++t) {
-    if (t + 1 < end) request(t + 1, (t + 1 - begin) & 1);
-    if (row0 < rows)
-      for (int sb = cg; sb < 4; sb += CG) block(t, sb);
-    wait_vmcnt<0>();
-    __syncthreads();
+    bool odd_next = false;
+    if (t > begin) {                                 // tile t + 1 has landed for every wave, and tile t - 1 is done with
+      if (t + 2 < end) wait_vmcnt<2 * CPW>(); else wait_vmcnt<0>();
+      __syncthreads();
+    }
+    if (t + 3 < end) request(t + 3);
+    if (t + 1 < end) odd_next = clear_rows(t + 1);
+    // what a row does not attend
+    const bool cached = t < cache_tiles;
+    const int col0 = (cached ? t : t - cache_tiles) * TILE_COLS + cg * 32;
+    if (cached) {
+      if (col0 + 32 > u.columns || (u.hole >= col0 && u.hole < col0 + 32)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int c = col0 + col_of(i);
+          s[i] = c < u.columns && c != u.hole ? s[i] : -INFINITY;
+        }
+      }
+    } else {
+      const unsigned bits = (col0 < p.n ? tree.anc[node][col0 >> 5] : 0u) >> (hi * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (bits >> ((i >> 2) * 8 + (i & 3)) & 1) ? s[i] : -INFINITY;
+    }
+    // The reference need not be the maximum: it is raised where a logit passes it by 2^8 (as at first), which is rare.
+    {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      if (__any(fmaf(top, sc, -ref) > 8.0f)) {
+        float raised = fmaxf(ref, top * sc);
+        raised = fmaxf(raised, __shfl_xor(raised, 32, 64));
+        const float by = fast_exp2(ref - raised);
+        sum *= by;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] *= by;
+        ref = raised;
+      }
+    }
+    if (odd && col0 < p.n) {                         // (after the raise, which would make a NaN of an infinity)
+      const unsigned bits = tree.anc[node][col0 >> 5];
+      const char* row_v = Vn + col0 * node_bytes + hi * 8;
+#pragma unroll 1
+      for (int c = 0; c < min(32, p.n - col0); ++c, row_v += node_bytes) {
+#pragma unroll
+        for (int d = 0; d < DB * 4; ++d) {           // dimensions 8 d + 4 hi + 0 .. 3
+          const uint2 w = *reinterpret_cast<const uint2*>(row_v + d * 16);
+          const unsigned x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float y = __uint_as_float(x[i] & ~(unsigned)((int)finite_word(x[i]) >> 31));       // 0 if it is finite
+            o[d >> 2][(d & 3) * 4 + i] += (bits >> c & 1) ? y : 0.f;
+          }
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(0x0f70);            // (no wait of the compiler's for these in the loop)
+    }
+    // logits of tile t + 1 (behind the last one: of whatever the stage holds, unused); probabilities of tile t and their
+    // product with V
+    f32x16_t next;
+    form_logits(t + 1, next);
+    const uint16_t* vp = v_stages + ((t - begin) & (STAGES - 1)) * TILE + v_off;
+    float add = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = fast_exp2(fmaf(s[i], sc, -ref));
+      add += s[i];
+    }
+    sum += add;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {                 // 16 columns: elements 8 ks .. + 7
+      uint4 h, m, l;
+      cut3(s[ks * 8], s[ks * 8 + 1], h.x, m.x, l.x);
+      cut3(s[ks * 8 + 2], s[ks * 8 + 3], h.y, m.y, l.y);
+      cut3(s[ks * 8 + 4], s[ks * 8 + 5], h.z, m.z, l.z);
+      cut3(s[ks * 8 + 6], s[ks * 8 + 7], h.w, m.w, l.w);
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        uint2 a[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int r = ks * 16 + x * 8;             // (multiples of 8 rows: a row's swizzle is that of its last three bits)
+          const int place = (d * 4 + v_piece) ^ vswz(v_row);
+          a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + r * D + place * 8)));
+        }
+        const uint4 v = make_uint4(a[0].x, a[0].y, a[1].x, a[1].y);
+        o[d] = mfma_wide(v, l, o[d]);
+        o[d] = mfma_wide(v, m, o[d]);
+        o[d] = mfma_wide(v, h, o[d]);
+      }
+    }
+    s = next;
+    odd = odd_next;
   }
+  __syncthreads();
 
   float* so = tr_smem;                               // [CG][ROWS][D + 4]
   float2* sm = reinterpret_cast<float2*>(tr_smem + CG * ROWS * OR);
+  {
+    const int r = cg * ROWS + rg * 32 + lr;
+    sum += __shfl_xor(sum, 32, 64);
+    if (hi == 0) sm[r] = make_float2(ref, sum);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = cg * ROWS + rg * 32 + rb * 16 + lr;
-    const float l = row_sum(sum[rb]);
-    if (q4 == 0) sm[r] = make_float2(ref[rb], l);
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-      *reinterpret_cast<float4*>(so + (size_t)r * OR + d * 16 + q4 * 4) = make_float4(o[rb][d][0], o[rb][d][1], o[rb][d][2], o[rb][d][3]);
+    for (int d = 0; d < DB * 4; ++d)
+      *reinterpret_cast<float4*>(so + (size_t)r * OR + d * 8 + hi * 4) =
+          make_float4(o[d >> 2][(d & 3) * 4], o[d >> 2][(d & 3) * 4 + 1], o[d >> 2][(d & 3) * 4 + 2], o[d >> 2][(d & 3) * 4 + 3]);
   }
   __syncthreads();
   finish_rows<D, CG, ROWS>(p, tree, so, sm, unit, tile, slice);
@@ -1138,12 +1167,12 @@ int launch_attend_rb(const Shape& s, const Args& a, hipStream_t st) {
 }
 template <int D, int RG>
 int launch_attend_tiled(const Shape& s, const Args& a, hipStream_t st) {
-  const size_t sums = (size_t)TR_WAVES * 32 * ((D + 4) * sizeof(float) + sizeof(float2)), stages = (size_t)4 * TILE_COLS * D * 2;
+  const size_t sums = (size_t)RG * 2 * 32 * ((D + 4) * sizeof(float) + sizeof(float2)), stages = (size_t)2 * STAGES * TILE_COLS * D * 2;
   const size_t lds = sums > stages ? sums : stages;
   auto kernel = tree_attend_tiled_kernel<D, RG>;
   if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
   const int items = s.row_tiles * s.slices * a.U;
-  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(RG * 128), lds, st, a);
   return launch_merge<D>(s, a, st);
 }
 template <typename T, int D>
