@@ -72,7 +72,29 @@ struct TreeBits {
   unsigned anc[MAX_NODES][MAX_WORDS];
   int up[MAX_NODES];
 };
+// Up to 64 nodes: the first wave alone, a node to a lane, generations through lane exchanges instead of barriers.
+__device__ inline void build_small_tree(TreeBits& sm, const int32_t* parents, int n) {
+  const int i = threadIdx.x;
+  if (i < 64) {
+    const int p = i < n ? parents[i] : -2;
+    int up = p >= -1 && p < i ? p : -2;
+    unsigned lo = i < 32 ? 1u << i : 0u, hi = i < 32 ? 0u : 1u << (i - 32);
+    while (__any(up >= 0)) {
+      const int from = up >= 0 ? up : i;
+      const unsigned l = __shfl(lo, from, 64), h = __shfl(hi, from, 64);
+      const int next = __shfl(up, from, 64);
+      if (up >= 0) { lo |= l; hi |= h; up = next; }
+    }
+    if (i < n) {
+      sm.anc[i][0] = lo;
+      sm.anc[i][1] = hi;
+      sm.up[i] = up;
+    }
+  }
+  __syncthreads();
+}
 __device__ inline void build_tree(TreeBits& sm, const int32_t* parents, int n) {
+  if (n <= 64) return build_small_tree(sm, parents, n);
   const int i = threadIdx.x, words = (n + 31) / 32;
   if (i < n) {
     const int p = parents[i];
@@ -975,17 +997,36 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(Args p, int rows_per_ti
   const int tile = row / rows_per_tile, r = row % rows_per_tile;
   const float* part = p.scratch + ((size_t)unit * p.row_tiles + tile) * slices * rows_per_tile * (D + 4) + (size_t)r * (D + 4);
   const size_t step = (size_t)rows_per_tile * (D + 4);
+  // eight slices at a time, those past the last one empty: a batch's reads are one wait
+  constexpr int BATCH = 8;
   float M = REF_NONE, L = 0.f;
-  for (int s = 0; s < slices; ++s) M = fmaxf(M, part[s * step + D]);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   bool present = true;
-  for (int s = 0; s < slices; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(part + s * step + D);
-    const float4 y = *reinterpret_cast<const float4*>(part + s * step + c);
-    const float f = fast_exp2(ml.x - M);
-    present = present && !(ml.y < 0.f);
-    L = fmaf(ml.y, f, L);
-    a.x = fmaf(y.x, f, a.x); a.y = fmaf(y.y, f, a.y); a.z = fmaf(y.z, f, a.z); a.w = fmaf(y.w, f, a.w);
+  for (int s0 = 0; s0 < slices; s0 += BATCH) {
+    float2 ml[BATCH];
+    float4 y[BATCH];
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      const float* src = part + min(s0 + x, slices - 1) * step;
+      ml[x] = *reinterpret_cast<const float2*>(src + D);
+      y[x] = *reinterpret_cast<const float4*>(src + c);
+    }
+    float top = M;
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) top = fmaxf(top, ml[x].x);
+    const float by = fast_exp2(M - top);
+    L *= by;
+    a.x *= by; a.y *= by; a.z *= by; a.w *= by;
+    M = top;
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      if (s0 + x < slices) {
+        const float f = fast_exp2(ml[x].x - M);
+        present = present && !(ml[x].y < 0.f);
+        L = fmaf(ml[x].y, f, L);
+        a.x = fmaf(y[x].x, f, a.x); a.y = fmaf(y[x].y, f, a.y); a.z = fmaf(y[x].z, f, a.z); a.w = fmaf(y[x].w, f, a.w);
+      }
+    }
   }
   const int b = unit / p.Hkv, kvh = unit % p.Hkv;
   const size_t at = ((size_t)b * p.n + (row >> p.g_bits)) * p.H + (kvh << p.g_bits) + (row & ((1 << p.g_bits) - 1));
