@@ -462,7 +462,6 @@ __device__ inline void add_not_finite(f32x4_t (&o)[RB][D / 16], const char* row,
 // Scratch of a call: one partial result per (unit, row tile, slice): [rows][D] sums relative to the row's reference, then
 // [rows][2] reference and sum.
 struct Shape {
-  bool tiled;
   int rows_per_tile, row_tiles, slices;
 };
 
@@ -527,7 +526,6 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
   const size_t node_bytes = (size_t)p.Hkv * ROWB;
   const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
   const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
-  const unsigned k_lane = q4 * 16, v_lane = lr * (DPL * (int)sizeof(T));       // this lane's piece of a row
 
   typename O::Keys k;
   typename O::Values v;
@@ -537,40 +535,46 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
       if (blk < cache_blocks)
         slot = slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(blk * O::COLS + (lane & (O::COLS - 1)), u.n - 1));
   };
-  auto load_keys = [&](int blk) {
+  // Lane-dependent addresses are worked out anew at each load (`anew`): kept across the loop they are thirty registers.
+  auto anew = [](int x) { asm volatile("" : "+v"(x)); return x; };
+  auto load_keys = [&](int blk) __attribute__((always_inline)) {
+    const int l = anew(lane), r = l & 15;
+    const unsigned piece = (l >> 4) * 16;
     if (blk < cache_blocks) {
       if constexpr (ROPE) {
 #pragma unroll
         for (int bk = 0; bk < BK; ++bk)
-          O::load_k(k, bk, Ku + (size_t)(unsigned)__shfl(slot, bk * 16 + lr, 64) * ROWB, k_lane);
+          O::load_k(k, bk, Ku + (size_t)(unsigned)__shfl(slot, bk * 16 + r, 64) * ROWB, piece);
       } else {
         const char* base = Ku + (size_t)blk * (O::COLS * ROWB);
         const int last = p.cap - 1 - blk * O::COLS;
 #pragma unroll
-        for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, base, (unsigned)min(bk * 16 + lr, last) * ROWB + k_lane);
+        for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, base, (unsigned)min(bk * 16 + r, last) * ROWB + piece);
       }
     } else {
       const int c0 = (blk - cache_blocks) * O::COLS;
 #pragma unroll
-      for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, Kn + min(c0 + bk * 16 + lr, p.n - 1) * node_bytes, k_lane);
+      for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, Kn + min(c0 + bk * 16 + r, p.n - 1) * node_bytes, piece);
     }
   };
-  auto load_values = [&](int blk) {
+  auto load_values = [&](int blk) __attribute__((always_inline)) {
+    const int l = anew(lane), g = l >> 4;
+    const unsigned piece = (l & 15) * (DPL * (int)sizeof(T));
     if (blk < cache_blocks) {
       if constexpr (ROPE) {
 #pragma unroll
         for (int j = 0; j < O::NCOL; ++j)
-          O::load_v(v, j, Vu + (size_t)(unsigned)__shfl(slot, O::col(q4, j), 64) * ROWB, v_lane);
+          O::load_v(v, j, Vu + (size_t)(unsigned)__shfl(slot, O::col(g, j), 64) * ROWB, piece);
       } else {
         const char* base = Vu + (size_t)blk * (O::COLS * ROWB);
         const int last = p.cap - 1 - blk * O::COLS;
 #pragma unroll
-        for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, base, (unsigned)min(O::col(q4, j), last) * ROWB + v_lane);
+        for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, base, (unsigned)min(O::col(g, j), last) * ROWB + piece);
       }
     } else {
       const int c0 = (blk - cache_blocks) * O::COLS;
 #pragma unroll
-      for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, Vn + min(c0 + O::col(q4, j), p.n - 1) * node_bytes, v_lane);
+      for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, Vn + min(c0 + O::col(g, j), p.n - 1) * node_bytes, piece);
     }
   };
   load_slots(begin + wave);
@@ -616,6 +620,9 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
   }
   const float sc = p.scale_log2e;
 
+  // One block from its operands; the next block's go where its own were as soon as they are used up.  (A second set of
+  // operands, requested a whole block ahead, was no faster: head_dim 64 23.4 us with it, 23.9 without at 256 units x 2048 slots;
+  // at head_dim 128 it does not fit the registers, 55.4 and 48.7.)
   for (int blk = begin + wave; blk < end; blk += TR_WAVES) {
     const bool cached = blk < cache_blocks;
     const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS, next = blk + TR_WAVES;
@@ -727,8 +734,8 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
 // ---------------------------------------------------------------------------------------------
 // attend, many rows: bf16 storage, tiles of columns shared by the workgroup's waves
 // ---------------------------------------------------------------------------------------------
-// With more than 32 rows a unit the kernel above reads every row of K and V once per 32 of them.  Here a workgroup owns 64
-// or 128 rows: RG groups of 32 rows x two waves that take one half of a tile's 64 columns each.  Tiles come by asynchronous
+// The kernel above reads every row of K and V once per 32 rows.  Here a workgroup owns 128 rows: RG groups of 32 x two waves
+// that take one half of a tile's 64 columns each.  Tiles come by asynchronous
 // copies into LDS, row-major as they lie in memory with the 16-byte pieces of a row swizzled, so that the operand reads (16
 // bytes of a row for K, the transposing read for V) spread over the banks.  v_mfma_f32_32x32x16_bf16: a wave's vector
 // instructions issue beside it, while a 16x16x32 holds them up (256 rows into 4096 slots 149 us with those).  A lane then
@@ -746,15 +753,14 @@ __device__ inline void async_copy16_at(const char* uniform_base, unsigned lane_o
                :: "v"(lane_offset), "s"(uniform_base), "s"(lds_base) : "memory");
 }
 
-template <int D, int RG>
-__global__ __launch_bounds__(RG * 128, RG / 2) void tree_attend_tiled_kernel(Args p) {
-  constexpr int CG = 2, WAVES = RG * CG, THREADS = WAVES * 64;
+template <int D>
+__global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p) {
+  constexpr int RG = 4, CG = 2, WAVES = TR_WAVES, THREADS = TR_THREADS;
   constexpr int ROWS = RG * 32, KS = D / 16, DB = D / 32, OR = D + 4, ROWB = D * 2;
   constexpr int PARTS = D / 8, RPC = 64 / PARTS;                   // 16-byte pieces of a row, rows of a 1 KB copy
   constexpr int WROWS = TILE_COLS / WAVES, CPW = WROWS / RPC;   // tile rows a wave copies, its copies of K (and of V) a tile
   constexpr int TILE = TILE_COLS * D;                              // elements of a staged tile
-  static_assert(TILE_COLS == CG * 32, "a wave takes 32 columns of every tile");
-  static_assert(THREADS >= MAX_NODES, "one thread per node");
+  static_assert(RG * CG == WAVES && TILE_COLS == CG * 32, "a wave takes 32 columns of every tile");
   extern __shared__ __attribute__((aligned(1024))) float tr_smem[];
   __shared__ TreeBits tree;
   uint16_t* k_stages = reinterpret_cast<uint16_t*>(tr_smem);
@@ -1171,19 +1177,26 @@ int pick_slices(const Params& p, int units_times_tiles, int blocks) {
 }
 int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
 
+// Rows of a workgroup, and slices so that there is a workgroup for each of the 256 compute units but no second round.  16 rows
+// run fastest where that leaves three slices or more (or there are few rows), 32 where it fills no more than one round, else
+// 128 that share the tiles' way from memory.  us a call, bf16 x 128 unless noted, rows/slices:
+//   units x rows, slots   8 x 104, 2048  16/4 14.5, 32/8 16.1, 128/16 20.9;   8 x 32  16/9 12.5, 32/9 15.0;   2 x 512, 4096  16/4 19.0, 32/8 19.1
+//   16 x 104, 2048  16/2 19.1, 32/4 18.6;   32 x 104  16/1 24.0, 32/2 23.2, 128/8 26.6;   64 x 52  16/1 24.4, 32/2 23.5
+//   128 x 24, 1024  16/1 16.1, 32/1 18.9;   256 x 32, 2048  16/1 62.6, 32/1 54.4;   128 x 64  16/1 51.9, 32/1 32.7, 128/1 63
+//   128 x 128, 4096  32/1 107, 128/2 90;   8 x 2048, 2048  32/1 68, 128/2 59, 128/1 79;   128 x 256, 4096  32/1 200, 128/1 146
+//   x 64: 128 x 128, 4096  32/1 62.1, 128/2 61.9;   8 x 2048, 2048  32/1 48.6, 128/2 47.9;   256 x 48, 2048  32/1 39.4
 Shape attend_shape(const Params& p, int n) {
+  const int rows = n * p.G, tiles16 = (rows + 15) / 16, tiles32 = (rows + 31) / 32, chip = 256, cols = block_cols(p);
   Shape s;
-  const int rows = n * p.G, cols = block_cols(p);
-  s.tiled = rows > 32 && p.dtype == TREEKV_BF16 && !(p.flags & TREEKV_POSITION_RERANK);
-  s.rows_per_tile = rows <= 16 ? 16 : !s.tiled ? 32 : rows <= 64 ? 64 : 128;
+  if ((long long)p.U * tiles16 <= (rows <= 32 ? chip : chip / 3)) s.rows_per_tile = 16;
+  else if (rows <= 64 || (long long)p.U * tiles32 <= chip || p.dtype != TREEKV_BF16 || (p.flags & TREEKV_POSITION_RERANK)) s.rows_per_tile = rows <= 16 ? 16 : 32;
+  else s.rows_per_tile = 128;
   s.row_tiles = (rows + s.rows_per_tile - 1) / s.rows_per_tile;
-  if (s.tiled) {
-    const int tiles = (p.cap + TILE_COLS - 1) / TILE_COLS + (n + TILE_COLS - 1) / TILE_COLS;
-    s.slices = 256 / (p.U * s.row_tiles);
-    s.slices = s.slices < 1 ? 1 : s.slices > tiles ? tiles : s.slices;
-  } else {
-    s.slices = pick_slices(p, p.U * s.row_tiles, (p.cap + cols - 1) / cols + (n + cols - 1) / cols);
-  }
+  // a wave has a block of columns at least, the large workgroup a tile
+  const int blocks = (p.cap + cols - 1) / cols + (n + cols - 1) / cols, tiles = (p.cap + TILE_COLS - 1) / TILE_COLS + (n + TILE_COLS - 1) / TILE_COLS;
+  const int most = s.rows_per_tile == 128 ? tiles : (blocks + TR_WAVES - 1) / TR_WAVES;
+  const long long fit = chip / ((long long)p.U * s.row_tiles);
+  s.slices = fit < 1 ? 1 : fit < most ? (int)fit : most;
   return s;
 }
 
@@ -1206,14 +1219,14 @@ int launch_attend_rb(const Shape& s, const Args& a, hipStream_t st) {
   hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
   return launch_merge<D>(s, a, st);
 }
-template <int D, int RG>
+template <int D>
 int launch_attend_tiled(const Shape& s, const Args& a, hipStream_t st) {
-  const size_t sums = (size_t)RG * 2 * 32 * ((D + 4) * sizeof(float) + sizeof(float2)), stages = (size_t)2 * STAGES * TILE_COLS * D * 2;
+  const size_t sums = (size_t)TR_WAVES * 32 * ((D + 4) * sizeof(float) + sizeof(float2)), stages = (size_t)2 * STAGES * TILE_COLS * D * 2;
   const size_t lds = sums > stages ? sums : stages;
-  auto kernel = tree_attend_tiled_kernel<D, RG>;
+  auto kernel = tree_attend_tiled_kernel<D>;
   if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
   const int items = s.row_tiles * s.slices * a.U;
-  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(RG * 128), lds, st, a);
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
   return launch_merge<D>(s, a, st);
 }
 template <typename T, int D>
@@ -1223,7 +1236,7 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
   const Args a = {p.K, p.V, p.meta, p.E, p.R, p.rope_tab, t.q, t.k, t.v, t.parents, out, lse, scratch, p.budget, p.cap, p.n_sink,
                   p.n_recent, p.m, p.U, p.H, p.Hkv, p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3, t.n, s.row_tiles, s.slices, p.scale_log2e};
   if constexpr (sizeof(T) == 2) {
-    if (s.tiled) return s.rows_per_tile == 64 ? launch_attend_tiled<D, 2>(s, a, st) : launch_attend_tiled<D, 4>(s, a, st);
+    if (s.rows_per_tile == 128) return launch_attend_tiled<D>(s, a, st);
   }
   if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(s, a, st) : launch_attend_rb<T, D, 1, false>(s, a, st);
   return rope ? launch_attend_rb<T, D, 2, true>(s, a, st) : launch_attend_rb<T, D, 2, false>(s, a, st);

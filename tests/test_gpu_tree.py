@@ -62,7 +62,8 @@ def make(binding, *, budget=48, batch=2, hkv=2, G=2, d=64, dtype="bf16", flags=0
     return kv
 
 
-def check_attend(kv, q, k, v, parents, out, lse):
+def check_attend(kv, q, k, v, parents, out, lse, every=1):
+    """Against the plain form, every `every`-th unit and the last."""
     import torch
 
     c, G = kv.cfg, kv.cfg.q_heads // kv.cfg.kv_heads
@@ -71,6 +72,8 @@ def check_attend(kv, q, k, v, parents, out, lse):
     out, lse = out.double().cpu(), lse.double().cpu()
     for b in range(c.batch):
         for h in range(c.kv_heads):
+            if (b * c.kv_heads + h) % every and (b, h) != (c.batch - 1, c.kv_heads - 1):
+                continue
             heads = slice(h * G, (h + 1) * G)
             want, want_lse, bound, lse_bound, _ = ref.attend_unit(kv, states[b * c.kv_heads + h], q[b, :, heads], k[b, :, h], v[b, :, h],
                                                                   parents[b])
@@ -95,6 +98,10 @@ SHAPES = [
     (1000, 1500, 5, 1, 2, 1, 128, "bf16", 0),              # several slices
     (1000, 1500, 5, 1, 2, 4, 64, "f32", 0),
     (200, 333, 31, 40, 4, 1, 64, "bf16", 0),               # many units: one slice
+    (100, 150, 20, 16, 8, 4, 128, "bf16", 0),              # many units and rows: 80 rows share tiles
+    (100, 70, 33, 16, 8, 4, 64, "bf16", 0),                # two row tiles, still filling
+    (300, 450, 256, 5, 8, 1, 128, "bf16", 0),              # the same in slices
+    (300, 450, 256, 5, 8, 1, 64, "bf16", 0),
     (48, 0, 3, 1, 1, 2, 64, "bf16", RERANK),
     (48, 30, 21, 2, 2, 2, 128, "bf16", RERANK),
     (48, 133, 40, 2, 2, 4, 64, "bf16", RERANK),
@@ -119,19 +126,19 @@ def test_attend(binding, shape, kind):
     out.fill_(7.0), lse.fill_(7.0)
     kv.tree_attend(q, k, v, torch.tensor(parents, dtype=torch.int32, device="cuda"), out, lse, scratch)
     assert torch.equal(before, kv.export_state())          # nothing was changed
-    check_attend(kv, q, k, v, parents, out, lse)
+    check_attend(kv, q, k, v, parents, out, lse, every=1 if batch * hkv < 20 else 37)
     again = torch.empty_like(out)
     kv.tree_attend(q, k, v, torch.tensor(parents, dtype=torch.int32, device="cuda"), again)    # no lse, scratch of its own
     assert torch.equal(out, again)
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
-@pytest.mark.parametrize("flags", [0, RERANK])
-def test_attend_with_rising_logits(binding, dtype, d, flags):
+@pytest.mark.parametrize("flags,batch,G", [(0, 1, 2), (RERANK, 1, 2), (0, 90, 8)])
+def test_attend_with_rising_logits(binding, dtype, d, flags, batch, G):
     """Large, ordered logits: every block of columns raises the reference of the sums."""
     import torch
 
-    kv = make(binding, budget=700, batch=1, hkv=1, G=2, d=d, dtype=dtype, flags=flags)
+    kv = make(binding, budget=700, batch=batch, hkv=1, G=G, d=d, dtype=dtype, flags=flags)
     q, k, v = tokens(kv, 700, 5)
     direction = torch.randn(d, generator=torch.Generator().manual_seed(1))
     direction = (direction / direction.norm()).cuda()
@@ -141,22 +148,22 @@ def test_attend_with_rising_logits(binding, dtype, d, flags):
         kv.prefill_chunk(*[x[:, at:at + 100].contiguous() for x in (q, k, v)], 100, out, ret, nret, ev)
     q, k, v = tokens(kv, 12, 6)
     q = (q.float() + 20.0 * direction).to(q.dtype)
-    parents = [tree("drafted", 12, random.Random(3))]
+    parents = [tree("drafted", 12, random.Random(3))] * batch
     out, lse, scratch = kv.new_tree_outputs(12)
     kv.tree_attend(q, k, v, torch.tensor(parents, dtype=torch.int32, device="cuda"), out, lse, scratch)
-    check_attend(kv, q, k, v, parents, out, lse)
+    check_attend(kv, q, k, v, parents, out, lse, every=45)
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
-@pytest.mark.parametrize("flags", [0, RERANK])
-def test_hidden_infinities_and_nans(binding, dtype, d, flags):
+@pytest.mark.parametrize("flags,batch", [(0, 1), (RERANK, 1), (0, 30)])
+def test_hidden_infinities_and_nans(binding, dtype, d, flags, batch):
     """A node's rows are not finite: who does not attend it gets the bits it gets without; who does, what arithmetic says."""
     import torch
 
-    kv = make(binding, budget=48, batch=1, hkv=2, G=4, d=d, dtype=dtype, flags=flags, fed=99)
+    kv = make(binding, budget=48, batch=batch, hkv=2, G=4, d=d, dtype=dtype, flags=flags, fed=99)
     n, inf, nan = 40, float("inf"), float("nan")
     parents = [-1, 0, 0, -1, 3, -2, 5] + [rng if rng < 5 else 4 for rng in range(n - 7)]
-    par = torch.tensor([parents], dtype=torch.int32, device="cuda")
+    par = torch.tensor([parents] * batch, dtype=torch.int32, device="cuda")
     q, k, v = tokens(kv, n, 8)
     clean, lse, scratch = kv.new_tree_outputs(n)
     kv.tree_attend(q, k, v, par, clean, lse, scratch)
@@ -168,6 +175,7 @@ def test_hidden_infinities_and_nans(binding, dtype, d, flags):
     k2[0, 6], v2[0, 6] = inf, nan                          # its child
     out, lse2, _ = kv.new_tree_outputs(n)
     kv.tree_attend(q2, k2, v2, par, out, lse2, scratch)
+    assert torch.equal(out[1:], clean[1:])
     out, clean = out.cpu()[0], clean.cpu()[0]
     chain = ref.chains(parents)
     for i in range(n):
@@ -188,7 +196,7 @@ def test_hidden_infinities_and_nans(binding, dtype, d, flags):
     # two of opposite sign seen together are a NaN
     v3 = v.clone()
     v3[0, 0, 0, 7], v3[0, 1, 0, 7] = inf, -inf
-    got = torch.empty_like(clean)[None].cuda()
+    got = kv.new_tree_outputs(n)[0]
     kv.tree_attend(q, k, v3, par, got, lse2, scratch)
     assert bool(torch.isnan(got[0, 1, :4, 7]).all()) and bool((got[0, 0, :4, 7] == inf).all()) and bool(torch.isfinite(got[0, 3]).all())
 
