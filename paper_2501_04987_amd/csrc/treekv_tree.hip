@@ -1090,6 +1090,22 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
   const int cs_stride = cap_cols + (p.max_chunk + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
   unsigned long long* acc = p.pf_colacc + (size_t)unit * cs_stride;
   T* sq = reinterpret_cast<T*>(tr_smem);
+  auto load_keys = [&](typename O::Keys& k, int blk) __attribute__((always_inline)) {
+    if (blk < cache_blocks && !ROPE) {
+      const char* base = Ku + (size_t)blk * (O::COLS * ROWB);
+      const int last = p.cap - 1 - blk * O::COLS;
+#pragma unroll
+      for (int bk = 0; bk < BK; ++bk) O::load_k(k, bk, base, (unsigned)min(bk * 16 + lr, last) * ROWB + q4 * 16);
+    } else {
+#pragma unroll
+      for (int bk = 0; bk < BK; ++bk) {
+        const int c = (blk < cache_blocks ? blk : blk - cache_blocks) * O::COLS + bk * 16 + lr;
+        const char* row = blk < cache_blocks ? Ku + (size_t)slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(c, u.n - 1)) * ROWB
+                                             : Kn + path[min(c, L - 1)] * node_bytes;
+        O::load_k(k, bk, row, q4 * 16);
+      }
+    }
+  };
   for (int r0 = 0; r0 < rows; r0 += CS_ROWS) {
     const int here = min(CS_ROWS, rows - r0), tiles = (here + 15) / 16;
     __syncthreads();                                 // the rows before are done with
@@ -1117,20 +1133,17 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
       row_lse[tid] = t.lse[((size_t)b * t.n + path[i]) * p.H + kvh * p.G + r % p.G] * LOG2E;
     }
     __syncthreads();
+    typename O::Keys k, next_k;
+    if (begin + wave < end) load_keys(k, begin + wave);
     for (int blk = begin + wave; blk < end; blk += TR_WAVES) {
       const bool cached = blk < cache_blocks;
       const int col0 = (cached ? blk : blk - cache_blocks) * O::COLS;
-      typename O::Keys k;
+      if (blk + TR_WAVES < end) load_keys(next_k, blk + TR_WAVES);
       int pos[BK];
 #pragma unroll
       for (int bk = 0; bk < BK; ++bk) {
         const int c = col0 + bk * 16 + lr;
-        const char* row;
-        if (!cached) row = Kn + path[min(c, L - 1)] * node_bytes;
-        else if (ROPE) row = Ku + (size_t)slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(c, u.n - 1)) * ROWB;
-        else row = Ku + (size_t)min(c, p.cap - 1) * ROWB;
         pos[bk] = cached ? min(c, u.n - 1) : u.n + min(c, L - 1);
-        O::load_k(k, bk, row, q4 * 16);
       }
       float col_sum[O::NCOL];
 #pragma unroll
@@ -1154,27 +1167,24 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tr
           col_sum[j] += seen ? e : 0.f;
         }
       }
+      float mine = 0.f;                              // lane lr of a group passes on the group's column lr
 #pragma unroll
       for (int j = 0; j < O::NCOL; ++j) {
         const float x = group_sum<16>(col_sum[j]);
-        const int c = col0 + O::col(q4, j);
-        if (lr == j && (cached ? c < u.columns && c != u.hole : c < L)) {
-          const int slot = ROPE && cached ? slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, c) : c;
-          unsigned long long* a = acc + (cached ? slot : cap_cols + c);
-          *a += (unsigned long long)(long long)(x * COLSUM_FIX + 0.5f);
-        }
+        mine = lr == j ? x : mine;
       }
+      const int c = col0 + O::col(q4, lr & (O::NCOL - 1));
+      if (lr < O::NCOL && (cached ? c < u.columns && c != u.hole : c < L)) {
+        const int slot = ROPE && cached ? slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, c) : c;
+        unsigned long long* a = acc + (cached ? slot : cap_cols + c);
+        const unsigned long long fix = (unsigned long long)(long long)(mine * COLSUM_FIX + 0.5f);
+        *a = r0 == 0 ? fix : *a + fix;               // (they are zero between calls)
+      }
+      k = next_k;
     }
   }
 }
 
-// Slices of a unit's columns: as many workgroups as the chip has compute units, each wave with a block at least.
-int pick_slices(const Params& p, int units_times_tiles, int blocks) {
-  int s = 256 / units_times_tiles;
-  const int most = (blocks + TR_WAVES - 1) / TR_WAVES;
-  s = s > most ? most : s;
-  return s < 1 ? 1 : s;
-}
 int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
 
 // Rows of a workgroup, and slices so that there is a workgroup for each of the 256 compute units but no second round.  16 rows
@@ -1245,7 +1255,9 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
 template <typename T, int D, bool ROPE>
 int launch_colsums_d(const Params& p, const Tree& t, int32_t* status, hipStream_t st) {
   const size_t lds = (size_t)(ROPE ? Ops<T, D>::QPARTS : 1) * CS_ROWS * q_row_elems<T, D>() * sizeof(T);
-  const int cols = block_cols(p), slices = pick_slices(p, p.U, (p.budget + cols - 1) / cols + (t.max_len + cols - 1) / cols);
+  // two workgroups for each of the 256 compute units, each wave with a block of columns at least
+  const int cols = block_cols(p), blocks = (p.cap + cols - 1) / cols + (t.max_len + cols - 1) / cols;
+  const int most = (blocks + TR_WAVES - 1) / TR_WAVES, fit = 512 / p.U, slices = fit < 1 ? 1 : fit < most ? fit : most;
   auto kernel = tree_colsum_kernel<T, D, ROPE>;
   if (lds > 48 * 1024 &&
       hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)))
