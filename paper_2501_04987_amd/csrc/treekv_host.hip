@@ -111,8 +111,18 @@ __global__ void scores_kernel(Params p, float* __restrict__ scores) {
 }
 
 // Retained rows in position order, zeros behind them.  A lane copies one 16-byte piece of GATHER_ROWS rows of K and of V, all
-// requested before the first is stored: 256 units x 2048 rows of 256 bytes 91 us, 5.9 TB/s in and out (139 with a workgroup of 64 a row).
+// requested before the first is stored: 256 units x 2048 rows of 256 bytes 91 us (139 with a workgroup of 64 a row).
+// STREAM: more than 64 MB are stored past the caches, where nothing of them would be left for a reader: 85 us, 6.3 TB/s in and out,
+// and the kernels around it find more of their own (a commit with its snapshot 144 -> 131 us).
 constexpr int GATHER_THREADS = 256, GATHER_ROWS = 4;
+constexpr size_t STREAM_BYTES = (size_t)64 << 20;
+template <bool STREAM>                                               // (chosen at run time, the compiler makes one ordinary store of the two)
+__device__ inline void store16(uint4* dst, const uint4& v) {
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4u, v), reinterpret_cast<v4u*>(dst));
+  else *dst = v;
+}
+template <bool STREAM>
 __global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uint4* __restrict__ Kout, uint4* __restrict__ Vout, int row_vec) {
   const int unit = blockIdx.y, per = GATHER_THREADS / row_vec;       // row_vec is a power of two, 32 at most
   const int* meta = p.meta + (size_t)unit * META_STRIDE;
@@ -136,12 +146,17 @@ __global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uin
   for (int x = 0; x < GATHER_ROWS; ++x) {
     const int i = first + x * per;
     const size_t dst = ((size_t)unit * p.budget + i) * row_vec + e;
-    if (i < p.budget) { Kout[dst] = k[x]; Vout[dst] = v[x]; }
+    if (i < p.budget) {
+      store16<STREAM>(Kout + dst, k[x]);
+      store16<STREAM>(Vout + dst, v[x]);
+    }
   }
 }
-dim3 gather_grid(const Params& p, int row_vec) {
-  const int rows = GATHER_THREADS / row_vec * GATHER_ROWS;
-  return dim3((p.budget + rows - 1) / rows, p.U);
+int gather(const Params& p, void* K_out, void* V_out, hipStream_t s) {
+  const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16, rows = GATHER_THREADS / row_vec * GATHER_ROWS;
+  auto kernel = (size_t)2 * p.U * p.budget * row_vec * 16 > STREAM_BYTES ? gather_kv_kernel<true> : gather_kv_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3((p.budget + rows - 1) / rows, p.U), dim3(GATHER_THREADS), 0, s, p, (uint4*)K_out, (uint4*)V_out, row_vec);
+  return finish_launch();
 }
 
 // ---- snapshots of a context's state (treekv_export_state / treekv_import_state) -------------------
@@ -318,11 +333,9 @@ int record_hip(treekv_ctx* ctx, int rc) {
 
 int launch_export_state(const Params& p, char* dst, hipStream_t s) {
   const treekv_state_layout l = state_layout(p);
-  const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16;
   hipLaunchKernelGGL(export_state_kernel, dim3(p.U, (p.budget + 255) / 256), dim3(256), 0, s, p, (int*)(dst + l.header), (int*)(dst + l.positions),
                      (int*)(dst + l.slots), (float*)(dst + l.S));
-  hipLaunchKernelGGL(gather_kv_kernel, gather_grid(p, row_vec), dim3(GATHER_THREADS), 0, s, p, (uint4*)(dst + l.K), (uint4*)(dst + l.V), row_vec);
-  return finish_launch();
+  return gather(p, dst + l.K, dst + l.V, s);
 }
 
 int launch_import_state(const Params& p, const char* src, int32_t* status, hipStream_t s) {
@@ -347,11 +360,7 @@ int launch_scores(const Params& p, float* scores, hipStream_t s) {
   return check_launch();
 }
 
-int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s) {
-  const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16;
-  hipLaunchKernelGGL(gather_kv_kernel, gather_grid(p, row_vec), dim3(GATHER_THREADS), 0, s, p, (uint4*)K_out, (uint4*)V_out, row_vec);
-  return check_launch();
-}
+int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s) { return gather(p, K_out, V_out, s); }
 
 }  // namespace tkv
 

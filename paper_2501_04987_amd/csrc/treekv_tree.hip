@@ -1063,7 +1063,7 @@ __device__ inline int path_length(const Tree& t, int b) {
 // grid (slices, U).  A column belongs to one lane group of one wave for the whole call, so its accumulator is added to
 // without atomics.
 template <typename T, int D, bool ROPE>
-__global__ __launch_bounds__(TR_THREADS, 2) void tree_colsum_kernel(Params p, Tree t, int slices, int32_t* __restrict__ status) {
+__global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(Params p, Tree t, int slices, int32_t* __restrict__ status) {
   using O = Ops<T, D>;
   constexpr int QR = q_row_elems<T, D>(), Q_PART = CS_ROWS * QR, BK = O::COLS / 16, ROWB = D * (int)sizeof(T);
   static_assert(TR_THREADS >= MAX_NODES, "one thread per token of the path");
