@@ -6,9 +6,10 @@ built, `load()` raises.
 """
 from __future__ import annotations
 
-import contextlib
+import array
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libtreekv.so")
@@ -99,8 +100,8 @@ def load() -> C.CDLL:
     lib.treekv_tree_scratch_bytes.restype = C.c_size_t
     lib.treekv_tree_attend.argtypes = [vp, vp, vp, vp, i32p, C.c_int, vp, vp, vp, C.c_size_t, vp]
     lib.treekv_tree_commit.argtypes = [vp, vp, vp, vp, i32p, vp, C.c_int, i32p, i32p, C.c_int, i32p, i32p, i32p, i32p, vp]
-    lib.treekv_fork.argtypes = [vp, vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int, vp]
-    lib.treekv_qkv_prepare.argtypes = [C.POINTER(treekv_qkv_args), vp]
+    lib.treekv_fork.argtypes = [vp, vp, vp, vp, C.c_int, vp]
+    lib.treekv_qkv_prepare.argtypes = [vp, vp]
     lib.treekv_probe_read.argtypes = [vp, C.c_size_t, C.c_int, C.c_int, vp, vp]
     lib.treekv_probe_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.treekv_probe_mfma.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), vp]
@@ -155,23 +156,19 @@ def wavelet_components(a, V, levels: int, per_head=None, mean=None):
     return per_head, mean
 
 
-def _want(t, what: str, dtype, shape, device):
-    """`t` is what a kernel will take it for: contiguous, of this type and shape, on this device."""
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{what}: {dtype} {tuple(shape)}, contiguous, on {device} is wanted, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+def _want(t, what: str, dtype, shape, index: int):
+    """`t` is what a kernel will take it for: contiguous, of this type and shape, on the GPU `index` (-1: the host)."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{what}: {dtype} {tuple(shape)}, contiguous, on device {index} is wanted, "
+                         f"not {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ', strided,'} on {t.device}")
 
 
-def _on(device):
-    """A context in which `device` is the current one: kernels are launched there, and the null stream is its."""
+def _elsewhere(index: int) -> bool:
+    """Whether GPU `index` is not the current one: kernels are launched on that, and the null stream is its."""
     import torch
 
-    if device.type != "cuda" or device.index is None or torch.cuda.current_device() == device.index:
-        return _NOTHING
-    return torch.cuda.device(device)
-
-
-_NOTHING = contextlib.nullcontext()
+    current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return index >= 0 and current() != index
 
 
 def rope_frequencies(rotary_dim: int, base: float = 10000.0, device="cuda"):
@@ -182,6 +179,20 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, device="cuda"):
     return torch.pow(torch.tensor(float(base), dtype=torch.float64), -2.0 * i / rotary_dim).to(device)
 
 
+_QKV = struct.Struct("10P3q7if")                 # treekv_qkv_args (packed so: a ctypes structure takes 3 us longer to fill)
+
+
+def _rows_in(x, name, dtype, tokens, d, index):
+    """The heads of an input of qkv_prepare and the distance between its tokens."""
+    n, heads, w = x.shape
+    if x.dtype is not dtype or x.get_device() != index or n != tokens or w != d:
+        raise ValueError(f"{name}: {dtype} [{tokens}, heads, {d}] on device {index} is wanted, not {x.dtype} {tuple(x.shape)} on {x.device}")
+    far, near, one = x.stride()
+    if one != 1 or (near != d and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous, not strides {x.stride()}")
+    return heads, far
+
+
 def qkv_prepare(q, k=None, v=None, *, q_weight=None, k_weight=None, eps: float = 1e-6, positions=None, inv_freq=None,
                 halves: bool = False, to_planes: bool = False, out=None):
     """treekv_qkv_prepare on torch tensors: q [tokens, q_heads, d], k and v [tokens, kv_heads, d] (any may be None), bf16 or
@@ -190,48 +201,58 @@ def qkv_prepare(q, k=None, v=None, *, q_weight=None, k_weight=None, eps: float =
     three contiguous results, allocated if None.  Returns them."""
     import torch
 
-    lib = load()
-    given = [x for x in (q, k, v) if x is not None]
-    if not given:
+    x = q if q is not None else k if k is not None else v
+    if x is None:
         raise ValueError("one of q, k and v at least")
-    tokens, _, d = given[0].shape
-    device, dtype = given[0].device, given[0].dtype
-    a = treekv_qkv_args(tokens=tokens, head_dim=d, flags=(TREEKV_ROPE_HALVES if halves else 0) | (TREEKV_ROPE_TO_PLANES if to_planes else 0),
-                        eps=eps, dtype={torch.bfloat16: TREEKV_BF16, torch.float32: TREEKV_F32}[dtype])
-    out = list(out) if out is not None else [None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v)]
-    for name, x, y in zip("qkv", (q, k, v), out):
-        if x is None:
-            continue
-        if x.dtype != dtype or x.device != device or x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != d:
-            raise ValueError(f"{name}: {dtype} [{tokens}, heads, {d}] on {device} is wanted, not {x.dtype} {tuple(x.shape)} on {x.device}")
-        if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
-            raise ValueError(f"{name}: the heads of a token must be contiguous, not strides {x.stride()}")
-        _want(y, f"out of {name}", dtype, x.shape, device)
-        setattr(a, name, x.data_ptr())
-        setattr(a, name + "_out", y.data_ptr())
-        setattr(a, name + "_stride", x.stride(0))
-    if k is not None and v is not None and k.shape != v.shape:
-        raise ValueError("k and v have the same heads")
-    a.q_heads = q.shape[1] if q is not None else 0
-    a.kv_heads = (k if k is not None else v).shape[1] if k is not None or v is not None else 0
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _want(w, name, dtype, (d,), device)
-            setattr(a, name, w.data_ptr())
-    if positions is not None or inv_freq is not None:
-        if positions is None or inv_freq is None:
-            raise ValueError("positions and inv_freq come together")
-        _want(positions, "positions", torch.int32, (tokens,), device)
-        _want(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),), device)
-        a.positions, a.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
-        a.rotary_dim = 2 * inv_freq.numel()
+    dtype, index = x.dtype, x.get_device()
+    tokens, _, d = x.shape
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError(f"bf16 or float32 is wanted, not {dtype}")
+    oq, ok, ov = out if out is not None else [None if y is None else torch.empty(y.shape, dtype=dtype, device=y.device) for y in (q, k, v)]
+    q_at = k_at = v_at = oq_at = ok_at = ov_at = qw_at = kw_at = pos_at = freq_at = 0
+    q_far = k_far = v_far = q_heads = kv_heads = rotary = 0
+    if q is not None:
+        q_heads, q_far = _rows_in(q, "q", dtype, tokens, d, index)
+        _want(oq, "out of q", dtype, q.shape, index)
+        q_at, oq_at = q.data_ptr(), oq.data_ptr()
+    if k is not None:
+        kv_heads, k_far = _rows_in(k, "k", dtype, tokens, d, index)
+        _want(ok, "out of k", dtype, k.shape, index)
+        k_at, ok_at = k.data_ptr(), ok.data_ptr()
+    if v is not None:
+        v_heads, v_far = _rows_in(v, "v", dtype, tokens, d, index)
+        if k is not None and v_heads != kv_heads:
+            raise ValueError("k and v have the same heads")
+        kv_heads = v_heads
+        _want(ov, "out of v", dtype, v.shape, index)
+        v_at, ov_at = v.data_ptr(), ov.data_ptr()
+    if q_weight is not None:
+        _want(q_weight, "q_weight", dtype, (d,), index)
+        qw_at = q_weight.data_ptr()
+    if k_weight is not None:
+        _want(k_weight, "k_weight", dtype, (d,), index)
+        kw_at = k_weight.data_ptr()
+    if positions is not None and inv_freq is not None:
+        planes = inv_freq.shape[0]
+        _want(positions, "positions", torch.int32, (tokens,), index)
+        _want(inv_freq, "inv_freq", torch.float64, (planes,), index)
+        pos_at, freq_at, rotary = positions.data_ptr(), inv_freq.data_ptr(), 2 * planes
+    elif positions is not None or inv_freq is not None:
+        raise ValueError("positions and inv_freq come together")
     elif to_planes:
-        a.rotary_dim = d
-    with _on(device):
-        rc = lib.treekv_qkv_prepare(C.byref(a), _raw_stream(device))
+        rotary = d
+    args = _QKV.pack(q_at, k_at, v_at, oq_at, ok_at, ov_at, qw_at, kw_at, pos_at, freq_at, q_far, k_far, v_far, tokens, q_heads,
+                     kv_heads, d, TREEKV_F32 if dtype is torch.float32 else TREEKV_BF16, rotary,
+                     (TREEKV_ROPE_HALVES if halves else 0) | (TREEKV_ROPE_TO_PLANES if to_planes else 0), eps)
+    lib = _lib or load()
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            rc = lib.treekv_qkv_prepare(args, _raw_stream(x.device))
+    else:
+        rc = lib.treekv_qkv_prepare(args, _raw_stream(x.device))
     if rc != TREEKV_OK:
         raise TreeKVError(rc, "treekv_qkv_prepare")
-    return tuple(out)
+    return oq, ok, ov
 
 
 class TreeKV:
@@ -263,6 +284,8 @@ class TreeKV:
             raise TreeKVError(rc, "treekv_init")
         self.cfg = treekv_config()
         self._lib.treekv_get_config(self._h, C.byref(self.cfg))
+        c = self.cfg
+        self._dims = (c.batch, c.q_heads, c.kv_heads, c.head_dim, c.budget)
         self.storage_dtype = torch.bfloat16 if self.cfg.dtype == TREEKV_BF16 else torch.float32
         nbytes = self._lib.treekv_workspace_bytes(self._h)
         if workspace is None:
@@ -367,6 +390,18 @@ class TreeKV:
         return K_out, V_out
 
     # -- speculative decoding ------------------------------------------------------------
+    def _call(self, what: str, *args):
+        """The ABI call `what` on this context and the current stream, with its GPU current."""
+        dev = self.workspace.device
+        call = getattr(self._lib, what)
+        if _elsewhere(self.workspace.get_device()):
+            with self._torch.cuda.device(dev):
+                rc = call(self._h, *args, _raw_stream(dev))
+        else:
+            rc = call(self._h, *args, _raw_stream(dev))
+        if rc != TREEKV_OK:
+            self._check(rc, what)
+
     def tree_scratch_bytes(self, nodes: int) -> int:
         return self._lib.treekv_tree_scratch_bytes(self._h, int(nodes))
 
@@ -379,57 +414,60 @@ class TreeKV:
         return out, lse, t.empty(need, dtype=t.uint8, device=self.device) if need else None
 
     def _want_tree(self, q, k, v, parents):
-        c, t, dev = self.cfg, self.storage_dtype, self.workspace.device
+        batch, q_heads, kv_heads, d, _ = self._dims
+        t, index = self.storage_dtype, self.workspace.get_device()
         n = parents.shape[-1]
-        _want(parents, "parents", self._torch.int32, (c.batch, n), dev)
-        _want(q, "q", t, (c.batch, n, c.q_heads, c.head_dim), dev)
-        _want(k, "k", t, (c.batch, n, c.kv_heads, c.head_dim), dev)
-        _want(v, "v", t, (c.batch, n, c.kv_heads, c.head_dim), dev)
-        return n, dev
+        _want(parents, "parents", self._torch.int32, (batch, n), index)
+        _want(q, "q", t, (batch, n, q_heads, d), index)
+        _want(k, "k", t, (batch, n, kv_heads, d), index)
+        _want(v, "v", t, (batch, n, kv_heads, d), index)
+        return n, index
 
     def tree_attend(self, q, k, v, parents, out, lse=None, scratch=None):
         """Attention of drafted trees; `scratch` (uint8, tree_scratch_bytes) is allocated for the call if None."""
-        n, dev = self._want_tree(q, k, v, parents)
-        f32, c = self._torch.float32, self.cfg
-        _want(out, "out", f32, (c.batch, n, c.q_heads, c.head_dim), dev)
+        n, index = self._want_tree(q, k, v, parents)
+        f32, (batch, q_heads, _, d, _) = self._torch.float32, self._dims
+        _want(out, "out", f32, (batch, n, q_heads, d), index)
+        lse_at = scratch_at = size = 0
         if lse is not None:
-            _want(lse, "lse", f32, (c.batch, n, c.q_heads), dev)
+            _want(lse, "lse", f32, (batch, n, q_heads), index)
+            lse_at = lse.data_ptr()
         if scratch is None:
             need = self.tree_scratch_bytes(n)
-            scratch = self._torch.empty(need, dtype=self._torch.uint8, device=dev) if need else None
-        elif scratch.device != dev or not scratch.is_contiguous():
-            raise ValueError(f"scratch: contiguous memory on {dev} is wanted")
-        with _on(dev):
-            self._check(self._lib.treekv_tree_attend(self._h, _ptr(q), _ptr(k), _ptr(v), _ptr(parents), n, _ptr(out), _ptr(lse),
-                                                     _ptr(scratch), 0 if scratch is None else scratch.nbytes, _raw_stream(dev)),
-                        "treekv_tree_attend")
+            scratch = self._torch.empty(need, dtype=self._torch.uint8, device=self.workspace.device) if need else None
+        if scratch is not None:
+            if scratch.get_device() != index or not scratch.is_contiguous():
+                raise ValueError(f"scratch: contiguous memory on device {index} is wanted")
+            scratch_at, size = scratch.data_ptr(), scratch.nbytes
+        self._call("treekv_tree_attend", q.data_ptr(), k.data_ptr(), v.data_ptr(), parents.data_ptr(), n, out.data_ptr(), lse_at,
+                   scratch_at, size)
 
     def tree_commit(self, q, k, v, parents, lse, path, path_len, retained, n_retained=None, evicted=None, status=None):
         """The accepted paths [batch, max_len] (path_len [batch] of them) of the attended trees enter the cache."""
-        n, dev = self._want_tree(q, k, v, parents)
-        c, i32 = self.cfg, self._torch.int32
+        n, index = self._want_tree(q, k, v, parents)
+        i32, (batch, q_heads, kv_heads, _, budget) = self._torch.int32, self._dims
         longest = path.shape[-1]
-        _want(lse, "lse", self._torch.float32, (c.batch, n, c.q_heads), dev)
-        _want(path, "path", i32, (c.batch, longest), dev)
-        _want(path_len, "path_len", i32, (c.batch,), dev)
-        _want(retained, "retained", i32, (c.batch, c.kv_heads, c.budget), dev)
-        for t, what, shape in ((n_retained, "n_retained", (c.batch, c.kv_heads)),
-                               (evicted, "evicted", (c.batch, c.kv_heads, longest)), (status, "status", (c.batch,))):
-            if t is not None:
-                _want(t, what, i32, shape, dev)
-        with _on(dev):
-            self._check(self._lib.treekv_tree_commit(self._h, _ptr(q), _ptr(k), _ptr(v), _ptr(parents), _ptr(lse), n, _ptr(path),
-                                                     _ptr(path_len), longest, _ptr(retained), _ptr(n_retained), _ptr(evicted),
-                                                     _ptr(status), _raw_stream(dev)), "treekv_tree_commit")
+        _want(lse, "lse", self._torch.float32, (batch, n, q_heads), index)
+        _want(path, "path", i32, (batch, longest), index)
+        _want(path_len, "path_len", i32, (batch,), index)
+        _want(retained, "retained", i32, (batch, kv_heads, budget), index)
+        if n_retained is not None:
+            _want(n_retained, "n_retained", i32, (batch, kv_heads), index)
+        if evicted is not None:
+            _want(evicted, "evicted", i32, (batch, kv_heads, longest), index)
+        if status is not None:
+            _want(status, "status", i32, (batch,), index)
+        self._call("treekv_tree_commit", q.data_ptr(), k.data_ptr(), v.data_ptr(), parents.data_ptr(), lse.data_ptr(), n,
+                   path.data_ptr(), path_len.data_ptr(), longest, retained.data_ptr(), _ptr(n_retained), _ptr(evicted), _ptr(status))
 
     def fork(self, source: "TreeKV", src, dst):
-        """Sequence dst[i] becomes a copy of `source`'s sequence src[i] (-1: is emptied); lists of host integers."""
-        src, dst = [int(x) for x in src], [int(x) for x in dst]
+        """Sequence dst[i] becomes a copy of `source`'s sequence src[i] (-1: is emptied); host integers."""
         if len(src) != len(dst):
             raise ValueError("src and dst have the same length")
-        if source.workspace.device != self.workspace.device:
+        if source.workspace.get_device() != self.workspace.get_device():
             raise ValueError("both contexts on one device")
-        ints = C.c_int32 * len(src)
-        with _on(self.workspace.device):
-            self._check(self._lib.treekv_fork(self._h, source._h, ints(*src), ints(*dst), len(src), _raw_stream(self.workspace.device)),
-                        "treekv_fork")
+        try:
+            pairs = [array.array("i", map(int, x)).tobytes() for x in (src, dst)]
+        except OverflowError:
+            raise ValueError("src and dst are 32-bit integers") from None
+        self._call("treekv_fork", source._h, *pairs, len(src))

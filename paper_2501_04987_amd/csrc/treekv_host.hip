@@ -110,6 +110,36 @@ __global__ void scores_kernel(Params p, float* __restrict__ scores) {
   }
 }
 
+// Where a snapshot's header, positions, slots and scores go.
+struct Books {
+  int *hdr, *pos, *slots;
+  float* S;
+};
+// Entry i of a unit's, in position order.
+__device__ inline void write_books(const Params& p, const Books& out, int unit, int i) {
+  const int* meta = p.meta + (size_t)unit * META_STRIDE;
+  const int n = meta[META_N], j = meta[META_J], rhead = meta[META_RHEAD], t = meta[META_T];
+  const int* Eu = p.E + (size_t)unit * 2 * p.m;
+  const int* PEu = p.PE + (size_t)unit * 2 * p.m;
+  const int* Ru = p.R + (size_t)unit * max(p.n_recent, 1);
+  if (i == 0) reinterpret_cast<int4*>(out.hdr)[unit] = make_int4(n, t, j + 1, 0);
+  if (i >= p.budget) return;
+  int po = -1, sl = -1;
+  float sc = 0.f;
+  if (i < n) {
+    po = sl = i;                        // while the cache fills, token i sits in slot i
+    if (n == p.budget) {
+      sl = logical_to_slot(p, Eu, Ru, rhead, j, i);
+      const int k = i - p.n_sink;
+      if (k >= p.m) po = t - p.n_recent + (k - p.m);
+      else if (k >= 0) po = PEu[tree_index(k, j)];
+    }
+    sc = p.S[(size_t)unit * p.cap + sl];
+  }
+  const size_t o = (size_t)unit * p.budget + i;
+  out.pos[o] = po; out.slots[o] = sl; out.S[o] = sc;
+}
+
 // Retained rows in position order, zeros behind them.  A lane copies one 16-byte piece of GATHER_ROWS rows of K and of V, all
 // requested before the first is stored: 256 units x 2048 rows of 256 bytes 91 us (139 with a workgroup of 64 a row).
 // STREAM: more than 64 MB are stored past the caches, where nothing of them would be left for a reader: 85 us, 6.3 TB/s in and out,
@@ -122,8 +152,12 @@ __device__ inline void store16(uint4* dst, const uint4& v) {
   if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4u, v), reinterpret_cast<v4u*>(dst));
   else *dst = v;
 }
-template <bool STREAM>
-__global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uint4* __restrict__ Kout, uint4* __restrict__ Vout, int row_vec) {
+// BOOKS: a snapshot; the workgroups behind those of the rows write the rest of it.
+template <bool STREAM, bool BOOKS>
+__global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uint4* __restrict__ Kout, uint4* __restrict__ Vout, int row_vec,
+                                                                   int row_groups, Books books) {
+  if (BOOKS && (int)blockIdx.x >= row_groups)
+    return write_books(p, books, blockIdx.y, ((int)blockIdx.x - row_groups) * GATHER_THREADS + threadIdx.x);
   const int unit = blockIdx.y, per = GATHER_THREADS / row_vec;       // row_vec is a power of two, 32 at most
   const int* meta = p.meta + (size_t)unit * META_STRIDE;
   const int n = meta[META_N], j = meta[META_J], rhead = meta[META_RHEAD];
@@ -152,10 +186,12 @@ __global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uin
     }
   }
 }
-int gather(const Params& p, void* K_out, void* V_out, hipStream_t s) {
+template <bool BOOKS>
+int gather(const Params& p, void* K_out, void* V_out, const Books& books, hipStream_t s) {
   const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16, rows = GATHER_THREADS / row_vec * GATHER_ROWS;
-  auto kernel = (size_t)2 * p.U * p.budget * row_vec * 16 > STREAM_BYTES ? gather_kv_kernel<true> : gather_kv_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3((p.budget + rows - 1) / rows, p.U), dim3(GATHER_THREADS), 0, s, p, (uint4*)K_out, (uint4*)V_out, row_vec);
+  const int groups = (p.budget + rows - 1) / rows, more = BOOKS ? (p.budget + GATHER_THREADS - 1) / GATHER_THREADS : 0;
+  auto kernel = (size_t)2 * p.U * p.budget * row_vec * 16 > STREAM_BYTES ? gather_kv_kernel<true, BOOKS> : gather_kv_kernel<false, BOOKS>;
+  hipLaunchKernelGGL(kernel, dim3(groups + more, p.U), dim3(GATHER_THREADS), 0, s, p, (uint4*)K_out, (uint4*)V_out, row_vec, groups, books);
   return finish_launch();
 }
 
@@ -174,38 +210,6 @@ treekv_state_layout state_layout(const Params& p) {
   l.V = take(U * c * p.D * esz);
   l.bytes = off;
   return l;
-}
-
-// Header, positions, slots and S of every unit, in position order (the K and V rows go through gather_kv_kernel).
-__global__ void export_state_kernel(Params p, int* __restrict__ hdr, int* __restrict__ pos, int* __restrict__ slots,
-                                    float* __restrict__ S) {
-  const int unit = blockIdx.x;
-  const int* meta = p.meta + (size_t)unit * META_STRIDE;
-  const int n = meta[META_N], j = meta[META_J], rhead = meta[META_RHEAD], t = meta[META_T];
-  const int* Eu = p.E + (size_t)unit * 2 * p.m;
-  const int* PEu = p.PE + (size_t)unit * 2 * p.m;
-  const int* Ru = p.R + (size_t)unit * max(p.n_recent, 1);
-  if (blockIdx.y == 0 && threadIdx.x < 4) {
-    const int h[4] = {n, t, j + 1, 0};
-    hdr[(size_t)unit * 4 + threadIdx.x] = h[threadIdx.x];
-  }
-  const int i = blockIdx.y * blockDim.x + threadIdx.x;
-  if (i < p.budget) {
-    int po = -1, sl = -1;
-    float sc = 0.f;
-    if (i < n) {
-      po = sl = i;                        // while the cache fills, token i sits in slot i
-      if (n == p.budget) {
-        sl = logical_to_slot(p, Eu, Ru, rhead, j, i);
-        const int k = i - p.n_sink;
-        if (k >= p.m) po = t - p.n_recent + (k - p.m);
-        else if (k >= 0) po = PEu[tree_index(k, j)];
-      }
-      sc = p.S[(size_t)unit * p.cap + sl];
-    }
-    const size_t o = (size_t)unit * p.budget + i;
-    pos[o] = po; slots[o] = sl; S[o] = sc;
-  }
 }
 
 // Checks one unit's snapshot and, if it describes a state Algorithm 1 can be in, rebuilds the unit's bookkeeping
@@ -333,9 +337,8 @@ int record_hip(treekv_ctx* ctx, int rc) {
 
 int launch_export_state(const Params& p, char* dst, hipStream_t s) {
   const treekv_state_layout l = state_layout(p);
-  hipLaunchKernelGGL(export_state_kernel, dim3(p.U, (p.budget + 255) / 256), dim3(256), 0, s, p, (int*)(dst + l.header), (int*)(dst + l.positions),
-                     (int*)(dst + l.slots), (float*)(dst + l.S));
-  return gather(p, dst + l.K, dst + l.V, s);
+  const Books books = {(int*)(dst + l.header), (int*)(dst + l.positions), (int*)(dst + l.slots), (float*)(dst + l.S)};
+  return gather<true>(p, dst + l.K, dst + l.V, books, s);
 }
 
 int launch_import_state(const Params& p, const char* src, int32_t* status, hipStream_t s) {
@@ -360,7 +363,7 @@ int launch_scores(const Params& p, float* scores, hipStream_t s) {
   return check_launch();
 }
 
-int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s) { return gather(p, K_out, V_out, s); }
+int launch_gather_kv(const Params& p, void* K_out, void* V_out, hipStream_t s) { return gather<false>(p, K_out, V_out, Books(), s); }
 
 }  // namespace tkv
 
