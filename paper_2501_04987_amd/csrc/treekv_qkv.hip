@@ -32,30 +32,94 @@ __device__ inline uint4 narrow(const float (&y)[4], float) {
   return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
 }
 
+// What happens to one 16-byte piece of a head (`part` of it; the lanes of a head lie side by side).  Returns the piece of the
+// output this lane writes.
 template <typename T, int D>
+__device__ inline int work_piece(const treekv_qkv_args& a, const float2* cs, bool turn, bool norm, const uint4& wraw, int part, uint4& raw) {
+  constexpr int EPL = Storage<T>::EPL, LPR = D / EPL;
+  const int half = a.rotary_dim / 2;
+  float x[EPL];
+  Storage<T>::widen(raw, x);
+  if (norm) {
+    float sum = 0.f, w[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], x[e], sum);
+    const float inv = rsqrtf(group_sum<LPR>(sum) * (1.0f / D) + a.eps);
+    Storage<T>::widen(wraw, w);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * w[e];
+  }
+  int to_part = part;
+  if (turn && (a.flags & TREEKV_ROPE_HALVES) && half > 0) {
+    // lanes of the first half hold the first dimensions of planes part * EPL .., those of the second half the second ones
+    const int lanes = half / EPL;
+    const bool turned = part < 2 * lanes, second = part >= lanes;
+    const int other = turned ? (second ? -lanes : lanes) : 0, plane = (second ? part - lanes : part) * EPL;
+    float ya[EPL], yb[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      const float o = __shfl(x[e], (threadIdx.x & 63) + other, 64);
+      const float2 t = a.positions && turned ? cs[plane + e] : make_float2(1.f, 0.f);
+      const float p0 = second ? o : x[e], p1 = second ? x[e] : o;
+      ya[e] = p0 * t.x - p1 * t.y;
+      yb[e] = p0 * t.y + p1 * t.x;
+    }
+    if (turned) {
+      if (a.flags & TREEKV_ROPE_TO_PLANES) {
+        // planes plane .. plane + EPL - 1 are 2 EPL output dimensions; this lane writes the first or the second EPL of them
+        to_part = 2 * (plane / EPL) + (second ? 1 : 0);
+#pragma unroll
+        for (int e = 0; e < EPL / 2; ++e) {
+          x[2 * e] = second ? ya[EPL / 2 + e] : ya[e];
+          x[2 * e + 1] = second ? yb[EPL / 2 + e] : yb[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) x[e] = second ? yb[e] : ya[e];
+      }
+    }
+  } else if (turn && a.positions && part * EPL < a.rotary_dim) {
+#pragma unroll
+    for (int e = 0; e < EPL; e += 2) {
+      const float2 t = cs[(part * EPL + e) / 2];
+      const float p0 = x[e], p1 = x[e + 1];
+      x[e] = p0 * t.x - p1 * t.y;
+      x[e + 1] = p0 * t.y + p1 * t.x;
+    }
+  }
+  raw = narrow(x, T());
+  return to_part;
+}
+
+// A workgroup takes ITER heads per lane group of one token (a run of its q, k and v heads), all requested before the angles are
+// formed.  ITER = 4 forms the angles once per token of 64 heads and keeps four loads in flight: 976 tokens of 48 heads x 128 8.6
+// -> 5.6 us; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 3.0 us, 3.5 with four).
+template <typename T, int D, int ITER>
 __global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int chunks) {
-  constexpr int EPL = Storage<T>::EPL, LPR = D / EPL, ROWS = QKV_THREADS / LPR;
+  constexpr int LPR = D / Storage<T>::EPL, ROWS = QKV_THREADS / LPR;
   __shared__ float2 cs[D / 2];
-  const int tid = threadIdx.x, part = tid % LPR, half = a.rotary_dim / 2;
+  const int tid = threadIdx.x, part = tid % LPR;
   const int nq = a.q ? a.q_heads : 0, nk = a.k ? a.kv_heads : 0, nv = a.v ? a.kv_heads : 0;
   const long long items = (long long)a.tokens * chunks;
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int token = (int)(item / chunks), row = (int)(item % chunks) * ROWS + tid / LPR;
-    const bool live = row < nq + nk + nv;
-    // the row's source, destination and what happens to it
-    const int kind = row < nq ? 0 : row < nq + nk ? 1 : 2;
-    const int head = row - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk);
-    const T* src = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
-                   (long long)token * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) + (long long)head * D;
-    T* dst = (T*)(kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out) +
-             ((long long)token * (kind == 0 ? a.q_heads : a.kv_heads) + head) * D;
-    const T* weight = (const T*)(kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr);
-    uint4 raw = make_uint4(0, 0, 0, 0), wraw = raw;
-    if (live) {
-      raw = reinterpret_cast<const uint4*>(src)[part];
-      if (weight) wraw = reinterpret_cast<const uint4*>(weight)[part];
+    const int token = (int)(item / chunks), first = (int)(item % chunks) * (ROWS * ITER) + tid / LPR;
+    // a head's source, destination and what happens to it
+    auto kind_of = [&](int row) { return row < nq ? 0 : row < nq + nk ? 1 : 2; };
+    auto head_of = [&](int row) { return row < nq ? row : row < nq + nk ? row - nq : row - nq - nk; };
+    uint4 raw[ITER], w[ITER];
+#pragma unroll
+    for (int x = 0; x < ITER; ++x) {
+      const int row = first + x * ROWS, kind = kind_of(row), head = head_of(row);
+      raw[x] = w[x] = make_uint4(0, 0, 0, 0);
+      if (row < nq + nk + nv) {
+        const T* src = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
+                       (long long)token * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) + (long long)head * D;
+        const void* weight = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
+        raw[x] = reinterpret_cast<const uint4*>(src)[part];
+        if (weight) w[x] = reinterpret_cast<const uint4*>(weight)[part];
+      }
     }
-    if (a.positions && tid < half) {
+    if (a.positions && tid < a.rotary_dim / 2) {
       // turns: the fraction is exact, whatever the number of whole ones
       const double turns = (double)a.positions[token] * a.inv_freq[tid] * 0.15915494309189533577;
       float s, c;
@@ -63,56 +127,17 @@ __global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int
       cs[tid] = make_float2(c, s);
     }
     __syncthreads();
-    float x[EPL];
-    Storage<T>::widen(raw, x);
-    if (weight) {
-      float sum = 0.f, w[EPL];
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], x[e], sum);
-      const float inv = rsqrtf(group_sum<LPR>(sum) * (1.0f / D) + a.eps);
-      Storage<T>::widen(wraw, w);
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * w[e];
-    }
-    int to_part = part;                              // the 16-byte piece of the output this lane writes
-    if (kind < 2 && (a.flags & TREEKV_ROPE_HALVES) && half > 0) {
-      // lanes of the first half hold the first dimensions of planes part * EPL .., those of the second half the second ones
-      const int lanes = half / EPL;
-      const bool turned = part < 2 * lanes, second = part >= lanes;
-      const int other = turned ? (second ? -lanes : lanes) : 0, plane = (second ? part - lanes : part) * EPL;
-      float ya[EPL], yb[EPL];
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        const float o = __shfl(x[e], (tid & 63) + other, 64);
-        const float2 t = a.positions && turned ? cs[plane + e] : make_float2(1.f, 0.f);
-        const float p0 = second ? o : x[e], p1 = second ? x[e] : o;
-        ya[e] = p0 * t.x - p1 * t.y;
-        yb[e] = p0 * t.y + p1 * t.x;
-      }
-      if (turned) {
-        if (a.flags & TREEKV_ROPE_TO_PLANES) {
-          // planes plane .. plane + EPL - 1 are 2 EPL output dimensions; this lane writes the first or the second EPL of them
-          to_part = 2 * (plane / EPL) + (second ? 1 : 0);
-#pragma unroll
-          for (int e = 0; e < EPL / 2; ++e) {
-            x[2 * e] = second ? ya[EPL / 2 + e] : ya[e];
-            x[2 * e + 1] = second ? yb[EPL / 2 + e] : yb[e];
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < EPL; ++e) x[e] = second ? yb[e] : ya[e];
-        }
-      }
-    } else if (kind < 2 && a.positions && part * EPL < a.rotary_dim) {
-#pragma unroll
-      for (int e = 0; e < EPL; e += 2) {
-        const float2 t = cs[(part * EPL + e) / 2];
-        const float p0 = x[e], p1 = x[e + 1];
-        x[e] = p0 * t.x - p1 * t.y;
-        x[e + 1] = p0 * t.y + p1 * t.x;
+    for (int x = 0; x < ITER; ++x) {
+      const int row = first + x * ROWS, kind = kind_of(row), head = head_of(row);
+      int to_part = part;
+      if (kind < 2) to_part = work_piece<T, D>(a, cs, true, kind == 0 ? a.q_weight != nullptr : a.k_weight != nullptr, w[x], part, raw[x]);
+      if (row < nq + nk + nv) {
+        T* dst = (T*)(kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out) +
+                 ((long long)token * (kind == 0 ? a.q_heads : a.kv_heads) + head) * D;
+        reinterpret_cast<uint4*>(dst)[to_part] = raw[x];
       }
     }
-    if (live) reinterpret_cast<uint4*>(dst)[to_part] = kind == 2 ? raw : narrow(x, T());
     __syncthreads();                                 // the next item's angles
   }
 }
@@ -121,9 +146,11 @@ template <typename T, int D>
 int launch_qkv_d(const treekv_qkv_args& a, hipStream_t s) {
   constexpr int ROWS = QKV_THREADS / (D / Storage<T>::EPL);
   const int rows = (a.q ? a.q_heads : 0) + (a.k ? a.kv_heads : 0) + (a.v ? a.kv_heads : 0);
-  const int chunks = (rows + ROWS - 1) / ROWS;
+  const bool few = (long long)a.tokens * ((rows + ROWS - 1) / ROWS) <= 512;          // two workgroups a compute unit
+  const int per = few ? ROWS : 4 * ROWS, chunks = (rows + per - 1) / per;
   const long long items = (long long)a.tokens * chunks, most = 1 << 20;
-  hipLaunchKernelGGL((qkv_kernel<T, D>), dim3((unsigned)(items < most ? items : most)), dim3(QKV_THREADS), 0, s, a, chunks);
+  auto kernel = few ? qkv_kernel<T, D, 1> : qkv_kernel<T, D, 4>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < most ? items : most)), dim3(QKV_THREADS), 0, s, a, chunks);
   return finish_launch();
 }
 
