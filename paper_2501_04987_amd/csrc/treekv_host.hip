@@ -145,13 +145,6 @@ __device__ inline void write_books(const Params& p, const Books& out, int unit, 
 // STREAM: more than 64 MB are stored past the caches, where nothing of them would be left for a reader: 85 us, 6.3 TB/s in and out,
 // and the kernels around it find more of their own (a commit with its snapshot 144 -> 131 us).
 constexpr int GATHER_THREADS = 256, GATHER_ROWS = 4;
-constexpr size_t STREAM_BYTES = (size_t)64 << 20;
-template <bool STREAM>                                               // (chosen at run time, the compiler makes one ordinary store of the two)
-__device__ inline void store16(uint4* dst, const uint4& v) {
-  typedef unsigned v4u __attribute__((ext_vector_type(4)));
-  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4u, v), reinterpret_cast<v4u*>(dst));
-  else *dst = v;
-}
 // BOOKS: a snapshot; the workgroups behind those of the rows write the rest of it.
 template <bool STREAM, bool BOOKS>
 __global__ __launch_bounds__(GATHER_THREADS) void gather_kv_kernel(Params p, uint4* __restrict__ Kout, uint4* __restrict__ Vout, int row_vec,

@@ -158,6 +158,15 @@ template <> struct Storage<float> {
   }
 };
 
+// Outputs of more than STREAM_BYTES are stored past the caches, where nothing of them would be left for a reader.
+constexpr size_t STREAM_BYTES = (size_t)64 << 20;
+template <bool STREAM>                       // (chosen at run time, the compiler makes one ordinary store of the two)
+__device__ inline void store16(uint4* dst, const uint4& v) {
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(v4u, v), reinterpret_cast<v4u*>(dst));
+  else *dst = v;
+}
+
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int CTRL>

@@ -92,9 +92,9 @@ __device__ inline int work_piece(const treekv_qkv_args& a, const float2* cs, boo
 }
 
 // A workgroup takes ITER heads per lane group of one token (a run of its q, k and v heads), all requested before the angles are
-// formed.  ITER = 4 forms the angles once per token of 64 heads and keeps four loads in flight: 976 tokens of 48 heads x 128 8.6
-// -> 5.6 us; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 3.0 us, 3.5 with four).
-template <typename T, int D, int ITER>
+// formed.  ITER = 4 forms the angles once per token of 64 heads and keeps four loads in flight: 32768 tokens of 48 heads x 128
+// 164 -> 153 us, 976 tokens 8.6; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 2.9 us).
+template <typename T, int D, int ITER, bool STREAM>
 __global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int chunks) {
   constexpr int LPR = D / Storage<T>::EPL, ROWS = QKV_THREADS / LPR;
   __shared__ float2 cs[D / 2];
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int
       if (row < nq + nk + nv) {
         T* dst = (T*)(kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out) +
                  ((long long)token * (kind == 0 ? a.q_heads : a.kv_heads) + head) * D;
-        reinterpret_cast<uint4*>(dst)[to_part] = raw[x];
+        store16<STREAM>(reinterpret_cast<uint4*>(dst) + to_part, raw[x]);
       }
     }
     __syncthreads();                                 // the next item's angles
@@ -149,7 +149,9 @@ int launch_qkv_d(const treekv_qkv_args& a, hipStream_t s) {
   const bool few = (long long)a.tokens * ((rows + ROWS - 1) / ROWS) <= 512;          // two workgroups a compute unit
   const int per = few ? ROWS : 4 * ROWS, chunks = (rows + per - 1) / per;
   const long long items = (long long)a.tokens * chunks, most = 1 << 20;
-  auto kernel = few ? qkv_kernel<T, D, 1> : qkv_kernel<T, D, 4>;
+  // (32768 tokens of 48 heads x 128: 145 us so, 5.6 TB/s in and out; 153 through the caches)
+  const bool stream = (size_t)a.tokens * rows * D * sizeof(T) > STREAM_BYTES;
+  auto kernel = few ? qkv_kernel<T, D, 1, false> : stream ? qkv_kernel<T, D, 4, true> : qkv_kernel<T, D, 4, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(items < most ? items : most)), dim3(QKV_THREADS), 0, s, a, chunks);
   return finish_launch();
 }
