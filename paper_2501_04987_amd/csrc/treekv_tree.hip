@@ -66,6 +66,12 @@ __device__ inline float row_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
+// The same value, in a form that keeps what is computed from it from being held across a loop.
+__device__ inline int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // The tree of one sequence, worked out by the whole workgroup: bit j of sm.anc[i] says that node i attends node j; `up` is
 // -1 for a node of the tree and -2 for an absent one.  Generations double from round to round.
 struct TreeBits {
@@ -535,8 +541,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
       if (blk < cache_blocks)
         slot = slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(blk * O::COLS + (lane & (O::COLS - 1)), u.n - 1));
   };
-  // Lane-dependent addresses are worked out anew at each load (`anew`): kept across the loop they are thirty registers.
-  auto anew = [](int x) { asm volatile("" : "+v"(x)); return x; };
+  // Lane-dependent addresses are worked out anew at each load: kept across the loop they are thirty registers.
   auto load_keys = [&](int blk) __attribute__((always_inline)) {
     const int l = anew(lane), r = l & 15;
     const unsigned piece = (l >> 4) * 16;
@@ -731,6 +736,93 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
   finish_rows<D, TR_WAVES, ROWS>(p, tree, so, sm, unit, tile, slice);
 }
 
+// A barrier for what the workgroup exchanges through LDS: __syncthreads() also waits for every load on its way to a register.
+__device__ inline void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---- pieces of the two kernels below, whose waves hold O^T as 32 x 32 blocks: a lane has 16 dimensions, 8 d + 4 (lane / 32)
+// + 0 .. 3 of each block, of one row ----
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4_t;
+
+// O^T += V^T P^T of 32 columns: `p` holds the row's probabilities of columns 8 (i / 4) + 4 (lane / 32) + i % 4, `vp` the lane's
+// place in the staged rows (16 lanes fetch 4 rows x 16 dimensions and each gets one dimension's column of them).
+template <int D>
+__device__ inline void add_wide_values(f32x16_t (&o)[D / 32], const f32x16_t& p, const uint16_t* vp, int v_piece, int v_swz) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {                   // 16 columns: elements 8 ks .. + 7
+    uint4 h, m, l;
+    cut3(p[ks * 8], p[ks * 8 + 1], h.x, m.x, l.x);
+    cut3(p[ks * 8 + 2], p[ks * 8 + 3], h.y, m.y, l.y);
+    cut3(p[ks * 8 + 4], p[ks * 8 + 5], h.z, m.z, l.z);
+    cut3(p[ks * 8 + 6], p[ks * 8 + 7], h.w, m.w, l.w);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      uint2 a[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)                    // (multiples of 8 rows: a row's swizzle is that of its last three bits)
+        a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                   (lds_short4_t*)(vp + (ks * 16 + x * 8) * D + ((d * 4 + v_piece) ^ v_swz) * 8)));
+      const uint4 v = make_uint4(a[0].x, a[0].y, a[1].x, a[1].y);
+      o[d] = mfma_wide(v, l, o[d]);
+      o[d] = mfma_wide(v, m, o[d]);
+      o[d] = mfma_wide(v, h, o[d]);
+    }
+  }
+}
+// Rows of a staged tile of V that must not reach the product whatever they hold, cleared by the whole workgroup: of cached
+// columns the free slot's and those behind the last token, of nodes the infinities and NaNs (true: there were some).
+template <int D>
+__device__ inline void clear_cached(uint16_t* vp, int c0, int columns, int hole) {
+  for (int x = threadIdx.x; x < 64 * (D / 8); x += blockDim.x) {
+    const int c = c0 + x / (D / 8);
+    if (c >= columns || c == hole) reinterpret_cast<uint4*>(vp)[x] = make_uint4(0, 0, 0, 0);
+  }
+}
+template <int D>
+__device__ inline bool clear_odd(uint16_t* vp) {
+  bool odd = false;
+  for (int x = threadIdx.x; x < 64 * (D / 8); x += blockDim.x) {
+    const uint4 was = reinterpret_cast<uint4*>(vp)[x];
+    const uint4 w = make_uint4(keep_finite(was.x), keep_finite(was.y), keep_finite(was.z), keep_finite(was.w));
+    if (w.x != was.x || w.y != was.y || w.z != was.z || w.w != was.w) {
+      odd = true;
+      reinterpret_cast<uint4*>(vp)[x] = w;
+    }
+  }
+  return __syncthreads_or(odd);
+}
+// The nodes' infinities and NaNs, from memory, to a row that attends them (`row_v`: this lane's first dimension of the first).
+template <int DB>
+__device__ inline void add_odd_values(f32x16_t (&o)[DB], const char* row_v, size_t node_bytes, int nodes, unsigned bits) {
+#pragma unroll 1
+  for (int c = 0; c < nodes; ++c, row_v += node_bytes) {
+#pragma unroll
+    for (int d = 0; d < DB * 4; ++d) {
+      const uint2 w = *reinterpret_cast<const uint2*>(row_v + d * 16);
+      const unsigned x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float y = __uint_as_float(x[i] & ~(unsigned)((int)finite_word(x[i]) >> 31));       // 0 if it is finite
+        o[d >> 2][(d & 3) * 4 + i] += (bits >> c & 1) ? y : 0.f;
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0f70);                // (no wait of the compiler's for these in the caller's loop)
+}
+template <int D>
+__device__ inline void leave_wide_sums(const f32x16_t (&o)[D / 32], float ref, float sum, float* so, float2* sm, int r, int hi) {
+  sum += __shfl_xor(sum, 32, 64);
+  if (hi == 0) sm[r] = make_float2(ref, sum);
+#pragma unroll
+  for (int d = 0; d < D / 8; ++d)
+    *reinterpret_cast<float4*>(so + (size_t)r * (D + 4) + d * 8 + hi * 4) =
+        make_float4(o[d >> 2][(d & 3) * 4], o[d >> 2][(d & 3) * 4 + 1], o[d >> 2][(d & 3) * 4 + 2], o[d >> 2][(d & 3) * 4 + 3]);
+}
+
 // ---------------------------------------------------------------------------------------------
 // attend, many rows: bf16 storage, tiles of columns shared by the workgroup's waves
 // ---------------------------------------------------------------------------------------------
@@ -743,8 +835,6 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
 // Iteration t forms the logits of tile t + 1 (matrix unit) beside the probabilities of tile t (vector unit) and ends with tile
 // t's product with V.  Four stages: tile t + 1 has landed, t + 2 and t + 3 are on their way, and the stage that t + 3 goes to
 // was last read in iteration t - 1, before the barrier.
-typedef short short4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) short4_t lds_short4_t;
 constexpr int TILE_COLS = 64, STAGES = 4;
 
 // async_copy16 with the source as a wave-uniform base and a lane's byte offset.
@@ -849,30 +939,12 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
   };
   // column, inside the wave's 32, of element i
   auto col_of = [&](int i) { return (i >> 2) * 8 + hi * 4 + (i & 3); };
-  // Rows of V that must not reach the product whatever they hold, cleared in a tile that has landed: the free slot's and those
-  // behind the last token, and the nodes' infinities and NaNs (true: there were some).
-  auto clear_rows = [&](int t) -> bool {
+  auto clear_rows = [&](int t) -> bool {             // in a tile that has landed
     uint16_t* vp = v_stages + ((t - begin) & (STAGES - 1)) * TILE;
-    if (t < cache_tiles) {
-      const int c0 = t * TILE_COLS;
-      if (c0 + TILE_COLS > u.columns || (u.hole >= c0 && u.hole < c0 + TILE_COLS))
-        for (int x = tid; x < TILE_COLS * PARTS; x += THREADS) {
-          const int c = c0 + x / PARTS;
-          if (c >= u.columns || c == u.hole) reinterpret_cast<uint4*>(vp)[x] = make_uint4(0, 0, 0, 0);
-        }
-      return false;
-    }
-    bool odd = false;
-    for (int x = tid; x < TILE_COLS * PARTS; x += THREADS) {
-      uint4 w = reinterpret_cast<uint4*>(vp)[x];
-      const uint4 was = w;
-      w = make_uint4(keep_finite(w.x), keep_finite(w.y), keep_finite(w.z), keep_finite(w.w));
-      if (w.x != was.x || w.y != was.y || w.z != was.z || w.w != was.w) {
-        odd = true;
-        reinterpret_cast<uint4*>(vp)[x] = w;
-      }
-    }
-    return __syncthreads_or(odd);
+    if (t >= cache_tiles) return clear_odd<D>(vp);
+    const int c0 = t * TILE_COLS;
+    if (c0 + TILE_COLS > u.columns || (u.hole >= c0 && u.hole < c0 + TILE_COLS)) clear_cached<D>(vp, c0, u.columns, u.hole);
+    return false;
   };
 
   // The queries have arrived, in a form the compiler sees: it does not know of the copies above, and a wait of its own for
@@ -922,24 +994,8 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
         ref = raised;
       }
     }
-    if (odd && col0 < p.n) {                         // (after the raise, which would make a NaN of an infinity)
-      const unsigned bits = tree.anc[node][col0 >> 5];
-      const char* row_v = Vn + col0 * node_bytes + hi * 8;
-#pragma unroll 1
-      for (int c = 0; c < min(32, p.n - col0); ++c, row_v += node_bytes) {
-#pragma unroll
-        for (int d = 0; d < DB * 4; ++d) {           // dimensions 8 d + 4 hi + 0 .. 3
-          const uint2 w = *reinterpret_cast<const uint2*>(row_v + d * 16);
-          const unsigned x[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float y = __uint_as_float(x[i] & ~(unsigned)((int)finite_word(x[i]) >> 31));       // 0 if it is finite
-            o[d >> 2][(d & 3) * 4 + i] += (bits >> c & 1) ? y : 0.f;
-          }
-        }
-      }
-      __builtin_amdgcn_s_waitcnt(0x0f70);            // (no wait of the compiler's for these in the loop)
-    }
+    if (odd && col0 < p.n)                           // (after the raise, which would make a NaN of an infinity)
+      add_odd_values<DB>(o, Vn + col0 * node_bytes + hi * 8, node_bytes, min(32, p.n - col0), tree.anc[node][col0 >> 5]);
     // logits of tile t + 1 (behind the last one: of whatever the stage holds, unused); probabilities of tile t and their
     // product with V
     f32x16_t next;
@@ -952,28 +1008,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
       add += s[i];
     }
     sum += add;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {                 // 16 columns: elements 8 ks .. + 7
-      uint4 h, m, l;
-      cut3(s[ks * 8], s[ks * 8 + 1], h.x, m.x, l.x);
-      cut3(s[ks * 8 + 2], s[ks * 8 + 3], h.y, m.y, l.y);
-      cut3(s[ks * 8 + 4], s[ks * 8 + 5], h.z, m.z, l.z);
-      cut3(s[ks * 8 + 6], s[ks * 8 + 7], h.w, m.w, l.w);
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        uint2 a[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int r = ks * 16 + x * 8;             // (multiples of 8 rows: a row's swizzle is that of its last three bits)
-          const int place = (d * 4 + v_piece) ^ vswz(v_row);
-          a[x] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t*)(vp + r * D + place * 8)));
-        }
-        const uint4 v = make_uint4(a[0].x, a[0].y, a[1].x, a[1].y);
-        o[d] = mfma_wide(v, l, o[d]);
-        o[d] = mfma_wide(v, m, o[d]);
-        o[d] = mfma_wide(v, h, o[d]);
-      }
-    }
+    add_wide_values<D>(o, s, vp, v_piece, vswz(v_row));
     s = next;
     odd = odd_next;
   }
@@ -981,15 +1016,256 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
 
   float* so = tr_smem;                               // [CG][ROWS][D + 4]
   float2* sm = reinterpret_cast<float2*>(tr_smem + CG * ROWS * OR);
-  {
-    const int r = cg * ROWS + rg * 32 + lr;
-    sum += __shfl_xor(sum, 32, 64);
-    if (hi == 0) sm[r] = make_float2(ref, sum);
+  leave_wide_sums<D>(o, ref, sum, so, sm, cg * ROWS + rg * 32 + lr, hi);
+  __syncthreads();
+  finish_rows<D, CG, ROWS>(p, tree, so, sm, unit, tile, slice);
+}
+
+// ---------------------------------------------------------------------------------------------
+// attend, positions re-assigned: bf16 storage, keys turned once for 64 rows
+// ---------------------------------------------------------------------------------------------
+// Turning a key and cutting it costs more than its products with 32 queries, so here the four waves of a workgroup (two groups
+// of 32 rows x two halves of a tile's 64 columns) share the work: a thread turns a quarter of one row, cuts it and leaves the
+// parts in LDS, with V as it is.  Turned values are cut in two fp16 parts (11 + 11 bits, rounded: what is left is 2^-24 of the
+// value), which takes three products (what is left out, low times low, is 2^-24 of the product) where bf16 parts take six; a
+// row is scaled by a power of two so that its largest element is near 2^13, and the scales go back on with the softmax's.
+// The next tile is on its way while one is worked on, keys and angles to registers, V to the other of its two stages; two
+// workgroups share a compute unit and fill each other's waits at the two barriers of a tile.
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+constexpr int TURN_THREADS = 256, TURN_ROWS = 64;
+
+__device__ inline f32x16_t mfma_half(const uint4& a, const uint4& b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+// Two values as fp16 parts h + l.
+__device__ inline void cut2(float a, float b, unsigned& h, unsigned& l) {
+  const f16x2_t hv = {(_Float16)a, (_Float16)b};
+  const f16x2_t lv = {(_Float16)(a - (float)hv.x), (_Float16)(b - (float)hv.y)};
+  h = __builtin_bit_cast(unsigned, hv);
+  l = __builtin_bit_cast(unsigned, lv);
+}
+// Larger of two packed bf16 magnitudes, half by half (as 15-bit integers).
+__device__ inline unsigned max_magnitudes(unsigned a, unsigned b) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7fff7fffu), __builtin_bit_cast(u16x2, b & 0x7fff7fffu)));
+}
+// The power of two that brings a row's largest magnitude (packed bf16) to [2^13, 2^14), and its inverse.
+__device__ inline float row_scale(unsigned packed, float& inverse) {
+  const unsigned top = max(packed & 0xffffu, packed >> 16), e = top >> 7;        // biased exponent
+  const bool odd = e == 0 || e == 255;                                           // nothing (or next to it), or not finite
+  inverse = odd ? 1.f : __uint_as_float(max(e, 14u) - 13 << 23);                 // 2^(e - 127 - 13)
+  return odd ? 1.f : __uint_as_float(min(267u - max(e, 14u), 254u) << 23);       // 2^(127 + 13 - e)
+}
+// One 16-byte piece scaled, turned and cut.
+__device__ inline void turn_cut(const uint4& raw, float scale, const float4& c01, const float4& c23, uint4& h, uint4& l) {
+  const float co[4] = {c01.x, c01.z, c23.x, c23.z}, si[4] = {c01.y, c01.w, c23.y, c23.w};
+  float x[8], y[8];
+  Storage<uint16_t>::widen(raw, x);
 #pragma unroll
-    for (int d = 0; d < DB * 4; ++d)
-      *reinterpret_cast<float4*>(so + (size_t)r * OR + d * 8 + hi * 4) =
-          make_float4(o[d >> 2][(d & 3) * 4], o[d >> 2][(d & 3) * 4 + 1], o[d >> 2][(d & 3) * 4 + 2], o[d >> 2][(d & 3) * 4 + 3]);
+  for (int e = 0; e < 8; ++e) x[e] *= scale;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    y[2 * e] = x[2 * e] * co[e] - x[2 * e + 1] * si[e];
+    y[2 * e + 1] = x[2 * e] * si[e] + x[2 * e + 1] * co[e];
   }
+  cut2(y[0], y[1], h.x, l.x);
+  cut2(y[2], y[3], h.y, l.y);
+  cut2(y[4], y[5], h.z, l.z);
+  cut2(y[6], y[7], h.w, l.w);
+}
+
+template <int D>
+__global__ __launch_bounds__(TURN_THREADS, 2) void tree_attend_turned_kernel(Args p) {
+  constexpr int RG = 2, CG = 2, ROWS = TURN_ROWS, KS = D / 16, DB = D / 32, OR = D + 4, ROWB = D * 2, PARTS = D / 8;
+  constexpr int PER = PARTS / 4;                                   // 16-byte pieces of a thread: four threads a row
+  constexpr int TILE = TILE_COLS * D;                              // elements of one part of a tile
+  static_assert(TILE_COLS * 4 == TURN_THREADS && RG * CG * 64 == TURN_THREADS, "a row to four threads");
+  extern __shared__ __attribute__((aligned(1024))) float tr_smem[];
+  __shared__ TreeBits tree;
+  __shared__ float col_scale[TILE_COLS];
+  uint16_t* kh = reinterpret_cast<uint16_t*>(tr_smem);
+  uint16_t* kl = kh + TILE;
+  uint16_t* vs = kl + TILE;                          // two stages
+  auto kswz = [](int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); };
+  auto vswz = [](int r) { return D == 128 ? ((r & 7) << 1) : (((r >> 1) & 3) << 1); };
+  const int items = p.row_tiles * p.slices * p.U, per_xcd = (items + 7) / 8;
+  const int item = ((int)blockIdx.x % 8) * per_xcd + (int)blockIdx.x / 8;
+  if (item >= items) return;
+  const int tile = item % p.row_tiles, slice = item / p.row_tiles % p.slices, unit = item / (p.row_tiles * p.slices);
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave / CG, cg = wave % CG;
+  const int kvh = unit % p.Hkv, b = unit / p.Hkv;
+  const Unit u = load_unit<true>(p.meta, p.E, p.R, p.m, p.n_recent, unit);
+  const int rows = p.n << p.g_bits, g_mask = (1 << p.g_bits) - 1, row = min(tile * ROWS + rg * 32 + lr, rows - 1);
+  const int cache_tiles = (u.n + TILE_COLS - 1) / TILE_COLS, tiles = cache_tiles + (p.n + TILE_COLS - 1) / TILE_COLS;
+  const int begin = (int)((long long)tiles * slice / p.slices), end = (int)((long long)tiles * (slice + 1) / p.slices);
+  const char* Ku = (const char*)p.K + (size_t)unit * p.cap * ROWB;
+  const char* Vu = (const char*)p.V + (size_t)unit * p.cap * ROWB;
+  const size_t node_bytes = (size_t)p.Hkv * ROWB;
+  const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+  const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
+
+  // this thread's part of a tile of keys: row t_row, pieces 4 x + l % 4 (four lanes take 64 bytes of a row at once).  Its wave copies the same 16 rows of V: copy x
+  // fills tile rows 16 wave + x * RPC + lane / PARTS, a lane taking the piece whose place its own is.
+  constexpr int RPC = 64 / PARTS, CPW = 16 / RPC;
+  const int t_row = tid >> 2;
+  uint4 raw_k[PER];
+  float4 angles[2 * PER];
+  const unsigned lds_v = __builtin_amdgcn_readfirstlane(lds_address(vs)) + wave * CPW * 1024;
+  int slot = 0;                                      // of its row in the tile to be requested next
+  auto find_slot = [&](int t) {
+    if (t < cache_tiles) slot = slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, min(t * TILE_COLS + t_row, u.n - 1));
+  };
+  // V first: what waits for the keys then waits for it too
+  auto request = [&](int t) {
+    const bool cached = t < cache_tiles;
+    const int c0 = (cached ? t : t - cache_tiles) * TILE_COLS;
+    const unsigned m0 = lds_v + ((t - begin) & 1) * (TILE * 2);
+    const int l = anew(lane), t_row = wave * 16 + (l >> 2), quarter = l & 3;
+#pragma unroll
+    for (int x = 0; x < CPW; ++x) {
+      const int r = x * RPC + l / PARTS, piece = (l % PARTS) ^ vswz(r);       // (16 rows a wave: its first row's swizzle is 0)
+      const size_t at = cached ? (size_t)(unsigned)__shfl(slot, r * 4, 64) * ROWB : min(c0 + wave * 16 + r, p.n - 1) * node_bytes;
+      async_copy16((cached ? Vu : Vn) + at + piece * 16, m0 + x * 1024);
+    }
+    const int node = min(c0 + t_row, p.n - 1), pos = cached ? min(c0 + t_row, u.n - 1) : u.n + depth_of(tree, node, p.n);
+    const uint4* kr = reinterpret_cast<const uint4*>(cached ? Ku + (size_t)(unsigned)slot * ROWB : Kn + node * node_bytes) + quarter;
+    const float4* cs = reinterpret_cast<const float4*>(p.tab + (size_t)pos * (D / 2)) + quarter * 2;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) raw_k[x] = kr[x * 4];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      angles[2 * x] = cs[x * 8];
+      angles[2 * x + 1] = cs[x * 8 + 1];
+    }
+  };
+  // its part of the keys into LDS
+  auto put = [&]() {
+    const int l = anew(lane), t_row = wave * 16 + (l >> 2), quarter = l & 3;
+    unsigned top = 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+      top = max_magnitudes(max_magnitudes(max_magnitudes(raw_k[x].x, raw_k[x].y), max_magnitudes(raw_k[x].z, raw_k[x].w)), top);
+    top = max_magnitudes(top, __shfl_xor(top, 1, 64));
+    top = max_magnitudes(top, __shfl_xor(top, 2, 64));
+    float inverse;
+    const float scale = row_scale(top, inverse);
+    if (quarter == 0) col_scale[t_row] = inverse;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      uint4 high, low;
+      turn_cut(raw_k[x], scale, angles[2 * x], angles[2 * x + 1], high, low);
+      const int place = t_row * PARTS + ((x * 4 + quarter) ^ kswz(t_row));
+      reinterpret_cast<uint4*>(kh)[place] = high;
+      reinterpret_cast<uint4*>(kl)[place] = low;
+    }
+  };
+  find_slot(begin);
+  build_tree(tree, p.parents + (size_t)b * p.n, p.n);
+  if (begin < end) request(begin);
+  find_slot(begin + 1);
+
+  // this lane's row (clamped: rows behind the last repeat it and are not written), turned and cut
+  const int node = row >> p.g_bits;
+  uint4 qh[KS], ql[KS];
+  float sc;
+  {
+    const uint4* src = reinterpret_cast<const uint4*>((const uint16_t*)p.q + (((size_t)b * p.n + node) * p.H + (kvh << p.g_bits) + (row & g_mask)) * D);
+    const float4* cs = reinterpret_cast<const float4*>(p.tab + (size_t)(u.n + depth_of(tree, node, p.n)) * (D / 2));
+    uint4 raw[KS];
+    unsigned top = 0;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      raw[x] = src[x * 2 + hi];
+      top = max_magnitudes(max_magnitudes(max_magnitudes(raw[x].x, raw[x].y), max_magnitudes(raw[x].z, raw[x].w)), top);
+    }
+    top = max_magnitudes(top, __shfl_xor(top, 32, 64));
+    float inverse;
+    const float scale = row_scale(top, inverse);
+    sc = p.scale_log2e * inverse;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) turn_cut(raw[x], scale, cs[(x * 2 + hi) * 2], cs[(x * 2 + hi) * 2 + 1], qh[x], ql[x]);
+  }
+
+  f32x16_t o[DB];
+  float ref = REF_NONE, sum = 0.f;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
+  auto col_of = [&](int i) { return (i >> 2) * 8 + hi * 4 + (i & 3); };      // column, inside the wave's 32, of element i
+
+  for (int t = begin; t < end; ++t) {
+    lds_barrier();                                   // the tile before is done with
+    put();                                           // (all of its loads have arrived, and the copies of V before them)
+    const bool cached = t < cache_tiles;
+    if (t + 1 < end) request(t + 1);
+    find_slot(t + 2);
+    lds_barrier();
+    uint16_t* vt = vs + ((t - begin) & 1) * TILE;
+    bool odd = false;
+    if (!cached) {
+      odd = clear_odd<D>(vt);
+    } else if ((t + 1) * TILE_COLS > u.n) {
+      clear_cached<D>(vt, t * TILE_COLS, u.n, -1);
+      lds_barrier();
+    }
+    const int col0 = (cached ? t : t - cache_tiles) * TILE_COLS + cg * 32;
+    if (col0 >= (cached ? u.n : p.n)) continue;      // (wave-uniform; every wave meets the barriers)
+    f32x16_t s = {};
+    const int l = anew(lane), k_row = l & 31;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int at = (cg * 32 + k_row) * D + ((x * 2 + (l >> 5)) ^ kswz(k_row)) * 8;
+      const uint4 h = *reinterpret_cast<const uint4*>(kh + at), low = *reinterpret_cast<const uint4*>(kl + at);
+      s = mfma_half(low, qh[x], s);
+      s = mfma_half(h, ql[x], s);
+      s = mfma_half(h, qh[x], s);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {                // scaled logits
+      const float4 f = *reinterpret_cast<const float4*>(col_scale + cg * 32 + col_of(i));
+      s[i] *= sc * f.x; s[i + 1] *= sc * f.y; s[i + 2] *= sc * f.z; s[i + 3] *= sc * f.w;
+    }
+    if (cached) {
+      if (col0 + 32 > u.n) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = col0 + col_of(i) < u.n ? s[i] : -INFINITY;
+      }
+    } else {
+      const unsigned bits = tree.anc[node][col0 >> 5] >> (hi * 4);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (bits >> ((i >> 2) * 8 + (i & 3)) & 1) ? s[i] : -INFINITY;
+    }
+    {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      if (__any(top - ref > 8.0f)) {
+        float raised = fmaxf(ref, top);
+        raised = fmaxf(raised, __shfl_xor(raised, 32, 64));
+        const float by = fast_exp2(ref - raised);
+        sum *= by;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] *= by;
+        ref = raised;
+      }
+    }
+    if (odd) add_odd_values<DB>(o, Vn + col0 * node_bytes + hi * 8, node_bytes, min(32, p.n - col0), tree.anc[node][col0 >> 5]);
+    float add = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = fast_exp2(s[i] - ref);
+      add += s[i];
+    }
+    sum += add;
+    const int l2 = anew(lane), v_row = (l2 >> 5) * 4 + ((l2 & 15) >> 2), v_piece = ((l2 >> 4) & 1) * 2 + ((l2 >> 1) & 1);
+    add_wide_values<D>(o, s, vt + (cg * 32 + v_row) * D + (l2 & 1) * 4, v_piece, vswz(v_row));
+  }
+  __syncthreads();
+
+  float* so = tr_smem;                               // [CG][ROWS][D + 4]
+  float2* sm = reinterpret_cast<float2*>(tr_smem + CG * ROWS * OR);
+  leave_wide_sums<D>(o, ref, sum, so, sm, cg * ROWS + rg * 32 + lr, hi);
   __syncthreads();
   finish_rows<D, CG, ROWS>(p, tree, so, sm, unit, tile, slice);
 }
@@ -1201,11 +1477,13 @@ Shape attend_shape(const Params& p, int n) {
   if ((long long)p.U * tiles16 <= (rows <= 32 ? chip : chip / 3)) s.rows_per_tile = 16;
   else if (rows <= 64 || (long long)p.U * tiles32 <= chip || p.dtype != TREEKV_BF16 || (p.flags & TREEKV_POSITION_RERANK)) s.rows_per_tile = rows <= 16 ? 16 : 32;
   else s.rows_per_tile = 128;
+  if (p.dtype == TREEKV_BF16 && (p.flags & TREEKV_POSITION_RERANK) && rows > 16) s.rows_per_tile = TURN_ROWS;
   s.row_tiles = (rows + s.rows_per_tile - 1) / s.rows_per_tile;
   // a wave has a block of columns at least, the large workgroup a tile
   const int blocks = (p.cap + cols - 1) / cols + (n + cols - 1) / cols, tiles = (p.cap + TILE_COLS - 1) / TILE_COLS + (n + TILE_COLS - 1) / TILE_COLS;
-  const int most = s.rows_per_tile == 128 ? tiles : (blocks + TR_WAVES - 1) / TR_WAVES;
-  const long long fit = chip / ((long long)p.U * s.row_tiles);
+  const bool staged = s.rows_per_tile >= TURN_ROWS;
+  const int most = staged ? tiles : (blocks + TR_WAVES - 1) / TR_WAVES;
+  const long long fit = (s.rows_per_tile == TURN_ROWS ? 2 * chip : chip) / ((long long)p.U * s.row_tiles);
   s.slices = fit < 1 ? 1 : fit < most ? (int)fit : most;
   return s;
 }
@@ -1239,6 +1517,16 @@ int launch_attend_tiled(const Shape& s, const Args& a, hipStream_t st) {
   hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TR_THREADS), lds, st, a);
   return launch_merge<D>(s, a, st);
 }
+template <int D>
+int launch_attend_turned(const Shape& s, const Args& a, hipStream_t st) {
+  const size_t sums = (size_t)2 * TURN_ROWS * ((D + 4) * sizeof(float) + sizeof(float2)), tile = (size_t)4 * TILE_COLS * D * 2;
+  const size_t lds = sums > tile ? sums : tile;
+  auto kernel = tree_attend_turned_kernel<D>;
+  if (hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
+  const int items = s.row_tiles * s.slices * a.U;
+  hipLaunchKernelGGL(kernel, dim3((items + 7) / 8 * 8), dim3(TURN_THREADS), lds, st, a);
+  return launch_merge<D>(s, a, st);
+}
 template <typename T, int D>
 int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, float* scratch, hipStream_t st) {
   const Shape s = attend_shape(p, t.n);
@@ -1247,6 +1535,7 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
                   p.n_recent, p.m, p.U, p.H, p.Hkv, p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3, t.n, s.row_tiles, s.slices, p.scale_log2e};
   if constexpr (sizeof(T) == 2) {
     if (s.rows_per_tile == 128) return launch_attend_tiled<D>(s, a, st);
+    if (s.rows_per_tile == TURN_ROWS) return launch_attend_turned<D>(s, a, st);
   }
   if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(s, a, st) : launch_attend_rb<T, D, 1, false>(s, a, st);
   return rope ? launch_attend_rb<T, D, 2, true>(s, a, st) : launch_attend_rb<T, D, 2, false>(s, a, st);
