@@ -644,6 +644,11 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) logits<D>(s[rb], k, q[rb]);
     }
+    // (scaled once, so that the largest meets a reference of its own bits, however large it is)
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) O::at(s[rb], j) *= sc;
     if (next < end) load_keys(next);
     // what a row does not attend
     if (cached) {
@@ -677,7 +682,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
       fresh_sum[rb] = sum[rb];
 #pragma unroll
       for (int j = 0; j < O::NCOL; ++j) {
-        O::at(e[rb], j) = fast_exp2(fmaf(O::at(s[rb], j), sc, -ref[rb]));
+        O::at(e[rb], j) = fast_exp2(O::at(s[rb], j) - ref[rb]);
         fresh_sum[rb] += O::at(e[rb], j);
       }
       worst = fmaxf(worst, fresh_sum[rb]);
@@ -688,11 +693,11 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_kernel(Args p) {
         float top = O::at(s[rb], 0);
 #pragma unroll
         for (int j = 1; j < O::NCOL; ++j) top = fmaxf(top, O::at(s[rb], j));
-        const float raised = row_max(fmaxf(ref[rb], top * sc)), by = fast_exp2(ref[rb] - raised);
+        const float raised = row_max(fmaxf(ref[rb], top)), by = fast_exp2(ref[rb] - raised);
         fresh_sum[rb] = sum[rb] * by;
 #pragma unroll
         for (int j = 0; j < O::NCOL; ++j) {
-          O::at(e[rb], j) = fast_exp2(fmaf(O::at(s[rb], j), sc, -raised));
+          O::at(e[rb], j) = fast_exp2(O::at(s[rb], j) - raised);
           fresh_sum[rb] += O::at(e[rb], j);
         }
 #pragma unroll
@@ -920,7 +925,12 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
   float ref = REF_NONE, sum = 0.f;
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
+  // Logits are scaled as the reference is taken from them, in one step. Past 2^20 the rounding of the reference alone could
+  // carry an exponential past the largest number (from 2^31 on): such a row's logits are scaled first (factor = 1). Scaling all of
+  // them first costs 3 us of 150 (64 nodes of 32 heads in 8 groups, batch 16, 4096 slots).
   const float sc = p.scale_log2e;
+  float factor = sc;
+  bool any_large = false;                            // in some row of the wave
   // where this lane reads its wave's operands from, inside a stage: K row lr; for V, 16 lanes fetch 4 rows x 16 dimensions
   // and each gets one dimension's column of them
   const int l16 = lane & 15, v_row = hi * 4 + (l16 >> 2);
@@ -966,6 +976,11 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
     // what a row does not attend
     const bool cached = t < cache_tiles;
     const int col0 = (cached ? t : t - cache_tiles) * TILE_COLS + cg * 32;
+    if (__builtin_expect(any_large, 0)) {
+      const float first = factor != sc ? sc : 1.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] *= first;
+    }
     if (cached) {
       if (col0 + 32 > u.columns || (u.hole >= col0 && u.hole < col0 + 32)) {
 #pragma unroll
@@ -984,14 +999,22 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      if (__any(fmaf(top, sc, -ref) > 8.0f)) {
-        float raised = fmaxf(ref, top * sc);
+      if (__any(fmaf(top, factor, -ref) > 8.0f)) {
+        float raised = fmaxf(ref, top * factor);
         raised = fmaxf(raised, __shfl_xor(raised, 32, 64));
         const float by = fast_exp2(ref - raised);
         sum *= by;
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] *= by;
         ref = raised;
+        const bool large = factor == sc && fabsf(ref) > 0x1p20f;
+        if (__any(large)) {
+          const float first = large ? sc : 1.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] *= first;
+          if (large) factor = 1.0f;
+          any_large = true;
+        }
       }
     }
     if (odd && col0 < p.n)                           // (after the raise, which would make a NaN of an infinity)
@@ -1004,7 +1027,7 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
     float add = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = fast_exp2(fmaf(s[i], sc, -ref));
+      s[i] = fast_exp2(fmaf(s[i], factor, -ref));
       add += s[i];
     }
     sum += add;
@@ -1129,7 +1152,9 @@ __global__ __launch_bounds__(TURN_THREADS, 2) void tree_attend_turned_kernel(Arg
       const size_t at = cached ? (size_t)(unsigned)__shfl(slot, r * 4, 64) * ROWB : min(c0 + wave * 16 + r, p.n - 1) * node_bytes;
       async_copy16((cached ? Vu : Vn) + at + piece * 16, m0 + x * 1024);
     }
-    const int node = min(c0 + t_row, p.n - 1), pos = cached ? min(c0 + t_row, u.n - 1) : u.n + depth_of(tree, node, p.n);
+    const int node = min(c0 + t_row, p.n - 1);
+    int pos = min(c0 + t_row, u.n - 1);
+    if (!cached) pos = u.n + depth_of(tree, node, p.n);
     const uint4* kr = reinterpret_cast<const uint4*>(cached ? Ku + (size_t)(unsigned)slot * ROWB : Kn + node * node_bytes) + quarter;
     const float4* cs = reinterpret_cast<const float4*>(p.tab + (size_t)pos * (D / 2)) + quarter * 2;
 #pragma unroll
@@ -1161,31 +1186,35 @@ __global__ __launch_bounds__(TURN_THREADS, 2) void tree_attend_turned_kernel(Arg
       reinterpret_cast<uint4*>(kl)[place] = low;
     }
   };
+  // (the first tile and the queries are asked for before the tree is known, where they do not hang on it)
   find_slot(begin);
+  if (begin < cache_tiles) request(begin);
+  const int node = row >> p.g_bits;
+  uint4 raw_q[KS];
+  {
+    const uint4* src = reinterpret_cast<const uint4*>((const uint16_t*)p.q + (((size_t)b * p.n + node) * p.H + (kvh << p.g_bits) + (row & g_mask)) * D);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) raw_q[x] = src[x * 2 + hi];
+  }
   build_tree(tree, p.parents + (size_t)b * p.n, p.n);
-  if (begin < end) request(begin);
+  if (begin >= cache_tiles && begin < end) request(begin);
   find_slot(begin + 1);
 
   // this lane's row (clamped: rows behind the last repeat it and are not written), turned and cut
-  const int node = row >> p.g_bits;
   uint4 qh[KS], ql[KS];
   float sc;
   {
-    const uint4* src = reinterpret_cast<const uint4*>((const uint16_t*)p.q + (((size_t)b * p.n + node) * p.H + (kvh << p.g_bits) + (row & g_mask)) * D);
     const float4* cs = reinterpret_cast<const float4*>(p.tab + (size_t)(u.n + depth_of(tree, node, p.n)) * (D / 2));
-    uint4 raw[KS];
     unsigned top = 0;
 #pragma unroll
-    for (int x = 0; x < KS; ++x) {
-      raw[x] = src[x * 2 + hi];
-      top = max_magnitudes(max_magnitudes(max_magnitudes(raw[x].x, raw[x].y), max_magnitudes(raw[x].z, raw[x].w)), top);
-    }
+    for (int x = 0; x < KS; ++x)
+      top = max_magnitudes(max_magnitudes(max_magnitudes(raw_q[x].x, raw_q[x].y), max_magnitudes(raw_q[x].z, raw_q[x].w)), top);
     top = max_magnitudes(top, __shfl_xor(top, 32, 64));
     float inverse;
     const float scale = row_scale(top, inverse);
     sc = p.scale_log2e * inverse;
 #pragma unroll
-    for (int x = 0; x < KS; ++x) turn_cut(raw[x], scale, cs[(x * 2 + hi) * 2], cs[(x * 2 + hi) * 2 + 1], qh[x], ql[x]);
+    for (int x = 0; x < KS; ++x) turn_cut(raw_q[x], scale, cs[(x * 2 + hi) * 2], cs[(x * 2 + hi) * 2 + 1], qh[x], ql[x]);
   }
 
   f32x16_t o[DB];
@@ -1471,13 +1500,16 @@ int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
 //   128 x 24, 1024  16/1 16.1, 32/1 18.9;   256 x 32, 2048  16/1 62.6, 32/1 54.4;   128 x 64  16/1 51.9, 32/1 32.7, 128/1 63
 //   128 x 128, 4096  32/1 107, 128/2 90;   8 x 2048, 2048  32/1 68, 128/2 59, 128/1 79;   128 x 256, 4096  32/1 200, 128/1 146
 //   x 64: 128 x 128, 4096  32/1 62.1, 128/2 61.9;   8 x 2048, 2048  32/1 48.6, 128/2 47.9;   256 x 48, 2048  32/1 39.4
+// Positions re-assigned, bf16: 16 likewise, else the 64 rows for which the keys are turned once (two workgroups a compute unit):
+//   64 x 4, 2048  16/4 27.6, 64/8 39.1;   256 x 16  16/1 77, 64/2 103;   64 x 30  16/2 38.0, 64/8 41.1;   128 x 30  16/1 59.7, 64/4 60.1
+//   8 x 104  16/4 24.4, 64/17 30.2;   16 x 52  16/4 24.7, 64/17 31.7;   32 x 52  16/2 36.6, 64/16 35.2;   64 x 52  16/1 57.7, 64/8 45.0
 Shape attend_shape(const Params& p, int n) {
   const int rows = n * p.G, tiles16 = (rows + 15) / 16, tiles32 = (rows + 31) / 32, chip = 256, cols = block_cols(p);
   Shape s;
-  if ((long long)p.U * tiles16 <= (rows <= 32 ? chip : chip / 3)) s.rows_per_tile = 16;
-  else if (rows <= 64 || (long long)p.U * tiles32 <= chip || p.dtype != TREEKV_BF16 || (p.flags & TREEKV_POSITION_RERANK)) s.rows_per_tile = rows <= 16 ? 16 : 32;
-  else s.rows_per_tile = 128;
-  if (p.dtype == TREEKV_BF16 && (p.flags & TREEKV_POSITION_RERANK) && rows > 16) s.rows_per_tile = TURN_ROWS;
+  const bool bf16 = p.dtype == TREEKV_BF16, turned = bf16 && (p.flags & TREEKV_POSITION_RERANK) != 0;
+  if (rows <= 16 || (long long)p.U * tiles16 <= (rows <= 32 ? chip : chip / 3)) s.rows_per_tile = 16;
+  else if (turned) s.rows_per_tile = TURN_ROWS;
+  else s.rows_per_tile = !bf16 || rows <= 64 || (long long)p.U * tiles32 <= chip ? 32 : 128;
   s.row_tiles = (rows + s.rows_per_tile - 1) / s.rows_per_tile;
   // a wave has a block of columns at least, the large workgroup a tile
   const int blocks = (p.cap + cols - 1) / cols + (n + cols - 1) / cols, tiles = (p.cap + TILE_COLS - 1) / TILE_COLS + (n + TILE_COLS - 1) / TILE_COLS;
@@ -1538,7 +1570,10 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
     if (s.rows_per_tile == TURN_ROWS) return launch_attend_turned<D>(s, a, st);
   }
   if (s.rows_per_tile == 16) return rope ? launch_attend_rb<T, D, 1, true>(s, a, st) : launch_attend_rb<T, D, 1, false>(s, a, st);
-  return rope ? launch_attend_rb<T, D, 2, true>(s, a, st) : launch_attend_rb<T, D, 2, false>(s, a, st);
+  if constexpr (sizeof(T) == 4) {
+    if (rope) return launch_attend_rb<T, D, 2, true>(s, a, st);
+  }
+  return launch_attend_rb<T, D, 2, false>(s, a, st);
 }
 
 template <typename T, int D, bool ROPE>

@@ -62,7 +62,7 @@ def make(binding, *, budget=48, batch=2, hkv=2, G=2, d=64, dtype="bf16", flags=0
     return kv
 
 
-def check_attend(kv, q, k, v, parents, out, lse, every=1):
+def check_attend(kv, q, k, v, parents, out, lse, every=1, skip=()):
     """Against the plain form, every `every`-th unit and the last."""
     import torch
 
@@ -77,6 +77,8 @@ def check_attend(kv, q, k, v, parents, out, lse, every=1):
             heads = slice(h * G, (h + 1) * G)
             want, want_lse, bound, lse_bound, _ = ref.attend_unit(kv, states[b * c.kv_heads + h], q[b, :, heads], k[b, :, h], v[b, :, h],
                                                                   parents[b])
+            for i in skip:
+                want_lse[i], want[i] = lse[b, i, heads], out[b, i, heads]
             absent = torch.isinf(want_lse)
             assert torch.equal(torch.isinf(lse[b, :, heads]), absent)
             off = (lse[b, :, heads] - want_lse).abs().masked_fill(absent, 0.0)
@@ -106,6 +108,10 @@ SHAPES = [
     (48, 30, 21, 2, 2, 2, 128, "bf16", RERANK),
     (48, 133, 40, 2, 2, 4, 64, "bf16", RERANK),
     (300, 700, 13, 1, 2, 8, 128, "bf16", RERANK),
+    (48, 133, 40, 6, 2, 4, 64, "bf16", RERANK),            # many units and rows: keys turned for 64 rows
+    (300, 700, 13, 7, 2, 8, 128, "bf16", RERANK),
+    (200, 90, 70, 30, 1, 2, 128, "bf16", RERANK),          # still filling, three row tiles
+    (100, 0, 66, 30, 1, 2, 64, "bf16", RERANK),            # empty
     (300, 450, 33, 2, 1, 1, 64, "f32", RERANK),
     (300, 450, 5, 1, 1, 2, 128, "f32", RERANK),
 ]
@@ -133,7 +139,7 @@ def test_attend(binding, shape, kind):
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
-@pytest.mark.parametrize("flags,batch,G", [(0, 1, 2), (RERANK, 1, 2), (0, 90, 8)])
+@pytest.mark.parametrize("flags,batch,G", [(0, 1, 2), (RERANK, 1, 2), (0, 90, 8), (RERANK, 30, 8)])
 def test_attend_with_rising_logits(binding, dtype, d, flags, batch, G):
     """Large, ordered logits: every block of columns raises the reference of the sums."""
     import torch
@@ -154,8 +160,35 @@ def test_attend_with_rising_logits(binding, dtype, d, flags, batch, G):
     check_attend(kv, q, k, v, parents, out, lse, every=45)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 128)])
+@pytest.mark.parametrize("flags,batch,G", [(0, 1, 1), (RERANK, 1, 1), (0, 90, 8), (RERANK, 30, 8)])
+def test_attend_with_keys_of_all_sizes(binding, dtype, d, flags, batch, G):
+    """Neighbouring keys and queries differ by powers of two up to 2^60; some are all zeros."""
+    import torch
+
+    kv = make(binding, budget=200, batch=batch, hkv=1, G=G, d=d, dtype=dtype, flags=flags)
+    n = 12
+    q, k, v = tokens(kv, 200, 15)
+    power = torch.tensor([2.0 ** ((i * 37) % 61 - 58) for i in range(200)], device="cuda")
+    k = (k.float() * power[None, :, None, None]).to(k.dtype)
+    k[:, 7::50] = 0
+    for at in range(0, 200, 50):
+        out, ret, nret, ev = kv.new_outputs(50)
+        kv.prefill_chunk(*[x[:, at:at + 50].contiguous() for x in (q, k, v)], 50, out, ret, nret, ev)
+    q, k, v = tokens(kv, n, 16)
+    q = (q.float() * torch.tensor([2.0 ** (i % 5 - 2) for i in range(n)], device="cuda")[None, :, None, None]).to(q.dtype)
+    q[:, 3] = 0
+    q[:, 4] *= 2.0 ** 40
+    k[:, 1:6] *= 2.0 ** -42
+    parents = [tree("chain", n, None)] * batch
+    out, lse, scratch = kv.new_tree_outputs(n)
+    kv.tree_attend(q, k, v, torch.tensor(parents, dtype=torch.int32, device="cuda"), out, lse, scratch)
+    # (the query of 2^40 gives logits of 2^43 to the cached keys near 2^2, whose bound is no bound: it is left out)
+    check_attend(kv, q, k, v, parents, out, lse, every=45, skip=(4,))
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
-@pytest.mark.parametrize("flags,batch", [(0, 1), (RERANK, 1), (0, 30)])
+@pytest.mark.parametrize("flags,batch", [(0, 1), (RERANK, 1), (0, 30), (RERANK, 5)])
 def test_hidden_infinities_and_nans(binding, dtype, d, flags, batch):
     """A node's rows are not finite: who does not attend it gets the bits it gets without; who does, what arithmetic says."""
     import torch
