@@ -1482,7 +1482,8 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
       if (lr < O::NCOL && (cached ? c < u.columns && c != u.hole : c < L)) {
         const int slot = ROPE && cached ? slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, c) : c;
         unsigned long long* a = acc + (cached ? slot : cap_cols + c);
-        const unsigned long long fix = (unsigned long long)(long long)(mine * COLSUM_FIX + 0.5f);
+        // (a probability is at most 1; exponentials of logits past 2^20, against an lse rounded twice, need not be)
+        const unsigned long long fix = (unsigned long long)(long long)(fminf(mine, (float)here) * COLSUM_FIX + 0.5f);
         *a = r0 == 0 ? fix : *a + fix;               // (they are zero between calls)
       }
       k = next_k;

@@ -315,6 +315,24 @@ def test_commit(binding, shape):
 
 @pytest.mark.parametrize("flags", [0, RERANK])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_commit_of_large_logits(binding, dtype, flags):
+    """Logits of some 2^40, where fp32 tells no two probabilities apart: what a column gains is still between 0 and 1 a row."""
+    kv = make(binding, batch=1, fed=30, dtype=dtype, flags=flags)
+    q, k, v = tokens(kv, 6, 81)
+    q *= 2.0 ** 38
+    before = ref.state(kv)
+    _, _, nret, _, status = run_commit(kv, q, k, v, [[-1, 0, 1, 2, 3, 0]], [[0, 1, 2, 3]], 4)
+    assert status.tolist() == [0] and bool((nret == 34).all())
+    for old, new in zip(before, ref.state(kv)):
+        assert new["pos"][:30] == old["pos"] and bool(new["S"].isfinite().all())
+        added = new["S"].clone()
+        added[:30] -= old["S"]
+        # (4 tokens of 2 heads, and a rounding of a sum below 64)
+        assert bool((added >= 0).all()) and bool((added <= 8 + 2.0 ** -18).all()), (float(added.min()), float(added.max()))
+
+
+@pytest.mark.parametrize("flags", [0, RERANK])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rounds_against_chunks_and_steps(binding, flags, dtype):
     """Verify and commit, round after round, sequences accepting different numbers of tokens, against a context of its own for
     each sequence that is fed the same tokens as chunks (one token: a decode step)."""
