@@ -61,8 +61,8 @@ __device__ inline int work_piece(const treekv_qkv_args& a, const float2* cs, boo
       const float o = __shfl(x[e], (threadIdx.x & 63) + other, 64);
       const float2 t = a.positions && turned ? cs[plane + e] : make_float2(1.f, 0.f);
       const float p0 = second ? o : x[e], p1 = second ? x[e] : o;
-      ya[e] = p0 * t.x - p1 * t.y;
-      yb[e] = p0 * t.y + p1 * t.x;
+      ya[e] = a.positions ? p0 * t.x - p1 * t.y : p0;        // (not turned at all: an infinity times 0 would be a NaN)
+      yb[e] = a.positions ? p0 * t.y + p1 * t.x : p1;
     }
     if (turned) {
       if (a.flags & TREEKV_ROPE_TO_PLANES) {

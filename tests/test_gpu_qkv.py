@@ -177,3 +177,19 @@ def test_into_a_cache_with_reassigned_positions(binding):
         outs.append(o)
     # logits of size 8 at most, d + 20 roundings each, in either context
     assert torch.allclose(outs[0], outs[1], rtol=0, atol=2 * 2 * 84 * 2.0 ** -24 * 64)
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_order_of_planes_alone(binding, dt, d):
+    """Neither normalised nor turned: the halves' pairs side by side, every value as it was, infinities and the largest too."""
+    import torch
+
+    dtype = getattr(torch, dt)
+    x = torch.randn(5, 3, d, generator=torch.Generator().manual_seed(d)).to(dtype)
+    x[0, 0, 3], x[1, 1, d // 2 + 3], x[2, 2, 7], x[3, 0, d - 1] = float("inf"), -float("inf"), torch.finfo(dtype).max, -0.0
+    got = binding.qkv_prepare(x.cuda(), x.cuda(), x.cuda(), halves=True, to_planes=True)
+    want = torch.stack([x[..., :d // 2], x[..., d // 2:]], dim=-1).flatten(-2)
+    for y in got[:2]:
+        assert torch.equal(y.cpu().view(torch.uint8), want.contiguous().view(torch.uint8))
+    assert torch.equal(got[2].cpu(), x)
