@@ -361,7 +361,7 @@ int treekv_fork(treekv_ctx* ctx, const treekv_ctx* from, const int32_t* src, con
  *              apart, so that all three can lie in one packed row; q_out, k_out, v_out contiguous.  A pair of input and
  *              output may be left out (both NULL).  q_out may be q itself where q is contiguous, likewise k and v; other
  *              overlaps of an output are refused.
- *   weights    [d] storage dtype, or NULL: no norm
+ *   weights    [d] storage dtype, 16-byte aligned, or NULL: no norm
  *   positions  [tokens] int32 and inv_freq [rotary_dim / 2] float64 (both device), or both NULL: no rotation (what a
  *              context with TREEKV_POSITION_RERANK takes).  Plane i is turned by position * inv_freq[i].
  *   rotary_dim leading dimensions of a head that are turned (a multiple of 16, at most d; 0: none); the others pass.

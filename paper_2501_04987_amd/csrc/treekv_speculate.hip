@@ -94,6 +94,7 @@ int treekv_qkv_prepare(const treekv_qkv_args* args, void* stream) {
   if (a.positions && a.rotary_dim == 0) return TREEKV_EINVAL;
   if ((a.q_weight && !a.q) || (a.k_weight && !a.k)) return TREEKV_EINVAL;
   if ((a.q_weight || a.k_weight) && !(a.eps >= 0.0f)) return TREEKV_EINVAL;
+  if (!aligned16(a.q_weight) || !aligned16(a.k_weight)) return TREEKV_EINVAL;
   if (a.head_dim != 64 && a.head_dim != 128) return TREEKV_EUNSUPPORTED;
   if (a.rotary_dim % 16 != 0 || a.q_heads > 65536 || a.kv_heads > 65536) return TREEKV_EUNSUPPORTED;
   const int64_t esz = a.dtype == TREEKV_BF16 ? 2 : 4;

@@ -101,7 +101,7 @@ def test_qkv_prepare(binding):
     for kw in (dict(tokens=0), dict(tokens=-1), dict(dtype=2), dict(q=None), dict(q_out=None), dict(k=None), dict(v_out=None), dict(q_heads=0),
                dict(kv_heads=0), dict(flags=2), dict(flags=4), dict(positions=None), dict(inv_freq=None), dict(rotary_dim=-16),
                dict(rotary_dim=144), dict(rotary_dim=0), dict(eps=-1.0), dict(eps=float("nan")), dict(q=0x10008), dict(k_out=0x50004),
-               dict(q_stride=504), dict(q_stride=516), dict(k_stride=-512), dict(v_stride=1 << 62),
+               dict(q_weight=0x72002), dict(k_weight=0x73008), dict(q_stride=504), dict(q_stride=516), dict(k_stride=-512), dict(v_stride=1 << 62),
                dict(q=None, q_out=None), dict(q=None, q_out=None, k=None, k_out=None, v=None, v_out=None),
                dict(k_out=0x40000 + 4 * 512 * 2 - 16), dict(q_out=0x20000), dict(q_out=0x10010), dict(q_out=0x10000, q_stride=768),
                dict(v_out=0x10000 + 3 * 1024), dict(q_out=0x70000), dict(k_out=0x71000), dict(v_out=0x72000), dict(q_out=0x73010)):
