@@ -1580,9 +1580,10 @@ int launch_attend_d(const Params& p, const Tree& t, float* out, float* lse, floa
 template <typename T, int D, bool ROPE>
 int launch_colsums_d(const Params& p, const Tree& t, int32_t* status, hipStream_t st) {
   const size_t lds = (size_t)(ROPE ? Ops<T, D>::QPARTS : 1) * CS_ROWS * q_row_elems<T, D>() * sizeof(T);
-  // two workgroups for each of the 256 compute units, each wave with a block of columns at least
+  // as many workgroups as run at once, two on each of the 256 compute units or, where keys are turned in 235 registers, one
+  // (64 units x 16 rows into 2048 slots: 22.6 us, 28.6 with two rounds), each wave with a block of columns at least
   const int cols = block_cols(p), blocks = (p.cap + cols - 1) / cols + (t.max_len + cols - 1) / cols;
-  const int most = (blocks + TR_WAVES - 1) / TR_WAVES, fit = 512 / p.U, slices = fit < 1 ? 1 : fit < most ? fit : most;
+  const int most = (blocks + TR_WAVES - 1) / TR_WAVES, fit = (ROPE && sizeof(T) == 2 ? 256 : 512) / p.U, slices = fit < 1 ? 1 : fit < most ? fit : most;
   auto kernel = tree_colsum_kernel<T, D, ROPE>;
   if (lds > 48 * 1024 &&
       hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)))
