@@ -333,6 +333,29 @@ def test_commit_of_large_logits(binding, dtype, flags):
 
 @pytest.mark.parametrize("flags", [0, RERANK])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_commit_weighs_with_the_given_lse(binding, dtype, flags):
+    """With every lse smaller by 3 each column gains e^3 times as much, past one a row too."""
+    import torch
+
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    n, parents, path = 6, i32([[-1, 0, 1, 2, 3, 0]]), i32([[0, 1, 2, 3]])
+    gains = []
+    for less in (0.0, 3.0):
+        kv = make(binding, batch=1, fed=30, dtype=dtype, flags=flags)
+        q, k, v = tokens(kv, n, 82, scale=3.0)
+        before = ref.state(kv)
+        out, lse, scratch = kv.new_tree_outputs(n)
+        kv.tree_attend(q, k, v, parents, out, lse, scratch)
+        kv.tree_commit(q, k, v, parents, lse - less, path, i32([4]), *kv.new_outputs()[1:3])
+        gains.append([x["S"] - torch.cat([y["S"], y["S"].new_zeros(4)]) for x, y in zip(ref.state(kv), before)])
+    for one, more in zip(*gains):
+        assert float(one.max()) > 0.5                      # (so that more is past one)
+        # logits and lse below 2^8 in size, in units of log2, are off by 2^-15 at most, the scores (below 2^9) by 2^-15 each time
+        assert bool(((more - one * 2.718281828459045 ** 3).abs() <= 2.0 ** -14 * more + 22 * 2.0 ** -15).all())
+
+
+@pytest.mark.parametrize("flags", [0, RERANK])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rounds_against_chunks_and_steps(binding, flags, dtype):
     """Verify and commit, round after round, sequences accepting different numbers of tokens, against a context of its own for
     each sequence that is fed the same tokens as chunks (one token: a decode step)."""
