@@ -1057,7 +1057,8 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
 // row is scaled by a power of two so that its largest element is near 2^13, and the scales go back on with the softmax's.
 // The next tile is on its way while one is worked on, keys and angles to registers, V to the other of its two stages; two
 // workgroups share a compute unit and fill each other's waits at the two barriers of a tile.  13 nodes of 8 groups of 4, batch
-// 8, 2048 slots: 42.5 us with the merge, of which 16 pass before the first product (order arrays, angles, the queries' cut).
+// 8, 2048 slots: 42.5 us with the merge, of which some 15 do not grow with the
+// cache (order arrays, first angles, the queries' cut, partial results); a tile more costs 6 us on every unit.
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 constexpr int TURN_THREADS = 256, TURN_ROWS = 64;
