@@ -104,6 +104,12 @@ SHAPES = [
     (100, 70, 33, 16, 8, 4, 64, "bf16", 0),                # two row tiles, still filling
     (300, 450, 256, 5, 8, 1, 128, "bf16", 0),              # the same in slices
     (300, 450, 256, 5, 8, 1, 64, "bf16", 0),
+    (100, 150, 12, 8, 8, 4, 128, "bf16", 0),               # 32 rows a workgroup
+    (100, 70, 12, 8, 8, 4, 64, "bf16", 0),
+    (60, 90, 20, 8, 8, 2, 128, "f32", 0),
+    (60, 40, 20, 8, 8, 2, 64, "f32", 0),
+    (60, 90, 20, 8, 8, 2, 64, "f32", RERANK),
+    (60, 90, 20, 8, 8, 2, 128, "f32", RERANK),
     (48, 0, 3, 1, 1, 2, 64, "bf16", RERANK),
     (48, 30, 21, 2, 2, 2, 128, "bf16", RERANK),
     (48, 133, 40, 2, 2, 4, 64, "bf16", RERANK),
