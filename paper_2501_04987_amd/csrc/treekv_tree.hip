@@ -36,7 +36,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 constexpr int TR_THREADS = 512, TR_WAVES = TR_THREADS / 64;
 constexpr int MAX_NODES = TREEKV_TREE_MAX_NODES, MAX_WORDS = MAX_NODES / 32;
-constexpr float REF_NONE = -1.0e30f;               // reference of a row that has seen nothing: finite, so that exp2(-inf - it) = 0
+constexpr float REF_NONE = -3.0e38f;               // reference of a row that has seen nothing: below every logit, and finite, so that exp2(-inf - it) = 0
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 constexpr float COLSUM_FIX = 1099511627776.0f;      // 2^40: column sums cross kernels as 64-bit fixed point
 constexpr int COLSUM_TILE = 128;                    // their two parts are rounded up to this

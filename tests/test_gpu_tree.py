@@ -194,6 +194,34 @@ def test_attend_with_keys_of_all_sizes(binding, dtype, d, flags, batch, G):
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("batch,G", [(1, 1), (90, 8)])
+def test_attend_with_the_lowest_logits(binding, dtype, d, batch, G):
+    """Every logit of a query is the same -10^33 or so: the values' mean comes out."""
+    import torch
+
+    kv = make(binding, budget=120, batch=batch, hkv=1, G=G, d=d, dtype=dtype)
+    q, k, v = tokens(kv, 100, 21)
+    q[:], k[:] = 0, 0
+    k[..., 0] = 2.0 ** 56
+    out, ret, nret, ev = kv.new_outputs(100)
+    kv.prefill_chunk(q, k, v, 100, out, ret, nret, ev)
+    n = 12
+    q2, _, v2 = tokens(kv, n, 22)
+    q2[:] = 0
+    q2[..., 0] = -(2.0 ** 56)
+    parents = torch.tensor([tree("chain", n, None)] * batch, dtype=torch.int32, device="cuda")
+    out, lse, scratch = kv.new_tree_outputs(n)
+    kv.tree_attend(q2, k[:, :n].contiguous(), v2, parents, out, lse, scratch)
+    want_lse = -(2.0 ** 112) * kv.cfg.softmax_scale        # (the log of 112 is nothing beside it)
+    assert bool(((lse.double() - want_lse).abs() <= 4 * 2.0 ** -24 * -want_lse).all())
+    for i in range(n):
+        seen = torch.cat([v[:, :, 0], v2[:, :i + 1, 0]], dim=1).double()
+        # sums of 101 + i values, the weights' sum, the quotient: a rounding each
+        room = (110 + i) * 2.0 ** -24 * seen.abs().mean(dim=1)
+        assert bool(((out[:, i].double() - seen.mean(dim=1)[:, None]).abs() <= room[:, None]).all()), i
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("flags,batch", [(0, 1), (RERANK, 1), (0, 30), (RERANK, 5)])
 def test_hidden_infinities_and_nans(binding, dtype, d, flags, batch):
     """A node's rows are not finite: who does not attend it gets the bits it gets without; who does, what arithmetic says."""
