@@ -1191,9 +1191,11 @@ __global__ __launch_bounds__(TURN_THREADS, 2) void tree_attend_turned_kernel(Arg
       reinterpret_cast<uint4*>(kl)[place] = low;
     }
   };
-  // (the first tile and the queries are asked for before the tree is known, where they do not hang on it)
+  // (the first tile and the queries are asked for before the tree is known, where they do not hang on it; a slice without a
+  // tile, of which a cache that is still filling has some, asks for nothing: nobody would wait for its copies into LDS, which
+  // becomes the sums')
   find_slot(begin);
-  if (begin < cache_tiles) request(begin);
+  if (begin < cache_tiles && begin < end) request(begin);
   const int node = row >> p.g_bits;
   uint4 raw_q[KS];
   {
