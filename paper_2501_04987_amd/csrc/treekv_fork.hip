@@ -2,9 +2,12 @@
 //
 // A unit's state is its cache rows, scores, order arrays and bookkeeping words, each copied as it lies: slots keep their
 // numbers, so that the copy goes on bit for bit as its source would.  A cache that is still filling has its n tokens in
-// slots 0 .. n-1 and the rows behind them are not copied.  Bound by memory: every live byte once in and once out (one sequence
+// slots 0 .. n-1; the rows behind them, and all rows of a sequence that is emptied, become zeros, as a reset leaves them: the
+// decode and chunk kernels multiply rows behind the last one by probabilities of zero, and what the sequence before left there
+// may be an infinity or a NaN.  Bound by memory: every live byte once in, every row once out (one sequence
 // of 8 heads x 4096 rows x 128 into 15: 65 us, 252 MB written at 3.9 TB/s; stored past the caches 62, but the read of the
-// copies that follows takes 11 longer).
+// copies that follows takes 11 longer).  The zeros are: 12 sequences of that size emptied beside one copied and the whole
+// exported 92 us, 128 through the caches.
 
 #include "treekv_internal.h"
 
@@ -34,7 +37,7 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(Params to, Params fr
     int* Rd = to.R + du * r;
     float* Sd = to.S + du * cap;
     int* meta_d = to.meta + du * META_STRIDE;
-    if (s < 0) {                                   // as after a reset (rows stay what they were: initialised memory)
+    if (s < 0) {                                   // as after a reset
       for (int i = tid; i < 2 * m; i += FORK_THREADS) Ed[i] = PEd[i] = i < m ? to.n_sink + i : 0;
       for (int i = tid; i < to.n_recent; i += FORK_THREADS) Rd[i] = to.n_sink + m + i;
       for (int i = tid; i < cap; i += FORK_THREADS) Sd[i] = 0.f;
@@ -51,9 +54,8 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(Params to, Params fr
     if (tid < META_STRIDE) meta_d[tid] = meta[tid];
     return;
   }
-  if (s < 0) return;
-  const int n = meta[META_N];
-  const size_t vecs = (size_t)(n < to.budget ? n : cap) * row_vec;
+  const int n = s < 0 ? 0 : meta[META_N];
+  const size_t vecs = (size_t)(n < to.budget ? n : cap) * row_vec, all = (size_t)cap * row_vec;
   const uint4* Ks = reinterpret_cast<const uint4*>(from.K) + su * cap * row_vec;
   const uint4* Vs = reinterpret_cast<const uint4*>(from.V) + su * cap * row_vec;
   uint4* Kd = reinterpret_cast<uint4*>(to.K) + du * cap * row_vec;
@@ -63,6 +65,10 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(Params to, Params fr
   for (int x = 0; x < FORK_VECS; ++x) {
     const size_t i = base + (size_t)x * FORK_THREADS;
     if (i < vecs) { Kd[i] = Ks[i]; Vd[i] = Vs[i]; }
+    else if (i < all) {                            // past the caches, where they would only be in the way
+      store16<true>(Kd + i, make_uint4(0, 0, 0, 0));
+      store16<true>(Vd + i, make_uint4(0, 0, 0, 0));
+    }
   }
 }
 
