@@ -74,8 +74,9 @@ __global__ void reset_kernel(Params p) {
   for (int i = threadIdx.x; i < p.cap; i += blockDim.x) p.S[(size_t)unit * p.cap + i] = 0.f;
   const size_t cs_cols = (size_t)(p.cap + 127) / 128 * 128 + (size_t)(p.max_chunk + 127) / 128 * 128;
   for (size_t i = threadIdx.x; i < cs_cols; i += blockDim.x) p.pf_colacc[(size_t)unit * cs_cols + i] = 0;
-  // Cache rows are always initialised memory: the decode kernel requests its first rows before it
-  // knows how many are live, and multiplies what it did not need by zero.
+  // Rows behind the last token are zeros (treekv_import_state, treekv_prefill_prompt and treekv_fork leave them so too): the decode
+  // kernel requests its first rows before it knows how many are live, and multiplies what it did not need by zero.  (The
+  // free row of a full cache holds the token evicted last, one of the same sequence.)
   const size_t vecs = (size_t)p.cap * p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16;
   uint4* Kz = reinterpret_cast<uint4*>(p.K) + (size_t)unit * vecs;
   uint4* Vz = reinterpret_cast<uint4*>(p.V) + (size_t)unit * vecs;
@@ -289,15 +290,23 @@ __global__ __launch_bounds__(256) void import_state_kernel(Params p, const int* 
   }
 }
 
+// One block per cache row: the snapshot's rows to their slots, zeros to the rows without a token (what another sequence
+// left there may not be finite, see reset_kernel).
 __global__ void import_rows_kernel(Params p, const uint4* __restrict__ Kin, const uint4* __restrict__ Vin, int row_vec) {
-  const int unit = blockIdx.y, i = blockIdx.x;   // one block per snapshot row
-  const int slot = p.pf_list[(size_t)unit * (p.cap + p.max_chunk) + i];
-  if (slot < 0) return;
+  const int unit = blockIdx.y, i = blockIdx.x;
+  const int slot = i < p.budget ? p.pf_list[(size_t)unit * (p.cap + p.max_chunk) + i] : -1;
+  int to = slot;
+  if (slot < 0) {                                // while the cache fills, token i sits in row i; once it is full one row is free
+    const int* meta = p.meta + (size_t)unit * META_STRIDE;
+    to = meta[META_N] == p.budget ? meta[META_FREE] : i;
+  }
   const size_t src = ((size_t)unit * p.budget + i) * row_vec;
-  const size_t dst = ((size_t)unit * p.cap + slot) * row_vec;
+  const size_t dst = ((size_t)unit * p.cap + to) * row_vec;
   for (int e = threadIdx.x; e < row_vec; e += blockDim.x) {
-    reinterpret_cast<uint4*>(p.K)[dst + e] = Kin[src + e];
-    reinterpret_cast<uint4*>(p.V)[dst + e] = Vin[src + e];
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+    if (slot >= 0) { k = Kin[src + e]; v = Vin[src + e]; }
+    reinterpret_cast<uint4*>(p.K)[dst + e] = k;
+    reinterpret_cast<uint4*>(p.V)[dst + e] = v;
   }
 }
 
@@ -339,7 +348,7 @@ int launch_import_state(const Params& p, const char* src, int32_t* status, hipSt
   const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16;
   hipLaunchKernelGGL(import_state_kernel, dim3(p.U), dim3(256), 0, s, p, (const int*)(src + l.header),
                      (const int*)(src + l.positions), (const int*)(src + l.slots), (const float*)(src + l.S), status);
-  hipLaunchKernelGGL(import_rows_kernel, dim3(p.budget, p.U), dim3(64), 0, s, p, (const uint4*)(src + l.K),
+  hipLaunchKernelGGL(import_rows_kernel, dim3(p.cap, p.U), dim3(64), 0, s, p, (const uint4*)(src + l.K),
                      (const uint4*)(src + l.V), row_vec);
   return finish_launch();
 }

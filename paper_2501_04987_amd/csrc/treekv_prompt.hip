@@ -610,7 +610,8 @@ __global__ __launch_bounds__(256) void prompt_blocks_kernel(Params p, int T, int
 }
 
 // ---------------------------------------------------------------------------------------------
-// handoff: the kept rows become slots 0 .. n-1 (logical order = slot order), and decoding's state is set
+// handoff: the kept rows become slots 0 .. n-1 (logical order = slot order), the rows behind them zeros (what the
+// sequence before left there may not be finite, and later calls multiply it by zero), and decoding's state is set
 // ---------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void prompt_handoff_kernel(Params p, const uint4* __restrict__ Kp,
                                                              const uint4* __restrict__ Vp, int T, int b, int n,
@@ -636,9 +637,13 @@ __global__ __launch_bounds__(256) void prompt_handoff_kernel(Params p, const uin
     int* PEu = p.PE + (size_t)unit * 2 * p.m;
     for (int k = p.m + tid; k < 2 * p.m; k += 256) Eu[k] = PEu[k] = 0;
   }
-  if (i >= p.budget) return;
+  if (i >= p.cap) return;
   int pos = -1;
-  if (i < n) {
+  if (i >= n) {
+    const size_t dst = ((size_t)unit * p.cap + i) * row_vec + e;
+    reinterpret_cast<uint4*>(p.K)[dst] = reinterpret_cast<uint4*>(p.V)[dst] = make_uint4(0, 0, 0, 0);
+    if (i >= p.budget) return;
+  } else {
     const int kb = p.pp_kept[(size_t)unit * p.budget + i / b];
     pos = kb * b + i % b;
     const size_t src = (((size_t)bq * T + pos) * p.Hkv + kvh) * row_vec + e;
@@ -754,7 +759,7 @@ int launch_prompt(const Params& p, const void* Qw, const void* K, const void* V,
                      block_means, evicted_blocks);
   const int row_vec = p.D * (p.dtype == TREEKV_BF16 ? 2 : 4) / 16, per_wg = 256 / row_vec;
   const int n = T < p.budget ? T : p.budget;
-  hipLaunchKernelGGL(prompt_handoff_kernel, dim3((p.budget + per_wg - 1) / per_wg, p.U), dim3(256), 0, s, p,
+  hipLaunchKernelGGL(prompt_handoff_kernel, dim3((p.cap + per_wg - 1) / per_wg, p.U), dim3(256), 0, s, p,
                      (const uint4*)K, (const uint4*)V, T, b, n, row_vec, retained, n_retained);
   // (with block means the scores kernel has written the caller's token scores)
   if (token_scores && !block_means &&
