@@ -329,7 +329,7 @@ int treekv_tree_attend(treekv_ctx* ctx, const void* q, const void* k, const void
  * treekv_tree_commit - the tokens path[b][0 .. path_len[b]) of sequence b's tree (the first a child of the last cached
  * token, each of the others a child of the one before) become its next tokens: their probabilities are added to the scores
  * and counts, then, with the averaged scores frozen, Algorithm 1's append / compare / evict / advance runs for
- * them in order.
+ * them in order.  A probability that is a NaN (its query, key or lse holds one) adds nothing to the scores.
  *   q, k, v, parents, n as given to treekv_tree_attend, lse as it wrote it, the context unchanged since
  *   path     [B, max_len] int32 (device), 1 <= max_len <= n;  path_len [B] int32 (device), 0 .. max_len
  *   retained [B, Hkv, c] int32, n_retained [B, Hkv] (may be NULL): as treekv_decode_step

@@ -1397,7 +1397,8 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
   if (L == 0) return;
   const int rows = L * p.G;
   // A probability is at most 1, but past 2^20 its logit and the lse, rounded twice, tell nothing of it: it is held to 1 there.
-  // Elsewhere it is held to what the accumulator has room for, whatever lse holds (one of another state may be too small).
+  // Elsewhere it is held to what the accumulator has room for, whatever lse holds (one of another state may be too small).  A NaN
+  // adds nothing: what a score has gained it keeps.
   const float room = 0x1p22f / rows;
   const int cache_blocks = (u.columns + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
   const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
@@ -1480,7 +1481,7 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
           const int c = col0 + O::col(q4, j);
           const bool seen = r < rows && (cached ? c < u.columns && c != u.hole : c <= i);
           const float e = fast_exp2(fmaf(O::at(s[0], j), p.scale_log2e, -l2));
-          col_sum[j] += seen ? fminf(e, most) : 0.f;
+          col_sum[j] += seen ? fminf(fmaxf(e, 0.f), most) : 0.f;       // (the larger of a NaN and 0 is 0)
         }
       }
       float mine = 0.f;                              // lane lr of a group passes on the group's column lr
