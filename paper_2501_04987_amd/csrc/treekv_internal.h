@@ -53,6 +53,7 @@ struct Params {
   float* partial;           // [U][nsplit][G][D+2] split decode scratch: a slice's partial (acc, max, sum)
   // prefill scratch
   unsigned long long* pf_colacc;   // [U][cache columns | chunk columns, each rounded up to 128] column sums of the chunk in flight, fixed point
+                            // (of a drafted path: fp32 in the low words); zero between calls
   float* pf_snew;           // [U][max_chunk] accumulated S of the chunk's tokens
   int* pf_flag;             // [U][cap + max_chunk] freed slots / dead chunk tokens, then destinations
   int* pf_list;             // [U][cap + max_chunk] free slots in ascending order

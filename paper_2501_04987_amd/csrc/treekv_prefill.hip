@@ -1491,6 +1491,7 @@ __host__ __device__ inline size_t replay_lds_words(int m, int cap, int r, int L)
 //
 // TREE: the tokens are the accepted path of a drafted tree.  Every unit has its own number of them, which the column sums'
 // kernel has left in META_PATH (none: nothing changes but `evicted`), at most L, and token i's rows are those of node path[i].
+// The accumulators hold fp32 numbers then, in their low words.
 struct NoPath {};
 struct DraftPath {
   const int32_t* path;      // [B, L] nodes
@@ -1591,17 +1592,21 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
 
   // ---- Algorithm 1's S update for the whole chunk: add the column sums the attend kernel left in the accumulators ----
   {
+    auto sum_of = [](unsigned long long a) {
+      if constexpr (TREE) return __uint_as_float((unsigned)a);
+      else return (float)(long long)a * (1.0f / COLSUM_FIX);
+    };
     // every accumulator that is read is also cleared for the next chunk (the others only ever received zeros)
     auto cache_col = [&](int x, float v, unsigned long long a) {
       if (x <= n0 && x != f0) {                                      // the columns every row tile visited
-        v += (float)(long long)a * (1.0f / COLSUM_FIX);
+        v += sum_of(a);
         Sg[x] = v;
         acc[x] = 0;
       }
       if constexpr (IN_LDS) Su[x] = v;
     };
     auto chunk_col = [&](int x, unsigned long long a) {
-      snew[x] = (float)(long long)a * (1.0f / COLSUM_FIX);
+      snew[x] = sum_of(a);
       acc[cap_cols + x] = 0;
     };
 #pragma unroll

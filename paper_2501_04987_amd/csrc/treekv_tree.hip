@@ -38,8 +38,7 @@ constexpr int TR_THREADS = 512, TR_WAVES = TR_THREADS / 64;
 constexpr int MAX_NODES = TREEKV_TREE_MAX_NODES, MAX_WORDS = MAX_NODES / 32;
 constexpr float REF_NONE = -3.0e38f;               // reference of a row that has seen nothing: below every logit, and finite, so that exp2(-inf - it) = 0
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
-constexpr float COLSUM_FIX = 1099511627776.0f;      // 2^40: column sums cross kernels as 64-bit fixed point
-constexpr int COLSUM_TILE = 128;                    // their two parts are rounded up to this
+constexpr int COLSUM_TILE = 128;                    // the column accumulators' two parts are rounded up to this
 
 __device__ inline f32x4_t mfma_bf16(const uint4& a, const uint4& b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -1397,9 +1396,9 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
   if (L == 0) return;
   const int rows = L * p.G;
   // A probability is at most 1, but past 2^20 its logit and the lse, rounded twice, tell nothing of it: it is held to 1 there.
-  // Elsewhere it is held to what the accumulator has room for, whatever lse holds (one of another state may be too small).  A NaN
+  // Elsewhere it is held to what keeps a sum finite, whatever lse holds (one of another state may be too small).  A NaN
   // adds nothing: what a score has gained it keeps.
-  const float room = 0x1p22f / rows;
+  constexpr float ROOM = 0x1p64f;
   const int cache_blocks = (u.columns + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
   const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
   const int cap_cols = (p.cap + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
@@ -1475,7 +1474,7 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
         }
         const int r = r0 + tile * 16 + lr, i = r / p.G;
         const float l2 = row_lse[tile * 16 + lr];
-        const float most = fabsf(l2) > 0x1p20f ? 1.0f : room;
+        const float most = fabsf(l2) > 0x1p20f ? 1.0f : ROOM;
 #pragma unroll
         for (int j = 0; j < O::NCOL; ++j) {
           const int c = col0 + O::col(q4, j);
@@ -1494,8 +1493,9 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
       if (lr < O::NCOL && (cached ? c < u.columns && c != u.hole : c < L)) {
         const int slot = ROPE && cached ? slot_at(u, p.budget, p.n_sink, p.m, p.n_recent, c) : c;
         unsigned long long* a = acc + (cached ? slot : cap_cols + c);
-        const unsigned long long fix = (unsigned long long)(long long)(mine * COLSUM_FIX + 0.5f);
-        *a = r0 == 0 ? fix : *a + fix;               // (they are zero between calls)
+        // fp32 sums in the accumulators' low words (fixed point, which the chunk path's atomics ask for, would cut those below
+        // 2^-16 short); zero between calls
+        *a = __float_as_uint(r0 == 0 ? mine : __uint_as_float((unsigned)*a) + mine);
       }
       k = next_k;
     }
