@@ -5,7 +5,9 @@
 // A head is D elements in D / 8 (bf16) or D / 4 (fp32) lanes of 16 bytes; the mean of squares is one sum over those lanes,
 // the two dimensions of a plane lie in one lane (2i, 2i+1) or, for halves, rotary_dim / 2 dimensions apart in the same head:
 // one exchange of lanes, since rotary_dim is a multiple of 16.  A token's angles are formed once per workgroup, in double (a
-// position of a million times a frequency near 1 leaves 2^-33 of a turn), reduced to a turn and then to fp32.
+// position of a million times a frequency near 1 leaves 2^-33 of a turn), and reduced to a turn.  With fp32 storage their sines
+// and cosines are taken in double too and rounded once; for bf16 the reduced angle is rounded to fp32 first, which moves them by
+// 2^-23 at most, where the result's half step is 2^-9.
 // Bound by memory: every head once in and once out.
 
 #include "treekv_internal.h"
@@ -30,6 +32,24 @@ __device__ inline uint4 narrow(const float (&y)[8], uint16_t) {
 }
 __device__ inline uint4 narrow(const float (&y)[4], float) {
   return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+}
+
+// Sine of h half turns, |h| < 2, rounded once: reduced to a quarter turn either way (exactly) and from there by its power series,
+// whose first term left out is 2^-45 of it (x^18 / 19!).  (The library's double functions, good for all 53 bits, take 44
+// registers more, and with fewer workgroups side by side 16384 tokens of 48 heads x 128 take 167 us in place of 150, as long as
+// with angles rounded to fp32 first.)
+__device__ inline float sine(double h) {
+  const double whole = rint(h), x = (h - whole) * 3.14159265358979323846, y = x * x;
+  double s = 1.0 / 355687428096000.0;                // 17!
+  s = fma(s, y, -1.0 / 1307674368000.0);
+  s = fma(s, y, 1.0 / 6227020800.0);
+  s = fma(s, y, -1.0 / 39916800.0);
+  s = fma(s, y, 1.0 / 362880.0);
+  s = fma(s, y, -1.0 / 5040.0);
+  s = fma(s, y, 1.0 / 120.0);
+  s = fma(s, y, -1.0 / 6.0);
+  const float r = (float)fma(s * y, x, x);
+  return (int)whole & 1 ? -r : r;
 }
 
 // What happens to one 16-byte piece of a head (`part` of it; the lanes of a head lie side by side).  Returns the piece of the
@@ -95,7 +115,7 @@ __device__ inline int work_piece(const treekv_qkv_args& a, const float2* cs, boo
 // formed.  ITER = 4 forms the angles once per token of 64 heads and keeps four loads in flight: 32768 tokens of 48 heads x 128
 // 164 -> 153 us, 976 tokens 8.6; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 2.9 us).
 template <typename T, int D, int ITER, bool STREAM>
-__global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int chunks) {
+__global__ __launch_bounds__(QKV_THREADS, 6) void qkv_kernel(treekv_qkv_args a, int chunks) {
   constexpr int LPR = D / Storage<T>::EPL, ROWS = QKV_THREADS / LPR;
   __shared__ float2 cs[D / 2];
   const int tid = threadIdx.x, part = tid % LPR;
@@ -119,11 +139,16 @@ __global__ __launch_bounds__(QKV_THREADS) void qkv_kernel(treekv_qkv_args a, int
         if (weight) w[x] = reinterpret_cast<const uint4*>(weight)[part];
       }
     }
-    if (a.positions && tid < a.rotary_dim / 2) {
-      // turns: the fraction is exact, whatever the number of whole ones
-      const double turns = (double)a.positions[token] * a.inv_freq[tid] * 0.15915494309189533577;
+    // half turns, less whole turns (the fraction is exact, whatever their number)
+    auto half_turns = [&](int plane) {
+      const double turns = (double)a.positions[token] * a.inv_freq[plane] * 0.15915494309189533577;
+      return 2.0 * (turns - rint(turns));
+    };
+    if constexpr (sizeof(T) == 4) {                  // a lane for each cosine, which is a sine a quarter turn on, and each sine
+      if (a.positions && tid < a.rotary_dim) (&cs[tid >> 1].x)[tid & 1] = sine(half_turns(tid >> 1) + (tid & 1 ? 0.0 : 0.5));
+    } else if (a.positions && tid < a.rotary_dim / 2) {
       float s, c;
-      sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+      sincospif((float)half_turns(tid), &s, &c);
       cs[tid] = make_float2(c, s);
     }
     __syncthreads();
