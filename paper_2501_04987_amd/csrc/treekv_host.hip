@@ -42,8 +42,7 @@ size_t carve(Params& p, char* base) {
   p.meta = (int*)take(U * META_STRIDE * 4);
   p.logits = (float*)take(U * p.G * cap * 4);
   p.partial = (float*)take(U * p.nsplit * p.G * (size_t)(p.D + 2) * 4);
-  const size_t cs_cols = (cap + 127) / 128 * 128 + ((size_t)p.max_chunk + 127) / 128 * 128;
-  p.pf_colacc = (unsigned long long*)take(U * cs_cols * 8);
+  p.pf_colacc = (unsigned long long*)take(U * colsum_stride(p) * 8);
   p.pf_snew = (float*)take(U * (size_t)p.max_chunk * 4);
   p.pf_flag = (int*)take(U * ext * 4);
   p.pf_list = (int*)take(U * ext * 4);
@@ -72,7 +71,7 @@ __global__ void reset_kernel(Params p) {
   for (int i = threadIdx.x; i < 2 * p.m; i += blockDim.x) Eu[i] = PEu[i] = i < p.m ? p.n_sink + i : 0;
   for (int i = threadIdx.x; i < p.n_recent; i += blockDim.x) Ru[i] = p.n_sink + p.m + i;
   for (int i = threadIdx.x; i < p.cap; i += blockDim.x) p.S[(size_t)unit * p.cap + i] = 0.f;
-  const size_t cs_cols = (size_t)(p.cap + 127) / 128 * 128 + (size_t)(p.max_chunk + 127) / 128 * 128;
+  const size_t cs_cols = colsum_stride(p);
   for (size_t i = threadIdx.x; i < cs_cols; i += blockDim.x) p.pf_colacc[(size_t)unit * cs_cols + i] = 0;
   // Rows behind the last token are zeros (treekv_import_state, treekv_prefill_prompt and treekv_fork leave them so too): the decode
   // kernel requests its first rows before it knows how many are live, and multiplies what it did not need by zero.  (The

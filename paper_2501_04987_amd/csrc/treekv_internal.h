@@ -52,7 +52,7 @@ struct Params {
   float* logits;            // split decode scratch: scaled logits (log2 domain), [U][cap][G]; G = 8: [U][2][cap][4]
   float* partial;           // [U][nsplit][G][D+2] split decode scratch: a slice's partial (acc, max, sum)
   // prefill scratch
-  unsigned long long* pf_colacc;   // [U][cache columns | chunk columns, each rounded up to 128] column sums of the chunk in flight, fixed point
+  unsigned long long* pf_colacc;   // [U][colsum_stride] column sums of the chunk in flight: the cache's columns, then the chunk's; fixed point
                             // (of a drafted path: fp32 in the low words); zero between calls
   float* pf_snew;           // [U][max_chunk] accumulated S of the chunk's tokens
   int* pf_flag;             // [U][cap + max_chunk] freed slots / dead chunk tokens, then destinations
@@ -71,6 +71,10 @@ struct Params {
                             // chunk's own) turned to their ranks, split into two bf16 parts
   uint16_t* pf_qrot;        // [hi, lo][B][max_chunk][H][D] bf16: the chunk's queries, likewise
 };
+// The column accumulators of a unit: the cache's columns, then the chunk's (or drafted path's), either part rounded up.
+constexpr int COLSUM_TILE = 128;
+__host__ __device__ inline int colsum_part(int columns) { return (columns + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE; }
+__host__ __device__ inline int colsum_stride(const Params& p) { return colsum_part(p.cap) + colsum_part(p.max_chunk); }
 constexpr int PROMPT_MAX_SPLITS = 64;
 constexpr int DECODE_MAX_SPLITS = 64;    // slices of a unit the decode step's merge is laid out for
 

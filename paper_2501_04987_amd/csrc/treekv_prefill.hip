@@ -522,9 +522,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 64 && !ROPE ? 4 : 2) void prefill_
   for (int d = 0; d < DB; ++d) { o0[d] = f32x4_t{0.f, 0.f, 0.f, 0.f}; o1[d] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
 
   // the unit's column-sum accumulators: [cache columns rounded up to a tile | chunk columns]
-  const int cap_cols = (p.cap + AT_COLS - 1) / AT_COLS * AT_COLS;
-  const int cs_stride = cap_cols + (p.max_chunk + AT_COLS - 1) / AT_COLS * AT_COLS;
-  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * cs_stride;
+  const int cap_cols = colsum_part(p.cap);
+  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * colsum_stride(p);
   // lanes lr = 0, 4, 8, 12 leave columns 0-1, 2-3 of block 0 and 0-1, 2-3 of block 1 of their lane group's four
   float* cs_lds = sC + rg * AT_COLS + cq * 32 + (lr >> 3) * 16 + q4 * 4 + ((lr >> 2) & 1) * 2;   // + (tile & 1) * 2 * AT_COLS
   // the waves of column quarter t & 3 pass tile t's sums on (during tile t+1): thread j of the pair owns column j
@@ -1075,9 +1074,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void prefill_attend_resident_kernel(
     return lr & 1 ? c.y : c.x;
   };
   // integer adds commute exactly: the sums are the same to the bit whatever order a unit's row tiles and heads arrive in
-  const int cap_cols = (p.cap + AT_COLS - 1) / AT_COLS * AT_COLS;
-  const int cs_stride = cap_cols + (p.max_chunk + AT_COLS - 1) / AT_COLS * AT_COLS;
-  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * cs_stride;
+  const int cap_cols = colsum_part(p.cap);
+  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * colsum_stride(p);
   auto add_columns = [&](int t, float sum) {         // lanes lr % 4 < 2 hold one column each
     const int blk = wave + t * RES_WAVES;
     const bool is_cache = blk < cache_blk;
@@ -1286,9 +1284,8 @@ __global__ __launch_bounds__(F32_THREADS) void prefill_attend_f32_kernel(Params 
   const float inv = my_row < L ? 1.0f / sum : 0.f;         // rows past the chunk must not reach the column sums
 
   // ---- sweep 2: probabilities, output, column sums ----
-  const int cap_cols = (p.cap + AT_COLS - 1) / AT_COLS * AT_COLS;
-  const int cs_stride = cap_cols + (p.max_chunk + AT_COLS - 1) / AT_COLS * AT_COLS;
-  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * cs_stride;
+  const int cap_cols = colsum_part(p.cap);
+  unsigned long long* cs_acc = p.pf_colacc + (size_t)unit * colsum_stride(p);
   f32x4_t o[VX][4];                                // [x][e]: component i is dim 64 x + 16 q4 + 4 i + e of row lr
 #pragma unroll
   for (int x = 0; x < VX; ++x)
@@ -1538,9 +1535,8 @@ __global__ __launch_bounds__(RP_THREADS) void prefill_replay_kernel(Params p, in
   // Everything the kernel reads from global memory is requested here in one go (what a unit's replay costs is
   // memory round trips: its data was last touched a whole chunk ago): the bookkeeping words, the old scores and
   // the chunk's column sums of the first PRE * 1024 columns, and, for the LDS variant, the order arrays.
-  const int cap_cols = (cap + AT_COLS - 1) / AT_COLS * AT_COLS;
-  const int cs_stride = cap_cols + (p.max_chunk + AT_COLS - 1) / AT_COLS * AT_COLS;
-  unsigned long long* acc = p.pf_colacc + (size_t)unit * cs_stride;
+  const int cap_cols = colsum_part(cap);
+  unsigned long long* acc = p.pf_colacc + (size_t)unit * colsum_stride(p);
   constexpr int PRE = 3;
   const int n0 = meta[META_N], f0 = meta[META_FREE], j0 = meta[META_J], rhead0 = meta[META_RHEAD], t0 = meta[META_T];
   float s_pre[PRE];

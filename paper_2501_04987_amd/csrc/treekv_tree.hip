@@ -38,7 +38,6 @@ constexpr int TR_THREADS = 512, TR_WAVES = TR_THREADS / 64;
 constexpr int MAX_NODES = TREEKV_TREE_MAX_NODES, MAX_WORDS = MAX_NODES / 32;
 constexpr float REF_NONE = -3.0e38f;               // reference of a row that has seen nothing: below every logit, and finite, so that exp2(-inf - it) = 0
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
-constexpr int COLSUM_TILE = 128;                    // the column accumulators' two parts are rounded up to this
 
 __device__ inline f32x4_t mfma_bf16(const uint4& a, const uint4& b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -1401,9 +1400,8 @@ __global__ __launch_bounds__(TR_THREADS, ROPE ? 2 : 4) void tree_colsum_kernel(P
   constexpr float ROOM = 0x1p64f;
   const int cache_blocks = (u.columns + O::COLS - 1) / O::COLS, blocks = cache_blocks + (L + O::COLS - 1) / O::COLS;
   const int begin = (int)((long long)blocks * slice / slices), end = (int)((long long)blocks * (slice + 1) / slices);
-  const int cap_cols = (p.cap + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
-  const int cs_stride = cap_cols + (p.max_chunk + COLSUM_TILE - 1) / COLSUM_TILE * COLSUM_TILE;
-  unsigned long long* acc = p.pf_colacc + (size_t)unit * cs_stride;
+  const int cap_cols = colsum_part(p.cap);
+  unsigned long long* acc = p.pf_colacc + (size_t)unit * colsum_stride(p);
   T* sq = reinterpret_cast<T*>(tr_smem);
   auto load_keys = [&](typename O::Keys& k, int blk) __attribute__((always_inline)) {
     if (blk < cache_blocks && !ROPE) {
