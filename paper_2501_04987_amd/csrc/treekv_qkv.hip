@@ -113,7 +113,8 @@ __device__ inline int work_piece(const treekv_qkv_args& a, const float2* cs, boo
 
 // A workgroup takes ITER heads per lane group of one token (a run of its q, k and v heads), all requested before the angles are
 // formed.  ITER = 4 forms the angles once per token of 64 heads and keeps four loads in flight: 32768 tokens of 48 heads x 128
-// 164 -> 153 us, 976 tokens 8.6; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 2.9 us).
+// 164 -> 153 us; a few tokens' heads are spread over more workgroups instead (one token of 96 heads 2.9 us).  976 tokens take
+// 8.3 us for 24 MB: a workgroup's only token waits for its position, its angles in double and a barrier before it is stored.
 template <typename T, int D, int ITER, bool STREAM>
 __global__ __launch_bounds__(QKV_THREADS, 6) void qkv_kernel(treekv_qkv_args a, int chunks) {
   constexpr int LPR = D / Storage<T>::EPL, ROWS = QKV_THREADS / LPR;
@@ -174,7 +175,8 @@ int launch_qkv_d(const treekv_qkv_args& a, hipStream_t s) {
   const bool few = (long long)a.tokens * ((rows + ROWS - 1) / ROWS) <= 512;          // two workgroups a compute unit
   const int per = few ? ROWS : 4 * ROWS, chunks = (rows + per - 1) / per;
   const long long items = (long long)a.tokens * chunks, most = 1 << 20;
-  // (32768 tokens of 48 heads x 128: 145 us so, 5.6 TB/s in and out; 153 through the caches)
+  // (32768 tokens of 48 heads x 128: 145 us so on the card where it took 153 through the caches; 145-161 from card to card,
+  // 5.0 to 5.6 TB/s in and out)
   const bool stream = (size_t)a.tokens * rows * D * sizeof(T) > STREAM_BYTES;
   auto kernel = few ? qkv_kernel<T, D, 1, false> : stream ? qkv_kernel<T, D, 4, true> : qkv_kernel<T, D, 4, false>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(items < most ? items : most)), dim3(QKV_THREADS), 0, s, a, chunks);

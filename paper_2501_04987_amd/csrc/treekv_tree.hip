@@ -832,12 +832,13 @@ __device__ inline void leave_wide_sums(const f32x16_t (&o)[D / 32], float ref, f
 // attend, many rows: bf16 storage, tiles of columns shared by the workgroup's waves
 // ---------------------------------------------------------------------------------------------
 // The kernel above reads every row of K and V once per 32 rows.  Here a workgroup owns 128 rows: RG groups of 32 x two waves
-// that take one half of a tile's 64 columns each.  Bound by instruction issue: 64 nodes of 8 groups of 4, batch 16, 4096 slots
-// 145-150 us, 0.47 PFLOP/s of the formula's operations and, P being three parts, 0.94 of matrix instructions.  Tiles come by
-// asynchronous copies into LDS, row-major as they lie in memory with the 16-byte pieces of a row swizzled, so that the operand reads (16
-// bytes of a row for K, the transposing read for V) spread over the banks.  v_mfma_f32_32x32x16_bf16: a wave's vector
-// instructions issue beside it, while a 16x16x32 holds them up (256 rows into 4096 slots 149 us with those).  A lane then
-// holds 16 columns of one row.
+// that take one half of a tile's 64 columns each.  64 nodes of 8 groups of 4, batch 16, 4096 slots: 145-158 us (from card to
+// card), 0.47-0.43 PFLOP/s of the formula's operations and, P being three parts, twice that of matrix instructions.  The matrix
+// unit is busy for 53 us of it and the vector unit for some 50, mostly one after the other: both waves of a SIMD pass the same barrier
+// every tile and so are in the same phase of it.  Tiles come by asynchronous copies into LDS, row-major as they lie in memory
+// with the 16-byte pieces of a row swizzled, so that the operand reads (16 bytes of a row for K, the transposing read for V)
+// spread over the banks.  v_mfma_f32_32x32x16_bf16: a wave's vector instructions issue beside it, while a 16x16x32 holds them up
+// (256 rows into 4096 slots 149 us with those, 145 with these).  A lane then holds 16 columns of one row.
 // Iteration t forms the logits of tile t + 1 (matrix unit) beside the probabilities of tile t (vector unit) and ends with tile
 // t's product with V.  Four stages: tile t + 1 has landed, t + 2 and t + 3 are on their way, and the stage that t + 3 goes to
 // was last read in iteration t - 1, before the barrier.
@@ -1055,8 +1056,8 @@ __global__ __launch_bounds__(TR_THREADS, 2) void tree_attend_tiled_kernel(Args p
 // row is scaled by a power of two so that its largest element is near 2^13, and the scales go back on with the softmax's.
 // The next tile is on its way while one is worked on, keys and angles to registers, V to the other of its two stages; two
 // workgroups share a compute unit and fill each other's waits at the two barriers of a tile.  13 nodes of 8 groups of 4, batch
-// 8, 2048 slots: 42.5 us with the merge, of which some 15 do not grow with the
-// cache (order arrays, first angles, the queries' cut, partial results); a tile more costs 6 us on every unit.
+// 8, 2048 slots: 42.5 us with the merge, of which some 15 do not grow with the cache (order arrays, first angles, the queries'
+// cut, partial results); a tile more costs 6 us on every unit.  The vector unit is busy for some 14 us of it, the matrix unit for 5.
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 constexpr int TURN_THREADS = 256, TURN_ROWS = 64;
@@ -1132,8 +1133,9 @@ __global__ __launch_bounds__(TURN_THREADS, 2) void tree_attend_turned_kernel(Arg
   const char* Kn = (const char*)p.k + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
   const char* Vn = (const char*)p.v + ((size_t)b * p.n * p.Hkv + kvh) * ROWB;
 
-  // this thread's part of a tile of keys: row t_row, pieces 4 x + l % 4 (four lanes take 64 bytes of a row at once).  Its wave copies the same 16 rows of V: copy x
-  // fills tile rows 16 wave + x * RPC + lane / PARTS, a lane taking the piece whose place its own is.
+  // this thread's part of a tile of keys: row t_row, pieces 4 x + l % 4 (four lanes take 64 bytes of a row at once).  Its wave
+  // copies the same 16 rows of V: copy x fills tile rows 16 wave + x * RPC + lane / PARTS, a lane taking the piece whose place
+  // its own is.
   constexpr int RPC = 64 / PARTS, CPW = 16 / RPC;
   const int t_row = tid >> 2;
   uint4 raw_k[PER];
@@ -1513,6 +1515,15 @@ int block_cols(const Params& p) { return p.dtype == TREEKV_BF16 ? 32 : 16; }
 // Positions re-assigned, bf16: 16 likewise, else the 64 rows for which the keys are turned once (two workgroups a compute unit):
 //   64 x 4, 2048  16/4 27.6, 64/8 39.1;   256 x 16  16/1 77, 64/2 103;   64 x 30  16/2 38.0, 64/8 41.1;   128 x 30  16/1 59.7, 64/4 60.1
 //   8 x 104  16/4 24.4, 64/17 30.2;   16 x 52  16/4 24.7, 64/17 31.7;   32 x 52  16/2 36.6, 64/16 35.2;   64 x 52  16/1 57.7, 64/8 45.0
+//   x 64: 64 x 4  16/4 18.1, 64/8 24.9;   8 x 104  16/4 16.3, 64/32 22.2;   32 x 52  16/2 23.4, 64/16 22.8;   64 x 52  16/1 32.8, 64/8 27.5
+//   128 x 30  16/1 33.1, 64/4 37.1;   256 x 16  16/1 37.9, 64/2 59.6;   256 x 48  16/1 102, 64/2 64.4;   32 x 160, 1024  16/1 35.7, 64/5 23.8
+// fp32 storage has 16 and 32 rows and the same rule, which takes the better of the two or one within 7 % of it, but for 16 x 256 and
+// 256 x 48 rows, where 32 rows are up to 15 % slower.  Positions as they are, then re-assigned in brackets:
+//   8 x 16, 2048  16/17 14.6, 32/17 17.4 (16.4, 20.0);   8 x 104  16/4 22.9, 32/8 24.0 (28.3, 27.4)
+//   64 x 16  16/4 28.6, 32/4 37.6 (35.2, 43.1);   64 x 52  16/1 57.1, 32/2 61.1 (76.9, 65.8);   256 x 16  16/1 95, 32/1 107 (109, 136)
+//   128 x 60, 1024  16/1 63.9, 32/1 58.8 (85.9, 62.9);   16 x 256  16/1 33.6, 32/2 38.5 (42.5, 39.6);   256 x 48  16/1 100, 32/1 111 (135, 128)
+//   x 64: 64 x 16, 2048  16/4 18.4, 32/4 20.9 (22.4, 26.7);   64 x 52  16/1 31.5, 32/2 29.0 (40.6, 38.0)
+//   128 x 60, 1024  16/1 29.6, 32/1 26.5 (39.7, 34.9);   16 x 256  16/1 18.2, 32/2 20.4 (24.3, 23.9);   256 x 48  16/1 51.7, 32/1 52.7 (65.1, 72.7)
 Shape attend_shape(const Params& p, int n) {
   const int rows = n * p.G, tiles16 = (rows + 15) / 16, tiles32 = (rows + 31) / 32, chip = 256, cols = block_cols(p);
   Shape s;
