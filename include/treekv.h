@@ -385,6 +385,112 @@ typedef struct treekv_qkv_args {
 } treekv_qkv_args;
 int treekv_qkv_prepare(const treekv_qkv_args* args, void* stream);
 
+/*
+ * A paged cache: keys and values of whole sequences, uncompressed or cut by accumulated weight, for what runs beside the
+ * contexts above: prompts before they are compressed, layers that are not, other evictions to compare with.  Stateless:
+ * the caller owns all memory and describes it by a treekv_paged_cache; the calls only enqueue work, read lengths and pages
+ * on the device and can be captured.
+ *
+ * Sequence b holds lens[b] tokens in slots 0 .. lens[b]-1; slot s is row s % page_size of page table[b][s / page_size].
+ * An entry of the table outside 0 .. pages-1 is a page that has been given up (or not yet given): it is never touched, its
+ * tokens are attended by nobody.  Several sequences may share pages that are only read; a page that a call writes (append,
+ * evict) must belong to one place of one sequence.
+ *
+ * A call's new tokens are packed: rows starts[b] .. starts[b+1]-1 belong to sequence b (starts [batch + 1] int32, device,
+ * ascending), any number of them, also none.  lens counts them already: they are the sequence's last tokens.
+ * status [batch] int32 (device, may be NULL): TREEKV_OK or TREEKV_EINVAL per sequence, the latter where lens[b] is not within
+ * 0 .. table_width * page_size or smaller than its new tokens, or starts are not ascending within 0 .. tokens (or give a
+ * sequence more than `longest` rows).  Such a sequence is left as it is, its rows of the outputs too; so are rows that belong
+ * to no sequence.
+ */
+typedef struct treekv_paged_cache {
+  void *k, *v;             /* [pages, Hkv, page_size, d] storage dtype, 16-byte aligned                      */
+  const int32_t* table;    /* [batch, table_width]                                                         */
+  int32_t* lens;           /* [batch]                                                                      */
+  float* weights;          /* [batch, Hkv, table_width * page_size] attention weight each token has gathered */
+  int32_t* positions;      /* the same shape: the tokens' positions in their streams.  Both NULL: not kept  */
+  int32_t pages, page_size, table_width, batch, q_heads, kv_heads, head_dim, dtype;
+  float softmax_scale;     /* multiplies q.k; 0 selects 1/sqrt(head_dim)                                    */
+} treekv_paged_cache;
+
+/*
+ * treekv_paged_append - the new tokens' keys and values go into their slots; their weights become 0.
+ *   k, v [tokens, Hkv, d] storage dtype, 16-byte aligned: the heads of a token contiguous, tokens *_stride elements apart
+ *   positions [tokens] int32 (device): exactly if the cache keeps them
+ * Errors: TREEKV_EINVAL; TREEKV_EUNSUPPORTED for d other than 64 or 128, a page_size that is not 16, 32, 64, 128 or 256, more
+ * than 2^30 slots a sequence, 2^20 (sequence, KV head) pairs, 65536 query heads or 2^27 tokens.
+ */
+int treekv_paged_append(const treekv_paged_cache* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                        const int32_t* starts, int tokens, const int32_t* positions, int32_t* status, void* stream);
+
+/* Device memory treekv_paged_attend needs for `tokens` rows, `longest` at most of one sequence; 0 if it needs none (or the
+ * arguments are not accepted).  It holds nothing between calls: one piece serves all calls that do not overlap. */
+size_t treekv_paged_attend_scratch_bytes(const treekv_paged_cache* cache, int tokens, int longest, int weigh);
+
+/*
+ * treekv_paged_attend - o = SoftMax(q K^T * scale) V of every new token over its sequence's tokens up to itself.
+ *   q   [tokens, H, d] storage dtype, tokens q_stride elements apart, 16-byte aligned
+ *   out [tokens, H, d] storage dtype; lse [tokens, H] float32 (may be NULL): log of the sum of exp(q k * scale)
+ *   weigh  not 0: the probabilities, of all new tokens and of the G query heads of a KV head, are added to the weights of
+ *          the tokens attended (a probability that is a NaN adds nothing); the cache must keep them
+ *   scratch 16-byte aligned, at least treekv_paged_attend_scratch_bytes (NULL if that is 0)
+ * A token with nothing to attend (all of its pages given up) gets 0, its lse is minus infinity.  What a token does not attend
+ * has no part in its results, whatever it holds, infinities and NaNs too.  Identical calls repeat bit for bit.
+ * Errors: as treekv_paged_append, and TREEKV_EINVAL unless 1 <= longest <= tokens and for scratch that is too small;
+ * TREEKV_EUNSUPPORTED for batch * longest * H beyond 2^28 and, with `weigh`, more than 2^30 weights.
+ */
+int treekv_paged_attend(const treekv_paged_cache* cache, const void* q, int64_t q_stride, const int32_t* starts, int tokens,
+                        int longest, void* out, float* lse, int weigh, void* scratch, size_t scratch_bytes, int32_t* status,
+                        void* stream);
+
+/* Device memory treekv_paged_evict needs, likewise. */
+size_t treekv_paged_evict_scratch_bytes(const treekv_paged_cache* cache);
+
+/*
+ * treekv_paged_evict - sequences with more than `budget` tokens are cut to that many, each KV head by itself: first the
+ * tokens at positions below n_sink and those at the last n_recent positions (above the sequence's largest minus n_recent)
+ * are kept, then those with the largest weights (a NaN counts as minus infinity); of equals the one in the lower slot.  Kept
+ * tokens in slots behind the budget take the slots below it that have become free, both in slot order; the others stay
+ * where they are.  lens becomes at most budget; pages behind it are the caller's again.
+ *   status as above; TREEKV_EINVAL also where one of the sequence's pages has been given up.
+ * Errors: TREEKV_EINVAL unless budget >= 1, n_sink, n_recent >= 0, n_sink + n_recent <= budget, for a cache without weights
+ * and positions and for scratch that is too small; TREEKV_EUNSUPPORTED as above.
+ */
+int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, int n_recent, void* scratch,
+                       size_t scratch_bytes, int32_t* status, void* stream);
+
+/*
+ * treekv_tree_verify - which of a drafted tree's tokens are accepted, between treekv_tree_attend and treekv_tree_commit (or,
+ * for a chain, after treekv_paged_attend).  Row 0 of target and draft is the distribution after the last cached token, row
+ * i + 1 the one after node i.  From the last cached token on, the children of the last accepted token are tried in the order
+ * of their nodes; the first accepted one is the next token of the path.  With P the target's and Q the drafter's distribution
+ * there (whatever is not above 0, NaNs too, counts as 0):
+ *   draft given: the children were drawn from Q, independently.  Child x is accepted if u * Q(x) < P(x); else
+ *                P := max(P - Q, 0) / its sum (unless that is 0) and the next child is tried.
+ *   draft NULL:  the children were picked without chance, all different.  Child x is accepted if u * (1 - the sum of P of the
+ *                siblings before it) < P(x); else x leaves P.
+ * The token that follows the path is drawn from what P has become: the smallest x with P(x) > 0 and
+ * sum of P up to x > u * sum of P; from the target's row if P is 0; -1 if that is 0 too.  Worked out in double.
+ *   target, draft [batch, n + 1, vocab] dtype, 16-byte aligned;  tokens, parents [batch, n] int32 (parents as for
+ *   treekv_tree_attend; a token outside 0 .. vocab-1 is passed over, its node an absent one)
+ *   uniforms [batch, n + 1] float32 in [0, 1): u of node i at i, u of the token that follows at n
+ *   path [batch, n] int32: the accepted nodes, then -1;  path_len, next_token [batch] int32
+ *   scratch 16-byte aligned, at least treekv_tree_verify_scratch_bytes (NULL if that is 0)
+ * Errors: TREEKV_EINVAL unless batch >= 1, 1 <= n <= TREEKV_TREE_MAX_NODES, vocab >= 1, for null or misaligned pointers and
+ * for scratch that is too small; TREEKV_EUNSUPPORTED for a vocab beyond 2^24.
+ */
+typedef struct treekv_verify_args {
+  const void *target, *draft;
+  const int32_t *tokens, *parents;
+  const float* uniforms;
+  int32_t *path, *path_len, *next_token;
+  void* scratch;
+  size_t scratch_bytes;
+  int32_t batch, n, vocab, dtype;
+} treekv_verify_args;
+size_t treekv_tree_verify_scratch_bytes(int batch, int n, int vocab);
+int treekv_tree_verify(const treekv_verify_args* args, void* stream);
+
 /* Static description of a status code. */
 const char* treekv_strerror(int status);
 

@@ -36,6 +36,8 @@ EXPORTS = [
     "treekv_scores", "treekv_state_bytes", "treekv_get_state_layout", "treekv_export_state", "treekv_import_state",
     "treekv_gather_kv", "treekv_wavelet_components", "treekv_strerror", "treekv_last_hip_error",
     "treekv_tree_scratch_bytes", "treekv_tree_attend", "treekv_tree_commit", "treekv_fork", "treekv_qkv_prepare",
+    "treekv_paged_append", "treekv_paged_attend_scratch_bytes", "treekv_paged_attend", "treekv_paged_evict_scratch_bytes",
+    "treekv_paged_evict", "treekv_tree_verify_scratch_bytes", "treekv_tree_verify",
 ]
 PROBE_EXPORTS = ["treekv_probe_read", "treekv_probe_copy", "treekv_probe_mfma"]       # include/treekv_probe.h
 
@@ -58,6 +60,17 @@ class treekv_qkv_args(C.Structure):
     _fields_ += [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
     _fields_ += [(n, C.c_int32) for n in ("tokens", "q_heads", "kv_heads", "head_dim", "dtype", "rotary_dim", "flags")]
     _fields_ += [("eps", C.c_float)]
+
+
+class treekv_paged_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "lens", "weights", "positions")]
+    _fields_ += [(n, C.c_int32) for n in ("pages", "page_size", "table_width", "batch", "q_heads", "kv_heads", "head_dim", "dtype")]
+    _fields_ += [("softmax_scale", C.c_float)]
+
+
+class treekv_verify_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("target", "draft", "tokens", "parents", "uniforms", "path", "path_len", "next_token", "scratch")]
+    _fields_ += [("scratch_bytes", C.c_size_t)] + [(n, C.c_int32) for n in ("batch", "n", "vocab", "dtype")]
 
 
 _lib = None
@@ -102,6 +115,16 @@ def load() -> C.CDLL:
     lib.treekv_tree_commit.argtypes = [vp, vp, vp, vp, i32p, vp, C.c_int, i32p, i32p, C.c_int, i32p, i32p, i32p, i32p, vp]
     lib.treekv_fork.argtypes = [vp, vp, vp, vp, C.c_int, vp]
     lib.treekv_qkv_prepare.argtypes = [vp, vp]
+    lib.treekv_paged_append.argtypes = [vp, vp, vp, C.c_int64, C.c_int64, i32p, C.c_int, i32p, i32p, vp]
+    lib.treekv_paged_attend_scratch_bytes.argtypes = [vp, C.c_int, C.c_int, C.c_int]
+    lib.treekv_paged_attend_scratch_bytes.restype = C.c_size_t
+    lib.treekv_paged_attend.argtypes = [vp, vp, C.c_int64, i32p, C.c_int, C.c_int, vp, vp, C.c_int, vp, C.c_size_t, i32p, vp]
+    lib.treekv_paged_evict_scratch_bytes.argtypes = [vp]
+    lib.treekv_paged_evict_scratch_bytes.restype = C.c_size_t
+    lib.treekv_paged_evict.argtypes = [vp, C.c_int, C.c_int, C.c_int, vp, C.c_size_t, i32p, vp]
+    lib.treekv_tree_verify_scratch_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+    lib.treekv_tree_verify_scratch_bytes.restype = C.c_size_t
+    lib.treekv_tree_verify.argtypes = [vp, vp]
     lib.treekv_probe_read.argtypes = [vp, C.c_size_t, C.c_int, C.c_int, vp, vp]
     lib.treekv_probe_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.treekv_probe_mfma.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), vp]
@@ -253,6 +276,189 @@ def qkv_prepare(q, k=None, v=None, *, q_weight=None, k_weight=None, eps: float =
     if rc != TREEKV_OK:
         raise TreeKVError(rc, "treekv_qkv_prepare")
     return oq, ok, ov
+
+
+_VERIFY = struct.Struct("9PN4i")                # treekv_verify_args
+
+
+def _call_on(device, index: int, what: str, *args):
+    """The stateless ABI call `what` on the current stream of GPU `index`, with that GPU current."""
+    import torch
+
+    lib = _lib or load()
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            rc = getattr(lib, what)(*args, _raw_stream(device))
+    else:
+        rc = getattr(lib, what)(*args, _raw_stream(device))
+    if rc != TREEKV_OK:
+        raise TreeKVError(rc, what)
+
+
+def _scratch_at(scratch, index: int):
+    if scratch is None:
+        return 0, 0
+    if scratch.get_device() != index or not scratch.is_contiguous():
+        raise ValueError(f"scratch: contiguous memory on device {index} is wanted")
+    return scratch.data_ptr(), scratch.nbytes
+
+
+def tree_verify_scratch(target, draft=None):
+    """What tree_verify takes as `scratch` for these rows (None where it needs none)."""
+    import torch
+
+    need = (_lib or load()).treekv_tree_verify_scratch_bytes(target.shape[0], target.shape[1] - 1, target.shape[2])
+    return torch.empty(need, dtype=torch.uint8, device=target.device) if need else None
+
+
+def tree_verify(target, tokens, parents, uniforms, path, path_len, next_token, *, draft=None, scratch=None):
+    """treekv_tree_verify on torch tensors: `target` and `draft` [batch, nodes + 1, vocab] probabilities, bf16 or float32 (row 0
+    after the last cached token, row i + 1 after node i; `draft` None: the drafter picked its tokens without chance), `tokens`
+    and `parents` [batch, nodes] int32, `uniforms` [batch, nodes + 1] float32 -> `path` [batch, nodes] (accepted nodes, then -1),
+    `path_len` and `next_token` [batch], int32.  `path` and `path_len` are what TreeKV.tree_commit takes."""
+    import torch
+
+    batch, rows, vocab = target.shape
+    n, dtype, index, i32 = rows - 1, target.dtype, target.get_device(), torch.int32
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError(f"bf16 or float32 is wanted, not {dtype}")
+    _want(target, "target", dtype, (batch, rows, vocab), index)
+    if draft is not None:
+        _want(draft, "draft", dtype, (batch, rows, vocab), index)
+    for x, name in ((tokens, "tokens"), (parents, "parents"), (path, "path")):
+        _want(x, name, i32, (batch, n), index)
+    for x, name in ((path_len, "path_len"), (next_token, "next_token")):
+        _want(x, name, i32, (batch,), index)
+    _want(uniforms, "uniforms", torch.float32, (batch, rows), index)
+    if scratch is None:
+        scratch = tree_verify_scratch(target, draft)
+    args = _VERIFY.pack(target.data_ptr(), 0 if draft is None else draft.data_ptr(), tokens.data_ptr(), parents.data_ptr(),
+                        uniforms.data_ptr(), path.data_ptr(), path_len.data_ptr(), next_token.data_ptr(), *_scratch_at(scratch, index),
+                        batch, n, vocab, TREEKV_F32 if dtype is torch.float32 else TREEKV_BF16)
+    _call_on(target.device, index, "treekv_tree_verify", args)
+
+
+class PagedKV:
+    """A paged cache of one attention layer on the GPU (treekv_paged_cache) and the calls on it.
+
+    `k`, `v` [pages, kv_heads, page_size, head_dim]; `table` [batch, table_width] int32, -1 where no page has been given; `lens`
+    [batch] int32; `weights` (float32) and `positions` (int32) [batch, kv_heads, table_width * page_size] if `tracked`.  The pool
+    and the tables may be given (layers share `table` and `lens`, caches a pool).  Their contents are the caller's: hand out
+    pages in `table`, set `lens` to count a step's new tokens before `append` and `attend`."""
+
+    def __init__(self, pages: int, page_size: int, heads: int, head_dim: int, *, kv_heads: int | None = None, batch: int = 1,
+                 table_width: int, dtype: str = "bf16", softmax_scale: float = 0.0, tracked: bool = True, device="cuda",
+                 k=None, v=None, table=None, lens=None):
+        import torch
+
+        load()
+        kv_heads = kv_heads or heads
+        self.storage_dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+        device = torch.device(device)
+        pool, track = (pages, kv_heads, page_size, head_dim), (batch, kv_heads, table_width * page_size)
+        new = lambda shape, t, value: torch.full(shape, value, dtype=t, device=device)  # noqa: E731
+        self._k = new(pool, self.storage_dtype, 0) if k is None else k
+        self._v = new(pool, self.storage_dtype, 0) if v is None else v
+        self._table = new((batch, table_width), torch.int32, -1) if table is None else table
+        self._lens = new((batch,), torch.int32, 0) if lens is None else lens
+        self._weights = new(track, torch.float32, 0) if tracked else None
+        self._positions = new(track, torch.int32, -1) if tracked else None
+        self.device, self._index = self._k.device, self._k.get_device()
+        _want(self._k, "k", self.storage_dtype, pool, self._index)
+        _want(self._v, "v", self.storage_dtype, pool, self._index)
+        _want(self._table, "table", torch.int32, (batch, table_width), self._index)
+        _want(self._lens, "lens", torch.int32, (batch,), self._index)
+        self._dims = (batch, heads, kv_heads, head_dim)
+        self.cache = treekv_paged_cache(_ptr(self._k), _ptr(self._v), _ptr(self._table), _ptr(self._lens), _ptr(self._weights),
+                                        _ptr(self._positions), pages, page_size, table_width, batch, heads, kv_heads, head_dim,
+                                        TREEKV_F32 if dtype == "f32" else TREEKV_BF16, softmax_scale)
+        self._at = C.addressof(self.cache)
+
+    def _own(name):                                    # noqa: N805  (the memory the calls were given; its values may change)
+        def put(self, value):
+            if value is not getattr(self, name):
+                raise AttributeError(f"{name[1:]}: change its values in place")
+        return property(lambda self: getattr(self, name), put)
+
+    k, v, table, lens, weights, positions = map(_own, ("_k", "_v", "_table", "_lens", "_weights", "_positions"))
+    del _own
+
+    def _rows(self, x, name, heads):
+        """Distance between the tokens of an input [tokens, heads, d]."""
+        if x.shape[1] != heads:
+            raise ValueError(f"{name}: {heads} heads are wanted, not {x.shape[1]}")
+        return _rows_in(x, name, self.storage_dtype, x.shape[0], self._dims[3], self._index)[1]
+
+    def _batch_ints(self, starts, status):
+        import torch
+
+        _want(starts, "starts", torch.int32, (self._dims[0] + 1,), self._index)
+        if status is not None:
+            _want(status, "status", torch.int32, (self._dims[0],), self._index)
+            return status.data_ptr()
+        return 0
+
+    def append(self, k, v, starts, positions=None, status=None):
+        """The new tokens' rows [tokens, kv_heads, head_dim] (tokens any distance apart) into the pages of their sequences."""
+        import torch
+
+        heads = self._dims[2]
+        k_far, v_far = self._rows(k, "k", heads), self._rows(v, "v", heads)
+        if k.shape[0] != v.shape[0]:
+            raise ValueError("k and v have the same tokens")
+        status_at = self._batch_ints(starts, status)
+        if positions is not None:
+            _want(positions, "positions", torch.int32, (k.shape[0],), self._index)
+        _call_on(self.device, self._index, "treekv_paged_append", self._at, k.data_ptr(), v.data_ptr(), k_far, v_far,
+                 starts.data_ptr(), k.shape[0], _ptr(positions), status_at)
+
+    def new_attend_scratch(self, tokens: int, longest: int, weigh: bool = False):
+        """What `attend` takes as `scratch` (None where it needs none)."""
+        import torch
+
+        need = (_lib or load()).treekv_paged_attend_scratch_bytes(self._at, int(tokens), int(longest), int(weigh))
+        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+
+    def attend(self, q, starts, longest: int, out=None, lse=None, *, weigh: bool = False, scratch=None, status=None):
+        """Causal attention of the new tokens q [tokens, heads, head_dim], `longest` at most of one sequence, over the pages;
+        `weigh` adds the probabilities to the weights of what they attend.  Returns out [tokens, heads, head_dim]."""
+        import torch
+
+        batch, heads, _, d = self._dims
+        far, tokens = self._rows(q, "q", heads), q.shape[0]
+        status_at = self._batch_ints(starts, status)
+        if out is None:
+            out = torch.empty(tokens, heads, d, dtype=self.storage_dtype, device=self.device)
+        _want(out, "out", self.storage_dtype, (tokens, heads, d), self._index)
+        lse_at = 0
+        if lse is not None:
+            _want(lse, "lse", torch.float32, (tokens, heads), self._index)
+            lse_at = lse.data_ptr()
+        if scratch is None:
+            scratch = self.new_attend_scratch(tokens, longest, weigh)
+        _call_on(self.device, self._index, "treekv_paged_attend", self._at, q.data_ptr(), far, starts.data_ptr(), tokens, int(longest),
+                 out.data_ptr(), lse_at, int(weigh), *_scratch_at(scratch, self._index), status_at)
+        return out
+
+    def new_evict_scratch(self):
+        """What `evict` takes as `scratch`."""
+        import torch
+
+        need = (_lib or load()).treekv_paged_evict_scratch_bytes(self._at)
+        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+
+    def evict(self, budget: int, n_sink: int, n_recent: int, *, scratch=None, status=None):
+        """Sequences with more than `budget` tokens keep the first, the last and the heaviest of them."""
+        import torch
+
+        status_at = 0
+        if status is not None:
+            _want(status, "status", torch.int32, (self._dims[0],), self._index)
+            status_at = status.data_ptr()
+        if scratch is None:
+            scratch = self.new_evict_scratch()
+        _call_on(self.device, self._index, "treekv_paged_evict", self._at, int(budget), int(n_sink), int(n_recent),
+                 *_scratch_at(scratch, self._index), status_at)
 
 
 class TreeKV:

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtreekv.so")
 SOURCES = ["treekv_host.hip", "treekv_decode.hip", "treekv_prefill.hip", "treekv_prompt.hip", "treekv_wavelet.hip",
-           "treekv_speculate.hip", "treekv_tree.hip", "treekv_fork.hip", "treekv_qkv.hip", "treekv_probe.hip"]
+           "treekv_speculate.hip", "treekv_tree.hip", "treekv_fork.hip", "treekv_qkv.hip", "treekv_serve.hip",
+           "treekv_paged.hip", "treekv_evict.hip", "treekv_verify.hip", "treekv_probe.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

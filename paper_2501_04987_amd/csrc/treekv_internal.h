@@ -128,6 +128,17 @@ int launch_tree_replay(const Params& p, const Tree& t, int32_t* retained, int32_
 int launch_fork(const Params& to, const Params& from, const int32_t* src, const int32_t* dst, int count, hipStream_t s);
 int launch_qkv(const treekv_qkv_args& a, hipStream_t s);
 
+// The paged cache and the verification of drafts (treekv_serve.hip has checked the arguments).
+int launch_paged_append(const treekv_paged_cache& c, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                        const int32_t* starts, int tokens, const int32_t* positions, int32_t* status, hipStream_t s);
+size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int longest, int weigh);
+int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
+                        void* out, float* lse, int weigh, void* scratch, int32_t* status, hipStream_t s);
+size_t paged_evict_scratch_bytes(const treekv_paged_cache& c);
+int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int n_recent, void* scratch, int32_t* status, hipStream_t s);
+size_t verify_scratch_bytes(int batch, int n, int vocab);
+int launch_verify(const treekv_verify_args& a, hipStream_t s);
+
 }  // namespace tkv
 
 struct treekv_ctx {
