@@ -407,7 +407,8 @@ typedef struct treekv_paged_cache {
   void *k, *v;             /* [pages, Hkv, page_size, d] storage dtype, 16-byte aligned                      */
   const int32_t* table;    /* [batch, table_width]                                                         */
   int32_t* lens;           /* [batch]                                                                      */
-  float* weights;          /* [batch, Hkv, table_width * page_size] attention weight each token has gathered */
+  float* weights;          /* [batch, Hkv, table_width * page_size] attention weight each token has gathered,
+                              16-byte aligned                                                              */
   int32_t* positions;      /* the same shape: the tokens' positions in their streams.  Both NULL: not kept  */
   int32_t pages, page_size, table_width, batch, q_heads, kv_heads, head_dim, dtype;
   float softmax_scale;     /* multiplies q.k; 0 selects 1/sqrt(head_dim)                                    */

@@ -93,7 +93,8 @@ struct Attend {
   char* out;
   float *lse, *part;
   int32_t* status;
-  int tokens, longest, tiles, shares;        // row tiles of the longest sequence; shares the columns are cut into
+  float* logits;                             // few rows and weights: scaled logits, [sequence][KV head][row][cap]
+  int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
   float scale_log2e;
 };
 
@@ -175,7 +176,8 @@ __device__ inline void finish_row(const Attend& a, const Seq& s, int h, int row,
 }
 
 // grid: shares of the columns x KV heads x row tiles.  RB: blocks of 16 rows.
-template <typename T, int D, int RB>
+// WEIGH (16 rows only): the logits are kept for the weights.
+template <typename T, int D, int RB, bool WEIGH>
 __global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Attend a) {
   using O = Ops<T, D>;
   constexpr int ROWS = RB * 16, DPL = O::DPL, OR = D + 4, BK = O::COLS / 16, COLS = O::COLS, ROWB = D * (int)sizeof(T);
@@ -252,6 +254,14 @@ __global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Att
         if (!whole && (!there[j * BK / O::NCOL] || c0 + O::col(q4, j) >= min(see[rb], hi))) y = -INFINITY;
         mx = fmaxf(mx, y);
       }
+      if constexpr (WEIGH) {
+        if (r < rows) {
+          float* keep = a.logits + (((size_t)sh.b * p.Hkv + h) * a.rows + r) * p.cap + c0 + 4 * q4;
+#pragma unroll
+          for (int z = 0; z < BK; ++z)
+            if (c0 + 16 * z < hi) *reinterpret_cast<f32x4_t*>(keep + 16 * z) = x.x[z];
+        }
+      }
       if (__any(mx > ref[rb] + 8.f)) {
         mx = row_max(mx);
         const float to = mx > ref[rb] + 8.f ? mx : ref[rb], f = fast_exp2(ref[rb] - to);
@@ -310,32 +320,24 @@ __global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Att
       L = fmaf(ml.y, g, L);
       f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
     }
-    if (sh.count > 1) {
-      float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
-      *reinterpret_cast<float4*>(part + c) = f;
-      if (c == 0) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
-    } else {
-      finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
-    }
+    float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
+    if (c == 0 && (WEIGH || sh.count > 1)) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
+    if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = f;
+    else finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
   }
 }
 
-// Shares of a sequence added.  grid: sequences x KV heads x row tiles.
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a) {
+// Shares of a sequence added, MR rows a workgroup.  grid: row tiles of MR x KV heads x sequences.
+template <typename T, int D, int MR>
+__device__ inline void merge_rows(const Attend& a, const Seq& s, const Share& sh, int h, int row0) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
-  const int tile = (int)(blockIdx.x % a.tiles), rest = (int)(blockIdx.x / a.tiles), h = rest % p.Hkv, b = rest / p.Hkv;
-  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  const int rows = s.n * p.G, row0 = tile * ROWS;
-  if (row0 >= rows) return;
-  Share sh;
-  if (!find_share(a, 0, b, sh) || sh.count <= 1) return;
-  for (int x = threadIdx.x; x < ROWS * (D / 4); x += PA_THREADS) {
-    const int y = x / (D / 4), c = x % (D / 4) * 4;
-    if (row0 + y >= rows) break;
-    const size_t far = (size_t)p.Hkv * a.tiles * ROWS * OR;
-    const float* part = a.part + (((size_t)sh.first * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
+  const int rows = s.n * p.G;
+  for (int x = threadIdx.x; x < MR * (D / 4); x += PA_THREADS) {
+    const int row = row0 + x / (D / 4), c = x % (D / 4) * 4;
+    if (row >= rows) break;
+    const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
+    const float* part = a.part + (((size_t)sh.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
     float M = REF_NONE, L = 0.f;
     for (int z = 0; z < sh.count; ++z) M = fmaxf(M, part[z * far + D]);
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -346,8 +348,77 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a) {
       L = fmaf(ml.y, g, L);
       f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
     }
-    finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
+    finish_row<T, D>(a, s, h, row, c, f, M, L);
   }
+}
+template <typename T, int D, int MR>
+__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles) {
+  const Pages& p = a.p;
+  const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  if (tile * MR >= s.n * p.G) return;
+  Share sh;
+  if (!find_share(a, 0, b, sh) || sh.count <= 1) return;
+  merge_rows<T, D, MR>(a, s, sh, h, tile * MR);
+}
+
+// The same where the logits of up to 16 rows have been kept: beside the merge (the first piece), each workgroup adds the rows'
+// probabilities of a piece of the columns to the weights.  The log sums it takes them by come from the shares, like the output's.
+// grid: pieces of the columns x KV heads x sequences.
+template <typename T, int D>
+__global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int pieces) {
+  constexpr int OR = D + 4;
+  __shared__ float log_sum[16];
+  const Pages& p = a.p;
+  const int piece = (int)(blockIdx.x % pieces), rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv, tid = threadIdx.x;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
+  if (rows == 0 || c0 >= s.len) return;
+  Share sh;
+  if (!find_share(a, 0, b, sh)) return;
+  const int c = c0 + 4 * tid;
+  const bool mine = c < s.len;
+  float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+  float* weights = p.weights + track_row(p, b, h) + c;
+  if (mine) w = *reinterpret_cast<const float4*>(weights);
+  if (tid < 64) {                              // four lanes a row, each with a quarter of the shares
+    const int row = tid >> 2;
+    float M = REF_NONE, L = 0.f;
+    if (row < rows) {
+      const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
+      const float* part = a.part + (((size_t)sh.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
+      for (int z = tid & 3; z < sh.count; z += 4) {
+        const float2 ml = *reinterpret_cast<const float2*>(part + z * far);
+        const float to = fmaxf(M, ml.x);
+        L = L * fast_exp2(M - to) + ml.y * fast_exp2(ml.x - to);
+        M = to;
+      }
+    }
+#pragma unroll
+    for (int x = 1; x <= 2; x <<= 1) {
+      const float M2 = __shfl_xor(M, x, 64), L2 = __shfl_xor(L, x, 64), to = fmaxf(M, M2);
+      L = L * fast_exp2(M - to) + L2 * fast_exp2(M2 - to);
+      M = to;
+    }
+    if ((tid & 3) == 0) log_sum[row] = M + log2f(L);       // (of no sum minus infinity: its logits are too, and give NaNs)
+  }
+  __syncthreads();
+  if (mine) {
+    const float* x = a.logits + ((size_t)b * p.Hkv + h) * a.rows * p.cap + c;
+    for (int row = 0; row < rows; ++row) {
+      const float4 y = *reinterpret_cast<const float4*>(x + (size_t)row * p.cap);
+      const float l = log_sum[row];
+      // (a NaN adds nothing)
+      w.x += fmaxf(fast_exp2(y.x - l), 0.f); w.y += fmaxf(fast_exp2(y.y - l), 0.f);
+      w.z += fmaxf(fast_exp2(y.z - l), 0.f); w.w += fmaxf(fast_exp2(y.w - l), 0.f);
+    }
+    if (c + 4 <= s.len) *reinterpret_cast<float4*>(weights) = w;
+    else {
+      const float z[4] = {w.x, w.y, w.z, w.w};
+      for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
+    }
+  }
+  if (piece == 0 && sh.count > 1) merge_rows<T, D, 16>(a, s, sh, h, 0);
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -406,43 +477,366 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
     }
 }
 
+// ---- many rows, bf16 -----------------------------------------------------------------------------
+// 128 rows a workgroup, 32 a wave; K and V pass through LDS in tiles of 64 columns, copied a tile ahead (one barrier a tile).
+// 32x32x16 products: S^T = K Q^T, where a lane has row l % 32 and, of each half of the tile, columns 8 (i/4) + 4 (l/32) + i % 4.
+// Those are its columns of the B operand of O^T += V^T P^T too (a sum does not ask for the order of its terms); the A operand
+// takes the same columns of a dimension out of LDS by two transposing reads.  A row's 16-byte pieces are stored under their
+// number XOR one of the row, so that the lanes of a read meet all banks.
+constexpr int TILE = 64, TILED_ROWS = 128, TILED_SUB = TILE / PA_WAVES;      // a wave copies the 16 columns of one page
+template <int D> __device__ inline int swap_k(int row) { return row & (D / 8 - 1); }
+template <int D> __device__ inline int swap_v(int row) { return (row & (D / 16 - 1)) << 1; }
+
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
+__device__ inline uint2 read_turned(const char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(lds_void_t*)p));
+}
+__device__ inline float other_half(float v) { return __shfl_xor(v, 32, 64); }
+
+// 16 rows of D / 8 pieces each from `src` (rows `far` bytes apart, or from `row_of`) into LDS at `to`.
+template <int D, class RowFn, class SwapFn>
+__device__ inline void copy_rows(unsigned to, RowFn row_of, SwapFn swap) {
+  constexpr int PIECES = D / 8, AT_ONCE = 64 / PIECES;
+  const int lane = threadIdx.x & 63, piece = lane % PIECES;
+#pragma unroll
+  for (int j = 0; j < TILED_SUB / AT_ONCE; ++j) {
+    const int row = j * AT_ONCE + lane / PIECES;
+    async_copy16(row_of(row) + ((piece ^ swap(row)) << 4), to + j * 1024);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
+  constexpr int KS = D / 16, DB = D / 32, ROWB = D * 2, HALF = TILE * ROWB, OR = D + 4;
+  extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of K, V
+  const Pages& p = a.p;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
+  if (blockIdx.x == 0 && a.status)
+    for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
+  // the tiles of a KV head and share, the longest first, on one XCD, whose L2 then has their columns
+  const int idx = (int)(blockIdx.x >> 3), group = idx / a.tiles * 8 + (int)(blockIdx.x & 7), tile = a.tiles - 1 - idx % a.tiles;
+  const int h = group % p.Hkv, w = group / p.Hkv;
+  Share sh;
+  if (!find_share(a, w, -1, sh)) return;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, sh.b);
+  const int rows = s.n * p.G, row0 = tile * TILED_ROWS;
+  if (row0 >= rows) return;
+  const int old = s.len - s.n;
+  const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + TILED_ROWS, rows) - 1) / p.G + 1;
+  const int lo = sh.index * sh.size, hi = min(lo + sh.size, end);
+  const int row = row0 + wave * 32 + r, at_row = min(row, rows - 1), token = at_row / p.G, head = h * p.G + at_row - token * p.G;
+  const int see = min(old + token + 1, hi);
+  uint4 q[KS];
+  {
+    const char* src = a.q + (s.first + token) * a.q_far + (size_t)head * ROWB + hf * 16;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) q[x] = *reinterpret_cast<const uint4*>(src + x * 32);
+  }
+  f32x16_t o[DB] = {};
+  float ref = REF_NONE, sum = 0.f;
+  const int32_t* table = p.table + (size_t)sh.b * p.width;
+  const int in_page = (1 << p.bits) - 1;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem));
+
+  // which quarters of the tile at c0 are there; their rows on the way into `stage`
+  auto request = [&](int c0, int stage) {
+    unsigned there = 0;
+    int mine = 0;
+#pragma unroll
+    for (int x = 0; x < PA_WAVES; ++x) {
+      const int c = c0 + TILED_SUB * x, page = c < hi ? table[c >> p.bits] : -1;
+      const bool ok = page >= 0 && page < p.pages;
+      there |= (unsigned)ok << x;
+      if (x == wave) mine = ok ? page : 0;
+    }
+    const size_t at = ((((size_t)mine * p.Hkv + h) << p.bits) + ((c0 + TILED_SUB * wave) & in_page)) * ROWB;
+    const unsigned to = lds0 + stage * 2 * HALF + wave * TILED_SUB * ROWB;
+    copy_rows<D>(to, [&](int x) { return p.k + at + x * ROWB; }, swap_k<D>);
+    copy_rows<D>(to + HALF, [&](int x) { return p.v + at + x * ROWB; }, swap_v<D>);
+    return there;
+  };
+
+  unsigned there = 0;
+  if (lo < hi) there = request(lo, 0);
+  int stage = 0;
+#pragma unroll 1
+  for (int c0 = lo; c0 < hi; c0 += TILE, stage ^= 1) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    const unsigned now = there;
+    if (c0 + TILE < hi) there = request(c0 + TILE, stage ^ 1);
+    char* k = pt_smem + stage * 2 * HALF;
+    char* v = k + HALF;
+    const bool whole = now == (1u << PA_WAVES) - 1 && c0 + TILE <= all_see;
+
+    f32x16_t x[2] = {};
+#pragma unroll
+    for (int y = 0; y < KS; ++y)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int kr = z * 32 + r;
+        x[z] = mfma_wide(*reinterpret_cast<const uint4*>(k + kr * ROWB + (((2 * y + hf) ^ swap_k<D>(kr)) << 4)), q[y], x[z]);
+      }
+    bool odd = false;
+    if (!whole) {
+      // rows of nobody become 0; what is not finite is taken out, and added below for the rows that attend it
+      bool mine = false;
+#pragma unroll
+      for (int y = 0; y < TILED_SUB * (D / 8) / 64; ++y) {
+        const int n = y * 64 + lane, vr = wave * TILED_SUB + n / (D / 8);
+        uint4* at = reinterpret_cast<uint4*>(v + vr * ROWB + (n % (D / 8) << 4));
+        uint4 u = *at;
+        if (!(now >> wave & 1) || c0 + vr >= hi) u = make_uint4(0, 0, 0, 0);
+        const unsigned f = finite_halves(u.x) & finite_halves(u.y) & finite_halves(u.z) & finite_halves(u.w) & 0x80008000u;
+        mine |= f != 0x80008000u;
+        *at = make_uint4(keep_finite(u.x), keep_finite(u.y), keep_finite(u.z), keep_finite(u.w));
+      }
+      odd = __syncthreads_or(mine);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[z][i] *= a.scale_log2e;
+        if (!whole) {
+          const int c = z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3);
+          if (!(now >> (c / TILED_SUB) & 1) || c0 + c >= see) x[z][i] = -INFINITY;
+        }
+        mx = fmaxf(mx, x[z][i]);
+      }
+    if (__any(mx > ref + 8.f)) {
+      mx = fmaxf(mx, other_half(mx));
+      const float to = mx > ref + 8.f ? mx : ref, f = fast_exp2(ref - to);
+      sum *= f;
+#pragma unroll
+      for (int e = 0; e < DB; ++e) o[e] *= f;
+      ref = to;
+    }
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[z][i] = fast_exp2(x[z][i] - ref);
+        sum += x[z][i];
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const uint4 pr = make_uint4(narrow2(x[z][8 * g], x[z][8 * g + 1]), narrow2(x[z][8 * g + 2], x[z][8 * g + 3]),
+                                    narrow2(x[z][8 * g + 4], x[z][8 * g + 5]), narrow2(x[z][8 * g + 6], x[z][8 * g + 7]));
+        const int vr = z * 32 + g * 16 + 4 * hf + ((lane & 15) >> 2);
+#pragma unroll
+        for (int e = 0; e < DB; ++e) {
+          // this lane's share of four rows of 16 dimensions: 8 bytes of piece 4 e + ..
+          const int piece = 4 * e + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), byte = (lane & 1) * 8;
+          const uint2 u0 = read_turned(v + vr * ROWB + ((piece ^ swap_v<D>(vr)) << 4) + byte);
+          const uint2 u1 = read_turned(v + (vr + 8) * ROWB + ((piece ^ swap_v<D>(vr + 8)) << 4) + byte);
+          o[e] = mfma_wide(make_uint4(u0.x, u0.y, u1.x, u1.y), pr, o[e]);
+        }
+      }
+    }
+    if (odd) {
+#pragma unroll 1
+      for (int c = c0; c < min(c0 + TILE, hi); ++c) {
+        if (!(now >> ((c - c0) / TILED_SUB) & 1)) continue;
+        const char* src = p.v + ((((size_t)table[c >> p.bits] * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB + hf * 8;
+#pragma unroll
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const uint2 u = *reinterpret_cast<const uint2*>(src + (32 * e + 8 * z) * 2);
+            const unsigned word[4] = {u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float bad = __uint_as_float(word[i] & ~(unsigned)((int)finite_word(word[i]) >> 31));
+              o[e][4 * z + i] += c < see ? bad : 0.f;
+            }
+          }
+      }
+    }
+  }
+  sum += other_half(sum);
+  if (row >= rows) return;
+  float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles * TILED_ROWS + row) * OR;
+  const size_t at = (size_t)(s.first + token) * p.H + head;
+  const bool any = !(sum == 0.f);
+  const float inv = any ? 1.0f / sum : 0.f;
+#pragma unroll
+  for (int e = 0; e < DB; ++e)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      const int c = 32 * e + 8 * z + 4 * hf;
+      const float4 f = make_float4(o[e][4 * z], o[e][4 * z + 1], o[e][4 * z + 2], o[e][4 * z + 3]);
+      if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = f;
+      else store4(a.out, at * D + c, any ? f : make_float4(0.f, 0.f, 0.f, 0.f), inv, uint16_t());
+    }
+  if (hf == 0) {
+    if (sh.count > 1) *reinterpret_cast<float2*>(part + D) = make_float2(ref, sum);
+    else if (a.lse) a.lse[at] = any ? (ref + log2f(sum)) * LN2 : -INFINITY;
+  }
+}
+
+// Weights of many rows: 64 columns a wave, their keys in registers; the rows' queries pass through LDS in tiles of 64.  A lane
+// has row l % 32 and adds up its columns over the rows it meets; the lanes are added at the end.  grid: column tiles x KV heads x
+// sequences.
+template <int D>
+__global__ __launch_bounds__(PA_THREADS, 2) void weigh_tiled_kernel(Attend a, int col_tiles) {
+  constexpr int KS = D / 16, ROWB = D * 2, STAGE = TILE * ROWB;
+  extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of queries
+  const Pages& p = a.p;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
+  const int idx = (int)(blockIdx.x >> 3), group = idx / col_tiles * 8 + (int)(blockIdx.x & 7), ct = idx % col_tiles;
+  const int h = group % p.Hkv, b = group / p.Hkv;
+  if (b >= p.B) return;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  const int first_col = ct * PA_WAVES * TILE, c0 = first_col + wave * TILE;
+  if (s.n == 0 || first_col >= s.len) return;
+  const int32_t* table = p.table + (size_t)b * p.width;
+  const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
+  uint4 k[2][KS];
+#pragma unroll
+  for (int z = 0; z < 2; ++z) {
+    const int c = c0 + z * 32 + r, page = c < s.len ? table[c >> p.bits] : -1;
+    const size_t at = ((((size_t)(page >= 0 && page < p.pages ? page : 0) * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB + hf * 16;
+#pragma unroll
+    for (int y = 0; y < KS; ++y) k[z][y] = *reinterpret_cast<const uint4*>(p.k + at + y * 32);
+  }
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem));
+  auto place = [&](int row, int& token) {             // of a row's query, in heads
+    row = min(row, rows - 1);
+    token = row / p.G;
+    return h * p.G + row - token * p.G;
+  };
+  auto request = [&](int row0, int stage) {
+    copy_rows<D>(lds0 + stage * STAGE + wave * TILED_SUB * ROWB, [&](int x) {
+      int token;
+      const int head = place(row0 + wave * TILED_SUB + x, token);
+      return a.q + (s.first + token) * a.q_far + (size_t)head * ROWB;
+    }, swap_k<D>);
+  };
+  auto log_sum = [&](int row) {                       // rows behind the last: exponentials of minus infinity
+    int token;
+    const int head = place(row, token);
+    const float l = a.lse[(size_t)(s.first + token) * p.H + head] * LOG2E;
+    return row < rows ? l : INFINITY;
+  };
+  f32x16_t acc[2] = {};
+  const int first = max(0, first_col - old) * p.G / TILE * TILE;
+  request(first, 0);
+  float l[2] = {log_sum(first + r), log_sum(first + 32 + r)};
+  int stage = 0;
+#pragma unroll 1
+  for (int row0 = first; row0 < rows; row0 += TILE, stage ^= 1) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    const float now[2] = {l[0], l[1]};
+    if (row0 + TILE < rows) {
+      request(row0 + TILE, stage ^ 1);
+      l[0] = log_sum(row0 + TILE + r);
+      l[1] = log_sum(row0 + TILE + 32 + r);
+    }
+    const char* q = pt_smem + stage * STAGE;
+    const bool whole = old + row0 / p.G + 1 >= c0 + TILE;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      f32x16_t x[2] = {};
+      const int qr = y * 32 + r;
+#pragma unroll
+      for (int e = 0; e < KS; ++e) {
+        const uint4 u = *reinterpret_cast<const uint4*>(q + qr * ROWB + (((2 * e + hf) ^ swap_k<D>(qr)) << 4));
+#pragma unroll
+        for (int z = 0; z < 2; ++z) x[z] = mfma_wide(k[z][e], u, x[z]);
+      }
+      const int see = old + min(row0 + qr, rows - 1) / p.G + 1 - c0;
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float e = fmaxf(fast_exp2(fmaf(x[z][i], a.scale_log2e, -now[y])), 0.f);          // (of a NaN 0)
+          if (!whole && z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3) >= see) e = 0.f;
+          acc[z][i] += e;
+        }
+    }
+  }
+  float* weights = p.weights + track_row(p, b, h);
+#pragma unroll
+  for (int z = 0; z < 2; ++z)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = group_sum<32>(acc[z][i]);
+      const int c = c0 + z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3);
+      if (r == 0 && c < s.len) {
+        const int page = table[c >> p.bits];
+        if (page >= 0 && page < p.pages) weights[c] += e;
+      }
+    }
+}
+
 // ---- launches ----------------------------------------------------------------------------------
 struct AttendShape {
   int rows, tiles, shares;                   // rows of a tile
-  size_t part, lse;                          // bytes of scratch: shares' results, log sums nobody asked for
+  bool tiled, keep;                          // many rows through LDS; logits kept for the weights
+  size_t part, logits, lse;                  // bytes of scratch: shares' results, logits, log sums nobody asked for
 };
 AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
-  const long long rows = (long long)longest * (c.q_heads / c.kv_heads);
+  const long long rows = (long long)longest * (c.q_heads / c.kv_heads), cap = (long long)c.table_width * c.page_size;
+  const long long units = (long long)c.batch * c.kv_heads;
   AttendShape s;
-  s.rows = rows <= 16 ? 16 : 32;
+  s.tiled = rows > 64 && c.dtype == TREEKV_BF16;
+  s.rows = rows <= 16 ? 16 : s.tiled ? TILED_ROWS : 32;
   s.tiles = (int)((rows + s.rows - 1) / s.rows);
-  const long long groups = (long long)c.kv_heads * s.tiles;
-  s.shares = (int)(groups >= 768 ? 1 : (768 + groups - 1) / groups);      // three workgroups a compute unit
-  const long long cap = (long long)c.table_width * c.page_size, most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
+  const long long groups = (long long)c.kv_heads * s.tiles, want = s.tiled ? 512 : 768;      // two, three workgroups a compute unit
+  const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
+  s.shares = (int)(groups >= want ? 1 : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
-  s.part = s.shares > 1 ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
-  s.lse = weigh ? align_up((size_t)tokens * c.q_heads * 4) : 0;
+  // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them
+  s.keep = weigh && rows <= 16 && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
+  s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
+  s.logits = s.keep ? align_up((size_t)units * s.rows * cap * 4) : 0;
+  s.lse = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 4) : 0;
   return s;
 }
 
 template <typename T, int D>
 int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream_t s) {
   constexpr int OR = D + 4;
-  const unsigned groups = (unsigned)(a.p.Hkv * a.tiles);
-  const unsigned grid = (unsigned)(a.shares + (a.shares > 1 ? a.p.B : a.p.B - 1)) * groups;
-  const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
-  auto kernel = sh.rows == 16 ? attend_kernel<T, D, 1> : attend_kernel<T, D, 2>;
-  if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
-  hipLaunchKernelGGL(kernel, dim3(grid), dim3(PA_THREADS), lds, s, a);
+  const Pages& p = a.p;
+  const unsigned pieces = (unsigned)(a.shares + (a.shares > 1 ? p.B : p.B - 1)), groups = pieces * p.Hkv;
+  if (sh.tiled) {
+    if constexpr (sizeof(T) == 2) {
+      const int lds = 4 * TILE * D * 2;
+      if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)attend_tiled_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return TREEKV_EHIP;
+      hipLaunchKernelGGL((attend_tiled_kernel<D>), dim3((groups + 7) / 8 * 8 * a.tiles), dim3(PA_THREADS), lds, s, a);
+    }
+  } else {
+    const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
+    auto kernel = sh.rows != 16 ? attend_kernel<T, D, 2, false> : sh.keep ? attend_kernel<T, D, 1, true> : attend_kernel<T, D, 1, false>;
+    if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
+    hipLaunchKernelGGL(kernel, dim3(groups * a.tiles), dim3(PA_THREADS), lds, s, a);
+  }
+  const unsigned units = (unsigned)(p.Hkv * p.B);
+  if (sh.keep) {
+    const int all = (p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS);
+    hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
+    return finish_launch();
+  }
   if (a.shares > 1) {
-    const unsigned all = (unsigned)a.p.B * groups;
-    if (sh.rows == 16) hipLaunchKernelGGL((merge_kernel<T, D, 16>), dim3(all), dim3(PA_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((merge_kernel<T, D, 32>), dim3(all), dim3(PA_THREADS), 0, s, a);
+    const int rows = a.longest * p.G, all = (rows + (sh.rows == 16 ? 15 : 31)) / (sh.rows == 16 ? 16 : 32);
+    if (sh.rows == 16) hipLaunchKernelGGL((merge_kernel<T, D, 16>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
+    else hipLaunchKernelGGL((merge_kernel<T, D, 32>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
   }
   if (weigh) {
-    constexpr int WIDE = PA_WAVES * 2 * Ops<T, D>::COLS;
-    const int col_tiles = (a.p.cap + WIDE - 1) / WIDE;
-    hipLaunchKernelGGL((weigh_kernel<T, D>), dim3((unsigned)col_tiles * a.p.Hkv * a.p.B), dim3(PA_THREADS), 0, s, a, col_tiles);
+    if (sh.tiled) {
+      if constexpr (sizeof(T) == 2) {
+        const int all = (p.cap + PA_WAVES * TILE - 1) / (PA_WAVES * TILE);
+        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3((units + 7) / 8 * 8 * all), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);
+      }
+    } else {
+      constexpr int WIDE = PA_WAVES * 2 * Ops<T, D>::COLS;
+      const int all = (p.cap + WIDE - 1) / WIDE;
+      hipLaunchKernelGGL((weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
+    }
   }
   return finish_launch();
 }
@@ -464,7 +858,7 @@ int launch_paged_append(const treekv_paged_cache& c, const void* k, const void* 
 
 size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const AttendShape s = attend_shape(c, tokens, longest, weigh);
-  return s.part + s.lse;
+  return s.part + s.logits + s.lse;
 }
 
 int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
@@ -477,9 +871,10 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.q_far = q_stride * (c.dtype == TREEKV_F32 ? 4 : 2);
   a.out = (char*)out;
   a.part = (float*)scratch;
-  a.lse = !lse && weigh ? (float*)((char*)scratch + sh.part) : lse;
+  a.logits = (float*)((char*)scratch + sh.part);
+  a.lse = !lse && sh.lse ? (float*)((char*)scratch + sh.part + sh.logits) : lse;
   a.status = status;
-  a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares;
+  a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
   if (c.dtype == TREEKV_F32) return c.head_dim == 128 ? launch_attend_d<float, 128>(a, sh, weigh, s) : launch_attend_d<float, 64>(a, sh, weigh, s);
   return c.head_dim == 128 ? launch_attend_d<uint16_t, 128>(a, sh, weigh, s) : launch_attend_d<uint16_t, 64>(a, sh, weigh, s);

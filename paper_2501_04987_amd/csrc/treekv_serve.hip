@@ -25,7 +25,7 @@ int esz_of(const treekv_paged_cache& c) { return c.dtype == TREEKV_F32 ? 4 : 2; 
 int cache_ok(const treekv_paged_cache* cache) {
   if (!cache) return TREEKV_EINVAL;
   const treekv_paged_cache& c = *cache;
-  if (!c.k || !c.v || !c.table || !c.lens || !aligned16(c.k) || !aligned16(c.v) || !c.weights != !c.positions) return TREEKV_EINVAL;
+  if (!c.k || !c.v || !c.table || !c.lens || !aligned16(c.k) || !aligned16(c.v) || !aligned16(c.weights) || !c.weights != !c.positions) return TREEKV_EINVAL;
   if (c.dtype != TREEKV_BF16 && c.dtype != TREEKV_F32) return TREEKV_EINVAL;
   if (c.pages < 1 || c.page_size < 1 || c.table_width < 1 || c.batch < 1 || c.kv_heads < 1 || c.q_heads < 1 || c.q_heads % c.kv_heads != 0)
     return TREEKV_EINVAL;

@@ -38,7 +38,7 @@ def hold(x):
 
 
 BAD_CACHES = [(dict(k=None), -1), (dict(v=None), -1), (dict(table=None), -1), (dict(lens=None), -1), (dict(k=0x10 * MB + 8), -1),
-              (dict(v=0x20 * MB + 4), -1), (dict(weights=None), -1), (dict(positions=None), -1), (dict(dtype=2), -1), (dict(pages=0), -1),
+              (dict(v=0x20 * MB + 4), -1), (dict(weights=None), -1), (dict(weights=0x32 * MB + 4), -1), (dict(positions=None), -1), (dict(dtype=2), -1), (dict(pages=0), -1),
               (dict(page_size=0), -1), (dict(page_size=-16), -1), (dict(table_width=0), -1), (dict(batch=0), -1), (dict(kv_heads=0), -1),
               (dict(q_heads=0), -1), (dict(q_heads=5), -1), (dict(softmax_scale=float("nan")), -1), (dict(softmax_scale=float("inf")), -1),
               (dict(head_dim=96), -4), (dict(page_size=8), -4), (dict(page_size=48), -4), (dict(page_size=512), -4),
