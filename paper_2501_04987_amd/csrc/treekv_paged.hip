@@ -9,7 +9,7 @@
 // shares   Few rows leave most of the chip idle, so the columns of the whole batch are cut into equal shares, which the device
 //          works out from the lengths: long sequences get more workgroups than short ones.  A sequence's shares are merged by a
 //          second kernel.
-// weights  the probabilities once more from q, k and lse, summed down the rows: a column belongs to one wave, so the sum needs
+// weights  the probabilities once more from q, k and each row's reference and sum, summed down the rows: a column belongs to one wave, so the sum needs
 //          no atomics and repeats bit for bit.
 
 #include "treekv_matrix.h"
@@ -92,6 +92,7 @@ struct Attend {
   int64_t q_far;                             // bytes from one token's heads to the next one's
   char* out;
   float *lse, *part;
+  float2* stat;                              // for the weights: a row's reference and 1 / its sum (infinity and 0 if it adds nothing)
   int32_t* status;
   float* logits;                             // few rows and weights: scaled logits, [sequence][KV head][row][cap]
   int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
@@ -114,7 +115,7 @@ __device__ inline int share_size(const Attend& a) {
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) total += __shfl_xor(total, x, 64);
   const long long each = (total + a.shares - 1) / a.shares;
-  return (int)max((each + 31) / 32 * 32, (long long)MIN_SHARE);
+  return __builtin_amdgcn_readfirstlane((int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30));
 }
 // By piece (want_b < 0) or, its first piece, by sequence.
 __device__ inline bool find_share(const Attend& a, int w, int want_b, Share& s) {
@@ -167,12 +168,16 @@ __device__ inline void store4(char* out, size_t at, const float4& a, float inv, 
 __device__ inline void store4(char* out, size_t at, const float4& a, float inv, float) {
   *reinterpret_cast<float4*>(out + at * 4) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
 }
+__device__ inline void finish_sums(const Attend& a, size_t at, float M, float L) {
+  if (a.lse) a.lse[at] = !(L == 0.f) ? (M + log2f(L)) * LN2 : -INFINITY;
+  if (a.stat) a.stat[at] = L > 0.f ? make_float2(M, 1.0f / L) : make_float2(INFINITY, 0.f);
+}
 template <typename T, int D>
 __device__ inline void finish_row(const Attend& a, const Seq& s, int h, int row, int c, const float4& o, float M, float L) {
   const size_t at = (size_t)(s.first + row / a.p.G) * a.p.H + h * a.p.G + row % a.p.G;
   const bool any = !(L == 0.f);                          // (a sum that is a NaN stays one)
   store4(a.out, at * D + c, any ? o : make_float4(0.f, 0.f, 0.f, 0.f), any ? 1.0f / L : 0.f, T());
-  if (c == 0 && a.lse) a.lse[at] = any ? (M + log2f(L)) * LN2 : -INFINITY;
+  if (c == 0) finish_sums(a, at, M, L);
 }
 
 // grid: shares of the columns x KV heads x row tiles.  RB: blocks of 16 rows.
@@ -217,16 +222,28 @@ __global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Att
   const int32_t* table = p.table + (size_t)sh.b * p.width;
   const int in_page = (1 << p.bits) - 1;
 
+  // the pages of the wave's next AT_ONCE blocks, 16 columns to a lane (a lookup per block would be waited for before its rows)
+  constexpr int AT_ONCE = 64 / BK;
+  auto look_up = [&](int c0) {
+    const int c = c0 + lane / BK * (PA_WAVES * COLS) + lane % BK * 16;
+    const int page = c < hi ? table[c >> p.bits] : -1;
+    return page >= 0 && page < p.pages ? page : -1;
+  };
+  int left = 0, pages = -1;
 #pragma unroll 1
-  for (int c0 = lo + wave * COLS; c0 < hi; c0 += PA_WAVES * COLS) {
+  for (int c0 = lo + wave * COLS; c0 < hi; c0 += PA_WAVES * COLS, ++left) {
+    if (left % AT_ONCE == 0) {
+      pages = look_up(c0);
+      left = 0;
+    }
     size_t at[BK];
     bool there[BK], whole = c0 + COLS <= all_see;
 #pragma unroll
     for (int x = 0; x < BK; ++x) {
-      const int c = c0 + 16 * x, page = c < hi ? table[c >> p.bits] : -1;
-      there[x] = page >= 0 && page < p.pages;
+      const int c = c0 + 16 * x, page = __builtin_amdgcn_readlane(pages, left * BK + x);
+      there[x] = page >= 0;
       whole &= there[x];
-      at[x] = ((((size_t)(there[x] ? page : 0) * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB;
+      at[x] = ((((size_t)max(page, 0) * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB;
     }
     typename O::Keys k;
     typename O::Values v;
@@ -452,7 +469,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
   for (int row0 = first; row0 < rows; row0 += 16) {
     const int row = min(row0 + r, rows - 1), i = row / p.G, head = h * p.G + row - i * p.G;
     const int see = row0 + r < rows ? old + i + 1 : 0;
-    const float to = a.lse[(size_t)(s.first + i) * p.H + head] * LOG2E;
+    const float2 to = a.stat[(size_t)(s.first + i) * p.H + head];
     typename O::Query q;
     O::load_q(q, reinterpret_cast<const T*>(a.q + (s.first + i) * a.q_far) + (size_t)head * D, q4);
 #pragma unroll
@@ -461,8 +478,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
       logits<D>(x, k[nb], q);
 #pragma unroll
       for (int j = 0; j < O::NCOL; ++j) {
-        const float y = fast_exp2(fmaf(O::at(x, j), a.scale_log2e, -to));
-        acc[nb][j] += c0 + nb * COLS + O::col(q4, j) < see && y > 0.f ? y : 0.f;     // (not a NaN)
+        const float y = fmaxf(fast_exp2(fmaf(O::at(x, j), a.scale_log2e, -to.x)), 0.f);     // (of a NaN 0)
+        acc[nb][j] += c0 + nb * COLS + O::col(q4, j) < see ? y * to.y : 0.f;
       }
     }
   }
@@ -478,12 +495,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
 }
 
 // ---- many rows, bf16 -----------------------------------------------------------------------------
-// 128 rows a workgroup, 32 a wave; K and V pass through LDS in tiles of 64 columns, copied a tile ahead (one barrier a tile).
-// 32x32x16 products: S^T = K Q^T, where a lane has row l % 32 and, of each half of the tile, columns 8 (i/4) + 4 (l/32) + i % 4.
-// Those are its columns of the B operand of O^T += V^T P^T too (a sum does not ask for the order of its terms); the A operand
-// takes the same columns of a dimension out of LDS by two transposing reads.  A row's 16-byte pieces are stored under their
-// number XOR one of the row, so that the lanes of a read meet all banks.
-constexpr int TILE = 64, TILED_ROWS = 128, TILED_SUB = TILE / PA_WAVES;      // a wave copies the 16 columns of one page
+// 32 rows a wave, four waves a workgroup; K and V pass through LDS in tiles of 64 columns, copied a tile ahead (one barrier a
+// tile).  32x32x16 products: S^T = K Q^T, where a lane has row l % 32 and, of each half of the tile, columns
+// 8 (i/4) + 4 (l/32) + i % 4.  Those are its columns of the B operand of O^T += V^T P^T too (a sum does not ask for the order of
+// its terms); the A operand takes the same columns of a dimension out of LDS by two transposing reads.  A row's 16-byte pieces are
+// stored under their number XOR one of the row, so that the lanes of a read meet all banks.
+// A tile is as much vector work (exponentials at a quarter of the rate, 26 cycles a logit and lane) as matrix work (32 cycles a
+// product), and a wave issues in order: the logits of the next tile are formed beside the exponentials of this one, the second
+// products beside the rest of them and the next maxima, interleaved by hand step by step.
+constexpr int TILE = 64, TILED_SUB = TILE / PA_WAVES;      // a wave copies the 16 columns of one page
 template <int D> __device__ inline int swap_k(int row) { return row & (D / 8 - 1); }
 template <int D> __device__ inline int swap_v(int row) { return (row & (D / 16 - 1)) << 1; }
 
@@ -493,23 +513,18 @@ __device__ inline uint2 read_turned(const char* p) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)(lds_void_t*)p));
 }
 __device__ inline float other_half(float v) { return __shfl_xor(v, 32, 64); }
-
-// 16 rows of D / 8 pieces each from `src` (rows `far` bytes apart, or from `row_of`) into LDS at `to`.
-template <int D, class RowFn, class SwapFn>
-__device__ inline void copy_rows(unsigned to, RowFn row_of, SwapFn swap) {
-  constexpr int PIECES = D / 8, AT_ONCE = 64 / PIECES;
-  const int lane = threadIdx.x & 63, piece = lane % PIECES;
-#pragma unroll
-  for (int j = 0; j < TILED_SUB / AT_ONCE; ++j) {
-    const int row = j * AT_ONCE + lane / PIECES;
-    async_copy16(row_of(row) + ((piece ^ swap(row)) << 4), to + j * 1024);
-  }
+// async_copy16 from a uniform base and a lane's offset.
+__device__ inline void async_copy16_at(const char* base, unsigned offset, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_base) : "memory");
 }
+
+constexpr int TILED_ROWS = PA_WAVES * 32;
 
 template <int D>
 __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   constexpr int KS = D / 16, DB = D / 32, ROWB = D * 2, HALF = TILE * ROWB, OR = D + 4;
-  extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of K, V
+  constexpr int PIECES = D / 8, AT_ONCE = 64 / PIECES, COPIES = TILED_SUB / AT_ONCE;    // rows a copy instruction brings
+  extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of K, then of V
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
   if (blockIdx.x == 0 && a.status)
@@ -525,59 +540,112 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   const int old = s.len - s.n;
   const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + TILED_ROWS, rows) - 1) / p.G + 1;
   const int lo = sh.index * sh.size, hi = min(lo + sh.size, end);
+  // logits are compared before they are scaled, so the scale's sign goes to the queries
+  const float scale = fabsf(a.scale_log2e);
   const int row = row0 + wave * 32 + r, at_row = min(row, rows - 1), token = at_row / p.G, head = h * p.G + at_row - token * p.G;
   const int see = min(old + token + 1, hi);
   uint4 q[KS];
   {
     const char* src = a.q + (s.first + token) * a.q_far + (size_t)head * ROWB + hf * 16;
+    const unsigned flip = a.scale_log2e < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int x = 0; x < KS; ++x) q[x] = *reinterpret_cast<const uint4*>(src + x * 32);
+    for (int x = 0; x < KS; ++x) {
+      const uint4 u = *reinterpret_cast<const uint4*>(src + x * 32);
+      q[x] = make_uint4(u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip);
+    }
   }
   f32x16_t o[DB] = {};
-  float ref = REF_NONE, sum = 0.f;
+  float ref = REF_NONE, sum = 0.f, mx = -INFINITY;
   const int32_t* table = p.table + (size_t)sh.b * p.width;
   const int in_page = (1 << p.bits) - 1;
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem));
-
-  // which quarters of the tile at c0 are there; their rows on the way into `stage`
-  auto request = [&](int c0, int stage) {
-    unsigned there = 0;
-    int mine = 0;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem)) + wave * TILED_SUB * ROWB;
+  unsigned from_k[COPIES], from_v[COPIES];
 #pragma unroll
-    for (int x = 0; x < PA_WAVES; ++x) {
-      const int c = c0 + TILED_SUB * x, page = c < hi ? table[c >> p.bits] : -1;
-      const bool ok = page >= 0 && page < p.pages;
-      there |= (unsigned)ok << x;
-      if (x == wave) mine = ok ? page : 0;
-    }
-    const size_t at = ((((size_t)mine * p.Hkv + h) << p.bits) + ((c0 + TILED_SUB * wave) & in_page)) * ROWB;
-    const unsigned to = lds0 + stage * 2 * HALF + wave * TILED_SUB * ROWB;
-    copy_rows<D>(to, [&](int x) { return p.k + at + x * ROWB; }, swap_k<D>);
-    copy_rows<D>(to + HALF, [&](int x) { return p.v + at + x * ROWB; }, swap_v<D>);
-    return there;
+  for (int j = 0; j < COPIES; ++j) {
+    const int x = j * AT_ONCE + lane / PIECES, piece = lane % PIECES;
+    from_k[j] = x * ROWB + ((piece ^ swap_k<D>(x)) << 4);
+    from_v[j] = x * ROWB + ((piece ^ swap_v<D>(x)) << 4);
+  }
+  // The pages of 16 tiles at a time, a quarter of a tile to a lane, the next ones already asked for: a lookup per tile would be
+  // waited for every time (with it, and nothing else to wait for, a tile took 5600 cycles of which 2048 are products).
+  const int tiles = (hi - lo + TILE - 1) / TILE;
+  auto look_up = [&](int window) {
+    const int c = lo + (window * 64 + lane) * TILED_SUB;
+    const int page = c < hi ? table[c >> p.bits] : -1;
+    return page >= 0 && page < p.pages ? page : -1;
+  };
+  int window = 0, page0 = lo < hi ? look_up(0) : -1, page1 = lo < hi ? look_up(1) : -1;
+  unsigned long long is0 = __ballot(page0 >= 0), is1 = __ballot(page1 >= 0);
+  // which quarters of tile t are there
+  auto quarters = [&](int t) { return (unsigned)((t >> 4 == window ? is0 : is1) >> (4 * (t & 15))) & 15u; };
+  // this wave's quarter of tile t on its way into a stage (of nobody's: any rows)
+  auto request = [&](const char* pool, const unsigned (&from)[COPIES], int t, unsigned to) {
+    const int at = 4 * (t & 15) + wave, page = t >> 4 == window ? __builtin_amdgcn_readlane(page0, at) : __builtin_amdgcn_readlane(page1, at);
+    const char* base = pool + ((((size_t)max(page, 0) * p.Hkv + h) << p.bits) + ((lo + t * TILE + TILED_SUB * wave) & in_page)) * ROWB;
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) async_copy16_at(base, from[j], lds0 + to + j * 1024);
+  };
+  // the reads of a tile's keys, and of its values turned: piece 4 e + .. of rows .. + 4 hf, 8 bytes a lane
+  const unsigned at_k = r * ROWB + ((hf ^ swap_k<D>(r)) << 4);                            // of step y: XOR 2 y pieces
+  const int turned_row = 4 * hf + ((lane & 15) >> 2);
+  const unsigned at_v = turned_row * ROWB + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1) ^ swap_v<D>(turned_row)) << 4) + (lane & 1) * 8;   // of e: XOR 4 e pieces
+  static_assert(8 % (D / 16) == 0 && 32 % (D / 8) == 0, "the rows of the other reads, 8 and 32 further on, are swapped alike");
+
+  f32x16_t x[2];
+  auto mask = [&](int c0, unsigned there) {
+    int last = see - c0 - 4 * hf;
+    asm volatile("" : "+v"(last));                   // (keeps the comparisons out of the tiles that need none)
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = z * 32 + 8 * (i >> 2) + (i & 3);
+        if (!(there >> (c / TILED_SUB) & 1) || c >= last) x[z][i] = -INFINITY;
+      }
+  };
+  auto largest = [&]() {
+    float m = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) m = fmaxf(m, x[i >> 4][i & 15]);
+    mx = m * scale;
   };
 
-  unsigned there = 0;
-  if (lo < hi) there = request(lo, 0);
-  int stage = 0;
-#pragma unroll 1
-  for (int c0 = lo; c0 < hi; c0 += TILE, stage ^= 1) {
-    wait_vmcnt<0>();
+  unsigned now = 0;
+  if (lo < hi) {
+    now = quarters(0);
+    request(p.k, from_k, 0, 0);
+    request(p.k, from_k, 1, HALF);
+    request(p.v, from_v, 0, 2 * HALF);
+    wait_vmcnt<2 * COPIES>();
     __syncthreads();
-    const unsigned now = there;
-    if (c0 + TILE < hi) there = request(c0 + TILE, stage ^ 1);
-    char* k = pt_smem + stage * 2 * HALF;
-    char* v = k + HALF;
-    const bool whole = now == (1u << PA_WAVES) - 1 && c0 + TILE <= all_see;
-
-    f32x16_t x[2] = {};
+    x[0] = x[1] = f32x16_t{};
 #pragma unroll
     for (int y = 0; y < KS; ++y)
 #pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int kr = z * 32 + r;
-        x[z] = mfma_wide(*reinterpret_cast<const uint4*>(k + kr * ROWB + (((2 * y + hf) ^ swap_k<D>(kr)) << 4)), q[y], x[z]);
-      }
+      for (int z = 0; z < 2; ++z) x[z] = mfma_wide(*reinterpret_cast<const uint4*>(pt_smem + z * 32 * ROWB + (at_k ^ (y << 5))), q[y], x[z]);
+    if (now != (1u << PA_WAVES) - 1 || lo + TILE > all_see) mask(lo, now);
+    largest();
+  }
+  int here = 0;                                        // this tile's stage (its keys are no longer needed)
+#pragma unroll 1
+  for (int t = 0; t < tiles; ++t) {
+    const int c0 = lo + t * TILE;
+    // the keys of the next tile and the values of this one are there, and nobody reads those of the last one any more
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (t >> 4 != window) {
+      ++window;
+      page0 = page1;
+      is0 = is1;
+      page1 = look_up(window + 1);
+      is1 = __ballot(page1 >= 0);
+    }
+    const unsigned next = quarters(t + 1);
+    request(p.k, from_k, t + 2, here);
+    request(p.v, from_v, t + 1, 2 * HALF + (HALF - here));
+    const char* k = pt_smem + (HALF - here);
+    char* v = pt_smem + 2 * HALF + here;
+    const bool whole = now == (1u << PA_WAVES) - 1 && c0 + TILE <= all_see;
     bool odd = false;
     if (!whole) {
       // rows of nobody become 0; what is not finite is taken out, and added below for the rows that attend it
@@ -594,47 +662,80 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
       }
       odd = __syncthreads_or(mine);
     }
-    float mx = -INFINITY;
+      if (__any(mx > ref + 8.f)) {
+        const float top = fmaxf(mx, other_half(mx));
+        const float to = top > ref + 8.f ? top : ref, f = fast_exp2(ref - to);
+        sum *= f;
 #pragma unroll
-    for (int z = 0; z < 2; ++z)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[z][i] *= a.scale_log2e;
-        if (!whole) {
-          const int c = z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3);
-          if (!(now >> (c / TILED_SUB) & 1) || c0 + c >= see) x[z][i] = -INFINITY;
-        }
-        mx = fmaxf(mx, x[z][i]);
+        for (int e = 0; e < DB; ++e) o[e] *= f;
+        ref = to;
       }
-    if (__any(mx > ref + 8.f)) {
-      mx = fmaxf(mx, other_half(mx));
-      const float to = mx > ref + 8.f ? mx : ref, f = fast_exp2(ref - to);
-      sum *= f;
+    // Probabilities of this tile beside the logits of the next (of what is behind the last one: not used), 16 columns of all rows
+    // after the other; three of these four groups beside the first products.  A step forms some exponentials, the arguments of the
+    // next step's, and takes in those of the last step; operands are read AHEAD steps before.
+    constexpr int STEPS = 2 * KS, VSTEPS = 4 * DB, GROUP = 8, ALL = 4 * GROUP, AHEAD = 2;
+    f32x16_t n[2] = {};
+    uint4 kf[AHEAD + 1], vf[AHEAD + 1];
+    float arg[ALL], e[ALL];
+    unsigned pr[16];
+    auto read_k = [&](int y) { return *reinterpret_cast<const uint4*>(k + (y & 1) * 32 * ROWB + (at_k ^ (y >> 1 << 5))); };
+    auto read_v = [&](int y) {
+      const char* src = v + y / DB * 16 * ROWB + (at_v ^ (y % DB << 6));
+      const uint2 u0 = read_turned(src), u1 = read_turned(src + 8 * ROWB);
+      return make_uint4(u0.x, u0.y, u1.x, u1.y);
+    };
+    auto argument = [&](int i) { const int g = i / GROUP; arg[i] = fmaf(x[g >> 1][8 * (g & 1) + i % 8], scale, -ref); };
+    auto take = [&](int i) {
+      const int g = i / GROUP;
+      sum += e[i];
+      if (i & 1) pr[4 * g + i % 8 / 2] = narrow2(e[i - 1], e[i]);
+    };
+    auto first_of = [&](int y) { return y < STEPS ? y * (3 * GROUP) / STEPS : min(ALL, 3 * GROUP + (y - STEPS) * GROUP / (VSTEPS / 2)); };
 #pragma unroll
-      for (int e = 0; e < DB; ++e) o[e] *= f;
-      ref = to;
+    for (int y = 0; y < AHEAD; ++y) kf[y] = read_k(y);
+#pragma unroll
+    for (int i = 0; i < first_of(1); ++i) argument(i);
+#pragma unroll
+    for (int y = 0; y < STEPS; ++y) {
+      if (y + AHEAD < STEPS) kf[(y + AHEAD) % (AHEAD + 1)] = read_k(y + AHEAD);
+      else vf[y + AHEAD - STEPS] = read_v(y + AHEAD - STEPS);
+      n[y & 1] = mfma_wide(kf[y % (AHEAD + 1)], q[y >> 1], n[y & 1]);
+#pragma unroll
+      for (int i = first_of(y); i < first_of(y + 1); ++i) e[i] = fast_exp2(arg[i]);
+#pragma unroll
+      for (int i = first_of(y + 1); i < first_of(y + 2); ++i) argument(i);
+      if (y > 0)
+#pragma unroll
+        for (int i = first_of(y - 1); i < first_of(y); ++i) take(i);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    float m;
+      m = n[0][0];
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
+    for (int z = 0; z < VSTEPS; ++z) {
+      const int y = STEPS + z, g = z / DB;
+      if (z + AHEAD < VSTEPS) vf[(z + AHEAD) % (AHEAD + 1)] = read_v(z + AHEAD);
+        o[z % DB] = mfma_wide(vf[z % (AHEAD + 1)], make_uint4(pr[4 * g], pr[4 * g + 1], pr[4 * g + 2], pr[4 * g + 3]), o[z % DB]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[z][i] = fast_exp2(x[z][i] - ref);
-        sum += x[z][i];
+      for (int i = first_of(y - 1); i < first_of(y); ++i) take(i);
+#pragma unroll
+      for (int i = first_of(y); i < first_of(y + 1); ++i) e[i] = fast_exp2(arg[i]);
+#pragma unroll
+      for (int i = first_of(y + 1); i < first_of(y + 2); ++i) argument(i);
+      if (z >= VSTEPS / 2) {
+        const int u = z - VSTEPS / 2;
+#pragma unroll
+        for (int i = u * 64 / VSTEPS; i < (u + 1) * 64 / VSTEPS; ++i)
+      m = fmaxf(m, n[i >> 4][i & 15]);
       }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const uint4 pr = make_uint4(narrow2(x[z][8 * g], x[z][8 * g + 1]), narrow2(x[z][8 * g + 2], x[z][8 * g + 3]),
-                                    narrow2(x[z][8 * g + 4], x[z][8 * g + 5]), narrow2(x[z][8 * g + 6], x[z][8 * g + 7]));
-        const int vr = z * 32 + g * 16 + 4 * hf + ((lane & 15) >> 2);
-#pragma unroll
-        for (int e = 0; e < DB; ++e) {
-          // this lane's share of four rows of 16 dimensions: 8 bytes of piece 4 e + ..
-          const int piece = 4 * e + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), byte = (lane & 1) * 8;
-          const uint2 u0 = read_turned(v + vr * ROWB + ((piece ^ swap_v<D>(vr)) << 4) + byte);
-          const uint2 u1 = read_turned(v + (vr + 8) * ROWB + ((piece ^ swap_v<D>(vr + 8)) << 4) + byte);
-          o[e] = mfma_wide(make_uint4(u0.x, u0.y, u1.x, u1.y), pr, o[e]);
-        }
-      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    x[0] = n[0];
+    x[1] = n[1];
+    mx = m * scale;
+    if (next != (1u << PA_WAVES) - 1 || c0 + 2 * TILE > all_see) {
+      mask(c0 + TILE, next);
+      largest();
     }
     if (odd) {
 #pragma unroll 1
@@ -642,47 +743,51 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
         if (!(now >> ((c - c0) / TILED_SUB) & 1)) continue;
         const char* src = p.v + ((((size_t)table[c >> p.bits] * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB + hf * 8;
 #pragma unroll
-        for (int e = 0; e < DB; ++e)
+        for (int f = 0; f < DB; ++f)
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
-            const uint2 u = *reinterpret_cast<const uint2*>(src + (32 * e + 8 * z) * 2);
+            const uint2 u = *reinterpret_cast<const uint2*>(src + (32 * f + 8 * z) * 2);
             const unsigned word[4] = {u.x << 16, u.x & 0xffff0000u, u.y << 16, u.y & 0xffff0000u};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float bad = __uint_as_float(word[i] & ~(unsigned)((int)finite_word(word[i]) >> 31));
-              o[e][4 * z + i] += c < see ? bad : 0.f;
+      o[f][4 * z + i] += c < see ? bad : 0.f;
             }
           }
       }
     }
+    now = next;
+    here = HALF - here;
   }
-  sum += other_half(sum);
+  wait_vmcnt<0>();                                     // (copies into LDS that nobody waits for)
+  const float total = sum + other_half(sum);
   if (row >= rows) return;
   float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles * TILED_ROWS + row) * OR;
   const size_t at = (size_t)(s.first + token) * p.H + head;
-  const bool any = !(sum == 0.f);
-  const float inv = any ? 1.0f / sum : 0.f;
+  const bool any = !(total == 0.f);
+  const float inv = any ? 1.0f / total : 0.f;
 #pragma unroll
-  for (int e = 0; e < DB; ++e)
+  for (int f = 0; f < DB; ++f)
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
-      const int c = 32 * e + 8 * z + 4 * hf;
-      const float4 f = make_float4(o[e][4 * z], o[e][4 * z + 1], o[e][4 * z + 2], o[e][4 * z + 3]);
-      if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = f;
-      else store4(a.out, at * D + c, any ? f : make_float4(0.f, 0.f, 0.f, 0.f), inv, uint16_t());
+      const int c = 32 * f + 8 * z + 4 * hf;
+      const float4 u = make_float4(o[f][4 * z], o[f][4 * z + 1], o[f][4 * z + 2], o[f][4 * z + 3]);
+      if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = u;
+      else store4(a.out, at * D + c, any ? u : make_float4(0.f, 0.f, 0.f, 0.f), inv, uint16_t());
     }
   if (hf == 0) {
-    if (sh.count > 1) *reinterpret_cast<float2*>(part + D) = make_float2(ref, sum);
-    else if (a.lse) a.lse[at] = any ? (ref + log2f(sum)) * LN2 : -INFINITY;
+    if (sh.count > 1) *reinterpret_cast<float2*>(part + D) = make_float2(ref, total);
+    else finish_sums(a, at, ref, total);
   }
 }
 
-// Weights of many rows: 64 columns a wave, their keys in registers; the rows' queries pass through LDS in tiles of 64.  A lane
+// Weights of many rows: 32 columns a wave, their keys in registers; the rows' queries pass through LDS in tiles of 64.  A lane
 // has row l % 32 and adds up its columns over the rows it meets; the lanes are added at the end.  grid: column tiles x KV heads x
 // sequences.
 template <int D>
-__global__ __launch_bounds__(PA_THREADS, 2) void weigh_tiled_kernel(Attend a, int col_tiles) {
+__global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, int col_tiles) {
   constexpr int KS = D / 16, ROWB = D * 2, STAGE = TILE * ROWB;
+  constexpr int PIECES = D / 8, AT_ONCE = 64 / PIECES, COPIES = TILED_SUB / AT_ONCE;
   extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of queries
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
@@ -690,94 +795,118 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_tiled_kernel(Attend a, in
   const int h = group % p.Hkv, b = group / p.Hkv;
   if (b >= p.B) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  const int first_col = ct * PA_WAVES * TILE, c0 = first_col + wave * TILE;
+  const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
   if (s.n == 0 || first_col >= s.len) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
-  uint4 k[2][KS];
-#pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    const int c = c0 + z * 32 + r, page = c < s.len ? table[c >> p.bits] : -1;
+  uint4 k[KS];
+  {
+    const int c = c0 + r, page = c < s.len ? table[c >> p.bits] : -1;
     const size_t at = ((((size_t)(page >= 0 && page < p.pages ? page : 0) * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB + hf * 16;
 #pragma unroll
-    for (int y = 0; y < KS; ++y) k[z][y] = *reinterpret_cast<const uint4*>(p.k + at + y * 32);
+    for (int y = 0; y < KS; ++y) k[y] = *reinterpret_cast<const uint4*>(p.k + at + y * 32);
   }
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem));
-  auto place = [&](int row, int& token) {             // of a row's query, in heads
-    row = min(row, rows - 1);
-    token = row / p.G;
-    return h * p.G + row - token * p.G;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem)) + wave * TILED_SUB * ROWB;
+  // A row as (token, head of the group), which goes on from tile to tile by whole tokens and a rest: no division in the loop.
+  // Rows behind the last are the last one.
+  struct Place {
+    int token, g;
   };
-  auto request = [&](int row0, int stage) {
-    copy_rows<D>(lds0 + stage * STAGE + wave * TILED_SUB * ROWB, [&](int x) {
-      int token;
-      const int head = place(row0 + wave * TILED_SUB + x, token);
-      return a.q + (s.first + token) * a.q_far + (size_t)head * ROWB;
-    }, swap_k<D>);
+  const int step = TILE / p.G, rest = TILE - step * p.G;
+  auto onwards = [&](Place& x) {
+    x.token += step;
+    x.g += rest;
+    if (x.g >= p.G) { x.g -= p.G; ++x.token; }
   };
-  auto log_sum = [&](int row) {                       // rows behind the last: exponentials of minus infinity
-    int token;
-    const int head = place(row, token);
-    const float l = a.lse[(size_t)(s.first + token) * p.H + head] * LOG2E;
-    return row < rows ? l : INFINITY;
-  };
-  f32x16_t acc[2] = {};
+  auto place = [&](int row) { Place x = {row / p.G, row % p.G}; return x; };
   const int first = max(0, first_col - old) * p.G / TILE * TILE;
-  request(first, 0);
-  float l[2] = {log_sum(first + r), log_sum(first + 32 + r)};
-  int stage = 0;
-#pragma unroll 1
-  for (int row0 = first; row0 < rows; row0 += TILE, stage ^= 1) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    const float now[2] = {l[0], l[1]};
-    if (row0 + TILE < rows) {
-      request(row0 + TILE, stage ^ 1);
-      l[0] = log_sum(row0 + TILE + r);
-      l[1] = log_sum(row0 + TILE + 32 + r);
+  const char* q0 = a.q + s.first * a.q_far + (size_t)h * p.G * ROWB;
+  const float2* stat0 = a.stat + (size_t)s.first * p.H + h * p.G;
+  Place from[COPIES], stats[2];
+  unsigned piece[COPIES];
+#pragma unroll
+  for (int j = 0; j < COPIES; ++j) {
+    const int x = j * AT_ONCE + lane / PIECES;
+    from[j] = place(first + wave * TILED_SUB + x);
+    piece[j] = ((lane % PIECES) ^ swap_k<D>(x)) << 4;
+  }
+#pragma unroll
+  for (int y = 0; y < 2; ++y) stats[y] = place(first + 32 * y + r);
+  auto request = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) {
+      const bool in = from[j].token < s.n;
+      async_copy16(q0 + (in ? from[j].token : s.n - 1) * a.q_far + (in ? from[j].g : 0) * ROWB + piece[j], lds0 + stage * STAGE + j * 1024);
+      onwards(from[j]);
     }
-    const char* q = pt_smem + stage * STAGE;
-    const bool whole = old + row0 / p.G + 1 >= c0 + TILE;
+  };
+  float2 l[2];
+  int see[2];
+  auto next_stats = [&]() {                           // rows behind the last: exponentials of minus infinity
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      f32x16_t x[2] = {};
-      const int qr = y * 32 + r;
-#pragma unroll
-      for (int e = 0; e < KS; ++e) {
-        const uint4 u = *reinterpret_cast<const uint4*>(q + qr * ROWB + (((2 * e + hf) ^ swap_k<D>(qr)) << 4));
-#pragma unroll
-        for (int z = 0; z < 2; ++z) x[z] = mfma_wide(k[z][e], u, x[z]);
-      }
-      const int see = old + min(row0 + qr, rows - 1) / p.G + 1 - c0;
-#pragma unroll
-      for (int z = 0; z < 2; ++z)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e = fmaxf(fast_exp2(fmaf(x[z][i], a.scale_log2e, -now[y])), 0.f);          // (of a NaN 0)
-          if (!whole && z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3) >= see) e = 0.f;
-          acc[z][i] += e;
-        }
+      const bool in = stats[y].token < s.n;
+      const float2 u = stat0[(size_t)(in ? stats[y].token : 0) * p.H + (in ? stats[y].g : 0)];
+      l[y] = in ? u : make_float2(INFINITY, 0.f);
+      see[y] = old + stats[y].token + 1 - c0;
+      onwards(stats[y]);
     }
+  };
+  f32x16_t acc = {};
+  request(0);
+  next_stats();
+  int stage = 0, token = first / p.G;                 // of the tile's first row, rounded down
+  const unsigned at_q = r * ROWB + ((hf ^ swap_k<D>(r)) << 4);        // of step e: XOR 2 e pieces
+  struct Yes { __device__ constexpr operator bool() const { return true; } };
+  struct No { __device__ constexpr operator bool() const { return false; } };
+  auto tile = [&](const char* q, const float2 (&now)[2], const int (&sees)[2], auto masked) {
+    unsigned from = at_q;
+    float scale = a.scale_log2e;
+    asm volatile("" : "+v"(from), "+v"(scale));       // (or what both forms of a tile share is worked out, and held, before the choice)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      f32x16_t x = {};
+#pragma unroll
+      for (int e = 0; e < KS; ++e) x = mfma_wide(k[e], *reinterpret_cast<const uint4*>(q + y * 32 * ROWB + (from ^ (e << 5))), x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float e = fmaxf(fast_exp2(fmaf(x[i], scale, -now[y].x)), 0.f);        // (of a NaN 0)
+        if (masked && 8 * (i >> 2) + 4 * hf + (i & 3) >= sees[y]) e = 0.f;
+        acc[i] = fmaf(e, now[y].y, acc[i]);
+      }
+    }
+  };
+#pragma unroll 1
+  for (int row0 = first; row0 < rows; row0 += TILE, stage ^= 1, token += step) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    const float2 now[2] = {l[0], l[1]};
+    const int sees[2] = {see[0], see[1]};
+    if (row0 + TILE < rows) {
+      request(stage ^ 1);
+      next_stats();
+    }
+    const char* q = pt_smem + stage * STAGE;
+    if (old + token + 1 >= c0 + 32) tile(q, now, sees, No());       // (`token` falls behind where G does not divide a tile)
+    else tile(q, now, sees, Yes());
   }
   float* weights = p.weights + track_row(p, b, h);
 #pragma unroll
-  for (int z = 0; z < 2; ++z)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = group_sum<32>(acc[z][i]);
-      const int c = c0 + z * 32 + 8 * (i >> 2) + 4 * hf + (i & 3);
-      if (r == 0 && c < s.len) {
-        const int page = table[c >> p.bits];
-        if (page >= 0 && page < p.pages) weights[c] += e;
-      }
+  for (int i = 0; i < 16; ++i) {
+    const float e = group_sum<32>(acc[i]);
+    const int c = c0 + 8 * (i >> 2) + 4 * hf + (i & 3);
+    if (r == 0 && c < s.len) {
+      const int page = table[c >> p.bits];
+      if (page >= 0 && page < p.pages) weights[c] += e;
     }
+  }
 }
 
 // ---- launches ----------------------------------------------------------------------------------
 struct AttendShape {
   int rows, tiles, shares;                   // rows of a tile
   bool tiled, keep;                          // many rows through LDS; logits kept for the weights
-  size_t part, logits, lse;                  // bytes of scratch: shares' results, logits, log sums nobody asked for
+  size_t part, logits, stat;                 // bytes of scratch: shares' results, logits, rows' references and sums
 };
 AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const long long rows = (long long)longest * (c.q_heads / c.kv_heads), cap = (long long)c.table_width * c.page_size;
@@ -794,7 +923,7 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   s.keep = weigh && rows <= 16 && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
   s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
   s.logits = s.keep ? align_up((size_t)units * s.rows * cap * 4) : 0;
-  s.lse = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 4) : 0;
+  s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
   return s;
 }
 
@@ -806,8 +935,9 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
   if (sh.tiled) {
     if constexpr (sizeof(T) == 2) {
       const int lds = 4 * TILE * D * 2;
-      if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)attend_tiled_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return TREEKV_EHIP;
-      hipLaunchKernelGGL((attend_tiled_kernel<D>), dim3((groups + 7) / 8 * 8 * a.tiles), dim3(PA_THREADS), lds, s, a);
+      auto kernel = attend_tiled_kernel<D>;
+      if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return TREEKV_EHIP;
+      hipLaunchKernelGGL(kernel, dim3((groups + 7) / 8 * 8 * a.tiles), dim3(PA_THREADS), lds, s, a);
     }
   } else {
     const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
@@ -829,7 +959,7 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
   if (weigh) {
     if (sh.tiled) {
       if constexpr (sizeof(T) == 2) {
-        const int all = (p.cap + PA_WAVES * TILE - 1) / (PA_WAVES * TILE);
+        const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
         hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3((units + 7) / 8 * 8 * all), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);
       }
     } else {
@@ -858,7 +988,7 @@ int launch_paged_append(const treekv_paged_cache& c, const void* k, const void* 
 
 size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const AttendShape s = attend_shape(c, tokens, longest, weigh);
-  return s.part + s.logits + s.lse;
+  return s.part + s.logits + s.stat;
 }
 
 int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
@@ -872,7 +1002,8 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.out = (char*)out;
   a.part = (float*)scratch;
   a.logits = (float*)((char*)scratch + sh.part);
-  a.lse = !lse && sh.lse ? (float*)((char*)scratch + sh.part + sh.logits) : lse;
+  a.stat = sh.stat ? (float2*)((char*)scratch + sh.part + sh.logits) : nullptr;
+  a.lse = lse;
   a.status = status;
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
