@@ -99,15 +99,19 @@ struct Attend {
   float scale_log2e;
 };
 
-// The columns of all sequences with new tokens, cut into pieces of `size`: a sequence's first piece starts at its first
-// token.  Piece w is piece `index` of `count` of sequence b, whose first is number `first`.
-struct Share {
-  int b, index, count, first, size;
+// The columns of all sequences with new tokens lie one after the other (each sequence's rounded up to whole blocks), and are cut
+// into shares of `size`.  Few rows: a workgroup takes one share, whatever sequences it runs through; what it has of sequence b is
+// partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round: a sequence's
+// shares start at its first token, so that each is of one sequence.
+struct Run {
+  int b, length;             // a sequence with columns, and their number
+  long long start;           // where they start
+  int first, count;          // its partial results
 };
 __device__ inline int tokens_to_read(const Attend& a, int b) {
   if (b >= a.p.B) return 0;
   const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
-  return s.n > 0 ? s.len : 0;
+  return s.n > 0 ? (s.len + 31) & ~31 : 0;
 }
 __device__ inline int share_size(const Attend& a) {
   long long total = 0;
@@ -117,26 +121,35 @@ __device__ inline int share_size(const Attend& a) {
   const long long each = (total + a.shares - 1) / a.shares;
   return __builtin_amdgcn_readfirstlane((int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30));
 }
-// By piece (want_b < 0) or, its first piece, by sequence.
-__device__ inline bool find_share(const Attend& a, int w, int want_b, Share& s) {
+__device__ inline long long uniform64(long long x) {
+  return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+}
+// The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
+__device__ inline bool find_run(const Attend& a, int size, bool own, long long at, int want_b, Run& run) {
   const int lane = threadIdx.x & 63;
-  s.size = share_size(a);
-  int before = 0;
+  long long before = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
-    const int mine = (tokens_to_read(a, b0 + lane) + s.size - 1) / s.size;
-    int sum = mine;
+    const int length = tokens_to_read(a, b0 + lane);
+    const long long mine = own ? (length + size - 1) / size : length;
+    long long sum = mine;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) {
-      const int y = __shfl_up(sum, x, 64);
+      const long long y = __shfl_up(sum, x, 64);
       if (lane >= x) sum += y;
     }
-    const unsigned long long hit = __ballot(want_b < 0 ? before + sum > w : b0 + lane == want_b);
+    const unsigned long long hit = __ballot(want_b < 0 ? mine > 0 && before + sum > at : b0 + lane == want_b);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      s.b = __builtin_amdgcn_readfirstlane(b0 + l);
-      s.count = __builtin_amdgcn_readfirstlane(__shfl(mine, l, 64));
-      s.first = __builtin_amdgcn_readfirstlane(before + __shfl(sum, l, 64)) - s.count;
-      s.index = w - s.first;
+      run.b = __builtin_amdgcn_readfirstlane(b0 + l);
+      run.length = __builtin_amdgcn_readfirstlane(__shfl(length, l, 64));
+      run.start = uniform64(before + __shfl(sum - mine, l, 64));
+      if (own) {
+        run.first = (int)run.start;
+        run.count = (run.length + size - 1) / size;
+      } else {
+        run.first = (int)(run.start / size) + run.b;
+        run.count = run.length ? (int)((run.start + run.length - 1) / size) - (int)(run.start / size) + 1 : 0;
+      }
       return true;
     }
     before += __shfl(sum, 63, 64);
@@ -183,7 +196,7 @@ __device__ inline void finish_row(const Attend& a, const Seq& s, int h, int row,
 // grid: shares of the columns x KV heads x row tiles.  RB: blocks of 16 rows.
 // WEIGH (16 rows only): the logits are kept for the weights.
 template <typename T, int D, int RB, bool WEIGH>
-__global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Attend a) {
+__global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   using O = Ops<T, D>;
   constexpr int ROWS = RB * 16, DPL = O::DPL, OR = D + 4, BK = O::COLS / 16, COLS = O::COLS, ROWB = D * (int)sizeof(T);
   extern __shared__ __attribute__((aligned(16))) float pa_smem[];
@@ -192,161 +205,188 @@ __global__ __launch_bounds__(PA_THREADS, RB == 1 ? 3 : 2) void attend_kernel(Att
   const int tile = (int)(blockIdx.x % a.tiles), rest = (int)(blockIdx.x / a.tiles), h = rest % p.Hkv, w = rest / p.Hkv;
   if (blockIdx.x == 0 && a.status)
     for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  Share sh;
-  if (!find_share(a, w, -1, sh)) return;
-  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, sh.b);
-  const int rows = s.n * p.G, row0 = tile * ROWS;
-  if (row0 >= rows) return;
-  const int old = s.len - s.n;
-  // columns: what the tile's first row sees all rows see, behind what its last row sees there is nothing for it
-  const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + ROWS, rows) - 1) / p.G + 1;
-  const int lo = sh.index * sh.size, hi = min(lo + sh.size, end);
-
-  typename O::Query q[RB];
-  int see[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = min(row0 + rb * 16 + r, rows - 1), i = row / p.G;
-    see[rb] = old + i + 1;
-    O::load_q(q[rb], reinterpret_cast<const T*>(a.q + (s.first + i) * a.q_far) + (size_t)(h * p.G + row - i * p.G) * D, q4);
-  }
-  f32x4_t o[RB][D / 16];
-  float ref[RB], sum[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    ref[rb] = REF_NONE;
-    sum[rb] = 0.f;
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[rb][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  const int32_t* table = p.table + (size_t)sh.b * p.width;
-  const int in_page = (1 << p.bits) - 1;
-
-  // the pages of the wave's next AT_ONCE blocks, 16 columns to a lane (a lookup per block would be waited for before its rows)
-  constexpr int AT_ONCE = 64 / BK;
-  auto look_up = [&](int c0) {
-    const int c = c0 + lane / BK * (PA_WAVES * COLS) + lane % BK * 16;
-    const int page = c < hi ? table[c >> p.bits] : -1;
-    return page >= 0 && page < p.pages ? page : -1;
-  };
-  int left = 0, pages = -1;
+  const int size = share_size(a);
+  const long long share_end = (long long)(w + 1) * size;
+  Run run;
 #pragma unroll 1
-  for (int c0 = lo + wave * COLS; c0 < hi; c0 += PA_WAVES * COLS, ++left) {
-    if (left % AT_ONCE == 0) {
-      pages = look_up(c0);
-      left = 0;
-    }
-    size_t at[BK];
-    bool there[BK], whole = c0 + COLS <= all_see;
-#pragma unroll
-    for (int x = 0; x < BK; ++x) {
-      const int c = c0 + 16 * x, page = __builtin_amdgcn_readlane(pages, left * BK + x);
-      there[x] = page >= 0;
-      whole &= there[x];
-      at[x] = ((((size_t)max(page, 0) * p.Hkv + h) << p.bits) + (c & in_page)) * ROWB;
-    }
-    typename O::Keys k;
-    typename O::Values v;
-#pragma unroll
-    for (int x = 0; x < BK; ++x) O::load_k(k, x, p.k + at[x], r * ROWB + q4 * 16);
-#pragma unroll
-    for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, p.v + at[j * BK / O::NCOL], (O::col(q4, j) & 15) * ROWB + r * DPL * (int)sizeof(T));
-    bool odd = false;
-    if (!whole) {
-#pragma unroll
-      for (int j = 0; j < O::NCOL; ++j)
-        if (!there[j * BK / O::NCOL] || c0 + O::col(q4, j) >= hi) O::clear_v(v, j);
-      odd = !all_finite<D>(v);
-      if (odd) drop_not_finite<D>(v);
-    }
+  for (long long from = (long long)w * size; from < share_end && find_run(a, size, false, from, -1, run); from = run.start + run.length) {
+    const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
+    const int rows = s.n * p.G, row0 = tile * ROWS;
+    if (row0 >= rows) continue;
+    const int old = s.len - s.n;
+    // columns: what the tile's first row sees all rows see, behind what its last row sees there is nothing for it
+    const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + ROWS, rows) - 1) / p.G + 1;
+    const int lo = (int)(from - run.start), hi = (int)min((long long)end, share_end - run.start);
+
+    typename O::Query q[RB];
+    int see[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      typename O::Logits x;
-      logits<D>(x, k, q[rb]);
-      float mx = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < O::NCOL; ++j) {
-        float& y = O::at(x, j);
-        y *= a.scale_log2e;
-        if (!whole && (!there[j * BK / O::NCOL] || c0 + O::col(q4, j) >= min(see[rb], hi))) y = -INFINITY;
-        mx = fmaxf(mx, y);
-      }
-      if constexpr (WEIGH) {
-        if (r < rows) {
-          float* keep = a.logits + (((size_t)sh.b * p.Hkv + h) * a.rows + r) * p.cap + c0 + 4 * q4;
-#pragma unroll
-          for (int z = 0; z < BK; ++z)
-            if (c0 + 16 * z < hi) *reinterpret_cast<f32x4_t*>(keep + 16 * z) = x.x[z];
-        }
-      }
-      if (__any(mx > ref[rb] + 8.f)) {
-        mx = row_max(mx);
-        const float to = mx > ref[rb] + 8.f ? mx : ref[rb], f = fast_exp2(ref[rb] - to);
-        sum[rb] *= f;
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) o[rb][e] *= f;
-        ref[rb] = to;
-      }
-#pragma unroll
-      for (int j = 0; j < O::NCOL; ++j) {
-        float& y = O::at(x, j);
-        y = fast_exp2(y - ref[rb]);
-        sum[rb] += y;
-      }
-      add_rounded<D>(o[rb], v, x);
+      const int row = min(row0 + rb * 16 + r, rows - 1), i = row / p.G;
+      see[rb] = old + i + 1;
+      O::load_q(q[rb], reinterpret_cast<const T*>(a.q + (s.first + i) * a.q_far) + (size_t)(h * p.G + row - i * p.G) * D, q4);
     }
-    if (odd) {
+    f32x4_t o[RB][D / 16];
+    float ref[RB], sum[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      ref[rb] = REF_NONE;
+      sum[rb] = 0.f;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) o[rb][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t* table = p.table + (size_t)run.b * p.width;
+    const int in_page = (1 << p.bits) - 1;
+
+    // the pages of the wave's next AT_ONCE blocks, 16 columns to a lane (a lookup per block would be waited for before its rows)
+    constexpr int AT_ONCE = 64 / BK;
+    auto look_up = [&](int c0) {
+      const int c = c0 + lane / BK * (PA_WAVES * COLS) + lane % BK * 16;
+      const int page = c < hi ? table[c >> p.bits] : -1;
+      return page >= 0 && page < p.pages ? page : -1;
+    };
+    int left = 0, pages = -1;
+    // a block's place: the bytes of its quarters' rows, which of them are there
+    struct Block {
+      size_t at[BK];
+      bool there[BK];
+    };
+    auto next_block = [&](int c0) {
+      if (left % AT_ONCE == 0) {
+        pages = look_up(c0);
+        left = 0;
+      }
+      Block b;
 #pragma unroll
       for (int x = 0; x < BK; ++x) {
-        if (!there[x]) continue;
-        unsigned bits[RB];
+        const int page = __builtin_amdgcn_readlane(pages, left * BK + x);
+        b.there[x] = page >= 0;
+        b.at[x] = ((((size_t)max(page, 0) * p.Hkv + h) << p.bits) + ((c0 + 16 * x) & in_page)) * ROWB;
+      }
+      ++left;
+      return b;
+    };
+    // keys are asked for a block ahead, values before the block's logits are formed
+    typename O::Keys k;
+    Block to_come = next_block(lo + wave * COLS);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) bits[rb] = (1u << max(0, min(min(see[rb], hi) - c0 - 16 * x, 16))) - 1;
-        add_not_finite<T, D, RB>(o, p.v + at[x] + DPL * 4 * q4 * (int)sizeof(T), ROWB, max(0, min(16, hi - c0 - 16 * x)), bits);
+    for (int x = 0; x < BK; ++x) O::load_k(k, x, p.k + to_come.at[x], r * ROWB + q4 * 16);
+#pragma unroll 1
+    for (int c0 = lo + wave * COLS; c0 < hi; c0 += PA_WAVES * COLS) {
+      const Block now = to_come;
+      const auto& at = now.at;
+      const auto& there = now.there;
+      bool whole = c0 + COLS <= all_see;
+#pragma unroll
+      for (int x = 0; x < BK; ++x) whole &= there[x];
+      typename O::Values v;
+#pragma unroll
+      for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, p.v + at[j * BK / O::NCOL], (O::col(q4, j) & 15) * ROWB + r * DPL * (int)sizeof(T));
+      typename O::Logits x_of[RB];
+      typename O::Keys k_next;
+      to_come = next_block(c0 + PA_WAVES * COLS);
+#pragma unroll
+      for (int x = 0; x < BK; ++x) O::load_k(k_next, x, p.k + to_come.at[x], r * ROWB + q4 * 16);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) logits<D>(x_of[rb], k, q[rb]);
+      k = k_next;
+      bool odd = false;
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j)
+          if (!there[j * BK / O::NCOL] || c0 + O::col(q4, j) >= hi) O::clear_v(v, j);
+        odd = !all_finite<D>(v);
+        if (odd) drop_not_finite<D>(v);
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        typename O::Logits& x = x_of[rb];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) {
+          float& y = O::at(x, j);
+          y *= a.scale_log2e;
+          if (!whole && (!there[j * BK / O::NCOL] || c0 + O::col(q4, j) >= min(see[rb], hi))) y = -INFINITY;
+          mx = fmaxf(mx, y);
+        }
+        if constexpr (WEIGH) {
+          if (r < rows) {
+            float* keep = a.logits + (((size_t)run.b * p.Hkv + h) * a.rows + r) * p.cap + c0 + 4 * q4;
+#pragma unroll
+            for (int z = 0; z < BK; ++z)
+              if (c0 + 16 * z < hi) *reinterpret_cast<f32x4_t*>(keep + 16 * z) = x.x[z];
+          }
+        }
+        if (__any(mx > ref[rb] + 8.f)) {
+          mx = row_max(mx);
+          const float to = mx > ref[rb] + 8.f ? mx : ref[rb], f = fast_exp2(ref[rb] - to);
+          sum[rb] *= f;
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) o[rb][e] *= f;
+          ref[rb] = to;
+        }
+#pragma unroll
+        for (int j = 0; j < O::NCOL; ++j) {
+          float& y = O::at(x, j);
+          y = fast_exp2(y - ref[rb]);
+          sum[rb] += y;
+        }
+        add_rounded<D>(o[rb], v, x);
+      }
+      if (odd) {
+#pragma unroll
+        for (int x = 0; x < BK; ++x) {
+          if (!there[x]) continue;
+          unsigned bits[RB];
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) bits[rb] = (1u << max(0, min(min(see[rb], hi) - c0 - 16 * x, 16))) - 1;
+          add_not_finite<T, D, RB>(o, p.v + at[x] + DPL * 4 * q4 * (int)sizeof(T), ROWB, max(0, min(16, hi - c0 - 16 * x)), bits);
+        }
       }
     }
-  }
 
-  // the waves' sums, [wave][row][D], and references
-  float* so = pa_smem;
-  float2* sm = reinterpret_cast<float2*>(pa_smem + PA_WAVES * ROWS * OR);
+    // the waves' sums, [wave][row][D], and references
+    float* so = pa_smem;
+    float2* sm = reinterpret_cast<float2*>(pa_smem + PA_WAVES * ROWS * OR);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const float total = row_sum(sum[rb]);
-    float* row = so + ((size_t)wave * ROWS + rb * 16 + r) * OR;
+    for (int rb = 0; rb < RB; ++rb) {
+      const float total = row_sum(sum[rb]);
+      float* row = so + ((size_t)wave * ROWS + rb * 16 + r) * OR;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int e = 0; e < D / 16; e += 4)
-        *reinterpret_cast<float4*>(row + (4 * q4 + i) * DPL + e) = make_float4(o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]);
-    if (q4 == 0) sm[wave * ROWS + rb * 16 + r] = make_float2(ref[rb], total);
-  }
-  __syncthreads();
-  for (int x = tid; x < ROWS * (D / 4); x += PA_THREADS) {
-    const int y = x / (D / 4), c = x % (D / 4) * 4;
-    if (row0 + y >= rows) break;
-    float M = REF_NONE, L = 0.f;
-#pragma unroll
-    for (int z = 0; z < PA_WAVES; ++z) M = fmaxf(M, sm[z * ROWS + y].x);
-    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int z = 0; z < PA_WAVES; ++z) {
-      const float2 ml = sm[z * ROWS + y];
-      const float g = fast_exp2(ml.x - M);
-      const float4 u = *reinterpret_cast<const float4*>(so + ((size_t)z * ROWS + y) * OR + c);
-      L = fmaf(ml.y, g, L);
-      f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
+        for (int e = 0; e < D / 16; e += 4)
+          *reinterpret_cast<float4*>(row + (4 * q4 + i) * DPL + e) = make_float4(o[rb][e][i], o[rb][e + 1][i], o[rb][e + 2][i], o[rb][e + 3][i]);
+      if (q4 == 0) sm[wave * ROWS + rb * 16 + r] = make_float2(ref[rb], total);
     }
-    float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
-    if (c == 0 && (WEIGH || sh.count > 1)) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
-    if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = f;
-    else finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
+    __syncthreads();
+    for (int x = tid; x < ROWS * (D / 4); x += PA_THREADS) {
+      const int y = x / (D / 4), c = x % (D / 4) * 4;
+      if (row0 + y >= rows) break;
+      float M = REF_NONE, L = 0.f;
+#pragma unroll
+      for (int z = 0; z < PA_WAVES; ++z) M = fmaxf(M, sm[z * ROWS + y].x);
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int z = 0; z < PA_WAVES; ++z) {
+        const float2 ml = sm[z * ROWS + y];
+        const float g = fast_exp2(ml.x - M);
+        const float4 u = *reinterpret_cast<const float4*>(so + ((size_t)z * ROWS + y) * OR + c);
+        L = fmaf(ml.y, g, L);
+        f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
+      }
+      float* part = a.part + (((size_t)(w + run.b) * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
+      if (c == 0 && (WEIGH || run.count > 1)) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
+      if (run.count > 1) *reinterpret_cast<float4*>(part + c) = f;
+      else finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
+    }
+    __syncthreads();                                     // (the sums in LDS make way for the next sequence's)
   }
 }
 
 // Shares of a sequence added, MR rows a workgroup.  grid: row tiles of MR x KV heads x sequences.
 template <typename T, int D, int MR>
-__device__ inline void merge_rows(const Attend& a, const Seq& s, const Share& sh, int h, int row0) {
+__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
   const int rows = s.n * p.G;
@@ -354,11 +394,11 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Share& sh
     const int row = row0 + x / (D / 4), c = x % (D / 4) * 4;
     if (row >= rows) break;
     const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
-    const float* part = a.part + (((size_t)sh.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
+    const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
     float M = REF_NONE, L = 0.f;
-    for (int z = 0; z < sh.count; ++z) M = fmaxf(M, part[z * far + D]);
+    for (int z = 0; z < run.count; ++z) M = fmaxf(M, part[z * far + D]);
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z = 0; z < sh.count; ++z) {
+    for (int z = 0; z < run.count; ++z) {
       const float2 ml = *reinterpret_cast<const float2*>(part + z * far + D);
       const float g = fast_exp2(ml.x - M);
       const float4 u = *reinterpret_cast<const float4*>(part + z * far + c);
@@ -369,14 +409,14 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Share& sh
   }
 }
 template <typename T, int D, int MR>
-__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles) {
+__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, bool own) {
   const Pages& p = a.p;
   const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   if (tile * MR >= s.n * p.G) return;
-  Share sh;
-  if (!find_share(a, 0, b, sh) || sh.count <= 1) return;
-  merge_rows<T, D, MR>(a, s, sh, h, tile * MR);
+  Run run;
+  if (!find_run(a, share_size(a), own, 0, b, run) || run.count <= 1) return;
+  merge_rows<T, D, MR>(a, s, run, h, tile * MR);
 }
 
 // The same where the logits of up to 16 rows have been kept: beside the merge (the first piece), each workgroup adds the rows'
@@ -391,8 +431,8 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
   if (rows == 0 || c0 >= s.len) return;
-  Share sh;
-  if (!find_share(a, 0, b, sh)) return;
+  Run run;
+  if (!find_run(a, share_size(a), false, 0, b, run)) return;
   const int c = c0 + 4 * tid;
   const bool mine = c < s.len;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -403,8 +443,8 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
     float M = REF_NONE, L = 0.f;
     if (row < rows) {
       const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
-      const float* part = a.part + (((size_t)sh.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
-      for (int z = tid & 3; z < sh.count; z += 4) {
+      const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
+      for (int z = tid & 3; z < run.count; z += 4) {
         const float2 ml = *reinterpret_cast<const float2*>(part + z * far);
         const float to = fmaxf(M, ml.x);
         L = L * fast_exp2(M - to) + ml.y * fast_exp2(ml.x - to);
@@ -435,7 +475,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
     }
   }
-  if (piece == 0 && sh.count > 1) merge_rows<T, D, 16>(a, s, sh, h, 0);
+  if (piece == 0 && run.count > 1) merge_rows<T, D, 16>(a, s, run, h, 0);
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -532,14 +572,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   // the tiles of a KV head and share, the longest first, on one XCD, whose L2 then has their columns
   const int idx = (int)(blockIdx.x >> 3), group = idx / a.tiles * 8 + (int)(blockIdx.x & 7), tile = a.tiles - 1 - idx % a.tiles;
   const int h = group % p.Hkv, w = group / p.Hkv;
-  Share sh;
-  if (!find_share(a, w, -1, sh)) return;
-  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, sh.b);
+  const int size = share_size(a);
+  Run run;
+  if (!find_run(a, size, true, w, -1, run)) return;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
   const int rows = s.n * p.G, row0 = tile * TILED_ROWS;
   if (row0 >= rows) return;
   const int old = s.len - s.n;
   const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + TILED_ROWS, rows) - 1) / p.G + 1;
-  const int lo = sh.index * sh.size, hi = min(lo + sh.size, end);
+  const int lo = (w - run.first) * size, hi = min(lo + size, end);
   // logits are compared before they are scaled, so the scale's sign goes to the queries
   const float scale = fabsf(a.scale_log2e);
   const int row = row0 + wave * 32 + r, at_row = min(row, rows - 1), token = at_row / p.G, head = h * p.G + at_row - token * p.G;
@@ -556,7 +597,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   }
   f32x16_t o[DB] = {};
   float ref = REF_NONE, sum = 0.f, mx = -INFINITY;
-  const int32_t* table = p.table + (size_t)sh.b * p.width;
+  const int32_t* table = p.table + (size_t)run.b * p.width;
   const int in_page = (1 << p.bits) - 1;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem)) + wave * TILED_SUB * ROWB;
   unsigned from_k[COPIES], from_v[COPIES];
@@ -772,11 +813,11 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
     for (int z = 0; z < 4; ++z) {
       const int c = 32 * f + 8 * z + 4 * hf;
       const float4 u = make_float4(o[f][4 * z], o[f][4 * z + 1], o[f][4 * z + 2], o[f][4 * z + 3]);
-      if (sh.count > 1) *reinterpret_cast<float4*>(part + c) = u;
+      if (run.count > 1) *reinterpret_cast<float4*>(part + c) = u;
       else store4(a.out, at * D + c, any ? u : make_float4(0.f, 0.f, 0.f, 0.f), inv, uint16_t());
     }
   if (hf == 0) {
-    if (sh.count > 1) *reinterpret_cast<float2*>(part + D) = make_float2(ref, total);
+    if (run.count > 1) *reinterpret_cast<float2*>(part + D) = make_float2(ref, total);
     else finish_sums(a, at, ref, total);
   }
 }
@@ -915,7 +956,7 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   s.tiled = rows > 64 && c.dtype == TREEKV_BF16;
   s.rows = rows <= 16 ? 16 : s.tiled ? TILED_ROWS : 32;
   s.tiles = (int)((rows + s.rows - 1) / s.rows);
-  const long long groups = (long long)c.kv_heads * s.tiles, want = s.tiled ? 512 : 768;      // two, three workgroups a compute unit
+  const long long groups = (long long)c.kv_heads * s.tiles, want = 512;      // two workgroups a compute unit
   const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
   s.shares = (int)(groups >= want ? 1 : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
@@ -931,7 +972,8 @@ template <typename T, int D>
 int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream_t s) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
-  const unsigned pieces = (unsigned)(a.shares + (a.shares > 1 ? p.B : p.B - 1)), groups = pieces * p.Hkv;
+  // shares (of one sequence each: one more a sequence at most)
+  const unsigned groups = (unsigned)(sh.tiled ? a.shares + (a.shares > 1 ? p.B : p.B - 1) : a.shares) * p.Hkv;
   if (sh.tiled) {
     if constexpr (sizeof(T) == 2) {
       const int lds = 4 * TILE * D * 2;
@@ -953,8 +995,8 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
   }
   if (a.shares > 1) {
     const int rows = a.longest * p.G, all = (rows + (sh.rows == 16 ? 15 : 31)) / (sh.rows == 16 ? 16 : 32);
-    if (sh.rows == 16) hipLaunchKernelGGL((merge_kernel<T, D, 16>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
-    else hipLaunchKernelGGL((merge_kernel<T, D, 32>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
+    if (sh.rows == 16) hipLaunchKernelGGL((merge_kernel<T, D, 16>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
+    else hipLaunchKernelGGL((merge_kernel<T, D, 32>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
   }
   if (weigh) {
     if (sh.tiled) {
