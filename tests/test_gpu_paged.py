@@ -281,7 +281,8 @@ def evicted(binding, ref, *args, kv=None, **kw):
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("lens,budget,sink,recent,ps", [
     ([17], 16, 0, 0, 16), ([100, 16, 17, 0], 16, 4, 8, 16), ([300, 299, 31], 1, 0, 1, 16), ([2100, 1025, 40], 1024, 4, 512, 64),
-    ([5000], 33, 0, 0, 128), ([70, 90], 64, 60, 4, 32), ([50], 40, 0, 40, 16), ([9000, 700], 4500, 2, 3, 256)])
+    ([5000], 33, 0, 0, 128), ([70, 90], 64, 60, 4, 32), ([50], 40, 0, 40, 16), ([9000, 700], 4500, 2, 3, 256), ([4096, 4097], 4000, 4, 2000, 64),
+    ([16384, 16385], 300, 4, 100, 256), ([32768, 32769], 20000, 4, 10000, 256)])
 def test_evict(binding, lens, budget, sink, recent, ps, dtype, d):
     ref = paged(lens=lens, news=[0] * len(lens), page_size=ps, kv_heads=2, group=1, d=d, dtype=dtype, seed=20)
     import torch
@@ -299,10 +300,11 @@ def test_evict(binding, lens, budget, sink, recent, ps, dtype, d):
 
 
 @pytest.mark.parametrize("case", ["equal", "zeros", "nans", "infinite", "negative", "few values", "one bit"])
-def test_evict_order(binding, case):
+@pytest.mark.parametrize("lens", [[1500, 900], [10000, 5000], [30000, 33000]])
+def test_evict_order(binding, case, lens):
     import torch
 
-    ref = paged(lens=[1500, 900], news=[0, 0], page_size=16, kv_heads=2, group=1, d=64, seed=21)
+    ref = paged(lens=lens, news=[0, 0], page_size=256, kv_heads=2, group=1, d=64, seed=21)
     w, g = ref.weights, ref.g
     if case == "equal":
         w.fill_(0.25)
@@ -320,6 +322,8 @@ def test_evict_order(binding, case):
     else:
         w.copy_((torch.full(w.shape, 1.0).view(torch.int32) + torch.randint(0, 3, w.shape, generator=g).int()).view(torch.float32))
     evicted(binding, ref, 400, 4, 100)
+    if lens[0] > 2000:
+        evicted(binding, ref, 399, 4, 100)
 
 
 def test_evict_leaves_sequences_with_pages_given_up(binding):
