@@ -97,12 +97,14 @@ struct Attend {
   float* logits;                             // few rows and weights: scaled logits, [sequence][KV head][row][cap]
   int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
   float scale_log2e;
+  bool wide;                                 // more columns than 32 bits count
 };
 
 // The columns of all sequences with new tokens lie one after the other (each sequence's rounded up to whole blocks), and are cut
 // into shares of `size`.  Few rows: a workgroup takes one share, whatever sequences it runs through; what it has of sequence b is
-// partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round: a sequence's
-// shares start at its first token, so that each is of one sequence.
+// partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round, and the smallest shares,
+// where a second sequence would double the time: a sequence's shares start at its first token, so that each is of one
+// sequence (its `own`).
 struct Run {
   int b, length;             // a sequence with columns, and their number
   long long start;           // where they start
@@ -113,46 +115,74 @@ __device__ inline int tokens_to_read(const Attend& a, int b) {
   const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
   return s.n > 0 ? (s.len + 31) & ~31 : 0;
 }
-__device__ inline int share_size(const Attend& a) {
-  long long total = 0;
-  for (int b = threadIdx.x & 63; b < a.p.B; b += 64) total += tokens_to_read(a, b);
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) total += __shfl_xor(total, x, 64);
-  const long long each = (total + a.shares - 1) / a.shares;
-  return __builtin_amdgcn_readfirstlane((int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30));
-}
 __device__ inline long long uniform64(long long x) {
   return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
 }
-// The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
-__device__ inline bool find_run(const Attend& a, int size, bool own, long long at, int want_b, Run& run) {
+// Sums up to each lane, and the last one's; `wide`: past 32 bits.
+__device__ inline long long wave_scan(long long x, bool wide, long long& all) {
   const int lane = threadIdx.x & 63;
+  if (wide) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long y = __shfl_up(x, d, 64);
+      if (lane >= d) x += y;
+    }
+    all = uniform64(__shfl(x, 63, 64));
+    return x;
+  }
+  int v = (int)x;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);      // within 16 lanes (row_shr)
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int r0 = __builtin_amdgcn_readlane(v, 15), r1 = r0 + __builtin_amdgcn_readlane(v, 31), r2 = r1 + __builtin_amdgcn_readlane(v, 47);
+  v += lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2;
+  all = __builtin_amdgcn_readlane(v, 63);
+  return v;
+}
+// What find_run asks of the lengths: the size of a share, and this lane's sequence among the first 64.
+struct Columns {
+  int size, length;
+  __device__ bool own() const { return size == MIN_SHARE; }
+};
+__device__ inline Columns columns_of(const Attend& a) {
+  const int lane = threadIdx.x & 63;
+  Columns c;
+  c.length = tokens_to_read(a, lane);
+  long long total, mine = c.length;
+  for (int b = 64 + lane; b < a.p.B; b += 64) mine += tokens_to_read(a, b);
+  wave_scan(mine, a.wide, total);
+  const long long each = a.wide ? (total + a.shares - 1) / a.shares : (int)(((unsigned)total + a.shares - 1) / (unsigned)a.shares);
+  c.size = (int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30);
+  return c;
+}
+// The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
+__device__ inline bool find_run(const Attend& a, const Columns& c, bool own, long long at, int want_b, Run& run) {
+  const int lane = threadIdx.x & 63, size = c.size;
   long long before = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
-    const int length = tokens_to_read(a, b0 + lane);
-    const long long mine = own ? (length + size - 1) / size : length;
-    long long sum = mine;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const long long y = __shfl_up(sum, x, 64);
-      if (lane >= x) sum += y;
-    }
+    const int length = b0 ? tokens_to_read(a, b0 + lane) : c.length, mine = own ? (length + size - 1) / size : length;
+    long long all;
+    const long long sum = wave_scan(mine, a.wide, all);
     const unsigned long long hit = __ballot(want_b < 0 ? mine > 0 && before + sum > at : b0 + lane == want_b);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      run.b = __builtin_amdgcn_readfirstlane(b0 + l);
-      run.length = __builtin_amdgcn_readfirstlane(__shfl(length, l, 64));
-      run.start = uniform64(before + __shfl(sum - mine, l, 64));
+      run.b = b0 + l;
+      run.length = __builtin_amdgcn_readlane(length, l);
+      const long long start = sum - mine;
+      run.start = before + (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(start >> 32), l) << 32 |
+                                       (unsigned)__builtin_amdgcn_readlane((int)start, l));
       if (own) {
         run.first = (int)run.start;
         run.count = (run.length + size - 1) / size;
       } else {
-        run.first = (int)(run.start / size) + run.b;
-        run.count = run.length ? (int)((run.start + run.length - 1) / size) - (int)(run.start / size) + 1 : 0;
+        const int first = a.wide ? (int)(run.start / size) : (int)run.start / size;
+        run.first = first + run.b;
+        run.count = !run.length ? 0 : (a.wide ? (int)((run.start + run.length - 1) / size) : ((int)run.start + run.length - 1) / size) - first + 1;
       }
       return true;
     }
-    before += __shfl(sum, 63, 64);
+    before += all;
   }
   return false;
 }
@@ -205,18 +235,22 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   const int tile = (int)(blockIdx.x % a.tiles), rest = (int)(blockIdx.x / a.tiles), h = rest % p.Hkv, w = rest / p.Hkv;
   if (blockIdx.x == 0 && a.status)
     for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  const int size = share_size(a);
-  const long long share_end = (long long)(w + 1) * size;
+  const Columns columns = columns_of(a);
+  const int size = columns.size;
+  const bool own = columns.own();
+  const long long share_end = own ? w + 1 : (long long)(w + 1) * size;
   Run run;
 #pragma unroll 1
-  for (long long from = (long long)w * size; from < share_end && find_run(a, size, false, from, -1, run); from = run.start + run.length) {
+  for (long long from = own ? w : (long long)w * size; from < share_end && find_run(a, columns, own, from, -1, run);
+       from = own ? share_end : run.start + run.length) {
     const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
     const int rows = s.n * p.G, row0 = tile * ROWS;
     if (row0 >= rows) continue;
     const int old = s.len - s.n;
     // columns: what the tile's first row sees all rows see, behind what its last row sees there is nothing for it
     const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + ROWS, rows) - 1) / p.G + 1;
-    const int lo = (int)(from - run.start), hi = (int)min((long long)end, share_end - run.start);
+    const int lo = own ? (w - run.first) * size : (int)(from - run.start);
+    const int hi = (int)min((long long)end, own ? (long long)lo + size : share_end - run.start);
 
     typename O::Query q[RB];
     int see[RB];
@@ -375,7 +409,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
         L = fmaf(ml.y, g, L);
         f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
       }
-      float* part = a.part + (((size_t)(w + run.b) * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
+      float* part = a.part + (((size_t)(own ? w : w + run.b) * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
       if (c == 0 && (WEIGH || run.count > 1)) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
       if (run.count > 1) *reinterpret_cast<float4*>(part + c) = f;
       else finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
@@ -395,27 +429,44 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
     if (row >= rows) break;
     const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
     const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
+    constexpr int AT_ONCE = 8;                         // shares on their way together
     float M = REF_NONE, L = 0.f;
-    for (int z = 0; z < run.count; ++z) M = fmaxf(M, part[z * far + D]);
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z = 0; z < run.count; ++z) {
-      const float2 ml = *reinterpret_cast<const float2*>(part + z * far + D);
-      const float g = fast_exp2(ml.x - M);
-      const float4 u = *reinterpret_cast<const float4*>(part + z * far + c);
-      L = fmaf(ml.y, g, L);
-      f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
+    for (int z0 = 0; z0 < run.count; z0 += AT_ONCE) {
+      float2 ml[AT_ONCE];
+      float4 u[AT_ONCE];
+#pragma unroll
+      for (int z = 0; z < AT_ONCE; ++z) {
+        const float* at = part + min(z0 + z, run.count - 1) * far;
+        ml[z] = *reinterpret_cast<const float2*>(at + D);
+        u[z] = *reinterpret_cast<const float4*>(at + c);
+      }
+      float to = M;
+#pragma unroll
+      for (int z = 0; z < AT_ONCE; ++z) to = fmaxf(to, ml[z].x);
+      const float was = fast_exp2(M - to);
+      L *= was; f.x *= was; f.y *= was; f.z *= was; f.w *= was;
+      M = to;
+#pragma unroll
+      for (int z = 0; z < AT_ONCE; ++z) {
+        if (z0 + z >= run.count) break;
+        const float g = fast_exp2(ml[z].x - M);
+        L = fmaf(ml[z].y, g, L);
+        f.x = fmaf(u[z].x, g, f.x); f.y = fmaf(u[z].y, g, f.y); f.z = fmaf(u[z].z, g, f.z); f.w = fmaf(u[z].w, g, f.w);
+      }
     }
     finish_row<T, D>(a, s, h, row, c, f, M, L);
   }
 }
 template <typename T, int D, int MR>
-__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, bool own) {
+__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, bool tiled) {
   const Pages& p = a.p;
   const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   if (tile * MR >= s.n * p.G) return;
   Run run;
-  if (!find_run(a, share_size(a), own, 0, b, run) || run.count <= 1) return;
+  const Columns columns = columns_of(a);
+  if (!find_run(a, columns, tiled || columns.own(), 0, b, run) || run.count <= 1) return;
   merge_rows<T, D, MR>(a, s, run, h, tile * MR);
 }
 
@@ -432,7 +483,8 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
   if (rows == 0 || c0 >= s.len) return;
   Run run;
-  if (!find_run(a, share_size(a), false, 0, b, run)) return;
+  const Columns columns = columns_of(a);
+  if (!find_run(a, columns, columns.own(), 0, b, run)) return;
   const int c = c0 + 4 * tid;
   const bool mine = c < s.len;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -572,9 +624,10 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   // the tiles of a KV head and share, the longest first, on one XCD, whose L2 then has their columns
   const int idx = (int)(blockIdx.x >> 3), group = idx / a.tiles * 8 + (int)(blockIdx.x & 7), tile = a.tiles - 1 - idx % a.tiles;
   const int h = group % p.Hkv, w = group / p.Hkv;
-  const int size = share_size(a);
+  const Columns columns = columns_of(a);
+  const int size = columns.size;
   Run run;
-  if (!find_run(a, size, true, w, -1, run)) return;
+  if (!find_run(a, columns, true, w, -1, run)) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
   const int rows = s.n * p.G, row0 = tile * TILED_ROWS;
   if (row0 >= rows) return;
@@ -972,8 +1025,8 @@ template <typename T, int D>
 int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream_t s) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
-  // shares (of one sequence each: one more a sequence at most)
-  const unsigned groups = (unsigned)(sh.tiled ? a.shares + (a.shares > 1 ? p.B : p.B - 1) : a.shares) * p.Hkv;
+  // shares (where they are of one sequence each, one more a sequence at most)
+  const unsigned groups = (unsigned)(a.shares + (a.shares > 1 ? p.B : p.B - 1)) * p.Hkv;
   if (sh.tiled) {
     if constexpr (sizeof(T) == 2) {
       const int lds = 4 * TILE * D * 2;
@@ -1048,6 +1101,7 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.lse = lse;
   a.status = status;
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
+  a.wide = (long long)c.batch * (a.p.cap + 31) > 1 << 30;
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
   if (c.dtype == TREEKV_F32) return c.head_dim == 128 ? launch_attend_d<float, 128>(a, sh, weigh, s) : launch_attend_d<float, 64>(a, sh, weigh, s);
   return c.head_dim == 128 ? launch_attend_d<uint16_t, 128>(a, sh, weigh, s) : launch_attend_d<uint16_t, 64>(a, sh, weigh, s);

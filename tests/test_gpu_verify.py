@@ -64,7 +64,7 @@ def check(binding, *case):
 
 @pytest.mark.parametrize("drawn", [True, False])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("B,n,V", [(1, 1, 1), (2, 1, 2), (5, 3, 7), (40, 9, 33), (3, 26, 4096), (2, 64, 5003), (16, 5, 32001), (1, 256, 129), (2, 7, 160001)])
+@pytest.mark.parametrize("B,n,V", [(1, 1, 1), (2, 1, 2), (5, 3, 7), (40, 9, 33), (3, 26, 4096), (2, 64, 5003), (16, 5, 32001), (1, 256, 129), (2, 7, 160001), (3, 40, 65537)])
 def test_trees(binding, B, n, V, dtype, drawn):
     check(binding, *inputs(B, n, V, dtype=dtype, drawn=drawn, seed=n + V))
 
@@ -75,44 +75,48 @@ def test_chains_near_and_far_from_the_target(binding, near):
     assert (int(length.sum()) > 400) if near < 1 else (int(length.min()) == 0)
 
 
-def test_many_siblings_refused(binding):
+@pytest.mark.parametrize("V", [300, 70000])
+def test_many_siblings_refused(binding, V):
     """A flat tree whose drafter is far off: refusal after refusal of the same row."""
     import torch
 
-    target, draft, tokens, parents, u = inputs(12, 40, 300, near=8.0, seed=3)
+    target, draft, tokens, parents, u = inputs(12, 40, V, near=8.0, seed=3)
     parents.fill_(-1)
     for b in range(12):
         tokens[b] = torch.multinomial(draft[b, 0].float(), 40, replacement=True, generator=torch.Generator().manual_seed(b)).int()
     u.clamp_(min=0.9)
     _, length, _ = check(binding, target, draft, tokens, parents, u)
     assert int((length == 0).sum()) > 0
-    _, length, _ = check(binding, target, None, torch.stack([torch.randperm(300)[:40].int() for _ in range(12)]), parents, u)
+    g = torch.Generator().manual_seed(9)
+    check(binding, target, None, torch.stack([torch.randperm(V, generator=g)[:40].int() for _ in range(12)]), parents, u)
 
 
+@pytest.mark.parametrize("V", [1000, 66000])
 @pytest.mark.parametrize("u", [0.0, 1.0 - 2.0 ** -24, 1.0, 2.0, -1.0, math.nan])
-def test_uniforms_at_the_ends(binding, u):
+def test_uniforms_at_the_ends(binding, u, V):
     for drawn in (True, False):
-        target, draft, tokens, parents, uniforms = inputs(4, 6, 1000, drawn=drawn, seed=4)
+        target, draft, tokens, parents, uniforms = inputs(4, 6, V, drawn=drawn, seed=4)
         uniforms[:, -1] = u
         check(binding, target, draft, tokens, parents, uniforms)
         uniforms.fill_(u)
         check(binding, target, draft, tokens, parents, uniforms)
 
 
-def test_equal_distributions_and_rows_of_nothing(binding):
+@pytest.mark.parametrize("V", [64, 65536])
+def test_equal_distributions_and_rows_of_nothing(binding, V):
     import torch
 
-    target, draft, tokens, parents, u = inputs(8, 4, 64, seed=5)
+    target, draft, tokens, parents, u = inputs(8, 4, V, seed=5)
     u[:, :-1] = 1.0                                           # u Q(x) < P(x) fails for P = Q: nothing is left, P stays
     check(binding, target, target.clone(), tokens, parents, u)
     target[2, 0], target[3], draft[5, 0] = 0.0, math.nan, 0.0
     target[6, 0] = -1.0
     path, length, follows = check(binding, target, draft, tokens, parents, u)
     assert follows[2] == -1 and follows[3] == -1 and follows[6] == -1
-    one = torch.zeros(8, 5, 64)
-    one[:, :, 63] = 1.0                                       # everything at the last token
+    one = torch.zeros(8, 5, V)
+    one[:, :, V - 1] = 1.0                                    # everything at the last token
     _, _, follows = check(binding, one, None, tokens, parents, u)
-    assert bool((follows == 63).all())
+    assert bool((follows == V - 1).all())
 
 
 def test_tokens_and_parents_that_are_none(binding):
@@ -123,14 +127,15 @@ def test_tokens_and_parents_that_are_none(binding):
     assert length[2] == 0 and length[3] == 0
 
 
-def test_the_drawn_token_over_all_of_the_row(binding):
+@pytest.mark.parametrize("V", [1031, 66047])
+def test_the_drawn_token_over_all_of_the_row(binding, V):
     """With nothing accepted the uniform number alone says which token follows: each token's share of [0, 1)."""
     import torch
 
-    V = 1031
     p = torch.softmax(torch.randn(1, 2, V, generator=torch.Generator().manual_seed(7)), dim=2)
+    at = torch.tensor([0, 1, 255, 256, 511, 512, 777, V - 2, V - 1])
+    p[0, 0, at] += 8 * float(p.max())                         # (wide enough for fp32 uniforms to fall into)
     cdf = p[0, 0].double().cumsum(0)
-    at = torch.tensor([0, 1, 255, 256, 511, 512, 777, 1029, 1030])
     middle = ((cdf[at] - p[0, 0, at].double() / 2) / cdf[-1]).float()
     u = torch.stack([torch.zeros(9), middle], dim=1)
     parents = torch.full((9, 1), -2, dtype=torch.int32)
