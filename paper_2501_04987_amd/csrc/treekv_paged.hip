@@ -15,6 +15,10 @@
 #include "treekv_matrix.h"
 #include "treekv_paged.h"
 
+// Multiply-adds only where they are written: a logit has to be rounded like the reference that it was compared to (fused with the
+// subtraction of the reference it would differ by what the reference lost, 2^7 from 2^31 on).
+#pragma clang fp contract(off)
+
 namespace tkv {
 
 namespace {
@@ -418,15 +422,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   }
 }
 
-// Shares of a sequence added, MR rows a workgroup.  grid: row tiles of MR x KV heads x sequences.
-template <typename T, int D, int MR>
-__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0) {
+// Shares of a sequence added, four dimensions of a row a thread.  grid: tiles of MERGE_ROWS rows x KV heads x sequences.
+template <int D> constexpr int MERGE_ROWS = PA_THREADS * 4 / D;
+template <typename T, int D>
+__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0, int end) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
   const int rows = s.n * p.G;
-  for (int x = threadIdx.x; x < MR * (D / 4); x += PA_THREADS) {
-    const int row = row0 + x / (D / 4), c = x % (D / 4) * 4;
-    if (row >= rows) break;
+  for (int row = row0 + (int)threadIdx.x / (D / 4); row < min(end, rows); row += MERGE_ROWS<D>) {
+    const int c = (int)threadIdx.x % (D / 4) * 4;
     const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
     const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
     constexpr int AT_ONCE = 8;                         // shares on their way together
@@ -458,16 +462,16 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
     finish_row<T, D>(a, s, h, row, c, f, M, L);
   }
 }
-template <typename T, int D, int MR>
+template <typename T, int D>
 __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, bool tiled) {
   const Pages& p = a.p;
   const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  if (tile * MR >= s.n * p.G) return;
+  if (tile * MERGE_ROWS<D> >= s.n * p.G) return;
   Run run;
   const Columns columns = columns_of(a);
   if (!find_run(a, columns, tiled || columns.own(), 0, b, run) || run.count <= 1) return;
-  merge_rows<T, D, MR>(a, s, run, h, tile * MR);
+  merge_rows<T, D>(a, s, run, h, tile * MERGE_ROWS<D>, (tile + 1) * MERGE_ROWS<D>);
 }
 
 // The same where the logits of up to 16 rows have been kept: beside the merge (the first piece), each workgroup adds the rows'
@@ -514,20 +518,22 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   __syncthreads();
   if (mine) {
     const float* x = a.logits + ((size_t)b * p.Hkv + h) * a.rows * p.cap + c;
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int row = 0; row < rows; ++row) {
       const float4 y = *reinterpret_cast<const float4*>(x + (size_t)row * p.cap);
       const float l = log_sum[row];
       // (a NaN adds nothing)
-      w.x += fmaxf(fast_exp2(y.x - l), 0.f); w.y += fmaxf(fast_exp2(y.y - l), 0.f);
-      w.z += fmaxf(fast_exp2(y.z - l), 0.f); w.w += fmaxf(fast_exp2(y.w - l), 0.f);
+      f.x += fmaxf(fast_exp2(y.x - l), 0.f); f.y += fmaxf(fast_exp2(y.y - l), 0.f);
+      f.z += fmaxf(fast_exp2(y.z - l), 0.f); f.w += fmaxf(fast_exp2(y.w - l), 0.f);
     }
+    w.x += f.x; w.y += f.y; w.z += f.z; w.w += f.w;          // (once: a weight is large beside what it gains)
     if (c + 4 <= s.len) *reinterpret_cast<float4*>(weights) = w;
     else {
       const float z[4] = {w.x, w.y, w.z, w.w};
       for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
     }
   }
-  if (piece == 0 && run.count > 1) merge_rows<T, D, 16>(a, s, run, h, 0);
+  if (piece == 0 && run.count > 1) merge_rows<T, D>(a, s, run, h, 0, 16);
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -570,7 +576,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
       logits<D>(x, k[nb], q);
 #pragma unroll
       for (int j = 0; j < O::NCOL; ++j) {
-        const float y = fmaxf(fast_exp2(fmaf(O::at(x, j), a.scale_log2e, -to.x)), 0.f);     // (of a NaN 0)
+        const float logit = O::at(x, j) * a.scale_log2e, y = fmaxf(fast_exp2(logit - to.x), 0.f);       // (of a NaN 0)
         acc[nb][j] += c0 + nb * COLS + O::col(q4, j) < see ? y * to.y : 0.f;
       }
     }
@@ -611,6 +617,9 @@ __device__ inline void async_copy16_at(const char* base, unsigned offset, unsign
 }
 
 constexpr int TILED_ROWS = PA_WAVES * 32;
+// An exponential's argument is one multiply-add, logit * scale - reference, which is off by what the reference was rounded by.  Past
+// this size that would tell (from 2^31 on it can be 2^7), and the logit is rounded before it like the reference.
+constexpr float LARGE = 1 << 20;
 
 template <int D>
 __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
@@ -650,6 +659,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   }
   f32x16_t o[DB] = {};
   float ref = REF_NONE, sum = 0.f, mx = -INFINITY;
+  bool large = false;                                  // a reference of the wave is
   const int32_t* table = p.table + (size_t)run.b * p.width;
   const int in_page = (1 << p.bits) - 1;
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem)) + wave * TILED_SUB * ROWB;
@@ -756,14 +766,21 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
       }
       odd = __syncthreads_or(mine);
     }
-      if (__any(mx > ref + 8.f)) {
-        const float top = fmaxf(mx, other_half(mx));
-        const float to = top > ref + 8.f ? top : ref, f = fast_exp2(ref - to);
-        sum *= f;
+    if (__any(mx > ref + 8.f)) {
+      const float top = fmaxf(mx, other_half(mx));
+      const float to = top > ref + 8.f ? top : ref, f = fast_exp2(ref - to);
+      sum *= f;
 #pragma unroll
-        for (int e = 0; e < DB; ++e) o[e] *= f;
-        ref = to;
-      }
+      for (int e = 0; e < DB; ++e) o[e] *= f;
+      ref = to;
+      large = __any(fabsf(ref) > LARGE);
+    }
+    float by = scale;
+    if (large) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] *= scale;
+      by = 1.f;
+    }
     // Probabilities of this tile beside the logits of the next (of what is behind the last one: not used), 16 columns of all rows
     // after the other; three of these four groups beside the first products.  A step forms some exponentials, the arguments of the
     // next step's, and takes in those of the last step; operands are read AHEAD steps before.
@@ -778,7 +795,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
       const uint2 u0 = read_turned(src), u1 = read_turned(src + 8 * ROWB);
       return make_uint4(u0.x, u0.y, u1.x, u1.y);
     };
-    auto argument = [&](int i) { const int g = i / GROUP; arg[i] = fmaf(x[g >> 1][8 * (g & 1) + i % 8], scale, -ref); };
+    auto argument = [&](int i) { const int g = i / GROUP; arg[i] = fmaf(x[g >> 1][8 * (g & 1) + i % 8], by, -ref); };
     auto take = [&](int i) {
       const int g = i / GROUP;
       sum += e[i];
@@ -962,9 +979,15 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
       f32x16_t x = {};
 #pragma unroll
       for (int e = 0; e < KS; ++e) x = mfma_wide(k[e], *reinterpret_cast<const uint4*>(q + y * 32 * ROWB + (from ^ (e << 5))), x);
+      float by = scale;
+      if (__any(fabsf(now[y].x) > LARGE && now[y].y > 0.f)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= scale;
+        by = 1.f;
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float e = fmaxf(fast_exp2(fmaf(x[i], scale, -now[y].x)), 0.f);        // (of a NaN 0)
+        float e = fmaxf(fast_exp2(fmaf(x[i], by, -now[y].x)), 0.f);        // (of a NaN 0)
         if (masked && 8 * (i >> 2) + 4 * hf + (i & 3) >= sees[y]) e = 0.f;
         acc[i] = fmaf(e, now[y].y, acc[i]);
       }
@@ -1047,9 +1070,8 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
     return finish_launch();
   }
   if (a.shares > 1) {
-    const int rows = a.longest * p.G, all = (rows + (sh.rows == 16 ? 15 : 31)) / (sh.rows == 16 ? 16 : 32);
-    if (sh.rows == 16) hipLaunchKernelGGL((merge_kernel<T, D, 16>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
-    else hipLaunchKernelGGL((merge_kernel<T, D, 32>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
+    const int all = (a.longest * p.G + MERGE_ROWS<D> - 1) / MERGE_ROWS<D>;
+    hipLaunchKernelGGL((merge_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
   }
   if (weigh) {
     if (sh.tiled) {

@@ -80,7 +80,7 @@ class Paged:
                     x = q[lo + i, h * self.G:(h + 1) * self.G].double()
                     s = x @ k.T * self.scale
                     # a logit is a sum of d products, scaled, in fp32; its error is that of its exponential and of the sums
-                    d_logit = (self.d + 8) * tiny * ((x.abs() @ k.abs().T).amax(dim=1) * self.scale + s.abs().amax(dim=1))
+                    d_logit = (self.d + 8) * tiny * ((x.abs() @ k.abs().T).amax(dim=1) * abs(self.scale) + s.abs().amax(dim=1))
                     total = torch.logsumexp(s, dim=1)
                     p = torch.exp(s - total[:, None])
                     # exponentials and sums of up to L terms in fp32, the reference's changes and the merges among them

@@ -60,6 +60,9 @@ SHAPES = [
     dict(lens=[600, 31], news=[130, 31], page_size=16, kv_heads=1, group=2, d=64),
     dict(lens=[16, 32, 48, 1, 2, 3, 15, 17] * 9, news=[1, 2, 0, 1, 1, 3, 2, 1] * 9, page_size=16, kv_heads=1, group=2, d=64),
     dict(lens=[1300], news=[40], page_size=128, kv_heads=1, group=16, d=128, scale=0.3),
+    dict(lens=[700, 90], news=[1, 1], page_size=16, kv_heads=2, group=3, d=64, scale=-0.2),
+    dict(lens=[200, 333], news=[200, 50], page_size=32, kv_heads=2, group=4, d=64, scale=-0.2),
+    dict(lens=[2900], news=[70], page_size=32, kv_heads=1, group=2, d=128),
 ]
 
 
@@ -132,6 +135,38 @@ def test_what_is_not_attended_has_no_part(binding, new, group, dtype):
         else:
             same = got[..., 5].isnan() if math.isnan(bad) else got[..., 5] == bad
             assert bool(same.all()) and bool(got[..., :5].isfinite().all()) and torch.equal(lse[i:], lse0[i:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 20, 200])
+@pytest.mark.parametrize("power", [22, 40])
+def test_logits_of_any_size(binding, power, new, dtype):
+    """Queries scaled by 2^22 and 2^40: one token has all of the weight, exactly, whatever its logit's last bits are."""
+    import torch
+
+    ref = paged(lens=[333], news=[new], page_size=16, kv_heads=1, group=2, d=64, dtype=dtype, seed=7)
+    q = (ref.q.double() * 2.0 ** power).to(ref.t)
+    kv = ref.on_gpu(binding)
+    before = kv.weights.clone()
+    lse = torch.empty(new, 2, device="cuda")
+    out = kv.attend(q.cuda(), ref.starts.cuda(), new, None, lse, weigh=True).cpu()
+    K, V = [ref.tokens(pool, 0, 0, 333)[0] for pool in (ref.k, ref.v)]
+    s = (q.double() @ K.T) * ref.scale
+    s = s.masked_fill(torch.arange(333) > (333 - new + torch.arange(new))[:, None, None], -math.inf)
+    two = s.topk(2, dim=2).values
+    sure = two[..., 0] - two[..., 1] > 2.0 ** -16 * two[..., 0].abs()       # no near tie: d + 8 roundings of 2^-24 of the terms' size
+    top = s.argmax(dim=2)
+    assert int(sure.sum()) > 0.9 * sure.numel()
+    assert torch.equal(out[sure], V.to(ref.t)[top][sure])
+    assert bool(((lse.cpu().double() - two[..., 0]).abs() <= 2.0 ** -16 * two[..., 0].abs())[sure].all())
+    gain = (kv.weights - before)[0, 0, :333].cpu().double()
+    want = torch.zeros(333, dtype=torch.float64)
+    for t in top[sure].tolist():
+        want[t] += 1
+    doubt = int((~sure).sum())
+    # (the weights began below 1: a gain is good to the roundings of sums up to 2 * new)
+    room = (2 * new + 2) ** 2 * 2.0 ** -24
+    assert bool((gain >= want - room).all()) and bool((gain <= want + doubt + room).all()) and abs(float(gain.sum()) - 2 * new) < 333 * room
 
 
 def test_weights_take_no_nan(binding):

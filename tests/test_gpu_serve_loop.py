@@ -119,6 +119,47 @@ def test_a_captured_step_replayed(binding):
             assert torch.equal(getattr((a, b)[i % 2], name), getattr(twin, name)), (i, name)
 
 
+@pytest.mark.parametrize("weigh", [False, True])
+def test_captured_chunks_and_long_vocabularies(binding, weigh):
+    """The kernels of many rows and the passes by several workgroups, captured and replayed beside eager calls."""
+    import torch
+
+    from tests.serve_reference import Paged
+
+    ref = Paged(lens=[150, 260], news=[150, 90], page_size=16, kv_heads=2, group=2, d=128, seed=14)
+    a, b = ref.on_gpu(binding), ref.on_gpu(binding)
+    starts, q = ref.starts.cuda(), torch.zeros_like(ref.q, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(15)
+    V = 70001
+    target, draft, u = torch.zeros(2, 7, V, device="cuda"), torch.zeros(2, 7, V, device="cuda"), torch.zeros(2, 7, device="cuda")
+    tokens, parents = torch.zeros(2, 6, dtype=torch.int32, device="cuda"), torch.tensor([[-1, -1, 0, 0, 2, 2]] * 2, dtype=torch.int32, device="cuda")
+    new = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    outs = [(torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda"), new(2, 6), new(2), new(2)) for _ in "ab"]
+    scratch, more = a.new_attend_scratch(ref.total, 150, weigh), binding.tree_verify_scratch(target, draft)
+
+    def step(kv, out, lse, path, length, follows):
+        kv.attend(q, starts, 150, out, lse, weigh=weigh, scratch=scratch)
+        binding.tree_verify(target, tokens, parents, u, path, length, follows, draft=draft, scratch=more)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        step(a, *outs[0])
+    for _ in range(5):
+        q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+        x = 2 * torch.randn(target.shape, generator=g, device="cuda")
+        target.copy_(torch.softmax(x, dim=2))
+        draft.copy_(torch.softmax(x + torch.randn(x.shape, generator=g, device="cuda"), dim=2))
+        tokens.copy_(torch.multinomial(draft[:, 0], 6, generator=g))
+        u.copy_(torch.rand(u.shape, generator=g, device="cuda"))
+        graph.replay()
+        step(b, *outs[1])
+        torch.cuda.synchronize()
+        for y, z in zip(*outs):
+            assert torch.equal(y, z)
+        assert torch.equal(a.weights, b.weights)
+
+
 def test_drafted_chains_over_pages(binding):
     """A chain of drafted tokens is appended and attended as a chunk; what is not accepted is taken back by its length."""
     import torch
