@@ -909,7 +909,7 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
   if (s.n == 0 || first_col >= s.len) return;
   const int32_t* table = p.table + (size_t)b * p.width;
-  const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
+  const int in_page = (1 << p.bits) - 1, old = s.len - s.n;
   uint4 k[KS];
   {
     const int c = c0 + r, page = c < s.len ? table[c >> p.bits] : -1;
@@ -918,55 +918,48 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
     for (int y = 0; y < KS; ++y) k[y] = *reinterpret_cast<const uint4*>(p.k + at + y * 32);
   }
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(pt_smem)) + wave * TILED_SUB * ROWB;
-  // A row as (token, head of the group), which goes on from tile to tile by whole tokens and a rest: no division in the loop.
-  // Rows behind the last are the last one.
-  struct Place {
-    int token, g;
-  };
-  const int step = TILE / p.G, rest = TILE - step * p.G;
-  auto onwards = [&](Place& x) {
-    x.token += step;
-    x.g += rest;
-    if (x.g >= p.G) { x.g -= p.G; ++x.token; }
-  };
-  auto place = [&](int row) { Place x = {row / p.G, row % p.G}; return x; };
-  const int first = max(0, first_col - old) * p.G / TILE * TILE;
+  // A tile holds whole tokens, so that its rows lie the same way from its first token on: their places are worked out once.
+  const int per = TILE / p.G;                          // tokens
   const char* q0 = a.q + s.first * a.q_far + (size_t)h * p.G * ROWB;
   const float2* stat0 = a.stat + (size_t)s.first * p.H + h * p.G;
-  Place from[COPIES], stats[2];
-  unsigned piece[COPIES];
+  int token_of[COPIES];
+  unsigned from[COPIES];                               // the piece of its row, without the token
 #pragma unroll
   for (int j = 0; j < COPIES; ++j) {
-    const int x = j * AT_ONCE + lane / PIECES;
-    from[j] = place(first + wave * TILED_SUB + x);
-    piece[j] = ((lane % PIECES) ^ swap_k<D>(x)) << 4;
+    const int x = j * AT_ONCE + lane / PIECES, row = wave * TILED_SUB + x;
+    token_of[j] = min(row / p.G, per - 1);             // (behind the tile's rows: any)
+    from[j] = row % p.G * ROWB + (((lane % PIECES) ^ swap_k<D>(x)) << 4);
   }
+  auto request = [&](int first, int stage) {
+    const char* base = q0 + first * a.q_far;
+    const int last = s.n - 1 - first;
 #pragma unroll
-  for (int y = 0; y < 2; ++y) stats[y] = place(first + 32 * y + r);
-  auto request = [&](int stage) {
-#pragma unroll
-    for (int j = 0; j < COPIES; ++j) {
-      const bool in = from[j].token < s.n;
-      async_copy16(q0 + (in ? from[j].token : s.n - 1) * a.q_far + (in ? from[j].g : 0) * ROWB + piece[j], lds0 + stage * STAGE + j * 1024);
-      onwards(from[j]);
-    }
+    for (int j = 0; j < COPIES; ++j)
+      async_copy16_at(base, (unsigned)min(token_of[j], last) * (unsigned)a.q_far + from[j], lds0 + stage * STAGE + j * 1024);
   };
+  int my_token[2], my_stat[2];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int row = 32 * y + r;
+    my_token[y] = row / p.G < per ? row / p.G : s.n;   // (behind the tile's rows: no token)
+    my_stat[y] = min(row / p.G, per - 1) * p.H + row % p.G;
+  }
   float2 l[2];
   int see[2];
-  auto next_stats = [&]() {                           // rows behind the last: exponentials of minus infinity
+  auto stats = [&](int first) {                        // rows of no token: exponentials of minus infinity
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const bool in = stats[y].token < s.n;
-      const float2 u = stat0[(size_t)(in ? stats[y].token : 0) * p.H + (in ? stats[y].g : 0)];
+      const bool in = my_token[y] < s.n - first;
+      const float2 u = stat0[(size_t)first * p.H + (in ? my_stat[y] : 0)];
       l[y] = in ? u : make_float2(INFINITY, 0.f);
-      see[y] = old + stats[y].token + 1 - c0;
-      onwards(stats[y]);
+      see[y] = old + first + my_token[y] + 1 - c0;
     }
   };
   f32x16_t acc = {};
-  request(0);
-  next_stats();
-  int stage = 0, token = first / p.G;                 // of the tile's first row, rounded down
+  const int begin = max(0, first_col - old);           // tokens before see none of the columns
+  request(begin, 0);
+  stats(begin);
+  int stage = 0;
   const unsigned at_q = r * ROWB + ((hf ^ swap_k<D>(r)) << 4);        // of step e: XOR 2 e pieces
   struct Yes { __device__ constexpr operator bool() const { return true; } };
   struct No { __device__ constexpr operator bool() const { return false; } };
@@ -994,17 +987,17 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
     }
   };
 #pragma unroll 1
-  for (int row0 = first; row0 < rows; row0 += TILE, stage ^= 1, token += step) {
+  for (int first = begin; first < s.n; first += per, stage ^= 1) {
     wait_vmcnt<0>();
     __syncthreads();
     const float2 now[2] = {l[0], l[1]};
     const int sees[2] = {see[0], see[1]};
-    if (row0 + TILE < rows) {
-      request(stage ^ 1);
-      next_stats();
+    if (first + per < s.n) {
+      request(first + per, stage ^ 1);
+      stats(first + per);
     }
     const char* q = pt_smem + stage * STAGE;
-    if (old + token + 1 >= c0 + 32) tile(q, now, sees, No());       // (`token` falls behind where G does not divide a tile)
+    if (old + first + 1 >= c0 + 32) tile(q, now, sees, No());
     else tile(q, now, sees, Yes());
   }
   float* weights = p.weights + track_row(p, b, h);
@@ -1022,7 +1015,7 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
 // ---- launches ----------------------------------------------------------------------------------
 struct AttendShape {
   int rows, tiles, shares;                   // rows of a tile
-  bool tiled, keep;                          // many rows through LDS; logits kept for the weights
+  bool tiled, keep, weigh_tiled;             // many rows through LDS; logits kept for the weights; weights of many rows through LDS
   size_t part, logits, stat;                 // bytes of scratch: shares' results, logits, rows' references and sums
 };
 AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
@@ -1037,6 +1030,8 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   s.shares = (int)(groups >= want ? 1 : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
   // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them
+  // (what that asks of the query rows' distance, the launch adds)
+  s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
   s.keep = weigh && rows <= 16 && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
   s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
   s.logits = s.keep ? align_up((size_t)units * s.rows * cap * 4) : 0;
@@ -1074,7 +1069,7 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
     hipLaunchKernelGGL((merge_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
   }
   if (weigh) {
-    if (sh.tiled) {
+    if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)
       if constexpr (sizeof(T) == 2) {
         const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
         hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3((units + 7) / 8 * 8 * all), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);

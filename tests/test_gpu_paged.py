@@ -63,6 +63,8 @@ SHAPES = [
     dict(lens=[700, 90], news=[1, 1], page_size=16, kv_heads=2, group=3, d=64, scale=-0.2),
     dict(lens=[200, 333], news=[200, 50], page_size=32, kv_heads=2, group=4, d=64, scale=-0.2),
     dict(lens=[2900], news=[70], page_size=32, kv_heads=1, group=2, d=128),
+    dict(lens=[90, 70], news=[20, 33], page_size=16, kv_heads=1, group=33, d=64),
+    dict(lens=[60, 50], news=[3, 4], page_size=16, kv_heads=1, group=70, d=64),
 ]
 
 
@@ -73,6 +75,17 @@ def test_attend(binding, shape, dtype):
     kv = ref.on_gpu(binding)
     check_attend(kv, ref, weigh=True)
     check_attend(kv, ref, weigh=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_queries_far_apart(binding, dtype):
+    """Tokens 16 MB apart: their places in a tile pass 32 bits."""
+    import torch
+
+    ref = paged(lens=[90], news=[70], page_size=16, kv_heads=1, group=2, d=64, dtype=dtype, seed=3)
+    wide = torch.empty(70, 1 << 24, dtype=ref.t, device="cuda")
+    wide[:, :128] = ref.q.view(70, 128).cuda()
+    check_attend(ref.on_gpu(binding), ref, q=wide[:, :128].unflatten(1, (2, 64)), weigh=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
