@@ -36,6 +36,20 @@ __device__ inline float row_sum(float v) {
 }
 
 
+// 8 and 16 bytes; ONCE: past the caches, which nobody asks for them again.
+template <bool ONCE>
+__device__ inline uint4 load16(const void* p) {
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  if constexpr (ONCE) return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p)));
+  else return *reinterpret_cast<const uint4*>(p);
+}
+template <bool ONCE>
+__device__ inline uint2 load8(const void* p) {
+  typedef unsigned v2u __attribute__((ext_vector_type(2)));
+  if constexpr (ONCE) return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const v2u*>(p)));
+  else return *reinterpret_cast<const uint2*>(p);
+}
+
 // Operands by storage type.  COLS: columns of a block.  Parts: bf16 parts of a turned value.
 template <typename T, int D> struct Ops;
 
@@ -49,10 +63,11 @@ struct Ops<uint16_t, D> {
 #pragma unroll
     for (int s = 0; s < KS; ++s) k.x[bk][s] = *reinterpret_cast<const uint4*>(base + row + s * 64);
   }
+  template <bool ONCE = false>
   __device__ static inline void load_v(Values& v, int j, const char* base, unsigned row) {
-    if constexpr (D == 128) v.x[j] = *reinterpret_cast<const uint4*>(base + row);
+    if constexpr (D == 128) v.x[j] = load16<ONCE>(base + row);
     else {
-      const uint2 r = *reinterpret_cast<const uint2*>(base + row);
+      const uint2 r = load8<ONCE>(base + row);
       v.x[j] = make_uint4(r.x, r.y, 0, 0);
     }
   }
@@ -87,10 +102,11 @@ struct Ops<float, D> {
 #pragma unroll
     for (int s = 0; s < KS; ++s) k.x[0][s] = *reinterpret_cast<const float4*>(base + row + s * 64);
   }
+  template <bool ONCE = false>
   __device__ static inline void load_v(Values& v, int j, const char* base, unsigned row) {
 #pragma unroll
     for (int e = 0; e < DPL; e += 4) {
-      const float4 r = *reinterpret_cast<const float4*>(base + row + e * 4);
+      const float4 r = __builtin_bit_cast(float4, load16<ONCE>(base + row + e * 4));
       v.x[j][e] = r.x; v.x[j][e + 1] = r.y; v.x[j][e + 2] = r.z; v.x[j][e + 3] = r.w;
     }
   }

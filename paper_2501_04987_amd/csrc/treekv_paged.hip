@@ -304,7 +304,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
       ++left;
       return b;
     };
-    // keys are asked for a block ahead, values before the block's logits are formed
+    // keys are asked for a block ahead, values before the block's logits are formed; up to 16 rows are one tile, whose values nobody
+    // else reads (past the caches 16 sequences of 16000 tokens take 117 us in place of 130, with weights 154 in place of 164; the keys
+    // too: 116 and 160, and 45 in place of 41 where 134 MB lie in the memory-side cache)
     typename O::Keys k;
     Block to_come = next_block(lo + wave * COLS);
 #pragma unroll
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
       for (int x = 0; x < BK; ++x) whole &= there[x];
       typename O::Values v;
 #pragma unroll
-      for (int j = 0; j < O::NCOL; ++j) O::load_v(v, j, p.v + at[j * BK / O::NCOL], (O::col(q4, j) & 15) * ROWB + r * DPL * (int)sizeof(T));
+      for (int j = 0; j < O::NCOL; ++j) O::template load_v<RB == 1>(v, j, p.v + at[j * BK / O::NCOL], (O::col(q4, j) & 15) * ROWB + r * DPL * (int)sizeof(T));
       typename O::Logits x_of[RB];
       typename O::Keys k_next;
       to_come = next_block(c0 + PA_WAVES * COLS);
