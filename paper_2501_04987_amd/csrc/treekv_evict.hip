@@ -7,7 +7,8 @@
 //   move    attention does not ask for the order of columns, so what is kept stays where it is: only tokens from slots behind
 //           the budget move, into the freed slots before it, as many rows as were kept there (of a decode step one, where
 //           closing the gaps would move half of the cache)
-// Two kernels: one workgroup per unit makes the choice and lists the moves, then all of the chip copies the rows.
+// Two kernels: one workgroup per unit makes the choice and lists the moves, then all of the chip copies the rows.  A unit of 32768
+// slots is bound by its workgroup's read of 262 KB (28 us of 33 for 32 units), one of 2049 by rounds of barriers (8 us of 13, 256 units).
 
 #include "treekv_paged.h"
 

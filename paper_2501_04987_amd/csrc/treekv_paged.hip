@@ -9,6 +9,9 @@
 // shares   Few rows leave most of the chip idle, so the columns of the whole batch are cut into equal shares, which the device
 //          works out from the lengths: long sequences get more workgroups than short ones.  A sequence's shares are merged by a
 //          second kernel.
+//          Bound by memory: 16 sequences of 4000 to 16000 tokens, 8 groups of 4 heads, a token each, 117 us, 6.05 TB/s of K and V.
+// many     More than 64 rows share K and V through LDS (below).  512 tokens of 8 groups of 4 heads over 32768: 287-305 us, 0.95 PFLOP/s
+//          where a large product of the library reaches 1.2.
 // weights  the probabilities once more from q, k and each row's reference and sum, summed down the rows: a column belongs to one wave, so the sum needs
 //          no atomics and repeats bit for bit.
 

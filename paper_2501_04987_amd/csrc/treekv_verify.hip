@@ -8,6 +8,9 @@
 // Sums are in double: 2^24 terms leave 2^-29 of a step of fp32, so whether a token is accepted or follows does not depend on
 // their order but within that.
 //
+// Bound by latency: 16 trees of 26 nodes over 131072 tokens 29-43 us (the rows take 3 at the rate of memory), four kernels that each
+// wait for the state, its sums and the rows; a chain of 5 over 32000 tokens 12-14 us.
+//
 // A sequence's rows are split among waves; the token that follows is found by the waves' sums, then among parts of the one it
 // lies in, then by a scan.
 
