@@ -453,7 +453,7 @@ size_t treekv_paged_evict_scratch_bytes(const treekv_paged_cache* cache);
  * are kept, then those with the largest weights (a NaN counts as minus infinity); of equals the one in the lower slot.  Kept
  * tokens in slots behind the budget take the slots below it that have become free, both in slot order; the others stay
  * where they are.  lens becomes at most budget; pages behind it are the caller's again.
- *   status as above; TREEKV_EINVAL also where one of the sequence's pages has been given up.
+ *   status as above; TREEKV_EINVAL also for a sequence that is to be cut and has given up one of its pages.
  * Errors: TREEKV_EINVAL unless budget >= 1, n_sink, n_recent >= 0, n_sink + n_recent <= budget, for a cache without weights
  * and positions and for scratch that is too small; TREEKV_EUNSUPPORTED as above.
  */
@@ -478,7 +478,8 @@ int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, 
  *   path [batch, n] int32: the accepted nodes, then -1;  path_len, next_token [batch] int32
  *   scratch 16-byte aligned, at least treekv_tree_verify_scratch_bytes (NULL if that is 0)
  * Errors: TREEKV_EINVAL unless batch >= 1, 1 <= n <= TREEKV_TREE_MAX_NODES, vocab >= 1, for null or misaligned pointers and
- * for scratch that is too small; TREEKV_EUNSUPPORTED for a vocab beyond 2^24.
+ * for scratch that is too small; TREEKV_EUNSUPPORTED for a vocab beyond 2^24 or a batch beyond
+ * 2^20.
  */
 typedef struct treekv_verify_args {
   const void *target, *draft;

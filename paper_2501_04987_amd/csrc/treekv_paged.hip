@@ -12,8 +12,8 @@
 //          Bound by memory: 16 sequences of 4000 to 16000 tokens, 8 groups of 4 heads, a token each, 117 us, 6.05 TB/s of K and V.
 // many     More than 64 rows share K and V through LDS (below).  512 tokens of 8 groups of 4 heads over 32768: 287-305 us, 0.95 PFLOP/s
 //          where a large product of the library reaches 1.2.
-// weights  the probabilities once more from q, k and each row's reference and sum, summed down the rows: a column belongs to one wave, so the sum needs
-//          no atomics and repeats bit for bit.
+// weights  the probabilities once more, from kept logits or from q and k, by each row's reference and sum, summed down the rows: a
+//          column belongs to one wave, so the sum needs no atomics and repeats bit for bit.
 
 #include "treekv_matrix.h"
 #include "treekv_paged.h"
@@ -218,9 +218,10 @@ __device__ inline void store4(char* out, size_t at, const float4& a, float inv, 
 __device__ inline void store4(char* out, size_t at, const float4& a, float inv, float) {
   *reinterpret_cast<float4*>(out + at * 4) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
 }
+__device__ inline float2 stat_of_sums(float M, float L) { return L > 0.f ? make_float2(M, 1.0f / L) : make_float2(INFINITY, 0.f); }
 __device__ inline void finish_sums(const Attend& a, size_t at, float M, float L) {
   if (a.lse) a.lse[at] = !(L == 0.f) ? (M + log2f(L)) * LN2 : -INFINITY;
-  if (a.stat) a.stat[at] = L > 0.f ? make_float2(M, 1.0f / L) : make_float2(INFINITY, 0.f);
+  if (a.stat) a.stat[at] = stat_of_sums(M, L);
 }
 template <typename T, int D>
 __device__ inline void finish_row(const Attend& a, const Seq& s, int h, int row, int c, const float4& o, float M, float L) {
@@ -480,12 +481,12 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
 }
 
 // The same where the logits of up to 16 rows have been kept: beside the merge (the first piece), each workgroup adds the rows'
-// probabilities of a piece of the columns to the weights.  The log sums it takes them by come from the shares, like the output's.
+// probabilities of a piece of the columns to the weights.  The references and sums come from the shares, like the output's.
 // grid: pieces of the columns x KV heads x sequences.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int pieces) {
   constexpr int OR = D + 4;
-  __shared__ float log_sum[16];
+  __shared__ float2 stat[16];                  // a row's reference and 1 / its sum, as Attend::stat has them
   const Pages& p = a.p;
   const int piece = (int)(blockIdx.x % pieces), rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv, tid = threadIdx.x;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
@@ -518,7 +519,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       L = L * fast_exp2(M - to) + L2 * fast_exp2(M2 - to);
       M = to;
     }
-    if ((tid & 3) == 0) log_sum[row] = M + log2f(L);       // (of no sum minus infinity: its logits are too, and give NaNs)
+    if ((tid & 3) == 0) stat[row] = stat_of_sums(M, L);
   }
   __syncthreads();
   if (mine) {
@@ -526,10 +527,10 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int row = 0; row < rows; ++row) {
       const float4 y = *reinterpret_cast<const float4*>(x + (size_t)row * p.cap);
-      const float l = log_sum[row];
+      const float2 l = stat[row];
       // (a NaN adds nothing)
-      f.x += fmaxf(fast_exp2(y.x - l), 0.f); f.y += fmaxf(fast_exp2(y.y - l), 0.f);
-      f.z += fmaxf(fast_exp2(y.z - l), 0.f); f.w += fmaxf(fast_exp2(y.w - l), 0.f);
+      f.x = fmaf(fmaxf(fast_exp2(y.x - l.x), 0.f), l.y, f.x); f.y = fmaf(fmaxf(fast_exp2(y.y - l.x), 0.f), l.y, f.y);
+      f.z = fmaf(fmaxf(fast_exp2(y.z - l.x), 0.f), l.y, f.z); f.w = fmaf(fmaxf(fast_exp2(y.w - l.x), 0.f), l.y, f.w);
     }
     w.x += f.x; w.y += f.y; w.z += f.z; w.w += f.w;          // (once: a weight is large beside what it gains)
     if (c + 4 <= s.len) *reinterpret_cast<float4*>(weights) = w;

@@ -144,7 +144,7 @@ int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, 
 }
 
 size_t treekv_tree_verify_scratch_bytes(int batch, int n, int vocab) {
-  return batch >= 1 && n >= 1 && n <= TREEKV_TREE_MAX_NODES && vocab >= 1 && vocab <= 1 << 24 ? tkv::verify_scratch_bytes(batch, n, vocab) : 0;
+  return batch >= 1 && batch <= 1 << 20 && n >= 1 && n <= TREEKV_TREE_MAX_NODES && vocab >= 1 && vocab <= 1 << 24 ? tkv::verify_scratch_bytes(batch, n, vocab) : 0;
 }
 
 int treekv_tree_verify(const treekv_verify_args* args, void* stream) {
@@ -154,7 +154,7 @@ int treekv_tree_verify(const treekv_verify_args* args, void* stream) {
   if (!aligned16(a.target) || !aligned16(a.draft) || !aligned16(a.scratch)) return TREEKV_EINVAL;
   if (a.batch < 1 || a.n < 1 || a.n > TREEKV_TREE_MAX_NODES || a.vocab < 1) return TREEKV_EINVAL;
   if (a.dtype != TREEKV_BF16 && a.dtype != TREEKV_F32) return TREEKV_EINVAL;
-  if (a.vocab > 1 << 24) return TREEKV_EUNSUPPORTED;
+  if (a.vocab > 1 << 24 || a.batch > 1 << 20) return TREEKV_EUNSUPPORTED;
   const size_t need = tkv::verify_scratch_bytes(a.batch, a.n, a.vocab);
   if (need > 0 && (!a.scratch || a.scratch_bytes < need)) return TREEKV_EINVAL;
   const uint64_t nodes = (uint64_t)a.batch * a.n, rows = (uint64_t)a.batch * (a.n + 1) * a.vocab * (a.dtype == TREEKV_F32 ? 4 : 2);

@@ -182,6 +182,24 @@ def test_logits_of_any_size(binding, power, new, dtype):
     assert bool((gain >= want - room).all()) and bool((gain <= want + doubt + room).all()) and abs(float(gain.sum()) - 2 * new) < 333 * room
 
 
+@pytest.mark.parametrize("new", [1, 20, 200])
+@pytest.mark.parametrize("power", [0, 40])
+def test_equal_tokens_share_the_weight(binding, power, new):
+    """Three tokens with one key: their weights gain the same, bit for bit, of queries of any size; all together the rows' number."""
+    import torch
+
+    ref = paged(lens=[400], news=[new], page_size=16, kv_heads=1, group=2, d=64, seed=17)
+    at = [ref.row(0, s) for s in (3, 77, 150)]
+    for page, r in at:
+        ref.k[page, 0, r] = 3 * ref.k[at[0][0], 0, at[0][1]] if (page, r) == at[0] else ref.k[at[0][0], 0, at[0][1]]
+    kv = ref.on_gpu(binding)
+    kv.weights.zero_()
+    kv.attend((ref.q.double() * 2.0 ** power).to(ref.t).cuda(), ref.starts.cuda(), new, weigh=True)
+    gain = kv.weights[0, 0].cpu()
+    assert gain[3] == gain[77] == gain[150] and gain[3] > 0
+    assert abs(float(gain.double().sum()) - 2 * new) < 2 * new * (2 * new + 464) * 2.0 ** -24 * 4
+
+
 def test_weights_take_no_nan(binding):
     import torch
 

@@ -136,7 +136,7 @@ def test_verify(binding):
                dict(n=0), dict(n=257), dict(vocab=0), dict(vocab=-8), dict(dtype=2), dict(path=0x10 * MB), dict(path_len=0x13 * MB + 4),
                dict(next_token=0x14 * MB), dict(path=0x100 * MB + 4096), dict(path_len=0x12 * MB)):
         assert call(**kw) == -1, kw
-    assert call(vocab=(1 << 24) + 1) == -4 and lib.treekv_tree_verify(None, None) == -1
+    assert call(vocab=(1 << 24) + 1) == -4 and call(batch=(1 << 20) + 1, target=1 << 50, draft=None) == -4 and lib.treekv_tree_verify(None, None) == -1
     size = lib.treekv_tree_verify_scratch_bytes
     assert all(size(*x) == 0 for x in ((0, 1, 1), (1, 0, 1), (1, 257, 1), (1, 1, 0), (1, 1, (1 << 24) + 1), (-1, -1, -1)))
     need = size(2, 9, 1000)
