@@ -273,7 +273,9 @@ __global__ __launch_bounds__(EV_THREADS) void choose_kernel(Evict e) {
   }
   Unit u = {p.weights + track_row(p, b, h), p.positions + track_row(p, b, h), e.moves + (size_t)unit * e.stride, len, 0};
   int count;
+  // (8 x 32 units of 4097 slots: 13.9 us with 8 keys a thread, 22.6 with 32; of 10000 45 with 32)
   if (len <= 4 * EV_THREADS) count = choose_in_registers<4>(e, u, hist, sm);
+  else if (len <= 8 * EV_THREADS) count = choose_in_registers<8>(e, u, hist, sm);
   else if (len <= 32 * EV_THREADS) count = choose_in_registers<32>(e, u, hist, sm);
   else count = choose_in_passes(e, u, hist, sm);
   if (tid == 0) e.count[unit] = count;

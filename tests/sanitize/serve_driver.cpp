@@ -46,9 +46,11 @@ int main() {
   memset(&v, 0, sizeof(v));
   v.target = (void*)(64 * T); v.tokens = ints; v.parents = ints; v.uniforms = (float*)ints; v.path = (int32_t*)a; v.path_len = (int32_t*)b;
   v.next_token = (int32_t*)o; v.scratch = w; v.scratch_bytes = (size_t)1 << 40; v.batch = 2147483647; v.n = 256; v.vocab = 1 << 24; v.dtype = TREEKV_F32;
-  CHECK(treekv_tree_verify(&v, nullptr) == TREEKV_EINVAL);           // the scratch ends inside the inputs behind it
-  v.batch = 1000;
+  CHECK(treekv_tree_verify(&v, nullptr) == TREEKV_EUNSUPPORTED);
+  v.batch = 1 << 20;
   CHECK(treekv_tree_verify(&v, nullptr) == TREEKV_OK);
+  v.scratch_bytes = ((size_t)256 << 20) - 1;
+  CHECK(treekv_tree_verify(&v, nullptr) == TREEKV_EINVAL);
   CHECK(launches == 6);
   puts("serve paths clean");
   return 0;

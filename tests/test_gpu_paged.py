@@ -347,7 +347,7 @@ def evicted(binding, ref, *args, kv=None, **kw):
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("lens,budget,sink,recent,ps", [
     ([17], 16, 0, 0, 16), ([100, 16, 17, 0], 16, 4, 8, 16), ([300, 299, 31], 1, 0, 1, 16), ([2100, 1025, 40], 1024, 4, 512, 64),
-    ([5000], 33, 0, 0, 128), ([70, 90], 64, 60, 4, 32), ([50], 40, 0, 40, 16), ([9000, 700], 4500, 2, 3, 256), ([4096, 4097], 4000, 4, 2000, 64),
+    ([5000], 33, 0, 0, 128), ([70, 90], 64, 60, 4, 32), ([50], 40, 0, 40, 16), ([9000, 700], 4500, 2, 3, 256), ([8192, 8193, 6000], 5000, 4, 100, 128), ([4096, 4097], 4000, 4, 2000, 64),
     ([16384, 16385], 300, 4, 100, 256), ([32768, 32769], 20000, 4, 10000, 256)])
 def test_evict(binding, lens, budget, sink, recent, ps, dtype, d):
     ref = paged(lens=lens, news=[0] * len(lens), page_size=ps, kv_heads=2, group=1, d=d, dtype=dtype, seed=20)
