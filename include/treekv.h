@@ -452,12 +452,15 @@ size_t treekv_paged_evict_scratch_bytes(const treekv_paged_cache* cache);
  * tokens at positions below n_sink and those at the last n_recent positions (above the sequence's largest minus n_recent)
  * are kept, then those with the largest weights (a NaN counts as minus infinity); of equals the one in the lower slot.  Kept
  * tokens in slots behind the budget take the slots below it that have become free, both in slot order; the others stay
- * where they are.  lens becomes at most budget; pages behind it are the caller's again.
+ * where they are.  lens_out[b] becomes min(lens[b], budget) (lens[b] for a refused sequence); pages behind it are the caller's
+ * again.
+ *   lens_out [batch] int32 (device) or NULL: lens itself, for a cache with lengths of its own.  Where several caches (layers) share
+ *            lens, all of them are evicted by it before it changes: each is given another array, whose values then become lens.
  *   status as above; TREEKV_EINVAL also for a sequence that is to be cut and has given up one of its pages.
  * Errors: TREEKV_EINVAL unless budget >= 1, n_sink, n_recent >= 0, n_sink + n_recent <= budget, for a cache without weights
  * and positions and for scratch that is too small; TREEKV_EUNSUPPORTED as above.
  */
-int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, int n_recent, void* scratch,
+int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, int n_recent, int32_t* lens_out, void* scratch,
                        size_t scratch_bytes, int32_t* status, void* stream);
 
 /*

@@ -121,7 +121,7 @@ def load() -> C.CDLL:
     lib.treekv_paged_attend.argtypes = [vp, vp, C.c_int64, i32p, C.c_int, C.c_int, vp, vp, C.c_int, vp, C.c_size_t, i32p, vp]
     lib.treekv_paged_evict_scratch_bytes.argtypes = [vp]
     lib.treekv_paged_evict_scratch_bytes.restype = C.c_size_t
-    lib.treekv_paged_evict.argtypes = [vp, C.c_int, C.c_int, C.c_int, vp, C.c_size_t, i32p, vp]
+    lib.treekv_paged_evict.argtypes = [vp, C.c_int, C.c_int, C.c_int, i32p, vp, C.c_size_t, i32p, vp]
     lib.treekv_tree_verify_scratch_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
     lib.treekv_tree_verify_scratch_bytes.restype = C.c_size_t
     lib.treekv_tree_verify.argtypes = [vp, vp]
@@ -343,7 +343,7 @@ class PagedKV:
 
     `k`, `v` [pages, kv_heads, page_size, head_dim]; `table` [batch, table_width] int32, -1 where no page has been given; `lens`
     [batch] int32; `weights` (float32) and `positions` (int32) [batch, kv_heads, table_width * page_size] if `tracked`.  The pool
-    and the tables may be given (layers share `table` and `lens`, caches a pool).  Their contents are the caller's: hand out
+    and the tables may be given (layers share `table` and `lens`, see `evict`; caches a pool).  Their contents are the caller's: hand out
     pages in `table`, set `lens` to count a step's new tokens before `append` and `attend`."""
 
     def __init__(self, pages: int, page_size: int, heads: int, head_dim: int, *, kv_heads: int | None = None, batch: int = 1,
@@ -447,17 +447,21 @@ class PagedKV:
         need = (_lib or load()).treekv_paged_evict_scratch_bytes(self._at)
         return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
 
-    def evict(self, budget: int, n_sink: int, n_recent: int, *, scratch=None, status=None):
-        """Sequences with more than `budget` tokens keep the first, the last and the heaviest of them."""
+    def evict(self, budget: int, n_sink: int, n_recent: int, *, lens_out=None, scratch=None, status=None):
+        """Sequences with more than `budget` tokens keep the first, the last and the heaviest of them.  `lens` is cut, or, where
+        layers share it, stays until all of them have been evicted: `lens_out` [batch] takes what it becomes."""
         import torch
 
-        status_at = 0
+        status_at = lens_at = 0
+        if lens_out is not None:
+            _want(lens_out, "lens_out", torch.int32, (self._dims[0],), self._index)
+            lens_at = lens_out.data_ptr()
         if status is not None:
             _want(status, "status", torch.int32, (self._dims[0],), self._index)
             status_at = status.data_ptr()
         if scratch is None:
             scratch = self.new_evict_scratch()
-        _call_on(self.device, self._index, "treekv_paged_evict", self._at, int(budget), int(n_sink), int(n_recent),
+        _call_on(self.device, self._index, "treekv_paged_evict", self._at, int(budget), int(n_sink), int(n_recent), lens_at,
                  *_scratch_at(scratch, self._index), status_at)
 
 

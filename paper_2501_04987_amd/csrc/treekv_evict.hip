@@ -24,7 +24,7 @@ struct Evict {
   int2* moves;               // [units][stride] slots: from, to
   int stride;                // most moves of a unit: each needs a slot below the budget and one behind it
   int* count;                // [units] moves; -1: the sequence is left as it is
-  int32_t* status;
+  int32_t *status, *lens_out;
 };
 
 __device__ inline unsigned order_of(float w) {
@@ -286,8 +286,8 @@ __global__ __launch_bounds__(MV_THREADS) void move_kernel(Evict e, int parts, in
   const Pages& p = e.p;
   const int unit = (int)(blockIdx.x / parts), part = (int)(blockIdx.x % parts), b = unit / p.Hkv, h = unit % p.Hkv;
   const int count = e.count[unit], tid = threadIdx.x;
+  if (part == 0 && h == 0 && tid == 0) e.lens_out[b] = count < 0 ? p.lens[b] : e.budget;
   if (count < 0) return;
-  if (part == 0 && h == 0 && tid == 0) p.lens[b] = e.budget;
   const int piece = tid & ((1 << piece_bits) - 1), step = MV_THREADS >> piece_bits;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int2* moves = e.moves + (size_t)unit * e.stride;
@@ -313,7 +313,8 @@ size_t paged_evict_scratch_bytes(const treekv_paged_cache& c) {
   return align_up(units * 4) + align_up(units * most * sizeof(int2));
 }
 
-int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int n_recent, void* scratch, int32_t* status, hipStream_t s) {
+int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int n_recent, int32_t* lens_out, void* scratch, int32_t* status,
+                       hipStream_t s) {
   const size_t units = (size_t)c.batch * c.kv_heads;
   Evict e;
   e.p = pages_of(c);
@@ -321,6 +322,7 @@ int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int 
   e.count = (int*)scratch;
   e.moves = (int2*)((char*)scratch + align_up(units * 4));
   e.status = status;
+  e.lens_out = lens_out ? lens_out : c.lens;
   e.stride = budget >= e.p.cap ? 0 : budget < e.p.cap - budget ? budget : e.p.cap - budget;
   hipLaunchKernelGGL(choose_kernel, dim3((unsigned)units), dim3(EV_THREADS), 0, s, e);
   const int piece_bits = __builtin_ctz(c.head_dim * (c.dtype == TREEKV_F32 ? 4 : 2) / 16);

@@ -135,7 +135,8 @@ size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int l
 int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
                         void* out, float* lse, int weigh, void* scratch, int32_t* status, hipStream_t s);
 size_t paged_evict_scratch_bytes(const treekv_paged_cache& c);
-int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int n_recent, void* scratch, int32_t* status, hipStream_t s);
+int launch_paged_evict(const treekv_paged_cache& c, int budget, int n_sink, int n_recent, int32_t* lens_out, void* scratch, int32_t* status,
+                       hipStream_t s);
 size_t verify_scratch_bytes(int batch, int n, int vocab);
 int launch_verify(const treekv_verify_args& a, hipStream_t s);
 

@@ -126,7 +126,7 @@ size_t treekv_paged_evict_scratch_bytes(const treekv_paged_cache* cache) {
   return cache_ok(cache) == TREEKV_OK && cache->weights ? tkv::paged_evict_scratch_bytes(*cache) : 0;
 }
 
-int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, int n_recent, void* scratch,
+int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, int n_recent, int32_t* lens_out, void* scratch,
                        size_t scratch_bytes, int32_t* status, void* stream) {
   const int rc = cache_ok(cache);
   if (rc != TREEKV_OK) return rc;
@@ -135,10 +135,11 @@ int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, 
   const size_t need = tkv::paged_evict_scratch_bytes(c);
   if (!scratch || !aligned16(scratch) || scratch_bytes < need) return TREEKV_EINVAL;
   const CacheRanges cr = cache_ranges(c);
-  const Range to[2] = {range(scratch, need), range(status, (uint64_t)c.batch * 4)};
-  if (!apart(to, 2, to, 2) || !apart(to, 2, cr.r, 6) || !apart(cr.r, 6, cr.r, 6)) return TREEKV_EINVAL;
+  const uint64_t ints = (uint64_t)c.batch * 4;
+  const Range to[3] = {range(scratch, need), range(status, ints), range(lens_out == c.lens ? nullptr : lens_out, ints)};
+  if (!apart(to, 3, to, 3) || !apart(to, 3, cr.r, 6) || !apart(cr.r, 6, cr.r, 6)) return TREEKV_EINVAL;
   fresh();
-  const int got = tkv::launch_paged_evict(c, budget, n_sink, n_recent, scratch, status, (hipStream_t)stream);
+  const int got = tkv::launch_paged_evict(c, budget, n_sink, n_recent, lens_out, scratch, status, (hipStream_t)stream);
   (void)tkv::take_hip_error();
   return got;
 }

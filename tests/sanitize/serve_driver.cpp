@@ -16,7 +16,7 @@ int launch_paged_append(const treekv_paged_cache&, const void*, const void*, int
 size_t paged_attend_scratch_bytes(const treekv_paged_cache&, int tokens, int, int weigh) { return weigh ? (size_t)tokens * 256 : 0; }
 int launch_paged_attend(const treekv_paged_cache&, const void*, int64_t, const int32_t*, int, int, void*, float*, int, void*, int32_t*, hipStream_t) { ++launches; return TREEKV_OK; }
 size_t paged_evict_scratch_bytes(const treekv_paged_cache& c) { return (size_t)c.batch * c.kv_heads * c.table_width * c.page_size * 4; }
-int launch_paged_evict(const treekv_paged_cache&, int, int, int, void*, int32_t*, hipStream_t) { ++launches; return TREEKV_OK; }
+int launch_paged_evict(const treekv_paged_cache&, int, int, int, int32_t*, void*, int32_t*, hipStream_t) { ++launches; return TREEKV_OK; }
 size_t verify_scratch_bytes(int batch, int, int) { return (size_t)batch * 256; }
 int launch_verify(const treekv_verify_args&, hipStream_t) { ++launches; return TREEKV_OK; }
 }  // namespace tkv
@@ -39,8 +39,8 @@ int main() {
   CHECK(treekv_paged_attend(&c, a, 65536 * 128, ints, 4, 4, o, nullptr, 1, w, 1023, nullptr, nullptr) == TREEKV_EINVAL);
   const size_t need = treekv_paged_evict_scratch_bytes(&c);
   CHECK(need == (size_t)1 << 31);
-  CHECK(treekv_paged_evict(&c, 2147483647, 2147483646, 1, w, need, nullptr, nullptr) == TREEKV_OK);
-  CHECK(treekv_paged_evict(&c, 2147483647, 2147483647, 2147483647, w, need, nullptr, nullptr) == TREEKV_EINVAL);
+  CHECK(treekv_paged_evict(&c, 2147483647, 2147483646, 1, nullptr, w, need, nullptr, nullptr) == TREEKV_OK);
+  CHECK(treekv_paged_evict(&c, 2147483647, 2147483647, 2147483647, c.lens, w, need, nullptr, nullptr) == TREEKV_EINVAL);
   CHECK(launches == 5);
   treekv_verify_args v;
   memset(&v, 0, sizeof(v));

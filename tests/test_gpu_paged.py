@@ -406,6 +406,55 @@ def test_evict_leaves_sequences_with_pages_given_up(binding):
     assert status.tolist() == [0, 0, binding.TREEKV_EINVAL, 0]
 
 
+def test_layers_that_share_lengths(binding):
+    """Each layer is evicted by the lengths that all of them had; a refused sequence and a short one keep theirs."""
+    import torch
+
+    ref = paged(lens=[100, 15, 90], news=[0] * 3, page_size=16, kv_heads=2, group=1, d=64, seed=23)
+    ref.table[2, 1] = -1
+    one = ref.on_gpu(binding)
+    lens = torch.full((3,), 9, dtype=torch.int32, device="cuda")
+    two = binding.PagedKV(ref.pages, 16, 2, 64, batch=3, table_width=ref.width, table=one.table, lens=one.lens)
+    other = paged(lens=[100, 15, 90], news=[0] * 3, page_size=16, kv_heads=2, group=1, d=64, seed=24)
+    other.table.copy_(ref.table)
+    for name in ("k", "v", "weights", "positions"):
+        getattr(two, name).copy_(getattr(other, name))
+    for kv in (one, two):
+        kv.evict(40, 2, 10, lens_out=lens)
+        assert one.lens.tolist() == [100, 15, 90] and lens.tolist() == [40, 15, 90]
+    for kv, r in ((one, ref), (two, other)):
+        r.evict(40, 2, 10)
+        for name in ("k", "v", "weights", "positions"):
+            assert torch.equal(getattr(kv, name).cpu(), getattr(r, name)), name
+    one.lens.copy_(lens)
+    one.evict(30, 2, 10, lens_out=one.lens)                   # as without it
+    assert one.lens.tolist() == [30, 15, 90]
+    with pytest.raises(ValueError):
+        one.evict(30, 2, 10, lens_out=lens[:2])
+
+
+def test_calls_beside_each_other(binding):
+    """One cache read by calls on two streams at once, each with its own scratch; two sequences of one table (beams)."""
+    import torch
+
+    ref = paged(lens=[700, 700, 300], news=[20, 20, 9], page_size=16, kv_heads=2, group=3, d=128, seed=25)
+    ref.table[1] = ref.table[0]
+    kv, q, starts = ref.on_gpu(binding), ref.q.cuda(), ref.starts.cuda()
+    q[20:40] = q[:20]
+    want = kv.attend(q, starts, 20)
+    assert torch.equal(want[:20], want[20:40])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros_like(want) for _ in range(2)]
+    scratch = [kv.new_attend_scratch(49, 20) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, o, x in zip(streams, outs, scratch):
+            with torch.cuda.stream(s):
+                kv.attend(q, starts, 20, o, scratch=x)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
 def test_results_repeat_bit_for_bit_on_other_streams(binding):
     import torch
 

@@ -52,11 +52,11 @@ def test_caches(binding):
         c = cache(binding, **kw)
         assert lib.treekv_paged_append(c, a, a, 128, 128, other, 3, other, None, None) == want, kw
         assert lib.treekv_paged_attend(c, a, 256, other, 3, 3, out, None, 0, other, 1 << 30, None, None) == want, kw
-        assert lib.treekv_paged_evict(c, 20, 2, 10, other, 1 << 30, None, None) == want, kw
+        assert lib.treekv_paged_evict(c, 20, 2, 10, None, other, 1 << 30, None, None) == want, kw
         assert lib.treekv_paged_attend_scratch_bytes(c, 3, 3, 1) == 0 and lib.treekv_paged_evict_scratch_bytes(c) == 0, kw
     assert lib.treekv_paged_append(None, a, a, 128, 128, other, 3, other, None, None) == -1
     assert lib.treekv_paged_attend(None, a, 256, other, 3, 3, out, None, 0, other, 1 << 30, None, None) == -1
-    assert lib.treekv_paged_evict(None, 20, 2, 10, other, 1 << 30, None, None) == -1
+    assert lib.treekv_paged_evict(None, 20, 2, 10, None, other, 1 << 30, None, None) == -1
     assert lib.treekv_paged_attend_scratch_bytes(None, 3, 3, 0) == 0 and lib.treekv_paged_evict_scratch_bytes(None) == 0
 
 
@@ -116,9 +116,9 @@ def test_evict(binding):
     lib, c = binding.load(), cache(binding)
     scratch, st = 0x70 * MB, 0x62 * MB
     need = lib.treekv_paged_evict_scratch_bytes(c)
-    good = [c, 20, 4, 10, scratch, need, st, None]
-    refuses(lib.treekv_paged_evict, good, [(1, 0), (1, -5), (2, -1), (3, -1), (2, 11), (3, 17), (3, 2147483647), (4, None), (4, scratch + 4), (5, need - 1),
-                                           (4, 0x10 * MB), (6, scratch), (6, 0x31 * MB), (0, cache(binding, weights=None, positions=None)),
+    good = [c, 20, 4, 10, 0x63 * MB, scratch, need, st, None]
+    refuses(lib.treekv_paged_evict, good, [(1, 0), (1, -5), (2, -1), (3, -1), (2, 11), (3, 17), (3, 2147483647), (5, None), (5, scratch + 4), (6, need - 1),
+                                           (5, 0x10 * MB), (7, scratch), (7, 0x31 * MB), (4, 0x31 * MB + 4), (4, st), (4, scratch), (4, 0x30 * MB), (0, cache(binding, weights=None, positions=None)),
                                            (0, cache(binding, v=0x10 * MB)), (0, cache(binding, lens=0x32 * MB))])
 
 
