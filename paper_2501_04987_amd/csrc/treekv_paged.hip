@@ -108,10 +108,9 @@ struct Attend {
 };
 
 // The columns of all sequences with new tokens lie one after the other (each sequence's rounded up to whole blocks), and are cut
-// into shares of `size`.  Few rows: a workgroup takes one share, whatever sequences it runs through; what it has of sequence b is
-// partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round, and the smallest shares,
-// where a second sequence would double the time: a sequence's shares start at its first token, so that each is of one
-// sequence (its `own`).
+// into shares of `size`.  Few rows over many columns: a workgroup takes one share, whatever sequences it runs through; what it has
+// of sequence b is partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round, and
+// small shares: a sequence's shares start at its first token, so that each is of one sequence (its `own`).
 struct Run {
   int b, length;             // a sequence with columns, and their number
   long long start;           // where they start
@@ -147,12 +146,18 @@ __device__ inline long long wave_scan(long long x, bool wide, long long& all) {
   all = __builtin_amdgcn_readlane(v, 63);
   return v;
 }
-// What find_run asks of the lengths: the size of a share, and this lane's sequence among the first 64.
+// What find_run asks of the lengths: the size of a share, whether shares are of one sequence each, and this lane's sequence among
+// the first 64.  A second sequence in a share costs a workgroup about what STRADDLE more columns do.  Up to SHORT columns a share,
+// a size that is larger by no more and gives every sequence shares of its own, no more of them than were to be, is taken (8
+// sequences of 2048 columns and one token, 8 KV heads: 22.0 -> 18.9 us); sequences that are more than the shares take one or
+// two each (64 of 500: 29.5 -> 24.2 us; of 2048 columns 67 either way).  Row tiles: what 128 rows write and read again for
+// another share costs about what it gains up to TILED_SHARE columns (200 tokens behind 1000, groups of 4: 33.3 -> 27.1 us).
+constexpr int STRADDLE = 256, SHORT = 1024, TILED_SHARE = 1024;
 struct Columns {
   int size, length;
-  __device__ bool own() const { return size == MIN_SHARE; }
+  bool own;
 };
-__device__ inline Columns columns_of(const Attend& a) {
+__device__ inline Columns columns_of(const Attend& a, bool tiled) {
   const int lane = threadIdx.x & 63;
   Columns c;
   c.length = tokens_to_read(a, lane);
@@ -161,11 +166,23 @@ __device__ inline Columns columns_of(const Attend& a) {
   wave_scan(mine, a.wide, total);
   const long long each = a.wide ? (total + a.shares - 1) / a.shares : (int)(((unsigned)total + a.shares - 1) / (unsigned)a.shares);
   c.size = (int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30);
+  if (tiled) c.size = max(c.size, min(2 * c.size, TILED_SHARE));
+  c.own = tiled || c.size == MIN_SHARE;
+  if (!c.own && c.size <= SHORT && !a.wide && a.shares > 1) {
+    c.own = a.p.B > a.shares;
+    if (a.p.B <= min(a.shares, 64))
+      for (int size = c.size; size <= c.size + STRADDLE; size += 64) {
+        long long count;
+        wave_scan((unsigned)(c.length + size - 1) / (unsigned)size, false, count);
+        if ((int)count <= a.shares) { c.size = size; c.own = true; break; }
+      }
+  }
   return c;
 }
 // The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
-__device__ inline bool find_run(const Attend& a, const Columns& c, bool own, long long at, int want_b, Run& run) {
+__device__ inline bool find_run(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
   const int lane = threadIdx.x & 63, size = c.size;
+  const bool own = c.own;
   long long before = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
     const int length = b0 ? tokens_to_read(a, b0 + lane) : c.length, mine = own ? (length + size - 1) / size : length;
@@ -243,13 +260,13 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   const int tile = (int)(blockIdx.x % a.tiles), rest = (int)(blockIdx.x / a.tiles), h = rest % p.Hkv, w = rest / p.Hkv;
   if (blockIdx.x == 0 && a.status)
     for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  const Columns columns = columns_of(a);
+  const Columns columns = columns_of(a, false);
   const int size = columns.size;
-  const bool own = columns.own();
+  const bool own = columns.own;
   const long long share_end = own ? w + 1 : (long long)(w + 1) * size;
   Run run;
 #pragma unroll 1
-  for (long long from = own ? w : (long long)w * size; from < share_end && find_run(a, columns, own, from, -1, run);
+  for (long long from = own ? w : (long long)w * size; from < share_end && find_run(a, columns, from, -1, run);
        from = own ? share_end : run.start + run.length) {
     const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
     const int rows = s.n * p.G, row0 = tile * ROWS;
@@ -428,26 +445,31 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   }
 }
 
-// Shares of a sequence added, four dimensions of a row a thread.  grid: tiles of MERGE_ROWS rows x KV heads x sequences.
+// Shares of a sequence added, four dimensions of a row a thread, `slices` (a power of two up to MERGE_ROWS) groups of threads
+// to a row: of MERGE_ROWS / slices rows at once, from row0 on, every `step` rows.
 template <int D> constexpr int MERGE_ROWS = PA_THREADS * 4 / D;
+struct Merged {
+  float4 f[PA_THREADS];
+  float2 ml[PA_THREADS];
+};
 template <typename T, int D>
-__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0, int end) {
-  constexpr int OR = D + 4;
+__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0, int step, int slices, Merged& sm) {
+  constexpr int OR = D + 4, WIDTH = D / 4;
   const Pages& p = a.p;
-  const int rows = s.n * p.G;
-  for (int row = row0 + (int)threadIdx.x / (D / 4); row < min(end, rows); row += MERGE_ROWS<D>) {
-    const int c = (int)threadIdx.x % (D / 4) * 4;
+  const int rows = s.n * p.G, tid = threadIdx.x, c = tid % WIDTH * 4, slice = tid / WIDTH & (slices - 1);
+  for (; row0 < rows; row0 += step) {
+    const int row = row0 + tid / WIDTH / slices;
     const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
-    const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR;
+    const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + min(row, rows - 1)) * OR;
     constexpr int AT_ONCE = 8;                         // shares on their way together
     float M = REF_NONE, L = 0.f;
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z0 = 0; z0 < run.count; z0 += AT_ONCE) {
+    for (int z0 = slice; z0 < run.count; z0 += AT_ONCE * slices) {
       float2 ml[AT_ONCE];
       float4 u[AT_ONCE];
 #pragma unroll
       for (int z = 0; z < AT_ONCE; ++z) {
-        const float* at = part + min(z0 + z, run.count - 1) * far;
+        const float* at = part + min(z0 + z * slices, run.count - 1) * far;
         ml[z] = *reinterpret_cast<const float2*>(at + D);
         u[z] = *reinterpret_cast<const float4*>(at + c);
       }
@@ -459,33 +481,56 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
       M = to;
 #pragma unroll
       for (int z = 0; z < AT_ONCE; ++z) {
-        if (z0 + z >= run.count) break;
+        if (z0 + z * slices >= run.count) break;
         const float g = fast_exp2(ml[z].x - M);
         L = fmaf(ml[z].y, g, L);
         f.x = fmaf(u[z].x, g, f.x); f.y = fmaf(u[z].y, g, f.y); f.z = fmaf(u[z].z, g, f.z); f.w = fmaf(u[z].w, g, f.w);
       }
     }
-    finish_row<T, D>(a, s, h, row, c, f, M, L);
+    if (slices > 1) {
+      __syncthreads();                                 // (the rows before have been read)
+      sm.f[tid] = f;
+      sm.ml[tid] = make_float2(M, L);
+      __syncthreads();
+      if (slice == 0) {
+        float to = M;
+        for (int z = 1; z < slices; ++z) to = fmaxf(to, sm.ml[tid + z * WIDTH].x);
+        const float was = fast_exp2(M - to);
+        L *= was; f.x *= was; f.y *= was; f.z *= was; f.w *= was;
+        M = to;
+        for (int z = 1; z < slices; ++z) {
+          const float2 ml = sm.ml[tid + z * WIDTH];
+          const float4 u = sm.f[tid + z * WIDTH];
+          const float g = fast_exp2(ml.x - M);
+          L = fmaf(ml.y, g, L);
+          f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
+        }
+      }
+    }
+    if (slice == 0 && row < rows) finish_row<T, D>(a, s, h, row, c, f, M, L);
   }
 }
+// grid: groups of MERGE_ROWS / slices rows x KV heads x sequences.
 template <typename T, int D>
-__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, bool tiled) {
+__global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, int slices, bool tiled) {
+  __shared__ Merged sm;
   const Pages& p = a.p;
   const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  if (tile * MERGE_ROWS<D> >= s.n * p.G) return;
+  if (tile * (MERGE_ROWS<D> / slices) >= s.n * p.G) return;
   Run run;
-  const Columns columns = columns_of(a);
-  if (!find_run(a, columns, tiled || columns.own(), 0, b, run) || run.count <= 1) return;
-  merge_rows<T, D>(a, s, run, h, tile * MERGE_ROWS<D>, (tile + 1) * MERGE_ROWS<D>);
+  const Columns columns = columns_of(a, tiled);
+  if (!find_run(a, columns, 0, b, run) || run.count <= 1) return;
+  merge_rows<T, D>(a, s, run, h, tile * (MERGE_ROWS<D> / slices), s.n * p.G, slices, sm);
 }
 
-// The same where the logits of up to 16 rows have been kept: beside the merge (the first piece), each workgroup adds the rows'
+// The same where the logits of up to 16 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
 // probabilities of a piece of the columns to the weights.  The references and sums come from the shares, like the output's.
 // grid: pieces of the columns x KV heads x sequences.
 template <typename T, int D>
-__global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int pieces) {
+__global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int pieces, int slices) {
   constexpr int OR = D + 4;
+  __shared__ Merged sm;
   __shared__ float2 stat[16];                  // a row's reference and 1 / its sum, as Attend::stat has them
   const Pages& p = a.p;
   const int piece = (int)(blockIdx.x % pieces), rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv, tid = threadIdx.x;
@@ -493,20 +538,20 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
   if (rows == 0 || c0 >= s.len) return;
   Run run;
-  const Columns columns = columns_of(a);
-  if (!find_run(a, columns, columns.own(), 0, b, run)) return;
+  const Columns columns = columns_of(a, false);
+  if (!find_run(a, columns, 0, b, run)) return;
   const int c = c0 + 4 * tid;
   const bool mine = c < s.len;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
   float* weights = p.weights + track_row(p, b, h) + c;
   if (mine) w = *reinterpret_cast<const float4*>(weights);
-  if (tid < 64) {                              // four lanes a row, each with a quarter of the shares
-    const int row = tid >> 2;
+  {                                            // 16 lanes a row, each with every 16th share
+    const int row = tid >> 4;
     float M = REF_NONE, L = 0.f;
     if (row < rows) {
       const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
       const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
-      for (int z = tid & 3; z < run.count; z += 4) {
+      for (int z = tid & 15; z < run.count; z += 16) {
         const float2 ml = *reinterpret_cast<const float2*>(part + z * far);
         const float to = fmaxf(M, ml.x);
         L = L * fast_exp2(M - to) + ml.y * fast_exp2(ml.x - to);
@@ -514,12 +559,12 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       }
     }
 #pragma unroll
-    for (int x = 1; x <= 2; x <<= 1) {
+    for (int x = 1; x <= 8; x <<= 1) {
       const float M2 = __shfl_xor(M, x, 64), L2 = __shfl_xor(L, x, 64), to = fmaxf(M, M2);
       L = L * fast_exp2(M - to) + L2 * fast_exp2(M2 - to);
       M = to;
     }
-    if ((tid & 3) == 0) stat[row] = stat_of_sums(M, L);
+    if ((tid & 15) == 0) stat[row] = stat_of_sums(M, L);
   }
   __syncthreads();
   if (mine) {
@@ -539,7 +584,10 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
     }
   }
-  if (piece == 0 && run.count > 1) merge_rows<T, D>(a, s, run, h, 0, 16);
+  if (run.count > 1) {
+    const int at_once = MERGE_ROWS<D> / slices, with = (s.len + 4 * PA_THREADS - 1) / (4 * PA_THREADS);
+    merge_rows<T, D>(a, s, run, h, piece * at_once, with * at_once, slices, sm);
+  }
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -639,10 +687,10 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   // the tiles of a KV head and share, the longest first, on one XCD, whose L2 then has their columns
   const int idx = (int)(blockIdx.x >> 3), group = idx / a.tiles * 8 + (int)(blockIdx.x & 7), tile = a.tiles - 1 - idx % a.tiles;
   const int h = group % p.Hkv, w = group / p.Hkv;
-  const Columns columns = columns_of(a);
+  const Columns columns = columns_of(a, true);
   const int size = columns.size;
   Run run;
-  if (!find_run(a, columns, true, w, -1, run)) return;
+  if (!find_run(a, columns, w, -1, run)) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
   const int rows = s.n * p.G, row0 = tile * TILED_ROWS;
   if (row0 >= rows) return;
@@ -1031,9 +1079,12 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   s.tiled = rows > 64 && c.dtype == TREEKV_BF16;
   s.rows = rows <= 16 ? 16 : s.tiled ? TILED_ROWS : 32;
   s.tiles = (int)((rows + s.rows - 1) / s.rows);
-  const long long groups = (long long)c.kv_heads * s.tiles, want = 512;      // two workgroups a compute unit
+  const long long groups = (long long)c.kv_heads * s.tiles, want = s.tiled ? 512 : 256;
+  // (few rows: one workgroup a compute unit has enough on its way, and leaves fewer shares to add: 16 sequences of 16000 columns
+  // and one token 118 us, with two 121, with three or four 123 to 134; row tiles: two, 168 us for 512 tokens behind 16000, with
+  // one 186, but one alone rather than two shares of what fills more than two thirds of the chip: 2000 tokens 60 us, with two 85)
   const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
-  s.shares = (int)(groups >= want ? 1 : (want + groups - 1) / groups);
+  s.shares = (int)(s.tiled ? max((want + groups / 2) / groups, 1ll) : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
   // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them
   // (what that asks of the query rows' distance, the launch adds)
@@ -1065,14 +1116,18 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
     hipLaunchKernelGGL(kernel, dim3(groups * a.tiles), dim3(PA_THREADS), lds, s, a);
   }
   const unsigned units = (unsigned)(p.Hkv * p.B);
+  // where a row has many shares, several groups of threads take up to eight each, all on their way together (one token behind
+  // 8000, 8 KV heads, 32 shares: 33.6 us with one group, 16.5 with four)
+  int slices = 1;
+  while (slices < MERGE_ROWS<D> && (a.shares / p.B + 1) > 8 * slices) slices *= 2;
   if (sh.keep) {
     const int all = (p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS);
-    hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all);
+    hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, slices);
     return finish_launch();
   }
   if (a.shares > 1) {
-    const int all = (a.longest * p.G + MERGE_ROWS<D> - 1) / MERGE_ROWS<D>;
-    hipLaunchKernelGGL((merge_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, sh.tiled);
+    const int at_once = MERGE_ROWS<D> / slices, all = (a.longest * p.G + at_once - 1) / at_once;
+    hipLaunchKernelGGL((merge_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, slices, sh.tiled);
   }
   if (weigh) {
     if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)

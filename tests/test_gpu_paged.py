@@ -77,6 +77,26 @@ def test_attend(binding, shape, dtype):
     check_attend(kv, ref, weigh=False)
 
 
+# Each way to cut the columns: a row of over a hundred shares; shares made larger so that each is of one sequence; sequences that
+# are more than the shares; sequences that share one; row tiles with larger shares.
+CUTS = [
+    dict(lens=[20000], news=[1], page_size=64, kv_heads=1, group=4, d=128),
+    dict(lens=[17000, 300], news=[5, 1], page_size=64, kv_heads=1, group=3, d=64),
+    dict(lens=[700, 130, 1000, 31, 512], news=[1, 2, 1, 1, 1], page_size=16, kv_heads=32, group=1, d=64),
+    dict(lens=[300, 31, 250, 0, 170, 200, 64], news=[1, 1, 1, 0, 1, 1, 1], page_size=32, kv_heads=64, group=2, d=64),
+    dict(lens=[150] * 70, news=[1] * 70, page_size=32, kv_heads=2, group=2, d=128),
+    dict(lens=[1501, 950], news=[1, 2], page_size=32, kv_heads=128, group=1, d=64),
+    dict(lens=[2600], news=[130], page_size=32, kv_heads=32, group=1, d=64),
+]
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("cut", range(len(CUTS)))
+def test_columns_cut_into_shares(binding, cut, weigh):
+    ref = paged(**CUTS[cut], seed=cut)
+    check_attend(ref.on_gpu(binding), ref, weigh=weigh)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_queries_far_apart(binding, dtype):
     """Tokens 16 MB apart: their places in a tile pass 32 bits."""
