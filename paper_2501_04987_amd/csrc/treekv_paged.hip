@@ -249,7 +249,7 @@ __device__ inline void finish_row(const Attend& a, const Seq& s, int h, int row,
 }
 
 // grid: shares of the columns x KV heads x row tiles.  RB: blocks of 16 rows.
-// WEIGH (16 rows only): the logits are kept for the weights.
+// WEIGH (one tile only): the logits are kept for the weights.
 template <typename T, int D, int RB, bool WEIGH>
 __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   using O = Ops<T, D>;
@@ -371,8 +371,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
           mx = fmaxf(mx, y);
         }
         if constexpr (WEIGH) {
-          if (r < rows) {
-            float* keep = a.logits + (((size_t)run.b * p.Hkv + h) * a.rows + r) * p.cap + c0 + 4 * q4;
+          if (rb * 16 + r < rows) {
+            float* keep = a.logits + (((size_t)run.b * p.Hkv + h) * a.rows + rb * 16 + r) * p.cap + c0 + 4 * q4;
 #pragma unroll
             for (int z = 0; z < BK; ++z)
               if (c0 + 16 * z < hi) *reinterpret_cast<f32x4_t*>(keep + 16 * z) = x.x[z];
@@ -524,19 +524,20 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   merge_rows<T, D>(a, s, run, h, tile * (MERGE_ROWS<D> / slices), s.n * p.G, slices, sm);
 }
 
-// The same where the logits of up to 16 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
+// The same where the logits of up to 32 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
 // probabilities of a piece of the columns to the weights.  The references and sums come from the shares, like the output's.
 // grid: pieces of the columns x KV heads x sequences.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int pieces, int slices) {
   constexpr int OR = D + 4;
   __shared__ Merged sm;
-  __shared__ float2 stat[16];                  // a row's reference and 1 / its sum, as Attend::stat has them
+  __shared__ float2 stat[32];                  // a row's reference and 1 / its sum, as Attend::stat has them
   const Pages& p = a.p;
   const int piece = (int)(blockIdx.x % pieces), rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv, tid = threadIdx.x;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
-  if (rows == 0 || c0 >= s.len) return;
+  const int at_once = MERGE_ROWS<D> / slices;
+  if (rows == 0 || (c0 >= s.len && piece * at_once >= rows)) return;
   Run run;
   const Columns columns = columns_of(a, false);
   if (!find_run(a, columns, 0, b, run)) return;
@@ -545,10 +546,9 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
   float* weights = p.weights + track_row(p, b, h) + c;
   if (mine) w = *reinterpret_cast<const float4*>(weights);
-  {                                            // 16 lanes a row, each with every 16th share
-    const int row = tid >> 4;
-    float M = REF_NONE, L = 0.f;
-    if (row < rows) {
+  if (c0 < s.len)
+    for (int row = tid >> 4; row < rows; row += 16) {          // 16 lanes a row, each with every 16th share
+      float M = REF_NONE, L = 0.f;
       const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
       const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
       for (int z = tid & 15; z < run.count; z += 16) {
@@ -557,19 +557,19 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
         L = L * fast_exp2(M - to) + ml.y * fast_exp2(ml.x - to);
         M = to;
       }
-    }
 #pragma unroll
-    for (int x = 1; x <= 8; x <<= 1) {
-      const float M2 = __shfl_xor(M, x, 64), L2 = __shfl_xor(L, x, 64), to = fmaxf(M, M2);
-      L = L * fast_exp2(M - to) + L2 * fast_exp2(M2 - to);
-      M = to;
+      for (int x = 1; x <= 8; x <<= 1) {
+        const float M2 = __shfl_xor(M, x, 64), L2 = __shfl_xor(L, x, 64), to = fmaxf(M, M2);
+        L = L * fast_exp2(M - to) + L2 * fast_exp2(M2 - to);
+        M = to;
+      }
+      if ((tid & 15) == 0) stat[row] = stat_of_sums(M, L);
     }
-    if ((tid & 15) == 0) stat[row] = stat_of_sums(M, L);
-  }
   __syncthreads();
   if (mine) {
     const float* x = a.logits + ((size_t)b * p.Hkv + h) * a.rows * p.cap + c;
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int row = 0; row < rows; ++row) {
       const float4 y = *reinterpret_cast<const float4*>(x + (size_t)row * p.cap);
       const float2 l = stat[row];
@@ -584,10 +584,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
     }
   }
-  if (run.count > 1) {
-    const int at_once = MERGE_ROWS<D> / slices, with = (s.len + 4 * PA_THREADS - 1) / (4 * PA_THREADS);
-    merge_rows<T, D>(a, s, run, h, piece * at_once, with * at_once, slices, sm);
-  }
+  if (run.count > 1) merge_rows<T, D>(a, s, run, h, piece * at_once, pieces * at_once, slices, sm);
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -1086,10 +1083,11 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
   s.shares = (int)(s.tiled ? max((want + groups / 2) / groups, 1ll) : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
-  // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them
+  // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them, for up to 32 rows (8 sequences
+  // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike)
   // (what that asks of the query rows' distance, the launch adds)
   s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
-  s.keep = weigh && rows <= 16 && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
+  s.keep = weigh && rows <= 32 && (size_t)units * s.rows * cap * 4 <= (size_t)1 << 30;
   s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
   s.logits = s.keep ? align_up((size_t)units * s.rows * cap * 4) : 0;
   s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
@@ -1111,7 +1109,7 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
     }
   } else {
     const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
-    auto kernel = sh.rows != 16 ? attend_kernel<T, D, 2, false> : sh.keep ? attend_kernel<T, D, 1, true> : attend_kernel<T, D, 1, false>;
+    auto kernel = sh.rows != 16 ? sh.keep ? attend_kernel<T, D, 2, true> : attend_kernel<T, D, 2, false> : sh.keep ? attend_kernel<T, D, 1, true> : attend_kernel<T, D, 1, false>;
     if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
     hipLaunchKernelGGL(kernel, dim3(groups * a.tiles), dim3(PA_THREADS), lds, s, a);
   }
@@ -1121,7 +1119,8 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
   int slices = 1;
   while (slices < MERGE_ROWS<D> && (a.shares / p.B + 1) > 8 * slices) slices *= 2;
   if (sh.keep) {
-    const int all = (p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS);
+    const int at_once = MERGE_ROWS<D> / slices;
+    const int all = max((p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS), (a.longest * p.G + at_once - 1) / at_once);
     hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, slices);
     return finish_launch();
   }

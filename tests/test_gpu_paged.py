@@ -87,13 +87,15 @@ CUTS = [
     dict(lens=[150] * 70, news=[1] * 70, page_size=32, kv_heads=2, group=2, d=128),
     dict(lens=[1501, 950], news=[1, 2], page_size=32, kv_heads=128, group=1, d=64),
     dict(lens=[2600], news=[130], page_size=32, kv_heads=32, group=1, d=64),
+    dict(lens=[900, 40, 333, 17], news=[5, 1, 8, 0], page_size=16, kv_heads=2, group=4, d=128),
+    dict(lens=[2300, 3], news=[3, 1], page_size=16, kv_heads=1, group=7, d=64),
 ]
 
 
-@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("weigh,dtype", [(False, "bf16"), (True, "bf16"), (True, "f32")])
 @pytest.mark.parametrize("cut", range(len(CUTS)))
-def test_columns_cut_into_shares(binding, cut, weigh):
-    ref = paged(**CUTS[cut], seed=cut)
+def test_columns_cut_into_shares(binding, cut, weigh, dtype):
+    ref = paged(**CUTS[cut], seed=cut, dtype=dtype)
     check_attend(ref.on_gpu(binding), ref, weigh=weigh)
 
 
@@ -122,7 +124,7 @@ def test_attend_strided_queries_and_an_untracked_cache(binding, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("news", [[1, 1, 1], [30, 45, 80]])
+@pytest.mark.parametrize("news", [[1, 1, 1], [14, 9, 16], [30, 45, 80]])
 def test_attend_pages_given_up(binding, news, dtype):
     """Pages that are -1 or beyond the pool, also all of a sequence's: its rows are 0, their log sums minus infinity."""
     ref = paged(lens=[120, 100, 80], news=news, page_size=16, kv_heads=2, group=2, d=128, dtype=dtype, seed=3)
@@ -136,7 +138,7 @@ def test_attend_pages_given_up(binding, news, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("new,group", [(1, 4), (40, 1), (150, 2)])
+@pytest.mark.parametrize("new,group", [(1, 4), (6, 4), (40, 1), (150, 2)])
 def test_what_is_not_attended_has_no_part(binding, new, group, dtype):
     """Infinities and NaNs behind the last token, in pages of nobody and in the chunk's later tokens: the rows before them come
     out bit for bit as without them, the rows that attend them are infinite or NaN where the formula is."""
@@ -171,7 +173,7 @@ def test_what_is_not_attended_has_no_part(binding, new, group, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("new", [1, 20, 200])
+@pytest.mark.parametrize("new", [1, 12, 20, 200])
 @pytest.mark.parametrize("power", [22, 40])
 def test_logits_of_any_size(binding, power, new, dtype):
     """Queries scaled by 2^22 and 2^40: one token has all of the weight, exactly, whatever its logit's last bits are."""
@@ -202,7 +204,7 @@ def test_logits_of_any_size(binding, power, new, dtype):
     assert bool((gain >= want - room).all()) and bool((gain <= want + doubt + room).all()) and abs(float(gain.sum()) - 2 * new) < 333 * room
 
 
-@pytest.mark.parametrize("new", [1, 20, 200])
+@pytest.mark.parametrize("new", [1, 12, 20, 200])
 @pytest.mark.parametrize("power", [0, 40])
 def test_equal_tokens_share_the_weight(binding, power, new):
     """Three tokens with one key: their weights gain the same, bit for bit, of queries of any size; all together the rows' number."""
