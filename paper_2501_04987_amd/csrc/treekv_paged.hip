@@ -510,6 +510,22 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
     if (slice == 0 && row < rows) finish_row<T, D>(a, s, h, row, c, f, M, L);
   }
 }
+// The tiles of a group (a KV head of a share or of a sequence) run on one XCD, whose L2 then has what they share, and with fewer
+// than 8 KV heads on as many XCDs as leaves none idle.  (2 KV heads, groups of 8, 2154 tokens behind
+// 15291: 714 -> 438 us against one XCD for each; the weights of 3084 tokens behind 5208, 2 heads: 105 -> 89 with the attention.)
+struct Place {
+  int group, tile;                             // (tile: maybe behind the last)
+};
+__device__ inline Place place_of(int heads, int tiles) {
+  const int together = min(heads & -heads, 8), of = 8 / together, each = (tiles + of - 1) / of;      // groups beside each other; XCDs of one
+  const int x = (int)(blockIdx.x & 7), i = (int)(blockIdx.x >> 3);
+  return {i / each * together + x % together, i % each * of + x / together};
+}
+unsigned places(unsigned groups, int heads, int tiles) {
+  const unsigned together = (unsigned)std::min(heads & -heads, 8), of = 8 / together;
+  return groups / together * ((tiles + of - 1) / of) * 8;
+}
+
 // grid: groups of MERGE_ROWS / slices rows x KV heads x sequences.
 template <typename T, int D>
 __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, int slices, bool tiled) {
@@ -681,9 +697,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
   if (blockIdx.x == 0 && a.status)
     for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  // the tiles of a KV head and share, the longest first, on one XCD, whose L2 then has their columns
-  const int idx = (int)(blockIdx.x >> 3), group = idx / a.tiles * 8 + (int)(blockIdx.x & 7), tile = a.tiles - 1 - idx % a.tiles;
-  const int h = group % p.Hkv, w = group / p.Hkv;
+  const Place place = place_of(p.Hkv, a.tiles);        // the longest tiles first
+  if (place.tile >= a.tiles) return;
+  const int tile = a.tiles - 1 - place.tile, h = place.group % p.Hkv, w = place.group / p.Hkv;
   const Columns columns = columns_of(a, true);
   const int size = columns.size;
   Run run;
@@ -953,9 +969,9 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of queries
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
-  const int idx = (int)(blockIdx.x >> 3), group = idx / col_tiles * 8 + (int)(blockIdx.x & 7), ct = idx % col_tiles;
-  const int h = group % p.Hkv, b = group / p.Hkv;
-  if (b >= p.B) return;
+  const Place place = place_of(p.Hkv, col_tiles);
+  const int ct = place.tile, h = place.group % p.Hkv, b = place.group / p.Hkv;
+  if (ct >= col_tiles) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
   if (s.n == 0 || first_col >= s.len) return;
@@ -1098,14 +1114,14 @@ template <typename T, int D>
 int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream_t s) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
-  // shares (where they are of one sequence each, one more a sequence at most)
-  const unsigned groups = (unsigned)(a.shares + (a.shares > 1 ? p.B : p.B - 1)) * p.Hkv;
+  // shares: where they are of one sequence each, one more for each sequence but one at most
+  const unsigned groups = (unsigned)(a.shares + p.B - 1) * p.Hkv;
   if (sh.tiled) {
     if constexpr (sizeof(T) == 2) {
       const int lds = 4 * TILE * D * 2;
       auto kernel = attend_tiled_kernel<D>;
       if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return TREEKV_EHIP;
-      hipLaunchKernelGGL(kernel, dim3((groups + 7) / 8 * 8 * a.tiles), dim3(PA_THREADS), lds, s, a);
+      hipLaunchKernelGGL(kernel, dim3(places(groups, p.Hkv, a.tiles)), dim3(PA_THREADS), lds, s, a);
     }
   } else {
     const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
@@ -1132,7 +1148,7 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
     if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)
       if constexpr (sizeof(T) == 2) {
         const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
-        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3((units + 7) / 8 * 8 * all), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);
+        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3(places(units, p.Hkv, all)), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);
       }
     } else {
       constexpr int WIDE = PA_WAVES * 2 * Ops<T, D>::COLS;
