@@ -1095,9 +1095,9 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   const long long groups = (long long)c.kv_heads * s.tiles, want = s.tiled ? 512 : 256;
   // (few rows: one workgroup a compute unit has enough on its way, and leaves fewer shares to add: 16 sequences of 16000 columns
   // and one token 118 us, with two 121, with three or four 123 to 134; row tiles: two, 168 us for 512 tokens behind 16000, with
-  // one 186, but one alone rather than two shares of what fills more than two thirds of the chip: 2000 tokens 60 us, with two 85)
+  // one 186, but no more of them than are at work together, 768 tokens 275 us, with a third more 305)
   const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
-  s.shares = (int)(s.tiled ? max((want + groups / 2) / groups, 1ll) : (want + groups - 1) / groups);
+  s.shares = (int)(s.tiled ? max(want / groups, 1ll) : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
   // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them, for up to 32 rows (8 sequences
   // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike)
