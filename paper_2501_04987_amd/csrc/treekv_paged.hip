@@ -103,6 +103,7 @@ struct Attend {
   int32_t* status;
   float* logits;                             // few rows and weights: scaled logits, [sequence][KV head][row][cap]
   int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
+  int least_rows, most_rows;                 // sequences with others are not this kernel's
   float scale_log2e;
   bool wide;                                 // more columns than 32 bits count
 };
@@ -119,7 +120,8 @@ struct Run {
 __device__ inline int tokens_to_read(const Attend& a, int b) {
   if (b >= a.p.B) return 0;
   const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
-  return s.n > 0 ? (s.len + 31) & ~31 : 0;
+  const int rows = s.n * a.p.G;
+  return rows >= a.least_rows && rows <= a.most_rows ? (s.len + 31) & ~31 : 0;
 }
 __device__ inline long long uniform64(long long x) {
   return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
@@ -526,18 +528,36 @@ unsigned places(unsigned groups, int heads, int tiles) {
   return groups / together * ((tiles + of - 1) / of) * 8;
 }
 
-// grid: groups of MERGE_ROWS / slices rows x KV heads x sequences.
-template <typename T, int D>
+// grid: groups of MERGE_ROWS / slices rows x KV heads x sequences.  PACKED: groups of all sequences one after the other x KV heads
+// (where the longest sequence's are many more than the others': one of 512 tokens among 31 of one, 56 -> 13 us).
+template <typename T, int D, bool PACKED>
 __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_tiles, int slices, bool tiled) {
   __shared__ Merged sm;
   const Pages& p = a.p;
-  const int tile = (int)(blockIdx.x % merge_tiles), rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
+  const int at_once = MERGE_ROWS<D> / slices, rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv;
+  int tile = (int)(blockIdx.x % merge_tiles), b = rest / p.Hkv;
+  if (PACKED) {
+    const int lane = threadIdx.x & 63;
+    unsigned long long hit = 0;
+    for (int b0 = 0; b0 < p.B && !hit; b0 += 64) {
+      const int mine = tokens_to_read(a, b0 + lane) ? (load_seq(p, a.starts, a.tokens, a.longest, b0 + lane).n * p.G + at_once - 1) / at_once : 0;
+      long long all;
+      const int sum = (int)wave_scan(mine, false, all);
+      hit = __ballot(sum > tile);
+      if (hit) {
+        b = __ffsll((long long)hit) - 1;
+        tile -= __builtin_amdgcn_readlane(sum - mine, b);
+        b += b0;
+      } else tile -= (int)all;
+    }
+    if (!hit) return;
+  }
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  if (tile * (MERGE_ROWS<D> / slices) >= s.n * p.G) return;
+  if (tile * at_once >= s.n * p.G) return;
   Run run;
   const Columns columns = columns_of(a, tiled);
   if (!find_run(a, columns, 0, b, run) || run.count <= 1) return;
-  merge_rows<T, D>(a, s, run, h, tile * (MERGE_ROWS<D> / slices), s.n * p.G, slices, sm);
+  merge_rows<T, D>(a, s, run, h, tile * at_once, s.n * p.G, slices, sm);
 }
 
 // The same where the logits of up to 32 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
@@ -553,7 +573,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int rows = s.n * p.G, c0 = piece * (4 * PA_THREADS);
   const int at_once = MERGE_ROWS<D> / slices;
-  if (rows == 0 || (c0 >= s.len && piece * at_once >= rows)) return;
+  if (rows < a.least_rows || rows > a.most_rows || (c0 >= s.len && piece * at_once >= rows)) return;
   Run run;
   const Columns columns = columns_of(a, false);
   if (!find_run(a, columns, 0, b, run)) return;
@@ -614,7 +634,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
   const int ct = (int)(blockIdx.x % col_tiles), rest = (int)(blockIdx.x / col_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int c0 = (ct * PA_WAVES + wave) * WIDE;
-  if (s.n == 0 || c0 >= s.len) return;
+  if (s.n * p.G < a.least_rows || c0 >= s.len) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
   typename O::Keys k[NB];
@@ -974,7 +994,7 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   if (ct >= col_tiles) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
-  if (s.n == 0 || first_col >= s.len) return;
+  if (s.n * p.G < a.least_rows || first_col >= s.len) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n;
   uint4 k[KS];
@@ -1082,8 +1102,9 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
 // ---- launches ----------------------------------------------------------------------------------
 struct AttendShape {
   int rows, tiles, shares;                   // rows of a tile
-  bool tiled, keep, weigh_tiled;             // many rows through LDS; logits kept for the weights; weights of many rows through LDS
-  size_t part, logits, stat;                 // bytes of scratch: shares' results, logits, rows' references and sums
+  int short_shares;                          // of the sequences with up to 16 rows, where they are taken by themselves
+  bool tiled, keep, short_keep, weigh_tiled; // many rows through LDS; logits kept for the weights; weights of many rows through LDS
+  size_t part, short_part, logits, stat;     // bytes of scratch: shares' results, logits, rows' references and sums
 };
 AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const long long rows = (long long)longest * (c.q_heads / c.kv_heads), cap = (long long)c.table_width * c.page_size;
@@ -1099,24 +1120,39 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
   s.shares = (int)(s.tiled ? max(want / groups, 1ll) : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
+  // A few chunks among many sequences of a token or two: those are attended by the kernel for few rows, in a launch of its own
+  // (512 tokens and 31 single ones behind 8000 each, 8 groups of 4: 268 us in place of 596, with weights 374 in place of 855).
+  s.short_shares = s.tiled && (long long)tokens * 4 <= (long long)longest * c.batch && c.q_heads / c.kv_heads <= 16
+                       ? (int)std::min<long long>((256 + c.kv_heads - 1) / c.kv_heads, most) : 0;
   // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them, for up to 32 rows (8 sequences
   // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike)
   // (what that asks of the query rows' distance, the launch adds)
   s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
   s.keep = weigh && rows <= 32 && (size_t)units * s.rows * cap * 4 <= (size_t)1 << 30;
+  s.short_keep = weigh && s.short_shares && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
   s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
-  s.logits = s.keep ? align_up((size_t)units * s.rows * cap * 4) : 0;
+  s.short_part = s.short_shares ? align_up((size_t)(s.short_shares + c.batch) * c.kv_heads * 16 * (c.head_dim + 4) * 4) : 0;
+  s.logits = s.keep || s.short_keep ? align_up((size_t)units * (s.keep ? s.rows : 16) * cap * 4) : 0;
   s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
   return s;
 }
 
+// Groups of threads for a row's shares: each takes up to eight, all on their way together (one token behind 8000, 8 KV heads, 32
+// shares: 33.6 us with one group, 16.5 with four).
+template <int D>
+int merge_slices(const Attend& a) {
+  int slices = 1;
+  while (slices < MERGE_ROWS<D> && (a.shares / a.p.B + 1) > 8 * slices) slices *= 2;
+  return slices;
+}
+// The attention of the sequences with least_rows to most_rows rows.
 template <typename T, int D>
-int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream_t s) {
+int launch_shares(const Attend& a, bool tiled, bool keep, hipStream_t s) {
   constexpr int OR = D + 4;
   const Pages& p = a.p;
   // shares: where they are of one sequence each, one more for each sequence but one at most
   const unsigned groups = (unsigned)(a.shares + p.B - 1) * p.Hkv;
-  if (sh.tiled) {
+  if (tiled) {
     if constexpr (sizeof(T) == 2) {
       const int lds = 4 * TILE * D * 2;
       auto kernel = attend_tiled_kernel<D>;
@@ -1124,27 +1160,50 @@ int launch_attend_d(const Attend& a, const AttendShape& sh, int weigh, hipStream
       hipLaunchKernelGGL(kernel, dim3(places(groups, p.Hkv, a.tiles)), dim3(PA_THREADS), lds, s, a);
     }
   } else {
-    const size_t lds = (size_t)PA_WAVES * sh.rows * (OR * 4 + 8);
-    auto kernel = sh.rows != 16 ? sh.keep ? attend_kernel<T, D, 2, true> : attend_kernel<T, D, 2, false> : sh.keep ? attend_kernel<T, D, 1, true> : attend_kernel<T, D, 1, false>;
+    const size_t lds = (size_t)PA_WAVES * a.rows * (OR * 4 + 8);
+    auto kernel = a.rows != 16 ? keep ? attend_kernel<T, D, 2, true> : attend_kernel<T, D, 2, false> : keep ? attend_kernel<T, D, 1, true> : attend_kernel<T, D, 1, false>;
     if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds))) return TREEKV_EHIP;
     hipLaunchKernelGGL(kernel, dim3(groups * a.tiles), dim3(PA_THREADS), lds, s, a);
   }
+  if (a.shares > 1 && !keep) {
+    const int slices = merge_slices<D>(a), at_once = MERGE_ROWS<D> / slices;
+    const int all = (std::min(a.longest * p.G, a.most_rows) + at_once - 1) / at_once;
+    const long long packed = (long long)a.tokens * p.G / at_once + p.B;
+    if (2 * packed < (long long)all * p.B)
+      hipLaunchKernelGGL((merge_kernel<T, D, true>), dim3((unsigned)(packed * p.Hkv)), dim3(PA_THREADS), 0, s, a, (int)packed, slices, tiled);
+    else hipLaunchKernelGGL((merge_kernel<T, D, false>), dim3((unsigned)(p.Hkv * p.B) * all), dim3(PA_THREADS), 0, s, a, all, slices, tiled);
+  }
+  return finish_launch();
+}
+
+// What they add to the weights, and the merge, where the logits have been kept.
+template <typename T, int D>
+int launch_kept(const Attend& a, hipStream_t s) {
+  const Pages& p = a.p;
+  const int slices = merge_slices<D>(a), at_once = MERGE_ROWS<D> / slices;
+  const int all = std::max((p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS), (std::min(a.longest * p.G, a.most_rows) + at_once - 1) / at_once);
+  hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3((unsigned)(p.Hkv * p.B) * all), dim3(PA_THREADS), 0, s, a, all, slices);
+  return finish_launch();
+}
+
+template <typename T, int D>
+int launch_attend_d(Attend a, const AttendShape& sh, int weigh, hipStream_t s) {
+  const Pages& p = a.p;
+  if (sh.short_shares) {
+    Attend few = a;
+    few.part = (float*)((char*)a.part + sh.part);
+    few.tiles = 1; few.rows = 16; few.shares = sh.short_shares;
+    few.most_rows = 16;
+    if (int e = launch_shares<T, D>(few, false, sh.short_keep, s)) return e;
+    if (sh.short_keep)
+      if (int e = launch_kept<T, D>(few, s)) return e;
+    a.least_rows = 17;
+  }
+  if (int e = launch_shares<T, D>(a, sh.tiled, sh.keep, s)) return e;
+  if (sh.keep) return launch_kept<T, D>(a, s);
   const unsigned units = (unsigned)(p.Hkv * p.B);
-  // where a row has many shares, several groups of threads take up to eight each, all on their way together (one token behind
-  // 8000, 8 KV heads, 32 shares: 33.6 us with one group, 16.5 with four)
-  int slices = 1;
-  while (slices < MERGE_ROWS<D> && (a.shares / p.B + 1) > 8 * slices) slices *= 2;
-  if (sh.keep) {
-    const int at_once = MERGE_ROWS<D> / slices;
-    const int all = max((p.cap + 4 * PA_THREADS - 1) / (4 * PA_THREADS), (a.longest * p.G + at_once - 1) / at_once);
-    hipLaunchKernelGGL((merge_weigh_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, slices);
-    return finish_launch();
-  }
-  if (a.shares > 1) {
-    const int at_once = MERGE_ROWS<D> / slices, all = (a.longest * p.G + at_once - 1) / at_once;
-    hipLaunchKernelGGL((merge_kernel<T, D>), dim3(units * all), dim3(PA_THREADS), 0, s, a, all, slices, sh.tiled);
-  }
   if (weigh) {
+    if (!sh.short_keep) a.least_rows = 1;
     if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)
       if constexpr (sizeof(T) == 2) {
         const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
@@ -1176,7 +1235,7 @@ int launch_paged_append(const treekv_paged_cache& c, const void* k, const void* 
 
 size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const AttendShape s = attend_shape(c, tokens, longest, weigh);
-  return s.part + s.logits + s.stat;
+  return s.part + s.short_part + s.logits + s.stat;
 }
 
 int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
@@ -1189,11 +1248,12 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.q_far = q_stride * (c.dtype == TREEKV_F32 ? 4 : 2);
   a.out = (char*)out;
   a.part = (float*)scratch;
-  a.logits = (float*)((char*)scratch + sh.part);
-  a.stat = sh.stat ? (float2*)((char*)scratch + sh.part + sh.logits) : nullptr;
+  a.logits = (float*)((char*)scratch + sh.part + sh.short_part);
+  a.stat = sh.stat ? (float2*)((char*)scratch + sh.part + sh.short_part + sh.logits) : nullptr;
   a.lse = lse;
   a.status = status;
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
+  a.least_rows = 1; a.most_rows = INT_MAX;
   a.wide = (long long)c.batch * (a.p.cap + 31) > 1 << 30;
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
   if (c.dtype == TREEKV_F32) return c.head_dim == 128 ? launch_attend_d<float, 128>(a, sh, weigh, s) : launch_attend_d<float, 64>(a, sh, weigh, s);

@@ -92,6 +92,23 @@ CUTS = [
 ]
 
 
+# Chunks among sequences of a token or two.
+MIXES = [
+    dict(lens=[700, 300, 40, 1, 513, 90, 77, 133], news=[200, 1, 2, 0, 1, 9, 1, 8], page_size=16, kv_heads=2, group=2, d=128),
+    dict(lens=[5, 1, 1500, 260, 31, 2, 900, 64, 17], news=[1, 1, 1, 100, 2, 2, 1, 1, 0], page_size=32, kv_heads=1, group=16, d=64),
+    dict(lens=[90, 70, 80, 0, 0, 0, 0, 0, 0], news=[70, 17, 9, 0, 0, 0, 0, 0, 0], page_size=64, kv_heads=3, group=1, d=64),
+    dict(lens=[400] * 70, news=[1] * 35 + [130] + [1] * 34, page_size=32, kv_heads=1, group=4, d=64),
+    dict(lens=[160, 300, 33, 20, 9], news=[80, 1, 1, 3, 2], page_size=16, kv_heads=1, group=17, d=64),
+]
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("mix", range(len(MIXES)))
+def test_chunks_among_single_tokens(binding, mix, weigh):
+    ref = paged(**MIXES[mix], seed=mix)
+    check_attend(ref.on_gpu(binding), ref, weigh=weigh)
+
+
 @pytest.mark.parametrize("weigh,dtype", [(False, "bf16"), (True, "bf16"), (True, "f32")])
 @pytest.mark.parametrize("cut", range(len(CUTS)))
 def test_columns_cut_into_shares(binding, cut, weigh, dtype):
