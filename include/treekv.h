@@ -425,7 +425,8 @@ int treekv_paged_append(const treekv_paged_cache* cache, const void* k, const vo
                         const int32_t* starts, int tokens, const int32_t* positions, int32_t* status, void* stream);
 
 /* Device memory treekv_paged_attend needs for `tokens` rows, `longest` at most of one sequence; 0 if it needs none (or the
- * arguments are not accepted).  It holds nothing between calls: one piece serves all calls that do not overlap. */
+ * arguments are not accepted).  Fewer rows can need more, as their columns are cut into more shares: the maximum over the calls
+ * to come is the one to keep.  It holds nothing between calls: one piece serves all calls that do not overlap. */
 size_t treekv_paged_attend_scratch_bytes(const treekv_paged_cache* cache, int tokens, int longest, int weigh);
 
 /*

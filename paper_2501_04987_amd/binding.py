@@ -413,7 +413,7 @@ class PagedKV:
                  starts.data_ptr(), k.shape[0], _ptr(positions), status_at)
 
     def new_attend_scratch(self, tokens: int, longest: int, weigh: bool = False):
-        """What `attend` takes as `scratch` (None where it needs none)."""
+        """What `attend` takes as `scratch` for these arguments (None where it needs none; fewer tokens can need more)."""
         import torch
 
         need = (_lib or load()).treekv_paged_attend_scratch_bytes(self._at, int(tokens), int(longest), int(weigh))
