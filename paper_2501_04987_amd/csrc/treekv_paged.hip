@@ -101,6 +101,7 @@ struct Attend {
   float *lse, *part;
   float2* stat;                              // for the weights: a row's reference and 1 / its sum (infinity and 0 if it adds nothing)
   int32_t* status;
+  float* gains;                              // splits of a column's rows: [split][sequence][KV head][cap]
   float* logits;                             // few rows and weights: scaled logits, [sequence][KV head][row][cap]
   int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
   int least_rows, most_rows;                 // sequences with others are not this kernel's
@@ -983,15 +984,15 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
 // has row l % 32 and adds up its columns over the rows it meets; the lanes are added at the end.  grid: column tiles x KV heads x
 // sequences.
 template <int D>
-__global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, int col_tiles) {
+__global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, int col_tiles, int splits) {
   constexpr int KS = D / 16, ROWB = D * 2, STAGE = TILE * ROWB;
   constexpr int PIECES = D / 8, AT_ONCE = 64 / PIECES, COPIES = TILED_SUB / AT_ONCE;
   extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of queries
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
-  const Place place = place_of(p.Hkv, col_tiles);
-  const int ct = place.tile, h = place.group % p.Hkv, b = place.group / p.Hkv;
-  if (ct >= col_tiles) return;
+  const Place place = place_of(p.Hkv, col_tiles * splits);
+  const int ct = place.tile % col_tiles, split = place.tile / col_tiles, h = place.group % p.Hkv, b = place.group / p.Hkv;
+  if (split >= splits) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
   if (s.n * p.G < a.least_rows || first_col >= s.len) return;
@@ -1043,9 +1044,13 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
     }
   };
   f32x16_t acc = {};
-  const int begin = max(0, first_col - old);           // tokens before see none of the columns
-  request(begin, 0);
-  stats(begin);
+  const int sees_it = max(0, first_col - old);         // tokens before see none of the columns
+  const int share = ((s.n - sees_it + per - 1) / per + splits - 1) / splits * per;
+  const int begin = min(sees_it + split * share, s.n), end = min(begin + share, s.n);
+  if (begin < end) {
+    request(begin, 0);
+    stats(begin);
+  }
   int stage = 0;
   const unsigned at_q = r * ROWB + ((hf ^ swap_k<D>(r)) << 4);        // of step e: XOR 2 e pieces
   struct Yes { __device__ constexpr operator bool() const { return true; } };
@@ -1074,12 +1079,12 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
     }
   };
 #pragma unroll 1
-  for (int first = begin; first < s.n; first += per, stage ^= 1) {
+  for (int first = begin; first < end; first += per, stage ^= 1) {
     wait_vmcnt<0>();
     __syncthreads();
     const float2 now[2] = {l[0], l[1]};
     const int sees[2] = {see[0], see[1]};
-    if (first + per < s.n) {
+    if (first + per < end) {
       request(first + per, stage ^ 1);
       stats(first + per);
     }
@@ -1094,17 +1099,34 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
     const int c = c0 + 8 * (i >> 2) + 4 * hf + (i & 3);
     if (r == 0 && c < s.len) {
       const int page = table[c >> p.bits];
-      if (page >= 0 && page < p.pages) weights[c] += e;
+      if (splits > 1) a.gains[(((size_t)split * p.B + b) * p.Hkv + h) * p.cap + c] = e;
+      else if (page >= 0 && page < p.pages) weights[c] += e;
     }
   }
+}
+
+// The splits' sums go to the weights.  grid: pieces of the columns x KV heads x sequences.
+__global__ __launch_bounds__(PA_THREADS) void add_gains_kernel(Attend a, int pieces, int splits) {
+  const Pages& p = a.p;
+  const int c = (int)(blockIdx.x % pieces) * PA_THREADS + threadIdx.x, rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv;
+  const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  if (s.n * p.G < a.least_rows || c >= s.len) return;
+  const int page = p.table[(size_t)b * p.width + (c >> p.bits)];
+  if (page < 0 || page >= p.pages) return;
+  const float* gain = a.gains + ((size_t)b * p.Hkv + h) * p.cap + c;
+  const size_t far = (size_t)p.B * p.Hkv * p.cap;
+  float e = 0.f;
+  for (int z = 0; z < splits; ++z) e += gain[z * far];
+  p.weights[track_row(p, b, h) + c] += e;
 }
 
 // ---- launches ----------------------------------------------------------------------------------
 struct AttendShape {
   int rows, tiles, shares;                   // rows of a tile
+  int weigh_splits;                          // parts of the rows that a column's weights are summed in
   int short_shares;                          // of the sequences with up to 16 rows, where they are taken by themselves
   bool tiled, keep, short_keep, weigh_tiled; // many rows through LDS; logits kept for the weights; weights of many rows through LDS
-  size_t part, short_part, logits, stat;     // bytes of scratch: shares' results, logits, rows' references and sums
+  size_t part, short_part, logits, stat, gains;     // bytes of scratch: shares' results, logits, rows' references and sums, splits' sums
 };
 AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const long long rows = (long long)longest * (c.q_heads / c.kv_heads), cap = (long long)c.table_width * c.page_size;
@@ -1133,6 +1155,15 @@ AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, i
   s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
   s.short_part = s.short_shares ? align_up((size_t)(s.short_shares + c.batch) * c.kv_heads * 16 * (c.head_dim + 4) * 4) : 0;
   s.logits = s.keep || s.short_keep ? align_up((size_t)units * (s.keep ? s.rows : 16) * cap * 4) : 0;
+  // few column tiles: each one's rows are shared between up to 16 workgroups, with two tiles of them at least, and their sums added
+  // in a launch of its own (attention and weights of 2048 tokens behind 2000, one group of 8: 297 -> 90 us, 512 of 8 groups of 4
+  // alone 65 -> 41; four tiles at least: 100 tokens behind 1000 37 us, with two 34)
+  s.weigh_splits = 1;
+  if (weigh && !s.keep && s.weigh_tiled) {
+    const long long tiles = (cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32) * units;
+    s.weigh_splits = (int)std::max(std::min({512 / tiles, rows / (2 * TILE), 16ll}), 1ll);
+  }
+  s.gains = s.weigh_splits > 1 ? align_up((size_t)s.weigh_splits * units * cap * 4) : 0;
   s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
   return s;
 }
@@ -1207,7 +1238,12 @@ int launch_attend_d(Attend a, const AttendShape& sh, int weigh, hipStream_t s) {
     if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)
       if constexpr (sizeof(T) == 2) {
         const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
-        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3(places(units, p.Hkv, all)), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all);
+        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3(places(units, p.Hkv, all * sh.weigh_splits)), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all,
+                           sh.weigh_splits);
+        if (sh.weigh_splits > 1) {
+          const int pieces = (p.cap + PA_THREADS - 1) / PA_THREADS;
+          hipLaunchKernelGGL(add_gains_kernel, dim3(units * pieces), dim3(PA_THREADS), 0, s, a, pieces, sh.weigh_splits);
+        }
       }
     } else {
       constexpr int WIDE = PA_WAVES * 2 * Ops<T, D>::COLS;
@@ -1235,7 +1271,7 @@ int launch_paged_append(const treekv_paged_cache& c, const void* k, const void* 
 
 size_t paged_attend_scratch_bytes(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
   const AttendShape s = attend_shape(c, tokens, longest, weigh);
-  return s.part + s.short_part + s.logits + s.stat;
+  return s.part + s.short_part + s.logits + s.stat + s.gains;
 }
 
 int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_stride, const int32_t* starts, int tokens, int longest,
@@ -1250,6 +1286,7 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.part = (float*)scratch;
   a.logits = (float*)((char*)scratch + sh.part + sh.short_part);
   a.stat = sh.stat ? (float2*)((char*)scratch + sh.part + sh.short_part + sh.logits) : nullptr;
+  a.gains = (float*)((char*)scratch + sh.part + sh.short_part + sh.logits + sh.stat);
   a.lse = lse;
   a.status = status;
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;

@@ -109,6 +109,25 @@ def test_chunks_among_single_tokens(binding, mix, weigh):
     check_attend(ref.on_gpu(binding), ref, weigh=weigh)
 
 
+@pytest.mark.parametrize("lens,news,hkv,group,d", [([900, 400], [600, 400], 1, 2, 128), ([700, 40, 300], [699, 1, 300], 2, 3, 64),
+                                                   ([1300], [1300], 1, 1, 64), ([260, 0, 300], [257, 0, 0], 1, 64, 64)])
+def test_weights_of_many_rows_over_few_columns(binding, lens, news, hkv, group, d):
+    """The rows of a column are summed in parts; what is in a page given up, and behind the last token, stays."""
+    import torch
+
+    ref = paged(lens=lens, news=news, page_size=32, kv_heads=hkv, group=group, d=d, seed=23)
+    ref.table[0, 2] = -1
+    kv = ref.on_gpu(binding)
+    before = kv.weights.clone()
+    check_attend(kv, ref, weigh=True)
+    for b, n in enumerate(lens):
+        assert torch.equal(kv.weights[b, :, n if news[b] else 0:], before[b, :, n if news[b] else 0:])
+    assert torch.equal(kv.weights[0, :, 64:96], before[0, :, 64:96])
+    again = ref.on_gpu(binding)
+    again.attend(ref.q.cuda(), ref.starts.cuda(), max(news), weigh=True)
+    assert torch.equal(again.weights, kv.weights)
+
+
 @pytest.mark.parametrize("weigh,dtype", [(False, "bf16"), (True, "bf16"), (True, "f32")])
 @pytest.mark.parametrize("cut", range(len(CUTS)))
 def test_columns_cut_into_shares(binding, cut, weigh, dtype):
