@@ -169,7 +169,7 @@ __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   wave_scan(mine, a.wide, total);
   const long long each = a.wide ? (total + a.shares - 1) / a.shares : (int)(((unsigned)total + a.shares - 1) / (unsigned)a.shares);
   c.size = (int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30);
-  if (tiled) c.size = max(c.size, min(2 * c.size, TILED_SHARE));
+  if (tiled && 2 * c.size <= TILED_SHARE) c.size *= 2;
   c.own = tiled || c.size == MIN_SHARE;
   if (!c.own && c.size <= SHORT && !a.wide && a.shares > 1) {
     c.own = a.p.B > a.shares;
@@ -514,19 +514,26 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
   }
 }
 // The tiles of a group (a KV head of a share or of a sequence) run on one XCD, whose L2 then has what they share, and with fewer
-// than 8 KV heads on as many XCDs as leaves none idle.  (2 KV heads, groups of 8, 2154 tokens behind
-// 15291: 714 -> 438 us against one XCD for each; the weights of 3084 tokens behind 5208, 2 heads: 105 -> 89 with the attention.)
+// than 8 KV heads on as many XCDs as leaves none idle, as far as there are tiles for them, which another group begins at another
+// of them; not where there are four groups or more for each XCD (of `turns` shares or sequences).  (2 KV heads, groups of 8, 2154
+// tokens behind 15291: 714 -> 438 us against one XCD for each; the weights of 3084 tokens behind 5208, 2 heads: 105 -> 71 with the
+// attention, and their rows shared between workgroups.)
 struct Place {
-  int group, tile;                             // (tile: maybe behind the last)
+  int group, tile;                             // (maybe behind the last)
 };
-__device__ inline Place place_of(int heads, int tiles) {
-  const int together = min(heads & -heads, 8), of = 8 / together, each = (tiles + of - 1) / of;      // groups beside each other; XCDs of one
-  const int x = (int)(blockIdx.x & 7), i = (int)(blockIdx.x >> 3);
-  return {i / each * together + x % together, i % each * of + x / together};
+__host__ __device__ inline int xcds_of_group(int heads, int turns, int tiles) {
+  int of = 1;
+  while (of < 8 && heads % (8 / of) != 0 && (long long)heads * turns < 4 * (8 / of) && 2 * of <= tiles) of *= 2;
+  return of;
 }
-unsigned places(unsigned groups, int heads, int tiles) {
-  const unsigned together = (unsigned)std::min(heads & -heads, 8), of = 8 / together;
-  return groups / together * ((tiles + of - 1) / of) * 8;
+__device__ inline Place place_of(int heads, int turns, int tiles) {
+  const int of = xcds_of_group(heads, turns, tiles), together = 8 / of, each = (tiles + of - 1) / of;       // groups beside each other
+  const int x = (int)(blockIdx.x & 7), i = (int)(blockIdx.x >> 3);
+  return {i / each * together + x % together, i % each * of + (x / together + i / each) % of};
+}
+unsigned places(unsigned groups, int heads, int turns, int tiles) {
+  const unsigned of = xcds_of_group(heads, turns, tiles), together = 8 / of;
+  return (groups + together - 1) / together * ((tiles + of - 1) / of) * 8;
 }
 
 // grid: groups of MERGE_ROWS / slices rows x KV heads x sequences.  PACKED: groups of all sequences one after the other x KV heads
@@ -718,7 +725,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
   if (blockIdx.x == 0 && a.status)
     for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  const Place place = place_of(p.Hkv, a.tiles);        // the longest tiles first
+  const Place place = place_of(p.Hkv, a.shares, a.tiles);        // the longest tiles first
   if (place.tile >= a.tiles) return;
   const int tile = a.tiles - 1 - place.tile, h = place.group % p.Hkv, w = place.group / p.Hkv;
   const Columns columns = columns_of(a, true);
@@ -990,9 +997,9 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of queries
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
-  const Place place = place_of(p.Hkv, col_tiles * splits);
+  const Place place = place_of(p.Hkv, p.B, col_tiles * splits);
   const int ct = place.tile % col_tiles, split = place.tile / col_tiles, h = place.group % p.Hkv, b = place.group / p.Hkv;
-  if (split >= splits) return;
+  if (split >= splits || b >= p.B) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
   if (s.n * p.G < a.least_rows || first_col >= s.len) return;
@@ -1188,7 +1195,7 @@ int launch_shares(const Attend& a, bool tiled, bool keep, hipStream_t s) {
       const int lds = 4 * TILE * D * 2;
       auto kernel = attend_tiled_kernel<D>;
       if (lds > 48 * 1024 && hip_failed(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return TREEKV_EHIP;
-      hipLaunchKernelGGL(kernel, dim3(places(groups, p.Hkv, a.tiles)), dim3(PA_THREADS), lds, s, a);
+      hipLaunchKernelGGL(kernel, dim3(places(groups, p.Hkv, a.shares, a.tiles)), dim3(PA_THREADS), lds, s, a);
     }
   } else {
     const size_t lds = (size_t)PA_WAVES * a.rows * (OR * 4 + 8);
@@ -1238,7 +1245,7 @@ int launch_attend_d(Attend a, const AttendShape& sh, int weigh, hipStream_t s) {
     if (sh.weigh_tiled && a.q_far < 1 << 24) {         // (places of 64 rows in 32 bits)
       if constexpr (sizeof(T) == 2) {
         const int all = (p.cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32);
-        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3(places(units, p.Hkv, all * sh.weigh_splits)), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all,
+        hipLaunchKernelGGL((weigh_tiled_kernel<D>), dim3(places(units, p.Hkv, p.B, all * sh.weigh_splits)), dim3(PA_THREADS), 2 * TILE * D * 2, s, a, all,
                            sh.weigh_splits);
         if (sh.weigh_splits > 1) {
           const int pieces = (p.cap + PA_THREADS - 1) / PA_THREADS;
