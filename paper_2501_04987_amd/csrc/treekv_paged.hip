@@ -17,6 +17,7 @@
 
 #include "treekv_matrix.h"
 #include "treekv_paged.h"
+#include "treekv_shares.h"
 
 // Multiply-adds only where they are written: a logit has to be rounded like the reference that it was compared to (fused with the
 // subtraction of the reference it would differ by what the reference lost, 2^7 from 2^31 on).
@@ -25,9 +26,6 @@
 namespace tkv {
 
 namespace {
-
-constexpr int PA_THREADS = 256, PA_WAVES = PA_THREADS / 64;
-constexpr int MIN_SHARE = 128;               // columns: a block for each wave
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
@@ -113,10 +111,9 @@ struct Attend {
 // into shares of `size`.  Few rows over many columns: a workgroup takes one share, whatever sequences it runs through; what it has
 // of sequence b is partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round, and
 // small shares: a sequence's shares start at its first token, so that each is of one sequence (its `own`).
-struct Run {
+struct Run : Runs {
   int b, length;             // a sequence with columns, and their number
   long long start;           // where they start
-  int first, count;          // its partial results
 };
 __device__ inline int tokens_to_read(const Attend& a, int b) {
   if (b >= a.p.B) return 0;
@@ -149,16 +146,9 @@ __device__ inline long long wave_scan(long long x, bool wide, long long& all) {
   all = __builtin_amdgcn_readlane(v, 63);
   return v;
 }
-// What find_run asks of the lengths: the size of a share, whether shares are of one sequence each, and this lane's sequence among
-// the first 64.  A second sequence in a share costs a workgroup about what STRADDLE more columns do.  Up to SHORT columns a share,
-// a size that is larger by no more and gives every sequence shares of its own, no more of them than were to be, is taken (8
-// sequences of 2048 columns and one token, 8 KV heads: 22.0 -> 18.9 us); sequences that are more than the shares take one or
-// two each (64 of 500: 29.5 -> 24.2 us; of 2048 columns 67 either way).  Row tiles: what 128 rows write and read again for
-// another share costs about what it gains up to TILED_SHARE columns (200 tokens behind 1000, groups of 4: 33.3 -> 27.1 us).
-constexpr int STRADDLE = 256, SHORT = 1024, TILED_SHARE = 1024;
-struct Columns {
-  int size, length;
-  bool own;
+// What find_run asks of the lengths: the cut, and this lane's sequence among the first 64.
+struct Columns : Cut {
+  int length;
 };
 __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   const int lane = threadIdx.x & 63;
@@ -167,19 +157,11 @@ __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   long long total, mine = c.length;
   for (int b = 64 + lane; b < a.p.B; b += 64) mine += tokens_to_read(a, b);
   wave_scan(mine, a.wide, total);
-  const long long each = a.wide ? (total + a.shares - 1) / a.shares : (int)(((unsigned)total + a.shares - 1) / (unsigned)a.shares);
-  c.size = (int)min(max((each + 31) / 32 * 32, (long long)MIN_SHARE), 1ll << 30);
-  if (tiled && 2 * c.size <= TILED_SHARE) c.size *= 2;
-  c.own = tiled || c.size == MIN_SHARE;
-  if (!c.own && c.size <= SHORT && !a.wide && a.shares > 1) {
-    c.own = a.p.B > a.shares;
-    if (a.p.B <= min(a.shares, 64))
-      for (int size = c.size; size <= c.size + STRADDLE; size += 64) {
-        long long count;
-        wave_scan((unsigned)(c.length + size - 1) / (unsigned)size, false, count);
-        if ((int)count <= a.shares) { c.size = size; c.own = true; break; }
-      }
-  }
+  static_cast<Cut&>(c) = cut_columns(total, a.shares, a.p.B, tiled, a.wide, [&](int size) {
+    long long count;
+    wave_scan(shares_in(c.length, size), false, count);
+    return (int)count;
+  });
   return c;
 }
 // The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
@@ -188,7 +170,7 @@ __device__ inline bool find_run(const Attend& a, const Columns& c, long long at,
   const bool own = c.own;
   long long before = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
-    const int length = b0 ? tokens_to_read(a, b0 + lane) : c.length, mine = own ? (length + size - 1) / size : length;
+    const int length = b0 ? tokens_to_read(a, b0 + lane) : c.length, mine = own ? shares_in(length, size) : length;
     long long all;
     const long long sum = wave_scan(mine, a.wide, all);
     const unsigned long long hit = __ballot(want_b < 0 ? mine > 0 && before + sum > at : b0 + lane == want_b);
@@ -199,14 +181,7 @@ __device__ inline bool find_run(const Attend& a, const Columns& c, long long at,
       const long long start = sum - mine;
       run.start = before + (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(start >> 32), l) << 32 |
                                        (unsigned)__builtin_amdgcn_readlane((int)start, l));
-      if (own) {
-        run.first = (int)run.start;
-        run.count = (run.length + size - 1) / size;
-      } else {
-        const int first = a.wide ? (int)(run.start / size) : (int)run.start / size;
-        run.first = first + run.b;
-        run.count = !run.length ? 0 : (a.wide ? (int)((run.start + run.length - 1) / size) : ((int)run.start + run.length - 1) / size) - first + 1;
-      }
+      static_cast<Runs&>(run) = runs_of(c, a.wide, run.start, run.length, run.b);
       return true;
     }
     before += all;
@@ -696,7 +671,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
 // A tile is as much vector work (exponentials at a quarter of the rate, 26 cycles a logit and lane) as matrix work (32 cycles a
 // product), and a wave issues in order: the logits of the next tile are formed beside the exponentials of this one, the second
 // products beside the rest of them and the next maxima, interleaved by hand step by step.
-constexpr int TILE = 64, TILED_SUB = TILE / PA_WAVES;      // a wave copies the 16 columns of one page
+constexpr int TILED_SUB = TILE / PA_WAVES;                 // a wave copies the 16 columns of one page
 template <int D> __device__ inline int swap_k(int row) { return row & (D / 8 - 1); }
 template <int D> __device__ inline int swap_v(int row) { return (row & (D / 16 - 1)) << 1; }
 
@@ -711,7 +686,6 @@ __device__ inline void async_copy16_at(const char* base, unsigned offset, unsign
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_base) : "memory");
 }
 
-constexpr int TILED_ROWS = PA_WAVES * 32;
 // An exponential's argument is one multiply-add, logit * scale - reference, which is off by what the reference was rounded by.  Past
 // this size that would tell (from 2^31 on it can be 2^7), and the logit is rounded before it like the reference.
 constexpr float LARGE = 1 << 20;
@@ -1128,53 +1102,6 @@ __global__ __launch_bounds__(PA_THREADS) void add_gains_kernel(Attend a, int pie
 }
 
 // ---- launches ----------------------------------------------------------------------------------
-struct AttendShape {
-  int rows, tiles, shares;                   // rows of a tile
-  int weigh_splits;                          // parts of the rows that a column's weights are summed in
-  int short_shares;                          // of the sequences with up to 16 rows, where they are taken by themselves
-  bool tiled, keep, short_keep, weigh_tiled; // many rows through LDS; logits kept for the weights; weights of many rows through LDS
-  size_t part, short_part, logits, stat, gains;     // bytes of scratch: shares' results, logits, rows' references and sums, splits' sums
-};
-AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int longest, int weigh) {
-  const long long rows = (long long)longest * (c.q_heads / c.kv_heads), cap = (long long)c.table_width * c.page_size;
-  const long long units = (long long)c.batch * c.kv_heads;
-  AttendShape s;
-  s.tiled = rows > 64 && c.dtype == TREEKV_BF16;
-  s.rows = rows <= 16 ? 16 : s.tiled ? TILED_ROWS : 32;
-  s.tiles = (int)((rows + s.rows - 1) / s.rows);
-  const long long groups = (long long)c.kv_heads * s.tiles, want = s.tiled ? 512 : 256;
-  // (few rows: one workgroup a compute unit has enough on its way, and leaves fewer shares to add: 16 sequences of 16000 columns
-  // and one token 118 us, with two 121, with three or four 123 to 134; row tiles: two, 168 us for 512 tokens behind 16000, with
-  // one 186, but no more of them than are at work together, 768 tokens 275 us, with a third more 305)
-  const long long most = ((long long)c.batch * cap + MIN_SHARE - 1) / MIN_SHARE;
-  s.shares = (int)(s.tiled ? max(want / groups, 1ll) : (want + groups - 1) / groups);
-  if (s.shares > most) s.shares = (int)most;
-  // A few chunks among many sequences of a token or two: those are attended by the kernel for few rows, in a launch of its own
-  // (512 tokens and 31 single ones behind 8000 each, 8 groups of 4: 268 us in place of 596, with weights 374 in place of 855).
-  s.short_shares = s.tiled && (long long)tokens * 4 <= (long long)longest * c.batch && c.q_heads / c.kv_heads <= 16
-                       ? (int)std::min<long long>((256 + c.kv_heads - 1) / c.kv_heads, most) : 0;
-  // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them, for up to 32 rows (8 sequences
-  // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike)
-  // (what that asks of the query rows' distance, the launch adds)
-  s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
-  s.keep = weigh && rows <= 32 && (size_t)units * s.rows * cap * 4 <= (size_t)1 << 30;
-  s.short_keep = weigh && s.short_shares && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
-  s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
-  s.short_part = s.short_shares ? align_up((size_t)(s.short_shares + c.batch) * c.kv_heads * 16 * (c.head_dim + 4) * 4) : 0;
-  s.logits = s.keep || s.short_keep ? align_up((size_t)units * (s.keep ? s.rows : 16) * cap * 4) : 0;
-  // few column tiles: each one's rows are shared between up to 16 workgroups, with two tiles of them at least, and their sums added
-  // in a launch of its own (attention and weights of 2048 tokens behind 2000, one group of 8: 297 -> 90 us, 512 of 8 groups of 4
-  // alone 65 -> 41; four tiles at least: 100 tokens behind 1000 37 us, with two 34)
-  s.weigh_splits = 1;
-  if (weigh && !s.keep && s.weigh_tiled) {
-    const long long tiles = (cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32) * units;
-    s.weigh_splits = (int)std::max(std::min({512 / tiles, rows / (2 * TILE), 16ll}), 1ll);
-  }
-  s.gains = s.weigh_splits > 1 ? align_up((size_t)s.weigh_splits * units * cap * 4) : 0;
-  s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
-  return s;
-}
-
 // Groups of threads for a row's shares: each takes up to eight, all on their way together (one token behind 8000, 8 KV heads, 32
 // shares: 33.6 us with one group, 16.5 with four).
 template <int D>
@@ -1298,7 +1225,7 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.status = status;
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
   a.least_rows = 1; a.most_rows = INT_MAX;
-  a.wide = (long long)c.batch * (a.p.cap + 31) > 1 << 30;
+  a.wide = past_32_bits(c);
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
   if (c.dtype == TREEKV_F32) return c.head_dim == 128 ? launch_attend_d<float, 128>(a, sh, weigh, s) : launch_attend_d<float, 64>(a, sh, weigh, s);
   return c.head_dim == 128 ? launch_attend_d<uint16_t, 128>(a, sh, weigh, s) : launch_attend_d<uint16_t, 64>(a, sh, weigh, s);
