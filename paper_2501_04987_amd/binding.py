@@ -343,8 +343,9 @@ class PagedKV:
 
     `k`, `v` [pages, kv_heads, page_size, head_dim]; `table` [batch, table_width] int32, -1 where no page has been given; `lens`
     [batch] int32; `weights` (float32) and `positions` (int32) [batch, kv_heads, table_width * page_size] if `tracked`.  The pool
-    and the tables may be given (layers share `table` and `lens`, see `evict`; caches a pool).  Their contents are the caller's: hand out
-    pages in `table`, set `lens` to count a step's new tokens before `append` and `attend`."""
+    and the tables may be given (layers share `table` and `lens`, see `evict`; caches a pool); what is not is made on the GPU of `k`, or on
+    `device` if that is not given either.  Their contents are the caller's: hand out pages in `table`, set `lens` to count a
+    step's new tokens before `append` and `attend`."""
 
     def __init__(self, pages: int, page_size: int, heads: int, head_dim: int, *, kv_heads: int | None = None, batch: int = 1,
                  table_width: int, dtype: str = "bf16", softmax_scale: float = 0.0, tracked: bool = True, device="cuda",
@@ -354,7 +355,7 @@ class PagedKV:
         load()
         kv_heads = kv_heads or heads
         self.storage_dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
-        device = torch.device(device)
+        device = torch.device(device) if k is None else k.device
         pool, track = (pages, kv_heads, page_size, head_dim), (batch, kv_heads, table_width * page_size)
         new = lambda shape, t, value: torch.full(shape, value, dtype=t, device=device)  # noqa: E731
         self._k = new(pool, self.storage_dtype, 0) if k is None else k
