@@ -399,9 +399,10 @@ int treekv_qkv_prepare(const treekv_qkv_args* args, void* stream);
  * A call's new tokens are packed: rows starts[b] .. starts[b+1]-1 belong to sequence b (starts [batch + 1] int32, device,
  * ascending), any number of them, also none.  lens counts them already: they are the sequence's last tokens.
  * status [batch] int32 (device, may be NULL): TREEKV_OK or TREEKV_EINVAL per sequence, the latter where lens[b] is not within
- * 0 .. table_width * page_size or smaller than its new tokens, or starts are not ascending within 0 .. tokens (or give a
- * sequence more than `longest` rows).  Such a sequence is left as it is, its rows of the outputs too; so are rows that belong
- * to no sequence.
+ * 0 .. table_width * page_size or smaller than its new tokens, or its two starts are not ascending within 0 .. tokens (or give
+ * it more than `longest` rows), or, starts ascending no more between the two, it begins before the end of an earlier sequence's
+ * rows.  Such a sequence is left as it is, its rows of the outputs too; so are rows that belong to no sequence.  The others are
+ * served.
  */
 typedef struct treekv_paged_cache {
   void *k, *v;             /* [pages, Hkv, page_size, d] storage dtype, 16-byte aligned                      */

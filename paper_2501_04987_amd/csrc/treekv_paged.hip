@@ -42,11 +42,8 @@ template <int TOK>
 __global__ __launch_bounds__(PA_THREADS) void append_kernel(Pages p, const char* k, const char* v, int64_t k_far, int64_t v_far,
                                                             const int32_t* starts, int tokens, const int32_t* positions,
                                                             int32_t* status, int piece_bits) {
-  __shared__ int at_b[TOK], at_slot[TOK], at_page[TOK];
-  const int tid = threadIdx.x;
-  if (blockIdx.x == 0 && status)
-    for (int b = tid; b < p.B; b += PA_THREADS) status[b] = load_seq(p, starts, tokens, tokens, b).ok ? TREEKV_OK : TREEKV_EINVAL;
-  const int t0 = (int)blockIdx.x * TOK;
+  __shared__ int at_b[TOK], at_slot[TOK], at_page[TOK], odd;       // odd: starts do not ascend; halving them does not find a row's sequence
+  const int tid = threadIdx.x, t0 = (int)blockIdx.x * TOK;
   if (tid < TOK) {
     const int t = t0 + tid;
     int b = -1, slot = 0, page = -1;
@@ -65,8 +62,32 @@ __global__ __launch_bounds__(PA_THREADS) void append_kernel(Pages p, const char*
       }
     }
     at_b[tid] = b; at_slot[tid] = slot; at_page[tid] = page;
+  } else if (tid >> 6 == 1) {
+    bool ascend = true;
+    for (int b = tid & 63; b < p.B; b += 64) ascend &= ascends(starts[b], starts[b + 1], tokens);
+    ascend = __all(ascend);
+    if (tid == 64) odd = !ascend;
   }
   __syncthreads();
+  if (__builtin_expect(odd, 0)) {
+    if (tid < TOK) at_b[tid] = -1;
+    __syncthreads();
+    if (tid < 64) {
+      int end = 0;
+      for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const int b = b0 + tid;
+        const Seq s = load_seqs(p, starts, tokens, tokens, b0, end);
+        for (int i = 0; i < TOK; ++i) {
+          const int t = t0 + i;
+          if (t >= tokens || t < s.first || t >= s.first + s.n) continue;          // (no row has two sequences)
+          const int slot = s.len - s.n + (t - s.first), page = p.table[(size_t)b * p.width + (slot >> p.bits)];
+          at_b[i] = b; at_slot[i] = slot; at_page[i] = page < p.pages ? page : -1;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && status) write_status(p, starts, tokens, tokens, odd, status, PA_THREADS);
   const int row_pieces = p.Hkv << piece_bits, all = 2 * row_pieces * TOK;
   for (int x = tid; x < all; x += PA_THREADS) {
     const int i = x / (2 * row_pieces);
@@ -115,11 +136,15 @@ struct Run : Runs {
   int b, length;             // a sequence with columns, and their number
   long long start;           // where they start
 };
-__device__ inline int tokens_to_read(const Attend& a, int b) {
-  if (b >= a.p.B) return 0;
-  const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
+__device__ inline int columns_in(const Attend& a, const Seq& s) {
   const int rows = s.n * a.p.G;
   return rows >= a.least_rows && rows <= a.most_rows ? (s.len + 31) & ~31 : 0;
+}
+// Sequence b0 + lane, b0 = 0, 64, .. in turn if starts do not ascend (`odd`; `end` as load_seqs has it).
+__device__ inline Seq seq_of_lane(const Attend& a, bool odd, int b0, int& end) {
+  if (__builtin_expect(odd, 0)) return load_seqs(a.p, a.starts, a.tokens, a.longest, b0, end);
+  const int b = b0 + (int)(threadIdx.x & 63);
+  return b < a.p.B ? load_seq(a.p, a.starts, a.tokens, a.longest, b) : Seq{0, 0, 0, false, true};
 }
 __device__ inline long long uniform64(long long x) {
   return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
@@ -149,13 +174,26 @@ __device__ inline long long wave_scan(long long x, bool wide, long long& all) {
 // What find_run asks of the lengths: the cut, and this lane's sequence among the first 64.
 struct Columns : Cut {
   int length;
+  bool odd;                  // starts do not ascend
 };
 __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   const int lane = threadIdx.x & 63;
   Columns c;
-  c.length = tokens_to_read(a, lane);
+  int end = 0;
+  const Seq s = seq_of_lane(a, false, 0, end);
+  c.length = columns_in(a, s);
+  bool ascend = s.ascends;
   long long total, mine = c.length;
-  for (int b = 64 + lane; b < a.p.B; b += 64) mine += tokens_to_read(a, b);
+  for (int b = 64 + lane; b < a.p.B; b += 64) {
+    const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
+    mine += columns_in(a, s);
+    ascend &= s.ascends;
+  }
+  c.odd = !__all(ascend);
+  if (__builtin_expect(c.odd, 0)) {
+    mine = c.length = columns_in(a, seq_of_lane(a, true, 0, end));
+    for (int b0 = 64; b0 < a.p.B; b0 += 64) mine += columns_in(a, seq_of_lane(a, true, b0, end));
+  }
   wave_scan(mine, a.wide, total);
   static_cast<Cut&>(c) = cut_columns(total, a.shares, a.p.B, tiled, a.wide, [&](int size) {
     long long count;
@@ -165,12 +203,14 @@ __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   return c;
 }
 // The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
-__device__ inline bool find_run(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
+template <bool ODD>
+__device__ inline bool find_run_in(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
   const int lane = threadIdx.x & 63, size = c.size;
   const bool own = c.own;
   long long before = 0;
+  int end = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
-    const int length = b0 ? tokens_to_read(a, b0 + lane) : c.length, mine = own ? shares_in(length, size) : length;
+    const int length = ODD || b0 ? columns_in(a, seq_of_lane(a, ODD, b0, end)) : c.length, mine = own ? shares_in(length, size) : length;
     long long all;
     const long long sum = wave_scan(mine, a.wide, all);
     const unsigned long long hit = __ballot(want_b < 0 ? mine > 0 && before + sum > at : b0 + lane == want_b);
@@ -187,6 +227,9 @@ __device__ inline bool find_run(const Attend& a, const Columns& c, long long at,
     before += all;
   }
   return false;
+}
+__device__ inline bool find_run(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
+  return __builtin_expect(c.odd, 0) ? find_run_in<true>(a, c, at, want_b, run) : find_run_in<false>(a, c, at, want_b, run);
 }
 
 template <int D>
@@ -236,9 +279,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, q4 = lane >> 4;
   const int tile = (int)(blockIdx.x % a.tiles), rest = (int)(blockIdx.x / a.tiles), h = rest % p.Hkv, w = rest / p.Hkv;
-  if (blockIdx.x == 0 && a.status)
-    for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
   const Columns columns = columns_of(a, false);
+  if (blockIdx.x == 0 && a.status) write_status(p, a.starts, a.tokens, a.longest, columns.odd, a.status, PA_THREADS);
   const int size = columns.size;
   const bool own = columns.own;
   const long long share_end = own ? w + 1 : (long long)(w + 1) * size;
@@ -519,11 +561,14 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   const Pages& p = a.p;
   const int at_once = MERGE_ROWS<D> / slices, rest = (int)(blockIdx.x / merge_tiles), h = rest % p.Hkv;
   int tile = (int)(blockIdx.x % merge_tiles), b = rest / p.Hkv;
+  Columns columns;
   if (PACKED) {
-    const int lane = threadIdx.x & 63;
+    columns = columns_of(a, tiled);
     unsigned long long hit = 0;
+    int end = 0;
     for (int b0 = 0; b0 < p.B && !hit; b0 += 64) {
-      const int mine = tokens_to_read(a, b0 + lane) ? (load_seq(p, a.starts, a.tokens, a.longest, b0 + lane).n * p.G + at_once - 1) / at_once : 0;
+      const Seq s = seq_of_lane(a, columns.odd, b0, end);
+      const int mine = columns_in(a, s) ? (s.n * p.G + at_once - 1) / at_once : 0;
       long long all;
       const int sum = (int)wave_scan(mine, false, all);
       hit = __ballot(sum > tile);
@@ -538,7 +583,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
   if (tile * at_once >= s.n * p.G) return;
   Run run;
-  const Columns columns = columns_of(a, tiled);
+  if (!PACKED) columns = columns_of(a, tiled);
   if (!find_run(a, columns, 0, b, run) || run.count <= 1) return;
   merge_rows<T, D>(a, s, run, h, tile * at_once, s.n * p.G, slices, sm);
 }
@@ -559,7 +604,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   if (rows < a.least_rows || rows > a.most_rows || (c0 >= s.len && piece * at_once >= rows)) return;
   Run run;
   const Columns columns = columns_of(a, false);
-  if (!find_run(a, columns, 0, b, run)) return;
+  if (!find_run(a, columns, 0, b, run) || !run.length) return;
   const int c = c0 + 4 * tid;
   const bool mine = c < s.len;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -616,8 +661,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, q4 = lane >> 4;
   const int ct = (int)(blockIdx.x % col_tiles), rest = (int)(blockIdx.x / col_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  const bool inside = begins_inside(a.starts, a.tokens, b, s.first);
   const int c0 = (ct * PA_WAVES + wave) * WIDE;
-  if (s.n * p.G < a.least_rows || c0 >= s.len) return;
+  if (s.n * p.G < a.least_rows || c0 >= s.len || inside) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
   typename O::Keys k[NB];
@@ -697,12 +743,11 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   extern __shared__ __attribute__((aligned(1024))) char pt_smem[];      // two stages of K, then of V
   const Pages& p = a.p;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, hf = lane >> 5;
-  if (blockIdx.x == 0 && a.status)
-    for (int b = tid; b < p.B; b += PA_THREADS) a.status[b] = load_seq(p, a.starts, a.tokens, a.longest, b).ok ? TREEKV_OK : TREEKV_EINVAL;
   const Place place = place_of(p.Hkv, a.shares, a.tiles);        // the longest tiles first
   if (place.tile >= a.tiles) return;
   const int tile = a.tiles - 1 - place.tile, h = place.group % p.Hkv, w = place.group / p.Hkv;
   const Columns columns = columns_of(a, true);
+  if (blockIdx.x == 0 && a.status) write_status(p, a.starts, a.tokens, a.longest, columns.odd, a.status, PA_THREADS);
   const int size = columns.size;
   Run run;
   if (!find_run(a, columns, w, -1, run)) return;
@@ -975,8 +1020,9 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   const int ct = place.tile % col_tiles, split = place.tile / col_tiles, h = place.group % p.Hkv, b = place.group / p.Hkv;
   if (split >= splits || b >= p.B) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
+  const bool inside = begins_inside(a.starts, a.tokens, b, s.first);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
-  if (s.n * p.G < a.least_rows || first_col >= s.len) return;
+  if (s.n * p.G < a.least_rows || first_col >= s.len || inside) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n;
   uint4 k[KS];
@@ -1091,7 +1137,8 @@ __global__ __launch_bounds__(PA_THREADS) void add_gains_kernel(Attend a, int pie
   const Pages& p = a.p;
   const int c = (int)(blockIdx.x % pieces) * PA_THREADS + threadIdx.x, rest = (int)(blockIdx.x / pieces), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  if (s.n * p.G < a.least_rows || c >= s.len) return;
+  const bool inside = begins_inside(a.starts, a.tokens, b, s.first);
+  if (s.n * p.G < a.least_rows || c >= s.len || inside) return;
   const int page = p.table[(size_t)b * p.width + (c >> p.bits)];
   if (page < 0 || page >= p.pages) return;
   const float* gain = a.gains + ((size_t)b * p.Hkv + h) * p.cap + c;

@@ -50,3 +50,129 @@ def test_more_columns_than_a_share_can_have(binding):
         assert bool(((out[b] - want).abs() <= eps * size).all()), float(((out[b] - want).abs() / (eps * size)).max())
         off = (lse[b] - (top + total.log())[:, 0]).abs()
         assert bool((off <= eps[:, 0] + 2.0 ** -22 * lse[b].abs()).all())
+
+
+def accepted(starts, lens, tokens, longest, cap):
+    """The rule of include/treekv.h, sequence by sequence."""
+    got, end = [], 0
+    for b, n in enumerate(lens):
+        lo, hi = starts[b], starts[b + 1]
+        own = 0 <= lo <= hi <= tokens
+        if own and hi - lo <= longest and hi - lo <= n <= cap and (hi == lo or lo >= end):
+            got.append(b)
+        if own and hi > lo:
+            end = max(end, hi)
+    return got
+
+
+def held(got, want, room):
+    import torch
+
+    off = (got.double().cpu() - want).abs()
+    off[got.cpu() == want] = 0.0
+    assert bool((off <= room).all()), float((off / room.clamp(min=1e-300)).max())
+
+
+# Starts that do not ascend from end to end, tokens and the longest chunk; lengths are 40 + 5 b.
+ODD = {
+    "one far too large": ([0, 2, 100, 6, 8], 8, 2),
+    "one negative": ([0, 2, -5, 6, 8], 8, 2),
+    "an overlap": ([0, 5, 3, 8, 9], 9, 5),
+    "one inside of another": ([0, 9, 2, 4, 12], 12, 9),
+    "a row of two": ([0, 4, 3, 3, 8, 10, 9, 12], 12, 5),
+    "from the end to the start": ([9, 8, 7, 5, 0], 9, 9),
+    "twice the same": ([0, 6, 0, 6, 6], 6, 6),
+    "the second half again": (list(range(0, 70, 2)) + list(range(20, 110, 2)), 110, 2),
+    "a border of 64 sequences": ([2 * i for i in range(64)] + [2000] + [100 + i for i in range(66)], 200, 2),
+    "rows that are nobody's": ([0, 3, 1 << 30, 7, 7, -(1 << 31), 9, 12], 12, 3),
+    "chunks of row tiles": ([0, 70, 60, 150, 149, 151, 151, 300], 300, 150),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("name", ODD)
+def test_starts_that_do_not_ascend(binding, name, group, dtype):
+    """Rows go to the first sequence that has them, the others are refused and left alone, by both calls alike."""
+    import torch
+
+    from tests.serve_reference import Paged
+
+    starts, tokens, longest = ODD[name]
+    B = len(starts) - 1
+    lens = [40 + 5 * b if B < 20 else 20 + b % 7 for b in range(B)]
+    if "tiles" in name:
+        lens = [n + 200 for n in lens]
+    # the reference has the rows of the accepted sequences; the pages of all
+    ref = Paged(lens=lens, news=[0] * B, page_size=16, kv_heads=2, group=group, d=64, dtype=dtype, seed=len(name))
+    cap = ref.width * 16
+    ok = accepted(starts, lens, tokens, longest, cap)
+    assert len(ok) < B
+    ref.starts, ref.total = torch.tensor(starts, dtype=torch.int32), tokens
+    ref.news = [starts[b + 1] - starts[b] if b in ok else 0 for b in range(B)]
+    ref.q = torch.randn(tokens, 2 * group, 64, generator=ref.g).to(ref.t)
+    kv, dev = ref.on_gpu(binding), ref.starts.cuda()
+    status = torch.full((B,), 9, dtype=torch.int32, device="cuda")
+    k, v = [torch.randn(tokens, 2, 64, generator=ref.g).to(ref.t) for _ in "kv"]
+    positions = torch.randint(0, 1 << 20, (tokens,), generator=ref.g).int()
+    kv.append(k.cuda(), v.cuda(), dev, positions.cuda(), status)
+    # (append has no `longest`)
+    fits = accepted(starts, lens, tokens, tokens, cap)
+    assert status.tolist() == [0 if b in fits else binding.TREEKV_EINVAL for b in range(B)]
+    assert fits == ok, "the cases are chosen so"
+    ref.append(k, v, positions)
+    for x in ("k", "v", "weights", "positions"):
+        assert torch.equal(getattr(kv, x).cpu(), getattr(ref, x)), x
+
+    mine = torch.zeros(tokens, dtype=torch.bool)
+    for b in ok:
+        assert not bool(mine[starts[b]:starts[b + 1]].any())
+        mine[starts[b]:starts[b + 1]] = True
+    for weigh in (False, True):
+        want = ref.attend(sequences=ok)
+        out, lse = torch.full_like(ref.q, 7.0, device="cuda"), torch.full((tokens, 2 * group), 7.0, device="cuda")
+        before = kv.weights.clone()
+        status.fill_(9)
+        kv.attend(ref.q.cuda(), dev, longest, out, lse, weigh=weigh, status=status)
+        assert status.tolist() == [0 if b in ok else binding.TREEKV_EINVAL for b in range(B)]
+        held(out.cpu()[mine], want["out"][mine], want["room"][mine])
+        held(lse.cpu()[mine], want["lse"][mine], want["lse_room"][mine])
+        assert bool((out.cpu()[~mine] == 7.0).all()) and bool((lse.cpu()[~mine] == 7.0).all())
+        if not weigh:
+            assert torch.equal(kv.weights, before)
+            continue
+        total = before.double().cpu() + want["gain"]
+        held(kv.weights, total, want["gain_room"] + 2.0 ** -23 * total.abs())
+        for b in range(B):
+            if not ref.news[b]:
+                assert torch.equal(kv.weights[b], before[b])
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+def test_starts_that_do_not_ascend_in_every_kernel(binding, weigh):
+    """Chunks beside single tokens, weights of many rows in parts, merges of several shares: with one sequence made to begin inside
+    of another's rows, the others' results are bit for bit those of a call in which it has no rows."""
+    import torch
+
+    from tests.serve_reference import Paged
+
+    for lens, news, group, d, dtype in (([900, 300, 40, 1000, 513, 90, 77, 133], [200, 1, 2, 9, 1, 9, 1, 8], 2, 128, "bf16"),
+                                        ([700, 400, 300], [600, 100, 300], 3, 64, "bf16"), ([700, 400, 300], [600, 100, 300], 3, 64, "f32"),
+                                        ([9000, 400, 3000, 60], [1, 2, 1, 2], 8, 64, "bf16"), ([600, 400, 300, 30], [40, 20, 30, 1], 1, 128, "bf16"),
+                                        ([300, 400], [150, 120], 70, 64, "bf16")):
+        ref = Paged(lens=lens, news=news, page_size=32, kv_heads=2, group=group, d=d, dtype=dtype, seed=5)
+        at, B = ref.starts.tolist(), ref.B
+        b = B // 2
+        # two more sequences: one whose starts fall, and one with rows of sequence b again
+        odd = at + [at[b], at[b + 1]]
+        none = at + [at[-1], at[-1]]
+        both = Paged(lens=lens + [50, lens[b]], news=news + [0, 0], page_size=32, kv_heads=2, group=group, d=d, dtype=dtype, seed=5)
+        got = []
+        for starts in (none, odd):
+            kv = both.on_gpu(binding)
+            out, lse = torch.full((ref.total, 2 * group, d), 7.0, dtype=ref.t, device="cuda"), torch.full((ref.total, 2 * group), 7.0, device="cuda")
+            status = torch.full((B + 2,), 9, dtype=torch.int32, device="cuda")
+            kv.attend(ref.q.cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), max(news), out, lse, weigh=weigh, status=status)
+            got.append((out, lse, kv.weights, status.tolist()))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][2], got[1][2])
+        assert got[0][3] == [0] * (B + 2) and got[1][3] == [0] * B + [binding.TREEKV_EINVAL] * 2
