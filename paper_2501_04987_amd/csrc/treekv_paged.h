@@ -31,53 +31,42 @@ struct Seq {
 };
 __device__ inline bool ascends(int lo, int hi, int tokens) { return lo >= 0 && hi >= lo && hi <= tokens; }
 // By what its own starts and length say.  Where starts ascend from end to end that is all there is to ask; else the sequence may
-// begin in front of the end of an earlier one, which has the rows then (load_seqs, begins_inside).
-__device__ inline Seq load_seq(const int32_t* starts, const int32_t* lens, int cap, int tokens, int longest, int b) {
-  const int lo = starts[b], hi = starts[b + 1], len = lens[b];
+// begin before the end of an earlier one, which has the rows then (begins_inside, load_seqs).
+__device__ inline Seq load_seq(const Pages& p, const int32_t* starts, int tokens, int longest, int b) {
+  const int lo = starts[b], hi = starts[b + 1], len = p.lens[b];
   Seq s;
   s.ascends = ascends(lo, hi, tokens);
-  s.ok = s.ascends && hi - lo <= longest && len >= hi - lo && len <= cap;
+  s.ok = s.ascends && hi - lo <= longest && len >= hi - lo && len <= p.cap;
   s.first = lo;
   s.n = s.ok ? hi - lo : 0;
   s.len = s.ok ? len : 0;
   return s;
 }
-__device__ inline Seq load_seq(const Pages& p, const int32_t* starts, int tokens, int longest, int b) {
-  return load_seq(starts, p.lens, p.cap, tokens, longest, b);
+// Whether rows of an earlier sequence lie behind row `first`, where b's begin.  By a whole wave, of one b.
+__device__ inline bool begins_inside(const int32_t* starts, int tokens, int b, int first) {
+  int end = 0;
+  for (int c0 = 0; c0 < b; c0 += 64) {
+    const int c = c0 + (int)(threadIdx.x & 63), lo = starts[min(c, b)], hi = starts[min(c, b) + 1];
+    end = max(end, c < b && ascends(lo, hi, tokens) && hi > lo ? hi : 0);
+  }
+  return __any(end > first);
 }
-// Sequences b0 + lane whatever starts are.  By a whole wave, b0 = 0, 64, .. in turn; `end`: of the rows of those before, 0 at first.
-// (A call, for it is hardly ever made, and in its place the attention would hold more in registers: 1000 sequences of 300 tokens
-// took 495 us with it in their place, 418 with a call.)
-struct SeqEnd {
-  Seq s;
-  int end;
-};
-__attribute__((noinline)) __device__ inline SeqEnd load_seqs_from(const int32_t* starts, const int32_t* lens, int B, int cap, int tokens, int longest,
-                                                           int b0, int end) {
+// Sequences b0 + lane with all that can be asked of them.  By a whole wave, b0 = 0, 64, .. in turn; `end`: of the rows of those before,
+// 0 at first.
+__device__ inline Seq load_seqs(const Pages& p, const int32_t* starts, int tokens, int longest, int b0, int& end) {
   const int lane = threadIdx.x & 63, b = b0 + lane;
   Seq s = {0, 0, 0, false, true};
   int mine = 0;                                        // where its rows end
-  if (b < B) {
-    s = load_seq(starts, lens, cap, tokens, longest, b);
+  if (b < p.B) {
+    s = load_seq(p, starts, tokens, longest, b);
     if (s.ascends && starts[b + 1] > s.first) mine = starts[b + 1];
   }
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) mine = max(mine, __shfl_up(mine, x, 64));       // (a lane without one below gets its own)
   const int before = __shfl_up(mine, 1, 64);
   if (s.n > 0 && s.first < max(lane ? before : 0, end)) s.ok = false, s.n = s.len = 0;
-  return {s, max(end, __builtin_amdgcn_readlane(mine, 63))};
-}
-__device__ inline Seq load_seqs(const Pages& p, const int32_t* starts, int tokens, int longest, int b0, int& end) {
-  const SeqEnd x = load_seqs_from(starts, p.lens, p.B, p.cap, tokens, longest, b0, end);
-  end = x.end;
-  return x.s;
-}
-// Whether rows of an earlier sequence lie behind row `first`, where b's begin.  By a whole wave, of one b.
-__device__ inline bool begins_inside(const int32_t* starts, int tokens, int b, int first) {
-  int end = 0;
-  for (int c = threadIdx.x & 63; c < b; c += 64)
-    if (ascends(starts[c], starts[c + 1], tokens) && starts[c + 1] > starts[c]) end = max(end, starts[c + 1]);
-  return __any(end > first);
+  end = max(end, __builtin_amdgcn_readlane(mine, 63));
+  return s;
 }
 // All sequences' status, by a workgroup of `threads`; `odd`: starts do not ascend.
 __device__ inline void write_status(const Pages& p, const int32_t* starts, int tokens, int longest, bool odd, int32_t* status, int threads) {

@@ -125,13 +125,13 @@ struct Attend {
   int tokens, longest, tiles, shares, rows;  // row tiles of the longest sequence; shares the columns are cut into; rows of a tile
   int least_rows, most_rows;                 // sequences with others are not this kernel's
   float scale_log2e;
-  bool wide;                                 // more columns than 32 bits count
+  bool wide, sparse;                         // more columns than 32 bits count; how partial results are numbered
 };
 
 // The columns of all sequences with new tokens lie one after the other (each sequence's rounded up to whole blocks), and are cut
-// into shares of `size`.  Few rows over many columns: a workgroup takes one share, whatever sequences it runs through; what it has
-// of sequence b is partial result (its number) + b, which no other has.  Many rows, where there are row tiles to go round, and
-// small shares: a sequence's shares start at its first token, so that each is of one sequence (its `own`).
+// into shares of `size`.  Few rows over many columns: a workgroup takes one share, whatever sequences it runs through.  Many rows,
+// where there are row tiles to go round, and small shares: a sequence's shares start at its first token, so that each is of one
+// sequence (its `own`).
 struct Run : Runs {
   int b, length;             // a sequence with columns, and their number
   long long start;           // where they start
@@ -140,11 +140,9 @@ __device__ inline int columns_in(const Attend& a, const Seq& s) {
   const int rows = s.n * a.p.G;
   return rows >= a.least_rows && rows <= a.most_rows ? (s.len + 31) & ~31 : 0;
 }
-// Sequence b0 + lane, b0 = 0, 64, .. in turn if starts do not ascend (`odd`; `end` as load_seqs has it).
-__device__ inline Seq seq_of_lane(const Attend& a, bool odd, int b0, int& end) {
-  if (__builtin_expect(odd, 0)) return load_seqs(a.p, a.starts, a.tokens, a.longest, b0, end);
-  const int b = b0 + (int)(threadIdx.x & 63);
-  return b < a.p.B ? load_seq(a.p, a.starts, a.tokens, a.longest, b) : Seq{0, 0, 0, false, true};
+// (Of one that begins before the end of an earlier one's rows too: its columns are counted like the others', and passed over.)
+__device__ inline int columns_of_seq(const Attend& a, int b) {
+  return b < a.p.B ? columns_in(a, load_seq(a.p, a.starts, a.tokens, a.longest, b)) : 0;
 }
 __device__ inline long long uniform64(long long x) {
   return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
@@ -179,10 +177,13 @@ struct Columns : Cut {
 __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   const int lane = threadIdx.x & 63;
   Columns c;
-  int end = 0;
-  const Seq s = seq_of_lane(a, false, 0, end);
-  c.length = columns_in(a, s);
-  bool ascend = s.ascends;
+  bool ascend = true;
+  c.length = 0;
+  if (lane < a.p.B) {
+    const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, lane);
+    c.length = columns_in(a, s);
+    ascend = s.ascends;
+  }
   long long total, mine = c.length;
   for (int b = 64 + lane; b < a.p.B; b += 64) {
     const Seq s = load_seq(a.p, a.starts, a.tokens, a.longest, b);
@@ -190,10 +191,6 @@ __device__ inline Columns columns_of(const Attend& a, bool tiled) {
     ascend &= s.ascends;
   }
   c.odd = !__all(ascend);
-  if (__builtin_expect(c.odd, 0)) {
-    mine = c.length = columns_in(a, seq_of_lane(a, true, 0, end));
-    for (int b0 = 64; b0 < a.p.B; b0 += 64) mine += columns_in(a, seq_of_lane(a, true, b0, end));
-  }
   wave_scan(mine, a.wide, total);
   static_cast<Cut&>(c) = cut_columns(total, a.shares, a.p.B, tiled, a.wide, [&](int size) {
     long long count;
@@ -203,14 +200,12 @@ __device__ inline Columns columns_of(const Attend& a, bool tiled) {
   return c;
 }
 // The sequence that holds column `at` of all (want_b < 0), or sequence want_b.  One share a sequence at least: `own`.
-template <bool ODD>
-__device__ inline bool find_run_in(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
+__device__ inline bool find_run(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
   const int lane = threadIdx.x & 63, size = c.size;
   const bool own = c.own;
   long long before = 0;
-  int end = 0;
   for (int b0 = 0; b0 < a.p.B; b0 += 64) {
-    const int length = ODD || b0 ? columns_in(a, seq_of_lane(a, ODD, b0, end)) : c.length, mine = own ? shares_in(length, size) : length;
+    const int length = b0 ? columns_of_seq(a, b0 + lane) : c.length, mine = own ? shares_in(length, size) : length;
     long long all;
     const long long sum = wave_scan(mine, a.wide, all);
     const unsigned long long hit = __ballot(want_b < 0 ? mine > 0 && before + sum > at : b0 + lane == want_b);
@@ -221,15 +216,28 @@ __device__ inline bool find_run_in(const Attend& a, const Columns& c, long long 
       const long long start = sum - mine;
       run.start = before + (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(start >> 32), l) << 32 |
                                        (unsigned)__builtin_amdgcn_readlane((int)start, l));
-      static_cast<Runs&>(run) = runs_of(c, a.wide, run.start, run.length, run.b);
+      static_cast<Runs&>(run) = runs_of(c, a.wide, run.start, run.length);
       return true;
     }
     before += all;
   }
   return false;
 }
-__device__ inline bool find_run(const Attend& a, const Columns& c, long long at, int want_b, Run& run) {
-  return __builtin_expect(c.odd, 0) ? find_run_in<true>(a, c, at, want_b, run) : find_run_in<false>(a, c, at, want_b, run);
+// Whether its rows are an earlier sequence's.
+__device__ inline bool refused(const Attend& a, const Columns& c, int b, const Seq& s) {
+  return __builtin_expect(c.odd, 0) && begins_inside(a.starts, a.tokens, b, s.first);
+}
+// Where a sequence's partial results lie, if it has any.  MERGED: only what is merged has them.
+template <bool MERGED>
+__device__ inline int first_part(const Attend& a, const Columns& c, const Run& run) {
+  long long before = run.start;                        // columns of earlier sequences
+  if (MERGED && a.sparse && c.own && run.count > 1) {
+    const int lane = threadIdx.x & 63;
+    long long mine = 0;
+    for (int b = lane; b < run.b; b += 64) mine += columns_of_seq(a, b);
+    wave_scan(mine, a.wide, before);
+  }
+  return part_of_first(c, a.wide, MERGED && a.sparse, run, before, run.b);
 }
 
 template <int D>
@@ -290,8 +298,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
        from = own ? share_end : run.start + run.length) {
     const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
     const int rows = s.n * p.G, row0 = tile * ROWS;
-    if (row0 >= rows) continue;
-    const int old = s.len - s.n;
+    if (row0 >= rows || refused(a, columns, run.b, s)) continue;
+    const int old = s.len - s.n, part0 = first_part<!WEIGH>(a, columns, run) + part_at(!WEIGH && a.sparse, w - run.first);
     // columns: what the tile's first row sees all rows see, behind what its last row sees there is nothing for it
     const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + ROWS, rows) - 1) / p.G + 1;
     const int lo = own ? (w - run.first) * size : (int)(from - run.start);
@@ -456,7 +464,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_kernel(Attend a) {
         L = fmaf(ml.y, g, L);
         f.x = fmaf(u.x, g, f.x); f.y = fmaf(u.y, g, f.y); f.z = fmaf(u.z, g, f.z); f.w = fmaf(u.w, g, f.w);
       }
-      float* part = a.part + (((size_t)(own ? w : w + run.b) * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
+      float* part = a.part + (((size_t)part0 * p.Hkv + h) * a.tiles + tile) * ROWS * OR + (size_t)y * OR;
       if (c == 0 && (WEIGH || run.count > 1)) *reinterpret_cast<float2*>(part + D) = make_float2(M, L);
       if (run.count > 1) *reinterpret_cast<float4*>(part + c) = f;
       else finish_row<T, D>(a, s, h, row0 + y, c, f, M, L);
@@ -472,15 +480,15 @@ struct Merged {
   float4 f[PA_THREADS];
   float2 ml[PA_THREADS];
 };
-template <typename T, int D>
-__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int h, int row0, int step, int slices, Merged& sm) {
+template <typename T, int D, bool MERGED>
+__device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run, int part0, int h, int row0, int step, int slices, Merged& sm) {
   constexpr int OR = D + 4, WIDTH = D / 4;
   const Pages& p = a.p;
   const int rows = s.n * p.G, tid = threadIdx.x, c = tid % WIDTH * 4, slice = tid / WIDTH & (slices - 1);
   for (; row0 < rows; row0 += step) {
     const int row = row0 + tid / WIDTH / slices;
     const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
-    const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + min(row, rows - 1)) * OR;
+    const float* part = a.part + (((size_t)part0 * p.Hkv + h) * a.tiles * a.rows + min(row, rows - 1)) * OR;
     constexpr int AT_ONCE = 8;                         // shares on their way together
     float M = REF_NONE, L = 0.f;
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -489,7 +497,7 @@ __device__ inline void merge_rows(const Attend& a, const Seq& s, const Run& run,
       float4 u[AT_ONCE];
 #pragma unroll
       for (int z = 0; z < AT_ONCE; ++z) {
-        const float* at = part + min(z0 + z * slices, run.count - 1) * far;
+        const float* at = part + part_at(MERGED && a.sparse, min(z0 + z * slices, run.count - 1)) * far;
         ml[z] = *reinterpret_cast<const float2*>(at + D);
         u[z] = *reinterpret_cast<const float4*>(at + c);
       }
@@ -564,10 +572,13 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   Columns columns;
   if (PACKED) {
     columns = columns_of(a, tiled);
+    const int lane = threadIdx.x & 63;
     unsigned long long hit = 0;
     int end = 0;
     for (int b0 = 0; b0 < p.B && !hit; b0 += 64) {
-      const Seq s = seq_of_lane(a, columns.odd, b0, end);
+      Seq s = {0, 0, 0, false, true};
+      if (__builtin_expect(columns.odd, 0)) s = load_seqs(p, a.starts, a.tokens, a.longest, b0, end);      // (or there were more groups than the grid has)
+      else if (b0 + lane < p.B) s = load_seq(p, a.starts, a.tokens, a.longest, b0 + lane);
       const int mine = columns_in(a, s) ? (s.n * p.G + at_once - 1) / at_once : 0;
       long long all;
       const int sum = (int)wave_scan(mine, false, all);
@@ -584,8 +595,8 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   if (tile * at_once >= s.n * p.G) return;
   Run run;
   if (!PACKED) columns = columns_of(a, tiled);
-  if (!find_run(a, columns, 0, b, run) || run.count <= 1) return;
-  merge_rows<T, D>(a, s, run, h, tile * at_once, s.n * p.G, slices, sm);
+  if (!find_run(a, columns, 0, b, run) || run.count <= 1 || refused(a, columns, b, s)) return;
+  merge_rows<T, D, true>(a, s, run, first_part<true>(a, columns, run), h, tile * at_once, s.n * p.G, slices, sm);
 }
 
 // The same where the logits of up to 32 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
@@ -604,7 +615,8 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
   if (rows < a.least_rows || rows > a.most_rows || (c0 >= s.len && piece * at_once >= rows)) return;
   Run run;
   const Columns columns = columns_of(a, false);
-  if (!find_run(a, columns, 0, b, run) || !run.length) return;
+  if (!find_run(a, columns, 0, b, run) || refused(a, columns, b, s)) return;
+  const int part0 = first_part<false>(a, columns, run);
   const int c = c0 + 4 * tid;
   const bool mine = c < s.len;
   float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -614,7 +626,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
     for (int row = tid >> 4; row < rows; row += 16) {          // 16 lanes a row, each with every 16th share
       float M = REF_NONE, L = 0.f;
       const size_t far = (size_t)p.Hkv * a.tiles * a.rows * OR;
-      const float* part = a.part + (((size_t)run.first * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
+      const float* part = a.part + (((size_t)part0 * p.Hkv + h) * a.tiles * a.rows + row) * OR + D;
       for (int z = tid & 15; z < run.count; z += 16) {
         const float2 ml = *reinterpret_cast<const float2*>(part + z * far);
         const float to = fmaxf(M, ml.x);
@@ -648,7 +660,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_weigh_kernel(Attend a, int p
       for (int i = 0; i < s.len - c; ++i) weights[i] = z[i];
     }
   }
-  if (run.count > 1) merge_rows<T, D>(a, s, run, h, piece * at_once, pieces * at_once, slices, sm);
+  if (run.count > 1) merge_rows<T, D, false>(a, s, run, part0, h, piece * at_once, pieces * at_once, slices, sm);
 }
 
 // ---- weights -----------------------------------------------------------------------------------
@@ -661,9 +673,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void weigh_kernel(Attend a, int col_
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 15, q4 = lane >> 4;
   const int ct = (int)(blockIdx.x % col_tiles), rest = (int)(blockIdx.x / col_tiles), h = rest % p.Hkv, b = rest / p.Hkv;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  const bool inside = begins_inside(a.starts, a.tokens, b, s.first);
   const int c0 = (ct * PA_WAVES + wave) * WIDE;
-  if (s.n * p.G < a.least_rows || c0 >= s.len || inside) return;
+  if (s.n * p.G < a.least_rows || c0 >= s.len) return;
+  if (begins_inside(a.starts, a.tokens, b, s.first)) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n, rows = s.n * p.G;
   typename O::Keys k[NB];
@@ -753,8 +765,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   if (!find_run(a, columns, w, -1, run)) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, run.b);
   const int rows = s.n * p.G, row0 = tile * TILED_ROWS;
-  if (row0 >= rows) return;
-  const int old = s.len - s.n;
+  if (row0 >= rows || refused(a, columns, run.b, s)) return;
+  const int old = s.len - s.n, part0 = first_part<true>(a, columns, run) + part_at(a.sparse, w - run.first);
   const int all_see = old + row0 / p.G + 1, end = old + (min(row0 + TILED_ROWS, rows) - 1) / p.G + 1;
   const int lo = (w - run.first) * size, hi = min(lo + size, end);
   // logits are compared before they are scaled, so the scale's sign goes to the queries
@@ -987,7 +999,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
   wait_vmcnt<0>();                                     // (copies into LDS that nobody waits for)
   const float total = sum + other_half(sum);
   if (row >= rows) return;
-  float* part = a.part + (((size_t)w * p.Hkv + h) * a.tiles * TILED_ROWS + row) * OR;
+  float* part = a.part + (((size_t)part0 * p.Hkv + h) * a.tiles * TILED_ROWS + row) * OR;
   const size_t at = (size_t)(s.first + token) * p.H + head;
   const bool any = !(total == 0.f);
   const float inv = any ? 1.0f / total : 0.f;
@@ -1020,9 +1032,9 @@ __global__ __launch_bounds__(PA_THREADS, 3) void weigh_tiled_kernel(Attend a, in
   const int ct = place.tile % col_tiles, split = place.tile / col_tiles, h = place.group % p.Hkv, b = place.group / p.Hkv;
   if (split >= splits || b >= p.B) return;
   const Seq s = load_seq(p, a.starts, a.tokens, a.longest, b);
-  const bool inside = begins_inside(a.starts, a.tokens, b, s.first);
   const int first_col = ct * (PA_WAVES * 32), c0 = first_col + wave * 32;
-  if (s.n * p.G < a.least_rows || first_col >= s.len || inside) return;
+  if (s.n * p.G < a.least_rows || first_col >= s.len) return;
+  if (begins_inside(a.starts, a.tokens, b, s.first)) return;
   const int32_t* table = p.table + (size_t)b * p.width;
   const int in_page = (1 << p.bits) - 1, old = s.len - s.n;
   uint4 k[KS];
@@ -1206,6 +1218,7 @@ int launch_attend_d(Attend a, const AttendShape& sh, int weigh, hipStream_t s) {
     few.part = (float*)((char*)a.part + sh.part);
     few.tiles = 1; few.rows = 16; few.shares = sh.short_shares;
     few.most_rows = 16;
+    few.sparse = is_sparse(few.shares, p.B, sh.short_keep);
     if (int e = launch_shares<T, D>(few, false, sh.short_keep, s)) return e;
     if (sh.short_keep)
       if (int e = launch_kept<T, D>(few, s)) return e;
@@ -1273,6 +1286,7 @@ int launch_paged_attend(const treekv_paged_cache& c, const void* q, int64_t q_st
   a.tokens = tokens; a.longest = longest; a.tiles = sh.tiles; a.shares = sh.shares; a.rows = sh.rows;
   a.least_rows = 1; a.most_rows = INT_MAX;
   a.wide = past_32_bits(c);
+  a.sparse = is_sparse(sh.shares, c.batch, sh.keep);
   a.scale_log2e = (c.softmax_scale != 0.f ? c.softmax_scale : 1.0f / sqrtf((float)c.head_dim)) * LOG2E;
   if (c.dtype == TREEKV_F32) return c.head_dim == 128 ? launch_attend_d<float, 128>(a, sh, weigh, s) : launch_attend_d<float, 64>(a, sh, weigh, s);
   return c.head_dim == 128 ? launch_attend_d<uint16_t, 128>(a, sh, weigh, s) : launch_attend_d<uint16_t, 64>(a, sh, weigh, s);

@@ -45,13 +45,26 @@ __host__ __device__ inline Cut cut_columns(long long total, int shares, int batc
 __host__ __device__ inline int shares_in(int length, int size) { return (int)(((unsigned)length + (unsigned)size - 1) / (unsigned)size); }
 // Sequence b's shares, `start` its first column among all (or its first share among all: `own`).
 struct Runs {
-  int first, count;                          // its partial results
+  int first, count;                          // its first share, how many
 };
-__host__ __device__ inline Runs runs_of(const Cut& c, bool wide, long long start, int length, int b) {
+__host__ __device__ inline Runs runs_of(const Cut& c, bool wide, long long start, int length) {
   if (c.own) return {(int)start, shares_in(length, c.size)};
   const int first = wide ? (int)(start / c.size) : (int)start / c.size;
-  return {first + b, !length ? 0 : (wide ? (int)((start + length - 1) / c.size) : ((int)start + length - 1) / c.size) - first + 1};
+  return {first, !length ? 0 : (wide ? (int)((start + length - 1) / c.size) : ((int)start + length - 1) / c.size) - first + 1};
 }
+// Where the partial results of a sequence's shares lie.
+//   dense   every share of every sequence has one: shares + batch of them.
+//   sparse  sequences of several shares have them.  Counted in columns, each of their shares goes on from, or is the first before, a
+//           border between two of `size`, and a border has one sequence before it and one behind: two places for
+//           each are enough, however many sequences there are.
+// That of its first share, `column` columns into all (asked for if sparse), and from there to that of its k-th.
+__host__ __device__ inline int part_of_first(const Cut& c, bool wide, bool sparse, const Runs& r, long long column, int b) {
+  if (!sparse) return c.own ? r.first : r.first + b;
+  return 2 * (!c.own ? r.first : wide ? (int)(column / c.size) : (int)column / c.size) + 1;
+}
+__host__ __device__ inline int part_at(bool sparse, int k) { return sparse ? (k ? 2 * k - 1 : 0) : k; }
+inline bool is_sparse(int shares, int batch, bool keep) { return !keep && shares < batch; }
+inline size_t parts(int shares, int batch, bool keep) { return shares == 1 && !keep ? 0 : is_sparse(shares, batch, keep) ? 2 * (size_t)shares : (size_t)shares + batch; }
 inline bool past_32_bits(const treekv_paged_cache& c) { return (long long)c.batch * ((long long)c.table_width * c.page_size + 31) > 1 << 30; }
 
 // ---- a call's shape, on the host ---------------------------------------------------------------
@@ -86,8 +99,8 @@ inline AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int lon
   s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
   s.keep = weigh && rows <= 32 && (size_t)units * s.rows * cap * 4 <= (size_t)1 << 30;
   s.short_keep = weigh && s.short_shares && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
-  s.part = s.shares > 1 || s.keep ? align_up((size_t)(s.shares + c.batch) * groups * s.rows * (c.head_dim + 4) * 4) : 0;
-  s.short_part = s.short_shares ? align_up((size_t)(s.short_shares + c.batch) * c.kv_heads * 16 * (c.head_dim + 4) * 4) : 0;
+  s.part = align_up(parts(s.shares, c.batch, s.keep) * groups * s.rows * (c.head_dim + 4) * 4);
+  s.short_part = s.short_shares ? align_up(parts(s.short_shares, c.batch, s.short_keep) * c.kv_heads * 16 * (c.head_dim + 4) * 4) : 0;
   s.logits = s.keep || s.short_keep ? align_up((size_t)units * (s.keep ? s.rows : 16) * cap * 4) : 0;
   // few column tiles: each one's rows are shared between up to 16 workgroups, with two tiles of them at least, and their sums added
   // in a launch of its own (attention and weights of 2048 tokens behind 2000, one group of 8: 297 -> 90 us, 512 of 8 groups of 4

@@ -39,14 +39,17 @@ static void walk(const char* name, const Case& x, const treekv_paged_cache& c, i
   });
   CHECK(cut.size >= MIN_SHARE && cut.size % 32 == 0);
   const ll slots = (ll)(part / ((size_t)c.kv_heads * tiles * rows * (c.head_dim + 4) * 4));
+  const bool sparse = is_sparse(shares, B, keep);
   std::vector<ll> start(B);
   std::vector<Runs> run(B);
   std::vector<ll> next(B, 0);              // columns seen
-  std::vector<int> pieces(B, 0);
-  ll at = 0;
+  std::vector<int> pieces(B, 0), part0(B);
+  ll at = 0, column = 0;
   for (int b = 0; b < B; ++b) {
     start[b] = at;
-    run[b] = runs_of(cut, wide, at, length[b], b);
+    run[b] = runs_of(cut, wide, at, length[b]);
+    part0[b] = part_of_first(cut, wide, sparse, run[b], column, b);
+    column += length[b];
     at += cut.own ? shares_in(length[b], cut.size) : length[b];
   }
   std::map<ll, int> taken;
@@ -64,10 +67,10 @@ static void walk(const char* name, const Case& x, const treekv_paged_cache& c, i
       const ll hi = std::min((ll)length[b], cut.own ? lo + cut.size : share_end - start[b]);
       CHECK(lo == next[b] && hi > lo && lo <= INT_MAX && hi <= INT_MAX);
       next[b] = hi;
-      const ll slot = cut.own ? w : w + b;
+      CHECK(w - run[b].first == pieces[b]);
       if (run[b].count > 1 || keep) {
-        CHECK(slot == run[b].first + pieces[b]);
-        CHECK(slot < slots && taken.emplace(slot, b).second);
+        const ll slot = part0[b] + part_at(sparse, pieces[b]);
+        CHECK(slot >= 0 && slot < slots && taken.emplace(slot, b).second);
       }
       if (run[b].count > 1) CHECK(shares > 1);           // (or nothing merges them)
       ++pieces[b];
@@ -104,6 +107,17 @@ int main() {
   check("one head", {TREEKV_BF16, 1, 4, 64, 128, 1, {1 << 30, 3, 1 << 29, 1 << 30, 1 << 30}, {1, 1, 1, 1, 1}});
   check("row tiles", {TREEKV_BF16, 8, 8, 64, 256, 8192, {1 << 30, 1 << 30, 4096}, {8192, 1, 4096}});
   check("row tiles of one", {TREEKV_BF16, 8, 64, 64, 256, 4096, {1 << 30}, {4096}});
+  // scratch goes by what a call has to merge, not by as many sequences as there are of the longest chunk
+  {
+    const char* name = "scratch";
+    treekv_paged_cache c;
+    memset(&c, 0, sizeof(c));
+    c.page_size = 32; c.table_width = 512; c.pages = 8; c.batch = 256; c.kv_heads = 8; c.q_heads = 32; c.head_dim = 128; c.dtype = TREEKV_BF16;
+    const AttendShape s = attend_shape(c, 1024 + 255, 1024, 0);
+    CHECK(s.part + s.short_part + s.logits + s.stat + s.gains < (size_t)200 << 20);            // (out: 10 MB)
+    c.dtype = TREEKV_F32;
+    CHECK(attend_shape(c, 256 * 200, 200, 0).part < (size_t)300 << 20);                        // (out: 838 MB)
+  }
   std::mt19937 g(5);
   auto any = [&](std::initializer_list<int> of) { return of.begin()[g() % of.size()]; };
   for (int i = 0; i < 6000; ++i) {

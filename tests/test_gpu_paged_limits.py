@@ -150,8 +150,8 @@ def test_starts_that_do_not_ascend(binding, name, group, dtype):
 
 @pytest.mark.parametrize("weigh", [False, True])
 def test_starts_that_do_not_ascend_in_every_kernel(binding, weigh):
-    """Chunks beside single tokens, weights of many rows in parts, merges of several shares: with one sequence made to begin inside
-    of another's rows, the others' results are bit for bit those of a call in which it has no rows."""
+    """Chunks beside single tokens, weights of many rows in parts, merges of several shares: with two more sequences, one whose
+    starts fall and one that begins inside of another's rows, the others come out as without them."""
     import torch
 
     from tests.serve_reference import Paged
@@ -159,20 +159,57 @@ def test_starts_that_do_not_ascend_in_every_kernel(binding, weigh):
     for lens, news, group, d, dtype in (([900, 300, 40, 1000, 513, 90, 77, 133], [200, 1, 2, 9, 1, 9, 1, 8], 2, 128, "bf16"),
                                         ([700, 400, 300], [600, 100, 300], 3, 64, "bf16"), ([700, 400, 300], [600, 100, 300], 3, 64, "f32"),
                                         ([9000, 400, 3000, 60], [1, 2, 1, 2], 8, 64, "bf16"), ([600, 400, 300, 30], [40, 20, 30, 1], 1, 128, "bf16"),
-                                        ([300, 400], [150, 120], 70, 64, "bf16")):
-        ref = Paged(lens=lens, news=news, page_size=32, kv_heads=2, group=group, d=d, dtype=dtype, seed=5)
-        at, B = ref.starts.tolist(), ref.B
-        b = B // 2
-        # two more sequences: one whose starts fall, and one with rows of sequence b again
-        odd = at + [at[b], at[b + 1]]
-        none = at + [at[-1], at[-1]]
-        both = Paged(lens=lens + [50, lens[b]], news=news + [0, 0], page_size=32, kv_heads=2, group=group, d=d, dtype=dtype, seed=5)
-        got = []
-        for starts in (none, odd):
-            kv = both.on_gpu(binding)
-            out, lse = torch.full((ref.total, 2 * group, d), 7.0, dtype=ref.t, device="cuda"), torch.full((ref.total, 2 * group), 7.0, device="cuda")
-            status = torch.full((B + 2,), 9, dtype=torch.int32, device="cuda")
-            kv.attend(ref.q.cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), max(news), out, lse, weigh=weigh, status=status)
-            got.append((out, lse, kv.weights, status.tolist()))
-        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][2], got[1][2])
-        assert got[0][3] == [0] * (B + 2) and got[1][3] == [0] * B + [binding.TREEKV_EINVAL] * 2
+                                        ([300, 400], [150, 120], 70, 64, "bf16"), ([400] * 70, [1] * 35 + [130] + [1] * 34, 4, 64, "bf16")):
+        ref = Paged(lens=lens + [50, 50], news=news + [0, 0], page_size=32, kv_heads=2, group=group, d=d, dtype=dtype, seed=5)
+        b, at = len(lens) // 2, ref.starts.tolist()[:-2]
+        starts = at + [at[b], at[b + 1]]
+        ref.lens[-1] = news[b] + 20
+        want, kv = ref.attend(), ref.on_gpu(binding)
+        before = kv.weights.clone()
+        out, lse = torch.full_like(ref.q, 7.0, device="cuda"), torch.full(ref.q.shape[:2], 7.0, device="cuda")
+        status = torch.full((ref.B,), 9, dtype=torch.int32, device="cuda")
+        kv.attend(ref.q.cuda(), torch.tensor(starts, dtype=torch.int32, device="cuda"), max(news), out, lse, weigh=weigh, status=status)
+        assert status.tolist() == [0] * len(lens) + [binding.TREEKV_EINVAL] * 2
+        held(out, want["out"], want["room"])
+        held(lse, want["lse"], want["lse_room"])
+        if weigh:
+            total = before.double().cpu() + want["gain"]
+            held(kv.weights, total, want["gain_room"] + 2.0 ** -23 * total.abs())
+        else:
+            assert torch.equal(kv.weights, before)
+        assert torch.equal(kv.weights[-2:], before[-2:])
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+def test_more_sequences_than_shares(binding, weigh):
+    """Partial results lie at the borders between shares where sequences outnumber them: some sequences of many shares among others."""
+    import torch
+
+    from tests.serve_reference import Paged
+
+    for B, long, hkv, group, d, new, dtype in ((40, (3, 17, 18, 39), 32, 1, 64, 1, "bf16"), (70, (0, 66), 16, 2, 64, 2, "f32"), (20, (1, 2, 19), 16, 7, 128, 40, "bf16"),
+                                               (12, (0, 11), 16, 3, 64, 30, "f32"), (9, (4,), 64, 2, 64, 90, "bf16")):
+        lens = [3000 if b in long else 40 + b for b in range(B)]
+        news = [new if b in long else 1 + b % 2 for b in range(B)]
+        ref = Paged(lens=lens, news=news, page_size=32, kv_heads=hkv, group=group, d=d, dtype=dtype, seed=B)
+        kv, some = ref.on_gpu(binding), sorted(set(long) | {0, 5})
+        out, lse = torch.full_like(ref.q, 7.0, device="cuda"), torch.full(ref.q.shape[:2], 7.0, device="cuda")
+        before = kv.weights.clone()
+        need = kv.new_attend_scratch(ref.total, new, weigh)
+        # scratch ends where it says: what lies behind it stays
+        room = torch.full((need.nbytes + 4096,) if need is not None else (4096,), 77, dtype=torch.uint8, device="cuda")
+        kv.attend(ref.q.cuda(), ref.starts.cuda(), max(news), out, lse, weigh=weigh, scratch=room[:need.nbytes] if need is not None else None)
+        assert bool((room[-4096:] == 77).all())
+        ref.hkv, keep = 1, ref.hkv                            # the reference for the first KV head of some sequences
+        q, ref.q = ref.q, ref.q[:, :group]
+        want = ref.attend(sequences=some)
+        ref.hkv, ref.q = keep, q
+        for b in some:
+            at = slice(int(ref.starts[b]), int(ref.starts[b + 1]))
+            held(out[at, :group], want["out"][at], want["room"][at])
+            held(lse[at, :group], want["lse"][at], want["lse_room"][at])
+            if weigh:
+                total = before[b, :1].double().cpu() + want["gain"][b]
+                held(kv.weights[b, :1], total, want["gain_room"][b] + 2.0 ** -23 * total.abs())
+        # the other heads by their own one-head caches would be the same sums; that none was left out:
+        assert not bool((out == 7.0).all(dim=2).any()) and not bool((lse == 7.0).any())
