@@ -596,7 +596,7 @@ __global__ __launch_bounds__(PA_THREADS) void merge_kernel(Attend a, int merge_t
   Run run;
   if (!PACKED) columns = columns_of(a, tiled);
   if (!find_run(a, columns, 0, b, run) || run.count <= 1 || refused(a, columns, b, s)) return;
-  merge_rows<T, D, true>(a, s, run, first_part<true>(a, columns, run), h, tile * at_once, s.n * p.G, slices, sm);
+  merge_rows<T, D, true>(a, s, run, first_part<true>(a, columns, run), h, tile * at_once, PACKED ? s.n * p.G : merge_tiles * at_once, slices, sm);
 }
 
 // The same where the logits of up to 32 rows have been kept: beside the merge of its rows, each workgroup adds all rows'
@@ -1191,11 +1191,9 @@ int launch_shares(const Attend& a, bool tiled, bool keep, hipStream_t s) {
   }
   if (a.shares > 1 && !keep) {
     const int slices = merge_slices<D>(a), at_once = MERGE_ROWS<D> / slices;
-    const int all = (std::min(a.longest * p.G, a.most_rows) + at_once - 1) / at_once;
-    const long long packed = (long long)a.tokens * p.G / at_once + p.B;
-    if (2 * packed < (long long)all * p.B)
-      hipLaunchKernelGGL((merge_kernel<T, D, true>), dim3((unsigned)(packed * p.Hkv)), dim3(PA_THREADS), 0, s, a, (int)packed, slices, tiled);
-    else hipLaunchKernelGGL((merge_kernel<T, D, false>), dim3((unsigned)(p.Hkv * p.B) * all), dim3(PA_THREADS), 0, s, a, all, slices, tiled);
+    const MergeGrid m = merge_grid(p.B, p.Hkv, p.G, a.tokens, std::min(a.longest * p.G, a.most_rows), at_once);
+    if (m.packed) hipLaunchKernelGGL((merge_kernel<T, D, true>), dim3((unsigned)p.Hkv * m.groups), dim3(PA_THREADS), 0, s, a, m.groups, slices, tiled);
+    else hipLaunchKernelGGL((merge_kernel<T, D, false>), dim3((unsigned)(p.Hkv * p.B) * m.groups), dim3(PA_THREADS), 0, s, a, m.groups, slices, tiled);
   }
   return finish_launch();
 }

@@ -11,7 +11,8 @@ using tkv::fresh;
 
 namespace {
 
-// A launch has fewer than 2^32 threads: 2^24 workgroups of 256, of 16 tokens (append), 32 rows (attend) or 128 slots (weights).
+// A launch has fewer than 2^32 threads: 2^24 workgroups of 256, of 16 tokens (append), 32 rows (attend; fewer rows are one tile of a
+// pair) or 128 slots (weights).  (The merge holds its workgroups to that by itself.)
 constexpr int64_t MAX_SLOTS = (int64_t)1 << 30, MAX_TOKENS = (int64_t)1 << 27, MAX_ROWS = (int64_t)1 << 28, MAX_WEIGHED = (int64_t)1 << 30;
 
 struct Range {

@@ -116,4 +116,20 @@ inline AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int lon
 }
 
 
+// A launch has fewer than 2^32 threads.
+constexpr long long MAX_GROUPS = (1ll << 32) / PA_THREADS - 1;
+// The merge's workgroups, `at_once` rows each: so many of every (sequence, KV head), or of every KV head for all sequences one after
+// the other (`packed`, where the longest sequence has many more than the others).  `rows`: the most of a sequence.  Where that would be
+// more than a launch can have, a sequence gets as many as there can be, which go on to its next rows.
+struct MergeGrid {
+  int groups;
+  bool packed;
+};
+inline MergeGrid merge_grid(int batch, int kv_heads, int G, int tokens, int rows, int at_once) {
+  const int all = (rows + at_once - 1) / at_once;
+  const long long packed = (long long)tokens * G / at_once + batch;
+  if (2 * packed < (long long)all * batch && packed * kv_heads <= MAX_GROUPS) return {(int)packed, true};
+  return {(int)std::min<long long>(all, MAX_GROUPS / ((long long)batch * kv_heads)), false};
+}
+
 }  // namespace tkv

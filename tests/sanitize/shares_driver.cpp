@@ -118,6 +118,21 @@ int main() {
     c.dtype = TREEKV_F32;
     CHECK(attend_shape(c, 256 * 200, 200, 0).part < (size_t)300 << 20);                        // (out: 838 MB)
   }
+  // a merge's launch: as many workgroups as there may be, each row of a sequence has one
+  for (int batch : {1, 20, 4096, 16384, 1 << 20})
+    for (int kv_heads : {1, 8, 32, 256})
+      for (int G : {1, 7, 32})
+        for (int longest : {1, 64, 255, 512, 1 << 20})
+          for (int at_once : {1, 2, 8, 16})
+            for (int full : {1, 2, 4, 1000}) {       // tokens: a part of what the longest chunk of all would be
+              const char* name = "merge";
+              if ((ll)batch * kv_heads > 1 << 20 || (ll)longest * G * kv_heads * batch > 1 << 28) continue;
+              const int tokens = (int)std::min(std::max((ll)batch * longest / full, (ll)longest), 1ll << 27), rows = longest * G;
+              const MergeGrid m = merge_grid(batch, kv_heads, G, tokens, rows, at_once);
+              const ll groups = (ll)m.groups * kv_heads * (m.packed ? 1 : batch);
+              CHECK(m.groups >= 1 && groups <= MAX_GROUPS);
+              if (m.packed) CHECK(m.groups >= ((ll)tokens * G + at_once - 1) / at_once);      // one or more a sequence, no row without
+            }
   std::mt19937 g(5);
   auto any = [&](std::initializer_list<int> of) { return of.begin()[g() % of.size()]; };
   for (int i = 0; i < 6000; ++i) {
