@@ -476,7 +476,8 @@ int treekv_paged_evict(const treekv_paged_cache* cache, int budget, int n_sink, 
  *   draft NULL:  the children were picked without chance, all different.  Child x is accepted if u * (1 - the sum of P of the
  *                siblings before it) < P(x); else x leaves P.
  * The token that follows the path is drawn from what P has become: the smallest x with P(x) > 0 and
- * sum of P up to x > u * sum of P; from the target's row if P is 0; -1 if that is 0 too.  Worked out in double.
+ * sum of P up to x > u * sum of P; from the target's row if P is 0; -1 if that is 0 too.  Worked out in double, from the first P
+ * less a multiple of Q: refusals that leave a part W of P have P good to some 2^-50 / W, and below that it is what rounding leaves.
  *   target, draft [batch, n + 1, vocab] dtype, 16-byte aligned;  tokens, parents [batch, n] int32 (parents as for
  *   treekv_tree_attend; a token outside 0 .. vocab-1 is passed over, its node an absent one)
  *   uniforms [batch, n + 1] float32 in [0, 1): u of node i at i, u of the token that follows at n

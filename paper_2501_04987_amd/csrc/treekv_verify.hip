@@ -5,8 +5,10 @@
 //   P_k = max(P - c_k Q, 0) / W_k,   W_k = sum of max(P - c_k Q, 0),   c_1 = 1,  c_k+1 = c_k + W_k
 // (each step subtracts Q from what the last one made sum to 1, that is, W_k times Q from what it was made of), so a refusal is
 // one pass over two rows, whatever came before it, and the next child is accepted if u Q(x) W_k < max(P(x) - c_k Q(x), 0).
-// Sums are in double: 2^24 terms leave 2^-29 of a step of fp32, so whether a token is accepted or follows does not depend on
-// their order but within that.
+// Sums are in double, 2^14 terms a lane at most: off by 2^-39 of themselves, 2^-15 of half a step of fp32.  A difference is off by
+// 2^-53 of c_k Q, so k refusals leave P_k good to k 2^-52 (terms of W_k) / W_k or better: W_k is the part of the first P that they
+// leave, and an error of c_k does not grow, for W_k falls where c_k rises.  (The rule step by step multiplies its roundings by what
+// each refusal takes.)
 //
 // Bound by latency: 16 trees of 26 nodes over 131072 tokens 29-43 us (the rows take 3 at the rate of memory), four kernels that each
 // wait for the state, its sums and the rows; a chain of 5 over 32000 tokens 12-14 us.
