@@ -412,7 +412,7 @@ typedef struct treekv_paged_cache {
                               16-byte aligned                                                              */
   int32_t* positions;      /* the same shape: the tokens' positions in their streams.  Both NULL: not kept  */
   int32_t pages, page_size, table_width, batch, q_heads, kv_heads, head_dim, dtype;
-  float softmax_scale;     /* multiplies q.k; 0 selects 1/sqrt(head_dim)                                    */
+  float softmax_scale;     /* multiplies q.k, up to 2^127 in size; 0 selects 1/sqrt(head_dim)               */
 } treekv_paged_cache;
 
 /*

@@ -30,7 +30,7 @@ int cache_ok(const treekv_paged_cache* cache) {
   if (c.dtype != TREEKV_BF16 && c.dtype != TREEKV_F32) return TREEKV_EINVAL;
   if (c.pages < 1 || c.page_size < 1 || c.table_width < 1 || c.batch < 1 || c.kv_heads < 1 || c.q_heads < 1 || c.q_heads % c.kv_heads != 0)
     return TREEKV_EINVAL;
-  if (!isfinite(c.softmax_scale)) return TREEKV_EINVAL;
+  if (!isfinite(c.softmax_scale * 1.44269504f)) return TREEKV_EINVAL;        // (logits are scaled by it times log2(e); a logit of 0 would be a NaN)
   if (c.head_dim != 64 && c.head_dim != 128) return TREEKV_EUNSUPPORTED;
   if (c.page_size < 16 || c.page_size > 256 || (c.page_size & (c.page_size - 1))) return TREEKV_EUNSUPPORTED;
   if (c.q_heads > 65536 || (int64_t)c.table_width * c.page_size > MAX_SLOTS || (int64_t)c.batch * c.kv_heads > (1 << 20)) return TREEKV_EUNSUPPORTED;

@@ -60,6 +60,17 @@ def test_caches(binding):
     assert lib.treekv_paged_attend_scratch_bytes(None, 3, 3, 0) == 0 and lib.treekv_paged_evict_scratch_bytes(None) == 0
 
 
+def test_a_scale_that_fp32_does_not_hold_in_base_2(binding):
+    """Logits are scaled by softmax_scale * log2(e) in fp32: where that is infinite a logit of 0 would be a NaN."""
+    lib = binding.load()
+    a, out, other = 0x40 * MB, 0x50 * MB, 0x60 * MB
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        c = cache(binding, softmax_scale=scale)
+        assert lib.treekv_paged_attend(c, a, 256, other, 3, 3, out, None, 0, other, 1 << 30, None, None) == -1, scale
+        assert lib.treekv_paged_attend_scratch_bytes(c, 3, 3, 1) == 0
+    assert lib.treekv_paged_attend_scratch_bytes(cache(binding, softmax_scale=2.3e38), 3, 3, 1) > 0
+
+
 def refuses(call, good, bad, want=-1):
     """`good` with each of the (place, value) of `bad` is refused."""
     for i, x in bad:
