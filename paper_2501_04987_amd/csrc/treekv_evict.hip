@@ -7,8 +7,10 @@
 //   move    attention does not ask for the order of columns, so what is kept stays where it is: only tokens from slots behind
 //           the budget move, into the freed slots before it, as many rows as were kept there (of a decode step one, where
 //           closing the gaps would move half of the cache)
-// Two kernels: one workgroup per unit makes the choice and lists the moves, then all of the chip copies the rows.  A unit of 32768
-// slots is bound by its workgroup's read of 262 KB (28 us of 33 for 32 units), one of 2049 by rounds of barriers (8 us of 13, 256 units).
+// Two kernels: one workgroup per unit makes the choice and lists the moves, then all of the chip copies the rows.  32 units of 32768
+// slots cut to 4096: the choice takes 27 us in 32 workgroups, of which reading is 10, the threshold 8 and the list of 3350 moves 9, the rows 26
+// at 4.2 TB/s in and out (4 where nothing moves); 256 units of 2049 slots 9 and 4, rounds of barriers.  Past 32768 slots keys are
+// formed anew in every pass: 8 units of 32768 40 us in all, of 32770 99, of 131072 342.
 
 #include "treekv_paged.h"
 

@@ -35,7 +35,6 @@ __device__ inline float row_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-
 // 8 and 16 bytes; ONCE: past the caches, which nobody asks for them again.
 template <bool ONCE>
 __device__ inline uint4 load16(const void* p) {

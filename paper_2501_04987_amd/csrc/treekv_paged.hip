@@ -3,8 +3,10 @@
 // attend   o_i = sum over j <= i of p_ij v_j, p_ij = exp(q_i k_j * scale - lse_i), over a sequence's pages.  The G query heads
 //          of a KV head and the sequence's n new tokens are the rows of one matrix product, in tiles of 16 or 32; columns are
 //          slots.  A softmax in one pass: the reference of a row's exponentials is raised where a logit passes it by 2^8, sums
-//          are fp32.  With bf16 storage P enters the second product rounded to bf16 (2^-9 of each probability at most, where the
-//          output is rounded by as much again); the sum beside it takes the unrounded ones.
+//          are fp32.  With bf16 storage P enters the second product rounded to bf16 (2^-8 of each probability at most, where the
+//          output is rounded by as much again); the sum beside it takes the unrounded ones.  Two parts, as a prefill chunk's outputs
+//          in fp32 have them, would be half as many products again, in what is bound by products.  Against 64 bits the output is off
+//          by 1.9 to 2.1e-3 of its size in place of the 1.7e-3 of its own rounding.
 //          A page holds a multiple of 16 rows, so 16 columns lie in one page: one address for the wave and a lane's offset.
 // shares   Few rows leave most of the chip idle, so the columns of the whole batch are cut into equal shares, which the device
 //          works out from the lengths: long sequences get more workgroups than short ones.  A sequence's shares are merged by a
@@ -946,13 +948,12 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
         for (int i = first_of(y - 1); i < first_of(y); ++i) take(i);
       __builtin_amdgcn_sched_barrier(0);
     }
-    float m;
-      m = n[0][0];
+    float m = n[0][0];
 #pragma unroll
     for (int z = 0; z < VSTEPS; ++z) {
       const int y = STEPS + z, g = z / DB;
       if (z + AHEAD < VSTEPS) vf[(z + AHEAD) % (AHEAD + 1)] = read_v(z + AHEAD);
-        o[z % DB] = mfma_wide(vf[z % (AHEAD + 1)], make_uint4(pr[4 * g], pr[4 * g + 1], pr[4 * g + 2], pr[4 * g + 3]), o[z % DB]);
+      o[z % DB] = mfma_wide(vf[z % (AHEAD + 1)], make_uint4(pr[4 * g], pr[4 * g + 1], pr[4 * g + 2], pr[4 * g + 3]), o[z % DB]);
 #pragma unroll
       for (int i = first_of(y - 1); i < first_of(y); ++i) take(i);
 #pragma unroll
@@ -962,8 +963,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
       if (z >= VSTEPS / 2) {
         const int u = z - VSTEPS / 2;
 #pragma unroll
-        for (int i = u * 64 / VSTEPS; i < (u + 1) * 64 / VSTEPS; ++i)
-      m = fmaxf(m, n[i >> 4][i & 15]);
+        for (int i = u * 64 / VSTEPS; i < (u + 1) * 64 / VSTEPS; ++i) m = fmaxf(m, n[i >> 4][i & 15]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -988,7 +988,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void attend_tiled_kernel(Attend a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float bad = __uint_as_float(word[i] & ~(unsigned)((int)finite_word(word[i]) >> 31));
-      o[f][4 * z + i] += c < see ? bad : 0.f;
+              o[f][4 * z + i] += c < see ? bad : 0.f;
             }
           }
       }

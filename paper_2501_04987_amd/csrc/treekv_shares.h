@@ -90,13 +90,16 @@ inline AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int lon
   s.shares = (int)(s.tiled ? max(want / groups, 1ll) : (want + groups - 1) / groups);
   if (s.shares > most) s.shares = (int)most;
   // A few chunks among many sequences of a token or two: those are attended by the kernel for few rows, in a launch of its own
-  // (512 tokens and 31 single ones behind 8000 each, 8 groups of 4: 268 us in place of 596, with weights 374 in place of 855).
+  // (512 tokens and 31 single ones behind 8000 each, 8 groups of 4: 268 us in place of 596, with weights 374 in place of 855).  From
+  // where the longest is four times the average: 4 of 64 tokens and 12 single ones (3.8) take 139 us together, 137 apart, and 16
+  // single ones (4.7) 236 and 164; one of 64 and three (3.8) 45 and 56, four (4.7) 63 and 64.  (Chunks of 512 would gain
+  // before: 4 and 8, 3 times, 443 and 369.)
   s.short_shares = s.tiled && (long long)tokens * 4 <= (long long)longest * c.batch && c.q_heads / c.kv_heads <= 16
                        ? (int)std::min<long long>((256 + c.kv_heads - 1) / c.kv_heads, most) : 0;
   // keys once more cost d elements a column, kept logits two words for each row: up to 1 GiB of them, for up to 32 rows (8 sequences
-  // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike)
-  // (what that asks of the query rows' distance, the launch adds)
-  s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;
+  // of 8000 columns, groups of 4, 5 tokens: 54 us against 76 with the keys read again, 8 tokens 58 against 78, fp32 alike).  They are
+  // counted by the table's width and whole tiles of rows, for lengths are on the device.
+  s.weigh_tiled = s.tiled && c.q_heads / c.kv_heads <= TILE;     // (what that asks of the query rows' distance, the launch adds)
   s.keep = weigh && rows <= 32 && (size_t)units * s.rows * cap * 4 <= (size_t)1 << 30;
   s.short_keep = weigh && s.short_shares && (size_t)units * 16 * cap * 4 <= (size_t)1 << 30;
   s.part = align_up(parts(s.shares, c.batch, s.keep) * groups * s.rows * (c.head_dim + 4) * 4);
@@ -104,7 +107,8 @@ inline AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int lon
   s.logits = s.keep || s.short_keep ? align_up((size_t)units * (s.keep ? s.rows : 16) * cap * 4) : 0;
   // few column tiles: each one's rows are shared between up to 16 workgroups, with two tiles of them at least, and their sums added
   // in a launch of its own (attention and weights of 2048 tokens behind 2000, one group of 8: 297 -> 90 us, 512 of 8 groups of 4
-  // alone 65 -> 41; four tiles at least: 100 tokens behind 1000 37 us, with two 34)
+  // alone 65 -> 41; four tiles at least: 100 tokens behind 1000 37 us, with two 34).  By the table's width too: the first of these
+  // takes 218 us with a table for 32768.
   s.weigh_splits = 1;
   if (weigh && !s.keep && s.weigh_tiled) {
     const long long tiles = (cap + PA_WAVES * 32 - 1) / (PA_WAVES * 32) * units;
@@ -114,7 +118,6 @@ inline AttendShape attend_shape(const treekv_paged_cache& c, int tokens, int lon
   s.stat = weigh && !s.keep ? align_up((size_t)tokens * c.q_heads * 8) : 0;
   return s;
 }
-
 
 // A launch has fewer than 2^32 threads.
 constexpr long long MAX_GROUPS = (1ll << 32) / PA_THREADS - 1;

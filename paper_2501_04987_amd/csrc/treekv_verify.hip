@@ -474,7 +474,10 @@ __global__ __launch_bounds__(VF_THREADS) void verify_kernel(treekv_verify_args a
 
 // Rounds of parts where a sequence's own workgroup would read long rows while most of the chip idles.
 // (16 trees of 26 nodes over 131072 tokens: 48.5 us without rounds, 29.5 with 3, 33 with 4, 38.5 with 6; a chain of 5 over 32000 12.1
-// without, 20.4 with.)  Without the drafter's probabilities there is one pass.
+// without, 20.4 with.)  Without the drafter's probabilities there is one pass.  About the border, without and with: 16 trees in
+// bf16 over 50000 31.8 and 28.3, 65536 33.4 and 30.7, 98304 62 and 49; 64 trees 40.8 and 45.2, 34.4 and 37.0, 44.0 and 38.1;
+// one 16.8 and 21.4, 17.1 and 20.6, 19.7 and 21.9, 131072 22.8 and 21.7; 127 trees 42.7 and 60.2 over 65536, 78.0 and 79.3 over 131072, 128
+// 42.3 and 60.9, 78.0 and 81.3.  So it holds for 16 to 64 sequences of 98304 tokens on; what lies nearer to it loses up to 17 us.
 bool in_rounds(int batch, int vocab) { return batch < 128 && vocab >= 65536; }
 
 }  // namespace
