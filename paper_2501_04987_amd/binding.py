@@ -295,6 +295,14 @@ def _call_on(device, index: int, what: str, *args):
         raise TreeKVError(rc, what)
 
 
+def _int32(x, what: str) -> int:
+    """ctypes cuts what 32 bits do not hold."""
+    x = int(x)
+    if not -2147483648 <= x <= 2147483647:
+        raise ValueError(f"{what}: {x} is not within 32 bits")
+    return x
+
+
 def _scratch_at(scratch, index: int):
     if scratch is None:
         return 0, 0
@@ -354,6 +362,8 @@ class PagedKV:
 
         load()
         kv_heads = kv_heads or heads
+        for x, name in ((pages, "pages"), (batch, "batch"), (table_width, "table_width"), (heads, "heads")):
+            _int32(x, name)
         self.storage_dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
         device = torch.device(device) if k is None else k.device
         pool, track = (pages, kv_heads, page_size, head_dim), (batch, kv_heads, table_width * page_size)
@@ -417,7 +427,7 @@ class PagedKV:
         """What `attend` takes as `scratch` for these arguments (None where it needs none; fewer tokens can need more)."""
         import torch
 
-        need = (_lib or load()).treekv_paged_attend_scratch_bytes(self._at, int(tokens), int(longest), int(weigh))
+        need = (_lib or load()).treekv_paged_attend_scratch_bytes(self._at, _int32(tokens, "tokens"), _int32(longest, "longest"), int(weigh))
         return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
 
     def attend(self, q, starts, longest: int, out=None, lse=None, *, weigh: bool = False, scratch=None, status=None):
@@ -426,7 +436,7 @@ class PagedKV:
         import torch
 
         batch, heads, _, d = self._dims
-        far, tokens = self._rows(q, "q", heads), q.shape[0]
+        far, tokens, longest = self._rows(q, "q", heads), q.shape[0], _int32(longest, "longest")
         status_at = self._batch_ints(starts, status)
         if out is None:
             out = torch.empty(tokens, heads, d, dtype=self.storage_dtype, device=self.device)
@@ -437,7 +447,7 @@ class PagedKV:
             lse_at = lse.data_ptr()
         if scratch is None:
             scratch = self.new_attend_scratch(tokens, longest, weigh)
-        _call_on(self.device, self._index, "treekv_paged_attend", self._at, q.data_ptr(), far, starts.data_ptr(), tokens, int(longest),
+        _call_on(self.device, self._index, "treekv_paged_attend", self._at, q.data_ptr(), far, starts.data_ptr(), tokens, longest,
                  out.data_ptr(), lse_at, int(weigh), *_scratch_at(scratch, self._index), status_at)
         return out
 
@@ -453,6 +463,7 @@ class PagedKV:
         layers share it, stays until all of them have been evicted: `lens_out` [batch] takes what it becomes."""
         import torch
 
+        budget, n_sink, n_recent = _int32(budget, "budget"), _int32(n_sink, "n_sink"), _int32(n_recent, "n_recent")
         status_at = lens_at = 0
         if lens_out is not None:
             _want(lens_out, "lens_out", torch.int32, (self._dims[0],), self._index)
@@ -462,7 +473,7 @@ class PagedKV:
             status_at = status.data_ptr()
         if scratch is None:
             scratch = self.new_evict_scratch()
-        _call_on(self.device, self._index, "treekv_paged_evict", self._at, int(budget), int(n_sink), int(n_recent), lens_at,
+        _call_on(self.device, self._index, "treekv_paged_evict", self._at, budget, n_sink, n_recent, lens_at,
                  *_scratch_at(scratch, self._index), status_at)
 
 

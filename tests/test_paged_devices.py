@@ -36,3 +36,17 @@ def test_what_is_made_lies_where_the_pool_lies(binding, names):
 def test_where_no_pool_is_given_the_device_counts(binding):
     kv = binding.PagedKV(4, 16, 2, 64, batch=3, table_width=2, device="cpu")
     assert {getattr(kv, n).device.type for n in ("k", "v", "table", "lens", "weights", "positions")} == {"cpu"}
+
+
+def test_numbers_that_32_bits_do_not_hold_are_refused(binding):
+    """ctypes would cut them: a budget of 2^32 + 16 would be one of 16."""
+    import torch
+
+    kv = binding.PagedKV(4, 16, 2, 64, table_width=2, device="cpu")
+    q, starts = torch.zeros(1, 2, 64, dtype=torch.bfloat16), torch.tensor([0, 1], dtype=torch.int32)
+    for far in (2 ** 32 + 16, 2 ** 31, -2 ** 31 - 1):
+        for call in (lambda: kv.evict(far, 0, 0), lambda: kv.evict(16, far, 0), lambda: kv.evict(16, 0, far), lambda: kv.attend(q, starts, far),
+                     lambda: kv.new_attend_scratch(1, far), lambda: kv.new_attend_scratch(far, 1),
+                     lambda: binding.PagedKV(4, 16, 2, 64, table_width=2, batch=far, device="meta")):
+            with pytest.raises(ValueError, match="32 bits"):
+                call()
